@@ -407,6 +407,116 @@ dybit_status dybit_gemm_static_ws(int64_t M, int64_t N, int64_t K,
                                   const void *B, dybit_fmt fb, const float *scale_b, int64_t ldb_bytes,
                                   float *C, int64_t ldc, int32_t *C_raw, void *stream);
 
+/* ---------------------------------------------------------------- fine-tuning a coded layer
+ * (no counterpart in the paper, which fine-tunes its quantized models without saying how): the operators that train
+ * and serve a linear layer whose weights are codes, beside its product (dybit_gemm).
+ *   - activation checkpoints: what a layer keeps of its input for the backward pass, as 8-bit codes with one
+ *     power-of-two scale per row (dybit_checkpoint_save / _load), and the weight gradient read from them
+ *     (dybit_checkpoint_wgrad);
+ *   - low-rank adapters beside a frozen coded projection, the tokens of many requests (each with its own adapter) in one
+ *     call (dybit_adapters), and their gradients with the layer's input read from a checkpoint
+ *     (dybit_adapters_backward).
+ * Matrices of real numbers are row-major with a row stride in elements; a pointer is aligned to its element.  Rows
+ * that start on 16-byte boundaries run fastest. */
+
+/* Element type of a matrix of real numbers. */
+typedef enum {
+    DYBIT_F32 = 0,
+    DYBIT_BF16 = 1,
+    DYBIT_F16 = 2
+} dybit_dtype;
+
+/* Stores an activation as 8-bit codes.  Per row: with amax = the largest finite |x| of the row and
+ * e = ceil(log2(amax)),
+ *     scales[row] = 2^(e - top)     (exponent clamped to -126..126; 1 for a row without a finite non-zero value)
+ *     code        = encode(x / scales[row])    the encoder of dybit_quantize_pack
+ * so the row's largest magnitude lands in (2^(top-1), 2^top] of the format's value axis.  Values near 1 are held most
+ * finely: top = 2 keeps most of a bell-shaped row in the linear part (relative error of the row near 2^-7), larger
+ * values suit rows with strong outliers.  The power of two makes the division and the product scale * value exact.
+ * NaN -> code 0; infinities and what exceeds the format's range saturate.
+ *   x      [dev]  rows x cols, row stride ld >= cols (elements)
+ *   fmt    8 bits, signed or unsigned (other widths: DYBIT_ERR_UNSUPPORTED)
+ *   top    0 .. m-1 (m magnitude bits: 7 signed, 8 unsigned)
+ *   codes  [dev]  rows x row_stride_bytes, 16-byte aligned; row_stride_bytes a multiple of 16, >= cols.  Bytes from cols
+ *          to the next multiple of 128 (or the end of the row) are written as code 0, what follows is left alone.  (A
+ *          stride of dybit_row_stride_bytes(cols, 8) makes the codes an operand of dybit_gemm's layout.)
+ *   scales [dev]  rows floats
+ * rows == 0 or cols == 0: nothing but scales (1) is written. */
+dybit_status dybit_checkpoint_save(const void *x, dybit_dtype tx, int64_t rows, int64_t cols, int64_t ld, dybit_fmt fmt,
+                                   int top, void *codes, int64_t row_stride_bytes, float *scales, void *stream);
+
+/* Reads it back: y = round_to_ty(fmul_rn(scale of the row, value(code))).  The scale of row r is
+ * scales[r * scale_stride]: 1 for the scales of dybit_checkpoint_save, 0 for one scale of the whole tensor (the
+ * pair that dybit_quantize_pack_2d writes). */
+dybit_status dybit_checkpoint_load(const void *codes, int64_t row_stride_bytes, const float *scales, int64_t scale_stride,
+                                   int64_t rows, int64_t cols, dybit_fmt fmt, void *y, dybit_dtype ty, int64_t ld,
+                                   void *stream);
+
+/* Weight gradient of a linear layer Y = X W^T from the checkpoint of its input:
+ *     dW[n][k] = sum_t dY[t][n] * x^[t][k],   x^[t][k] = scale_t * value(code[t][k])
+ * with fp32 accumulation.  x^ enters the product as bf16: exact for a power-of-two scale, and for scale_stride 0 (the
+ * scale multiplies the sum), rounded to nearest otherwise.  dY enters exactly: bf16 as it is, f16 as the sum of two
+ * bf16 numbers, f32 as the sum of three (what three leave over is below 2^-24 of the element).
+ *   dY    [dev]  T x N, row stride lddy;   codes, scales as above, T rows of K codes
+ *   dW    [dev]  N x K floats, row stride lddw, overwritten (zeros for T == 0)
+ *   ws    [dev]  dybit_checkpoint_wgrad_workspace_bytes(...) bytes, 1024-byte aligned */
+size_t dybit_checkpoint_wgrad_workspace_bytes(int64_t T, int64_t N, int64_t K, dybit_dtype tdy);
+dybit_status dybit_checkpoint_wgrad(int64_t T, int64_t N, int64_t K, const void *dY, dybit_dtype tdy, int64_t lddy,
+                                    const void *codes, int64_t row_stride_bytes, dybit_fmt fmt, const float *scales,
+                                    int64_t scale_stride, float *dW, int64_t lddw, void *ws, size_t ws_bytes,
+                                    void *stream);
+
+/* The tokens of a batch grouped by adapter.  One plan serves every call with the same tokens: all projections of all
+ * layers, forward and backward.  An id outside 0 .. n_adapters-1 (-1 by convention) is a token without an adapter.
+ * Tokens of one adapter keep their order, so results do not depend on anything but the arguments.
+ *   ids   [dev]  T int32
+ *   plan  [dev]  dybit_adapters_plan_bytes(T, n_adapters) bytes, 16-byte aligned, overwritten
+ * n_adapters 1 .. DYBIT_MAX_ADAPTERS. */
+#define DYBIT_MAX_ADAPTERS 4096
+size_t dybit_adapters_plan_bytes(int64_t T, int n_adapters);
+dybit_status dybit_adapters_plan(int64_t T, const int32_t *ids, int n_adapters, void *plan, size_t plan_bytes,
+                                 void *stream);
+
+/* Low-rank adapters beside a projection that all tokens share.  With a = ids[t]:
+ *     V[t]  = A_a x_t                              R numbers, fp32
+ *     y[t]  = base[t] + sum_r (alpha_a * V[t][r]) * B_a[r]
+ * and V[t] = 0, y[t] = base[t] for a token without an adapter.  Sums are kept in fp32 and y is rounded once.
+ *   X     [dev]  T x K, row stride ldx
+ *   A     [dev]  n_adapters x R x K, dense (rank-major)
+ *   B     [dev]  n_adapters x R x N, dense (rank-major: the transpose of the usual N x R factor)
+ *   tw    type of A and B.  (tx, tw) is (f32, bf16), (bf16, bf16) or (f16, f16)
+ *   alpha [dev]  n_adapters floats, or NULL for 1
+ *   plan  [dev]  of the same T and n_adapters
+ *   base  [dev]  T x N, row stride ldbase, or NULL for 0;  Y [dev] T x N, row stride ldy, may be base itself
+ *   ty    type of base and Y: f32, or tx
+ *   V     [dev]  T x R floats, dense, 16-byte aligned, or NULL: what dybit_adapters_backward wants of the forward pass
+ * R is a multiple of 8 up to DYBIT_MAX_RANK (an adapter of lower rank has zero rows in A and B). */
+#define DYBIT_MAX_RANK 128
+dybit_status dybit_adapters(int64_t T, int64_t K, int64_t N, int R, const void *X, dybit_dtype tx, int64_t ldx,
+                            int n_adapters, const void *A, const void *B, dybit_dtype tw, const float *alpha,
+                            const void *plan, const void *base, int64_t ldbase, dybit_dtype ty, void *Y, int64_t ldy,
+                            float *V, void *stream);
+
+/* Its gradients, the layer's input read from an 8-bit checkpoint:
+ *     U[t]  = alpha_a * B_a dY[t]                  fp32
+ *     dX[t] = dXbase[t] + sum_r U[t][r] A_a[r]
+ *     dA_a  = sum_{t of a} U[t]^T x^[t],   dB_a = alpha_a * sum_{t of a} V[t]^T dY[t]
+ * dX[t] = dXbase[t] for a token without an adapter; dA_a = dB_a = 0 for an adapter without tokens.
+ *   dY     [dev]  T x N, row stride lddy;  dXbase (or NULL), dX [dev] T x K, dX may be dXbase
+ *   tdy    type of dY, dXbase and dX: f32 or bf16 (f16: DYBIT_ERR_UNSUPPORTED);  A and B are bf16
+ *   codes, row_stride_bytes, fmt, scales, scale_stride: the checkpoint of X, T rows of K codes
+ *   V      [dev]  T x R floats, from dybit_adapters
+ *   dA, dB [dev]  n_adapters x R x K and n_adapters x R x N floats, overwritten
+ *   ws     [dev]  dybit_adapters_backward_workspace_bytes(...) bytes, 1024-byte aligned
+ * The order of the sums is fixed by the arguments: equal calls give equal bits. */
+size_t dybit_adapters_backward_workspace_bytes(int64_t T, int64_t K, int64_t N, int R, int n_adapters);
+dybit_status dybit_adapters_backward(int64_t T, int64_t K, int64_t N, int R, const void *dY, dybit_dtype tdy, int64_t lddy,
+                                     const void *codes, int64_t row_stride_bytes, dybit_fmt fmt, const float *scales,
+                                     int64_t scale_stride, int n_adapters, const void *A, const void *B,
+                                     dybit_dtype tw, const float *alpha, const void *plan, const float *V,
+                                     const void *dXbase, int64_t lddxbase, void *dX, int64_t lddx, float *dA,
+                                     float *dB, void *ws, size_t ws_bytes, void *stream);
+
 /* Reads and clears the device status word of the current device.  Blocks
  * until `stream` has drained.  DYBIT_ERR_DEVICE_TIMEOUT means a kernel gave
  * up on a bounded wait (results of that call are invalid); DYBIT_OK

@@ -10,12 +10,13 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 LIB_PATH = os.path.join(_PKG, "libdybit.so")
 DEBUG_LIB_PATH = os.path.join(_PKG, "libdybit_debug.so")     # the same sources with -DDYBIT_DEBUG_BOUNDS (range checks)
-_SOURCES = [os.path.join(_PKG, "csrc", "dybit_lib.cu")]
+_SOURCES = [os.path.join(_PKG, "csrc", f) for f in ("dybit_lib.cu", "dybit_finetune.cu")]
+_OBJECTS = os.path.join(_PKG, "build")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
     "-std=c++17", "-O3", "-lineinfo",
-    "-shared", "-Xcompiler", "-fPIC",
+    "-Xcompiler", "-fPIC",
 ]
 
 
@@ -38,21 +39,46 @@ def is_stale(path: str = LIB_PATH) -> bool:
     return any(os.path.getmtime(p) > t for p in _deps())
 
 
+def _object_is_stale(obj: str) -> bool:
+    """Whether a file that the object was compiled from (nvcc's list of dependencies beside it) is newer than it."""
+    try:
+        t = os.path.getmtime(obj)
+        with open(obj + ".d") as f:
+            deps = f.read().replace("\\\n", " ").split(":", 1)[1].split()
+        return any(os.path.getmtime(p) > t for p in deps)
+    except (OSError, IndexError):
+        return True
+
+
 def build_library(force: bool = False, verbose: bool = False, debug_bounds: bool = False) -> str:
     """Compile the CUDA sources into paper_2302_12510_b200/libdybit.so (or, with debug_bounds, into
-    libdybit_debug.so: the build whose global stores are range-checked, see DYBIT_CHECK in csrc/dybit_common.cuh)."""
+    libdybit_debug.so: the build whose global stores are range-checked, see DYBIT_CHECK in csrc/dybit_common.cuh).
+    The translation units are compiled side by side."""
     out = DEBUG_LIB_PATH if debug_bounds else LIB_PATH
     if not force and not is_stale(out):
         return out
+    os.makedirs(_OBJECTS, exist_ok=True)
+    flags = NVCC_FLAGS + (["-DDYBIT_DEBUG_BOUNDS"] if debug_bounds else []) + (["-Xptxas", "-v"] if verbose else []) + [
+        "-I", os.path.join(_ROOT, "include"), "-I", os.path.join(_PKG, "csrc")]
+    objects, jobs = [], []
+    for src in _SOURCES:
+        obj = os.path.join(_OBJECTS, os.path.basename(src) + (".debug.o" if debug_bounds else ".o"))
+        objects.append(obj)
+        if force or _object_is_stale(obj):
+            tmp = obj + ".tmp%d" % os.getpid()
+            cmd = [_nvcc()] + flags + ["-c", "-MD", "-MF", obj + ".d", "-o", tmp, src]
+            jobs.append((obj, tmp, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    logs = [(obj, tmp, p, p.communicate()[0]) for obj, tmp, p in jobs]
+    for obj, tmp, p, log in logs:
+        if p.returncode != 0:
+            raise RuntimeError("nvcc failed:\n" + log)
+        if verbose:
+            print(log)
+        os.replace(tmp, obj)
     tmp = out + ".tmp%d" % os.getpid()
-    cmd = [_nvcc()] + NVCC_FLAGS + (["-DDYBIT_DEBUG_BOUNDS"] if debug_bounds else []) + (["-Xptxas", "-v"] if verbose else []) + [
-        "-I", os.path.join(_ROOT, "include"), "-I", os.path.join(_PKG, "csrc"),
-        "-o", tmp] + _SOURCES
-    proc = subprocess.run(cmd, capture_output=True, text=True)
+    proc = subprocess.run([_nvcc()] + NVCC_FLAGS + ["-shared", "-o", tmp] + objects, capture_output=True, text=True)
     if proc.returncode != 0:
         raise RuntimeError("nvcc failed:\n" + proc.stdout + proc.stderr)
-    if verbose:
-        print(proc.stderr)
     os.replace(tmp, out)
     return out
 

@@ -26,6 +26,9 @@ __all__ = [
     "ConvLayers", "dybit_quantize_expand_layers", "dybit_conv2d_prepared", "dybit_conv2d_prepared_layers",
     "dybit_gemm_batched_workspace_bytes", "dybit_rmse", "dybit_rmse_sweep", "dybit_fake_quant", "dybit_fake_quant_backward",
     "dybit_search_bitwidths",
+    "dybit_checkpoint_save", "dybit_checkpoint_load", "dybit_checkpoint_wgrad", "dybit_checkpoint_wgrad_workspace_bytes",
+    "AdapterPlan", "dybit_adapters_plan", "dybit_adapters_plan_bytes", "dybit_adapters", "dybit_adapters_backward",
+    "dybit_adapters_backward_workspace_bytes",
 ]
 
 
@@ -132,6 +135,19 @@ def _load() -> C.CDLL:
     lib.dybit_fake_quant_backward.argtypes = [vp, vp, i64, _CFmt, vp, vp, vp]
     lib.dybit_search_bitwidths.argtypes = [i32, C.POINTER(C.c_double), C.POINTER(C.c_double), i32, C.c_double, i32,
                                            C.POINTER(i32), C.POINTER(i32)]
+    lib.dybit_checkpoint_save.argtypes = [vp, i32, i64, i64, i64, _CFmt, i32, vp, i64, vp, vp]
+    lib.dybit_checkpoint_load.argtypes = [vp, i64, vp, i64, i64, i64, _CFmt, vp, i32, i64, vp]
+    lib.dybit_checkpoint_wgrad_workspace_bytes.restype = sz
+    lib.dybit_checkpoint_wgrad_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.dybit_checkpoint_wgrad.argtypes = [i64, i64, i64, vp, i32, i64, vp, i64, _CFmt, vp, i64, vp, i64, vp, sz, vp]
+    lib.dybit_adapters_plan_bytes.restype = sz
+    lib.dybit_adapters_plan_bytes.argtypes = [i64, i32]
+    lib.dybit_adapters_plan.argtypes = [i64, vp, i32, vp, sz, vp]
+    lib.dybit_adapters.argtypes = [i64, i64, i64, i32, vp, i32, i64, i32, vp, vp, i32, vp, vp, vp, i64, i32, vp, i64, vp, vp]
+    lib.dybit_adapters_backward_workspace_bytes.restype = sz
+    lib.dybit_adapters_backward_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+    lib.dybit_adapters_backward.argtypes = [i64, i64, i64, i32, vp, i32, i64, vp, i64, _CFmt, vp, i64, i32, vp, vp, i32,
+                                            vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
     lib.dybit_gemm_static_ws.argtypes = [i64, i64, i64, vp, _CFmt, vp, i64, vp, _CFmt, vp, i64, vp, i64, vp, vp]
     return lib
 
@@ -669,3 +685,204 @@ def dybit_search_bitwidths(lat, rmse, num_layers: int, strategy: str, constraint
     _check(lib.dybit_search_bitwidths(num_layers, la, ra, 0 if strategy == "speedup" else 1, float(constraint),
                                       int(top_k), w, a), "dybit_search_bitwidths")
     return list(w), list(a)
+
+
+# ---------------------------------------------------------------- fine-tuning a coded layer
+
+_DTYPE_CODE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _matrix(x: torch.Tensor, name: str, cols: Optional[int] = None, rows: Optional[int] = None) -> int:
+    """Checks a 2-D device matrix of real numbers with contiguous rows; returns its dybit_dtype."""
+    code = _DTYPE_CODE.get(x.dtype)
+    if code is None or not x.is_cuda or x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
+        raise ValueError(f"{name} must be a 2-D float32, bfloat16 or float16 CUDA tensor with unit inner stride")
+    if (cols is not None and x.shape[1] != cols) or (rows is not None and x.shape[0] != rows):
+        raise ValueError(f"{name} has shape {tuple(x.shape)}, expected ({'any' if rows is None else rows}, {'any' if cols is None else cols})")
+    return code
+
+
+def _ld(x: torch.Tensor) -> int:
+    """Row stride of a matrix; torch gives one row any stride, which must not be below its length."""
+    return max(x.stride(0), x.shape[1]) if x.shape[0] <= 1 else x.stride(0)
+
+
+def _codes8(codes: torch.Tensor, rows: int, cols: int, scales: torch.Tensor) -> Tuple[int, int]:
+    """Checks a matrix of 8-bit codes and its scales; returns (row stride in bytes, number of scales)."""
+    if codes.dtype != torch.uint8 or not codes.is_cuda or codes.dim() != 2 or codes.shape[0] != rows or codes.shape[1] < cols or \
+            (codes.stride(1) != 1 and codes.shape[1] > 1):
+        raise ValueError("codes must be a 2-D uint8 CUDA tensor [rows][row bytes >= cols] with unit inner stride")
+    if scales.dtype != torch.float32 or not scales.is_cuda or not scales.is_contiguous():
+        raise ValueError("scales must be a contiguous float32 CUDA tensor")
+    return _ld(codes), scales.numel()
+
+
+def _scale_stride(scales: torch.Tensor, rows: int, per_row: bool) -> int:
+    if scales.numel() < (rows if per_row else 1):
+        raise ValueError("scales must hold one value per row, or the scale of the whole tensor")
+    return 1 if per_row else 0
+
+
+def dybit_checkpoint_save(x: torch.Tensor, fmt, top: int = 2, codes: Optional[torch.Tensor] = None,
+                          scales: Optional[torch.Tensor] = None, stream=None):
+    """8-bit codes of an activation [rows][cols] with one power-of-two scale per row; the largest magnitude of a row
+    lands in (2^(top-1), 2^top].  Returns (codes uint8 [rows][row bytes], scales float32 [rows])."""
+    t = _matrix(x, "x")
+    rows, cols = x.shape
+    if codes is None:
+        codes = torch.empty((rows, (cols + 127) // 128 * 128), dtype=torch.uint8, device=x.device)
+    if scales is None:
+        scales = torch.empty(rows, dtype=torch.float32, device=x.device)
+    stride, n = _codes8(codes, rows, cols, scales)
+    if n < rows:
+        raise ValueError("scales must hold one value per row")
+    if codes.shape[1] < min(stride, (cols + 127) // 128 * 128):
+        raise ValueError("codes must have room for the columns rounded up to 128, or to the end of its rows")
+    _check(lib.dybit_checkpoint_save(x.data_ptr(), t, rows, cols, _ld(x), _fmt(fmt), int(top), codes.data_ptr(), stride,
+                                     scales.data_ptr(), _stream(stream)), "dybit_checkpoint_save")
+    return codes, scales
+
+
+def dybit_checkpoint_load(codes: torch.Tensor, cols: int, fmt, scales: torch.Tensor, dtype: torch.dtype = torch.float32,
+                          out: Optional[torch.Tensor] = None, per_row: bool = True, stream=None):
+    """The activation [rows][cols] that a checkpoint stands for.  per_row=False: scales is the pair {scale, 1/scale} of
+    the whole tensor, as dybit_quantize_pack_2d writes it."""
+    rows = codes.shape[0]
+    stride, _ = _codes8(codes, rows, cols, scales)
+    if out is None:
+        out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
+    t = _matrix(out, "out", cols, rows)
+    _check(lib.dybit_checkpoint_load(codes.data_ptr(), stride, scales.data_ptr(), _scale_stride(scales, rows, per_row), rows,
+                                     int(cols), _fmt(fmt), out.data_ptr(), t, _ld(out), _stream(stream)),
+           "dybit_checkpoint_load")
+    return out
+
+
+def dybit_checkpoint_wgrad_workspace_bytes(T: int, N: int, K: int, dtype: torch.dtype) -> int:
+    return int(lib.dybit_checkpoint_wgrad_workspace_bytes(int(T), int(N), int(K), _DTYPE_CODE[dtype]))
+
+
+def _workspace(need: int, ws: Optional[torch.Tensor], device):
+    """(address, bytes, tensor to keep) of a 1024-byte aligned workspace."""
+    if ws is None:
+        ws = torch.empty(need + 1024, dtype=torch.uint8, device=device)
+    at = ws.data_ptr()
+    off = -at % 1024
+    return at + off, ws.numel() - off, ws
+
+
+def dybit_checkpoint_wgrad(dY: torch.Tensor, codes: torch.Tensor, K: int, fmt, scales: torch.Tensor,
+                           out: Optional[torch.Tensor] = None, per_row: bool = True,
+                           ws: Optional[torch.Tensor] = None, stream=None):
+    """dW [N][K] float32 = dY^T x^ with x^ [T][K] read from an 8-bit checkpoint."""
+    t = _matrix(dY, "dY")
+    T, N = dY.shape
+    stride, _ = _codes8(codes, T, K, scales)
+    if out is None:
+        out = torch.empty((N, K), dtype=torch.float32, device=dY.device)
+    if _matrix(out, "out", K, N) != 0:
+        raise ValueError("out must be float32")
+    at, size, ws = _workspace(lib.dybit_checkpoint_wgrad_workspace_bytes(T, N, K, t), ws, dY.device)
+    _check(lib.dybit_checkpoint_wgrad(T, N, K, dY.data_ptr(), t, _ld(dY), codes.data_ptr(), stride, _fmt(fmt),
+                                      scales.data_ptr(), _scale_stride(scales, T, per_row), out.data_ptr(), _ld(out), at, size,
+                                      _stream(stream)), "dybit_checkpoint_wgrad")
+    return out
+
+
+def dybit_adapters_plan_bytes(T: int, n_adapters: int) -> int:
+    return int(lib.dybit_adapters_plan_bytes(int(T), int(n_adapters)))
+
+
+def dybit_adapters_plan(ids: torch.Tensor, n_adapters: int, plan: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Groups the tokens of a batch by adapter: ids int32 [T], outside 0 .. n_adapters-1 for a token without one.
+    Returns the plan's buffer (uint8)."""
+    if ids.dtype != torch.int32 or not ids.is_cuda or ids.dim() != 1 or not ids.is_contiguous():
+        raise ValueError("ids must be a contiguous 1-D int32 CUDA tensor")
+    T = ids.numel()
+    if plan is None:
+        plan = torch.empty(dybit_adapters_plan_bytes(T, n_adapters), dtype=torch.uint8, device=ids.device)
+    _check(lib.dybit_adapters_plan(T, ids.data_ptr(), int(n_adapters), plan.data_ptr(), plan.numel(), _stream(stream)),
+           "dybit_adapters_plan")
+    return plan
+
+
+class AdapterPlan:
+    """The plan of one batch of tokens, for every call with the same tokens (dybit_adapters_plan)."""
+
+    def __init__(self, ids: torch.Tensor, n_adapters: int, stream=None):
+        self.T, self.n = ids.numel(), int(n_adapters)
+        self.buffer = dybit_adapters_plan(ids, n_adapters, stream=stream)
+
+
+def _factors(A: torch.Tensor, B: torch.Tensor, alpha: Optional[torch.Tensor], plan: AdapterPlan) -> Tuple[int, int, int, int]:
+    """Checks the factors [n][R][K] and [n][R][N]; returns (R, K, N, dybit_dtype)."""
+    if A.dim() != 3 or B.dim() != 3 or A.shape[:2] != B.shape[:2] or A.shape[0] != plan.n or A.dtype != B.dtype or \
+            not (A.is_cuda and B.is_cuda and A.is_contiguous() and B.is_contiguous()) or A.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("A and B must be contiguous 16-bit CUDA tensors [n_adapters][R][K] and [n_adapters][R][N]")
+    if alpha is not None and (alpha.dtype != torch.float32 or not alpha.is_cuda or not alpha.is_contiguous() or alpha.numel() != plan.n):
+        raise ValueError("alpha must be a contiguous float32 CUDA tensor with one value per adapter")
+    return A.shape[1], A.shape[2], B.shape[2], _DTYPE_CODE[A.dtype]
+
+
+def dybit_adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, alpha: Optional[torch.Tensor], plan: AdapterPlan,
+                   base: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                   want_v: bool = False, v: Optional[torch.Tensor] = None, stream=None):
+    """y[t] = base[t] + alpha_a * (x[t] A_a^T) B_a with a the adapter of token t: x [T][K], A [n][R][K], B [n][R][N].
+    out may be base.  Returns (y [T][N], V [T][R] float32 or None); V is what dybit_adapters_backward takes."""
+    R, K, N, tw = _factors(A, B, alpha, plan)
+    T = plan.T
+    tx = _matrix(x, "x", K, T)
+    if base is not None:
+        tb = _matrix(base, "base", N, T)
+    if out is None:
+        out = torch.empty((T, N), dtype=base.dtype if base is not None else (out_dtype or x.dtype), device=x.device)
+    ty = _matrix(out, "out", N, T)
+    if base is not None and tb != ty:
+        raise ValueError("base and out must have one dtype")
+    if want_v and v is None:
+        v = torch.empty((T, R), dtype=torch.float32, device=x.device)
+    if v is not None and (v.dtype != torch.float32 or not v.is_cuda or not v.is_contiguous() or tuple(v.shape) != (T, R)):
+        raise ValueError("v must be a contiguous float32 CUDA tensor [T][R]")
+    _check(lib.dybit_adapters(T, K, N, R, x.data_ptr(), tx, _ld(x), plan.n, A.data_ptr(), B.data_ptr(), tw,
+                              None if alpha is None else alpha.data_ptr(), plan.buffer.data_ptr(),
+                              None if base is None else base.data_ptr(), 0 if base is None else _ld(base), ty, out.data_ptr(),
+                              _ld(out), None if v is None else v.data_ptr(), _stream(stream)), "dybit_adapters")
+    return out, v
+
+
+def dybit_adapters_backward_workspace_bytes(T: int, K: int, N: int, R: int, n_adapters: int) -> int:
+    return int(lib.dybit_adapters_backward_workspace_bytes(int(T), int(K), int(N), int(R), int(n_adapters)))
+
+
+def dybit_adapters_backward(dY: torch.Tensor, codes: torch.Tensor, fmt, scales: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
+                            alpha: Optional[torch.Tensor], plan: AdapterPlan, v: torch.Tensor,
+                            dx_base: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                            dA: Optional[torch.Tensor] = None, dB: Optional[torch.Tensor] = None,
+                            per_row: bool = True, ws: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of dybit_adapters with its input read from an 8-bit checkpoint (codes [T][row bytes], scales).  dx may
+    be dx_base.  Returns (dx [T][K] like dY, dA [n][R][K] float32, dB [n][R][N] float32)."""
+    R, K, N, tw = _factors(A, B, alpha, plan)
+    T, n = plan.T, plan.n
+    t = _matrix(dY, "dY", N, T)
+    stride, _ = _codes8(codes, T, K, scales)
+    if v.dtype != torch.float32 or not v.is_cuda or not v.is_contiguous() or tuple(v.shape) != (T, R):
+        raise ValueError("v must be a contiguous float32 CUDA tensor [T][R]")
+    if dx is None:
+        dx = torch.empty((T, K), dtype=dY.dtype, device=dY.device)
+    if _matrix(dx, "dx", K, T) != t or (dx_base is not None and _matrix(dx_base, "dx_base", K, T) != t):
+        raise ValueError("dx and dx_base must have dY's dtype")
+    if dA is None:
+        dA = torch.empty((n, R, K), dtype=torch.float32, device=dY.device)
+    if dB is None:
+        dB = torch.empty((n, R, N), dtype=torch.float32, device=dY.device)
+    for g, like in ((dA, A), (dB, B)):
+        if g.dtype != torch.float32 or not g.is_cuda or not g.is_contiguous() or g.shape != like.shape:
+            raise ValueError("dA and dB must be contiguous float32 CUDA tensors shaped like A and B")
+    at, size, ws = _workspace(lib.dybit_adapters_backward_workspace_bytes(T, K, N, R, n), ws, dY.device)
+    _check(lib.dybit_adapters_backward(T, K, N, R, dY.data_ptr(), t, _ld(dY), codes.data_ptr(), stride, _fmt(fmt),
+                                       scales.data_ptr(), _scale_stride(scales, T, per_row), n, A.data_ptr(), B.data_ptr(), tw,
+                                       None if alpha is None else alpha.data_ptr(), plan.buffer.data_ptr(), v.data_ptr(),
+                                       None if dx_base is None else dx_base.data_ptr(), 0 if dx_base is None else _ld(dx_base),
+                                       dx.data_ptr(), _ld(dx), dA.data_ptr(), dB.data_ptr(), at, size, _stream(stream)),
+           "dybit_adapters_backward")
+    return dx, dA, dB

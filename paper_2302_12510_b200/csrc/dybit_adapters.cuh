@@ -1,0 +1,781 @@
+// Low-rank adapters of many requests beside a shared projection, and their gradients.
+//
+//   forward    V_t = A_a x_t,             y_t  = base_t   + sum_r alpha_a V_t[r] B_a[r]
+//   backward   U_t = alpha_a B_a dY_t,    dX_t = dXbase_t + sum_r U_t[r] A_a[r],
+//              dA_a = sum_t U_t^T x^_t,   dB_a = sum_t alpha_a V_t^T dY_t
+// With both factors rank-major the two lines that map tokens to tokens are one operator with the factors exchanged
+// (adapter_tokens_kernel); the two gradients are one more (adapter_grad_kernel).
+//
+// All of it is bound by memory: a token costs 4 R multiplications per element read, R = 8 .. 128.  The products run on
+// mma.sync, which takes its operands from registers: a tcgen05 tile would have to stage every element in shared memory
+// (and the codes once more as bf16) for 128 x 8..64 outputs, and its 128 rows would be mostly empty in a decode step.
+#pragma once
+
+#include "dybit_adapters_plan.cuh"
+#include "dybit_checkpoint.cuh"
+#include "dybit_code8.cuh"
+#include "dybit_sm100.cuh"
+
+namespace dybit {
+
+using namespace sm100;
+
+// ------------------------------------------------------------------ matrix instructions on registers
+
+template <typename TW>
+__device__ __forceinline__ void mma16(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+    if constexpr (sizeof(TW) == 2 && __is_same(TW, __half)) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    } else {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    }
+}
+
+__device__ __forceinline__ void mma8_tf32(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// What is left of x after its leading part `head`; nothing of an infinity (whose difference would be NaN).
+__device__ __forceinline__ float rest_of(float x, float head) {
+    return fabsf(x) == __uint_as_float(0x7f800000u) ? 0.0f : __fsub_rn(x, head);
+}
+__device__ __forceinline__ float top16(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+
+// Two fp32 numbers as three pairs of bf16 whose sums they are: eight significand bits each, cut off, so 24 in all and
+// nothing is lost (down to bf16's smallest numbers).
+__device__ __forceinline__ void split3(float x, float y, unsigned &hi, unsigned &mid, unsigned &lo) {
+    hi = __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632);
+    const float x1 = rest_of(x, top16(x)), y1 = rest_of(y, top16(y));
+    mid = __byte_perm(__float_as_uint(x1), __float_as_uint(y1), 0x7632);
+    lo = pack_bf16(__fsub_rn(x1, top16(x1)), __fsub_rn(y1, top16(y1)));
+}
+
+// ------------------------------------------------------------------ tokens -> tokens
+
+struct AdapterTokens {
+    const void *x;               // tokens x K
+    int64_t ldx;
+    const void *w1, *w2;         // n x R x K, n x R x N
+    const float *alpha;
+    const int *plan;
+    const void *base;
+    int64_t ldbase;
+    void *y;
+    int64_t ldy;
+    float *v_out;                // forward: tokens x R, or null
+    int64_t T, K, N;
+    int n, R;
+    int vec_x, vec_w1, vec_y, vec_w2;      // rows can be moved in vectors (16 bytes; 4 elements for y and w2)
+    // backward: fragments for adapter_grad_kernel
+    const float *v_in;
+    const float *scales;
+    int64_t scale_stride;
+    uint4 *frag_u, *frag_v;
+};
+
+// Sixteen consecutive elements of a row at column k (the lane's share of a 64-column block), as raw words.
+template <typename T, int WORDS>
+__device__ __forceinline__ void load16(unsigned (&w)[WORDS], const T *row, int64_t k, int64_t K, bool vec, bool there) {
+    static_assert(WORDS == 4 * (int)sizeof(T), "sixteen elements");
+    constexpr int E = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < WORDS / 4; ++i) {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        const int64_t c = k + i * E;
+        if (there && c < K) {
+            if (vec && c + E <= K) {
+                v = __ldg(reinterpret_cast<const uint4 *>(row + c));
+            } else {
+                T e[E];
+#pragma unroll
+                for (int j = 0; j < E; ++j) e[j] = c + j < K ? row[c + j] : from_f32<T>(0.0f);
+                v = *reinterpret_cast<const uint4 *>(e);
+            }
+        }
+        w[4 * i] = v.x;
+        w[4 * i + 1] = v.y;
+        w[4 * i + 2] = v.z;
+        w[4 * i + 3] = v.w;
+    }
+}
+
+// Four consecutive elements of a row as floats, zeros beyond `cols`.
+template <typename T>
+__device__ __forceinline__ float4 load4(const T *row, int64_t c, int64_t cols, bool vec) {
+    if (c >= cols) return make_float4(0.f, 0.f, 0.f, 0.f);
+    if (vec && c + 4 <= cols) {
+        if constexpr (sizeof(T) == 4) {
+            return *reinterpret_cast<const float4 *>(row + c);
+        } else {
+            const uint2 v = *reinterpret_cast<const uint2 *>(row + c);
+            const float2 a = unpack2<T>(v.x), b = unpack2<T>(v.y);
+            return make_float4(a.x, a.y, b.x, b.y);
+        }
+    }
+    float f[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = c + j < cols ? to_f32(row[c + j]) : 0.0f;
+    return make_float4(f[0], f[1], f[2], f[3]);
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T *row, int64_t c, int64_t cols, bool vec, const float4 f) {
+    if (c >= cols) return;
+    if (vec && c + 4 <= cols) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(row + c) = f;
+        else *reinterpret_cast<uint2 *>(row + c) = make_uint2(pack2<T>(f.x, f.y), pack2<T>(f.z, f.w));
+        return;
+    }
+    const float e[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (c + j < cols) row[c + j] = from_f32<T>(e[j]);
+}
+
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+__device__ __forceinline__ uint32_t cluster_nctarank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
+// Fragments of a 16 (ranks) x 16 (tokens) block for adapter_grad_kernel: lane (g, q) of the reader takes ranks g, g + 8
+// and tokens 4q .. 4q + 3; three uint4 (leading, middle and last bf16 parts) of 32 lanes follow one another.
+__device__ __forceinline__ void store_fragment(uint4 *frag, int lane, const float (&f0)[4], const float (&f1)[4]) {
+    uint4 part[3];
+    split3(f0[0], f0[1], part[0].x, part[1].x, part[2].x);
+    split3(f1[0], f1[1], part[0].y, part[1].y, part[2].y);
+    split3(f0[2], f0[3], part[0].z, part[1].z, part[2].z);
+    split3(f1[2], f1[3], part[0].w, part[1].w, part[2].w);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) frag[i * 32 + lane] = part[i];
+}
+
+constexpr int kTokWarps = 8;
+constexpr int kTokThreads = kTokWarps * 32;
+
+template <int RT, int MT>
+struct TokSmem {
+    static constexpr int kTile = 16 * MT * RT;                 // floats of one token tile of V
+    static constexpr int kPad = RT + 4;                        // row of the tile that feeds the second product
+    static constexpr int kBytes = (kTokWarps * kTile + kTile + 16 * MT * kPad) * 4;
+};
+
+// One cluster per tile of up to 16 * MT tokens of one adapter.  Its CTAs share the columns of x in the first product
+// and those of y in the second; in between they sum up their parts of V through distributed shared memory.  RT is the
+// rank rounded up (16, 32, 64, 128); missing ranks, tokens and columns are read as zeros.
+//
+// First product: a warp takes 64 columns at a time.  Lane (g = lane / 4, q = lane % 4) loads columns 16q .. 16q+15 of
+// token rows g, g + 8 and of factor rows g (+ 8 per n-tile) with 16-byte loads and uses them as the four K = 16 slices
+// of the fragment layout: the order of columns inside a sum is free as long as both operands take the same.
+// Second product: tf32, with V cut into two tf32 numbers (what is left over is below 2^-21 of V; the factors are exact
+// in tf32).  The 64 columns of a warp are dealt to fragment columns so that a lane ends up with four consecutive ones.
+template <typename TX, typename TW, typename TY, int RT, int MT, bool BWD>
+__global__ void __launch_bounds__(kTokThreads, 2) adapter_tokens_kernel(const AdapterTokens p) {
+    constexpr int NT = RT / 8, TM = 16 * MT, XW = 4 * (int)sizeof(TX);
+    using Smem = TokSmem<RT, MT>;
+    extern __shared__ __align__(16) float smem_f[];
+    float *s_warp = smem_f;                                    // [warps][TM][RT]
+    float *s_part = smem_f + kTokWarps * Smem::kTile;          // [TM][RT], read by the whole cluster
+    float *s_v = s_part + Smem::kTile;                         // [TM][RT + 4]
+    __shared__ int s_token[TM];
+    pdl_enter();
+    const PlanLayout L(p.T, p.n);
+    const int cs = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
+    const int tile_id = (int)blockIdx.x / cs;
+    constexpr int kList = MT == 1 ? 0 : (MT == 2 ? 1 : 2);
+    if (tile_id >= p.plan[kList]) return;                      // the whole cluster
+    const AdapterTile tile = reinterpret_cast<const AdapterTile *>(p.plan + L.tiles[kList])[tile_id];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    const int R = p.R;
+    if (threadIdx.x < TM) s_token[threadIdx.x] = threadIdx.x < tile.count ? p.plan[L.perm + tile.start + threadIdx.x] : -1;
+    __syncthreads();
+
+    if (tile.adapter >= 0) {
+        // ---- V = x A^T over this CTA's columns, this warp's blocks of 64
+        const TW *w1 = static_cast<const TW *>(p.w1) + (int64_t)tile.adapter * R * p.K;
+        const int blocks = (int)((p.K + 63) / 64), per = (blocks + cs - 1) / cs;
+        const int last = min(blocks, (rank + 1) * per);
+        float acc[MT][NT][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
+        for (int b = rank * per + warp; b < last; b += kTokWarps) {
+            const int64_t k = (int64_t)b * 64 + q * 16;
+            unsigned w[NT][8];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) load16<TW, 8>(w[j], w1 + (int64_t)(j * 8 + g) * p.K, k, p.K, p.vec_w1, j * 8 + g < R);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                if (m * 16 >= tile.count) break;
+                const int t0 = s_token[m * 16 + g], t1 = s_token[m * 16 + g + 8];
+                unsigned x0[XW], x1[XW];
+                load16<TX, XW>(x0, static_cast<const TX *>(p.x) + (int64_t)t0 * p.ldx, k, p.K, p.vec_x, t0 >= 0);
+                load16<TX, XW>(x1, static_cast<const TX *>(p.x) + (int64_t)t1 * p.ldx, k, p.K, p.vec_x, t1 >= 0);
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    if constexpr (sizeof(TX) == 2) {
+#pragma unroll
+                        for (int j = 0; j < NT; ++j)
+                            mma16<TW>(acc[m][j], x0[2 * s], x1[2 * s], x0[2 * s + 1], x1[2 * s + 1], w[j][2 * s], w[j][2 * s + 1]);
+                    } else {
+                        unsigned a[4][3];
+                        split3(__uint_as_float(x0[4 * s]), __uint_as_float(x0[4 * s + 1]), a[0][0], a[0][1], a[0][2]);
+                        split3(__uint_as_float(x1[4 * s]), __uint_as_float(x1[4 * s + 1]), a[1][0], a[1][1], a[1][2]);
+                        split3(__uint_as_float(x0[4 * s + 2]), __uint_as_float(x0[4 * s + 3]), a[2][0], a[2][1], a[2][2]);
+                        split3(__uint_as_float(x1[4 * s + 2]), __uint_as_float(x1[4 * s + 3]), a[3][0], a[3][1], a[3][2]);
+#pragma unroll
+                        for (int i = 2; i >= 0; --i)
+#pragma unroll
+                            for (int j = 0; j < NT; ++j)
+                                mma16<TW>(acc[m][j], a[0][i], a[1][i], a[2][i], a[3][i], w[j][2 * s], w[j][2 * s + 1]);
+                    }
+                }
+            }
+        }
+        // ---- sum over the warps, then over the cluster
+        float *mine = s_warp + warp * Smem::kTile;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                *reinterpret_cast<float2 *>(mine + (m * 16 + g) * RT + j * 8 + 2 * q) = make_float2(acc[m][j][0], acc[m][j][1]);
+                *reinterpret_cast<float2 *>(mine + (m * 16 + g + 8) * RT + j * 8 + 2 * q) = make_float2(acc[m][j][2], acc[m][j][3]);
+            }
+        __syncthreads();
+        for (int i = threadIdx.x; i < Smem::kTile / 4; i += kTokThreads) {
+            float4 s = reinterpret_cast<const float4 *>(s_warp)[i];
+#pragma unroll
+            for (int w = 1; w < kTokWarps; ++w) {
+                const float4 o = reinterpret_cast<const float4 *>(s_warp + w * Smem::kTile)[i];
+                s.x += o.x;
+                s.y += o.y;
+                s.z += o.z;
+                s.w += o.w;
+            }
+            reinterpret_cast<float4 *>(s_part)[i] = s;
+        }
+        cluster_arrive();
+        cluster_wait();
+        const float alpha = p.alpha != nullptr ? __ldg(p.alpha + tile.adapter) : 1.0f;
+        for (int i = threadIdx.x; i < Smem::kTile / 4; i += kTokThreads) {
+            const uint32_t here = smem_u32(s_part + 4 * i);
+            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int c = 0; c < cs; ++c) {
+                const float4 o = ld_cluster_f4(mapa_u32(here, (uint32_t)c));
+                s.x += o.x;
+                s.y += o.y;
+                s.z += o.z;
+                s.w += o.w;
+            }
+            const int row = 4 * i / RT, r = 4 * i % RT;
+            if (!BWD && p.v_out != nullptr && rank == 0 && row < tile.count && r < R)
+                *reinterpret_cast<float4 *>(p.v_out + (int64_t)s_token[row] * R + r) = s;
+            *reinterpret_cast<float4 *>(s_v + row * Smem::kPad + r) = make_float4(alpha * s.x, alpha * s.y, alpha * s.z, alpha * s.w);
+        }
+        cluster_arrive();                                      // (waited for before the CTA leaves)
+        __syncthreads();
+        if constexpr (BWD) {
+            // U (times the row's scale) from CTA 0, alpha V from CTA 1 or the same
+            const int steps = (tile.count + 15) / 16, mtr = (R + 15) / 16;
+            for (int half = 0; half < 2; ++half) {
+                if (rank != half % cs) continue;
+                for (int i = warp; i < steps * mtr; i += kTokWarps) {
+                    const int st = i / mtr, m = i % mtr;
+                    float f[2][4];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int row = st * 16 + 4 * q + e, r = m * 16 + g + 8 * h;
+                            float v = 0.0f;
+                            if (row < tile.count && r < R) {
+                                const int64_t t = s_token[row];
+                                if (half == 0) v = s_v[row * Smem::kPad + r] * (p.scales != nullptr ? __ldg(p.scales + t * p.scale_stride) : 1.0f);
+                                else v = alpha * __ldg(p.v_in + t * R + r);
+                            }
+                            f[h][e] = v;
+                        }
+                    store_fragment((half == 0 ? p.frag_u : p.frag_v) + ((int64_t)(tile.step + st) * mtr + m) * 96, lane, f[0], f[1]);
+                }
+            }
+        }
+    } else if (!BWD && p.v_out != nullptr && rank == 0) {
+        for (int i = threadIdx.x; i < tile.count * R; i += kTokThreads) p.v_out[(int64_t)s_token[i / R] * R + i % R] = 0.0f;
+    }
+
+    // ---- y = base + V B over this CTA's groups of 64 columns
+    const TW *w2 = static_cast<const TW *>(p.w2) + (int64_t)max(tile.adapter, 0) * R * p.N;
+    const int groups = (int)((p.N + 63) / 64), slices = tile.adapter >= 0 ? R / 8 : 0;
+    const int gcol = (g & 1) * 16 + (g >> 1) * 4;              // the lane's columns as fragment column g: + jh * 32 + jl
+    for (int gi = rank * kTokWarps + warp; gi < groups; gi += cs * kTokWarps) {
+        const int64_t n0 = (int64_t)gi * 64;
+#pragma unroll 1
+        for (int m = 0; m < MT; ++m) {
+            if (m * 16 >= tile.count) break;
+            int tok[2] = {s_token[m * 16 + g], s_token[m * 16 + g + 8]};
+            float4 out[2][4];                                  // base first: [row][jh * 2 + b]
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    out[h][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (p.base != nullptr && tok[h] >= 0)
+                        out[h][i] = load4<TY>(static_cast<const TY *>(p.base) + (int64_t)tok[h] * p.ldbase, n0 + i * 16 + q * 4, p.N, p.vec_y);
+                }
+            float acc[8][4];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[j][i] = 0.0f;
+#pragma unroll 2
+            for (int s = 0; s < slices; ++s) {
+                const float *row0 = s_v + (m * 16 + g) * Smem::kPad + s * 8 + q, *row1 = row0 + 8 * Smem::kPad;
+                const float av[4] = {row0[0], row1[0], row0[4], row1[4]};
+                unsigned hi[4], lo[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    hi[i] = __float_as_uint(av[i]) & 0xffffe000u;
+                    lo[i] = __float_as_uint(rest_of(av[i], __uint_as_float(hi[i])));
+                }
+                const TW *b0 = w2 + (int64_t)(s * 8 + q) * p.N, *b1 = b0 + 4 * p.N;
+#pragma unroll
+                for (int jh = 0; jh < 2; ++jh) {
+                    const float4 f0 = load4<TW>(b0, n0 + jh * 32 + gcol, p.N, p.vec_w2), f1 = load4<TW>(b1, n0 + jh * 32 + gcol, p.N, p.vec_w2);
+                    const float e0[4] = {f0.x, f0.y, f0.z, f0.w}, e1[4] = {f1.x, f1.y, f1.z, f1.w};
+#pragma unroll
+                    for (int jl = 0; jl < 4; ++jl) {
+                        mma8_tf32(acc[jh * 4 + jl], lo[0], lo[1], lo[2], lo[3], __float_as_uint(e0[jl]), __float_as_uint(e1[jl]));
+                        mma8_tf32(acc[jh * 4 + jl], hi[0], hi[1], hi[2], hi[3], __float_as_uint(e0[jl]), __float_as_uint(e1[jl]));
+                    }
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (tok[h] < 0) continue;
+                TY *row = static_cast<TY *>(p.y) + (int64_t)tok[h] * p.ldy;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int jh = i >> 1, b = i & 1;
+                    float4 o = out[h][i];
+                    o.x += acc[jh * 4][2 * h + b];
+                    o.y += acc[jh * 4 + 1][2 * h + b];
+                    o.z += acc[jh * 4 + 2][2 * h + b];
+                    o.w += acc[jh * 4 + 3][2 * h + b];
+                    store4<TY>(row, n0 + i * 16 + q * 4, p.N, p.vec_y, o);
+                }
+            }
+        }
+    }
+    if (tile.adapter >= 0) cluster_wait();                     // the others may still read this CTA's part of V
+}
+
+// ------------------------------------------------------------------ gradients of the factors
+
+enum class GradSrc { CodesSigned, CodesUnsigned, Bf16, F32 };
+
+struct AdapterGradSide {
+    const void *src;             // tokens x cols: codes or dY
+    int64_t ld;                  // elements (bytes for codes)
+    int64_t cols;
+    const uint4 *frag;           // fragments of the left operand, by step
+    float *out;                  // n x R x cols
+    float *partial;              // partial slots x R x cols
+    int vec;
+};
+struct AdapterGrad {
+    AdapterGradSide side[2];     // 0: dA from the codes, 1: dB from dY
+    const int *plan;
+    int64_t T;
+    int n, R;
+    int blocks0;                 // blocks along x that belong to side 0
+    int wc;                      // groups of 64 columns per block: 1, 2 or 4; the other warps share the tokens
+};
+
+// Eight columns of one token row.
+template <GradSrc S> struct SrcWords { static constexpr int n = S == GradSrc::F32 ? 8 : (S == GradSrc::Bf16 ? 4 : 2); };
+template <GradSrc S>
+__device__ __forceinline__ void load_src8(unsigned (&w)[SrcWords<S>::n], const void *src, int64_t ld, int token, int64_t c, int64_t cols, bool vec) {
+    constexpr int W = SrcWords<S>::n;
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = 0u;
+    if (token < 0 || c >= cols) return;
+    if constexpr (W == 2) {                                    // rows of codes are padded to 16: eight are always there
+        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(src) + (int64_t)token * ld + c));
+        w[0] = v.x;
+        w[1] = v.y;
+    } else {
+        using T = typename Elem<S == GradSrc::F32 ? DYBIT_F32 : DYBIT_BF16>::type;
+        const T *row = static_cast<const T *>(src) + (int64_t)token * ld + c;
+        if (vec && c + 8 <= cols) {
+#pragma unroll
+            for (int i = 0; i < W / 4; ++i) {
+                const uint4 v = __ldg(reinterpret_cast<const uint4 *>(row) + i);
+                w[4 * i] = v.x;
+                w[4 * i + 1] = v.y;
+                w[4 * i + 2] = v.z;
+                w[4 * i + 3] = v.w;
+            }
+        } else {
+            T e[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = c + j < cols ? row[j] : from_f32<T>(0.0f);
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[i] = reinterpret_cast<const unsigned *>(e)[i];
+        }
+    }
+}
+
+// Column j (0 .. 7) of two token rows as pairs of bf16: the number of parts it takes to hold them exactly.
+template <GradSrc S> struct SrcParts { static constexpr int n = S == GradSrc::F32 ? 3 : 1; };
+template <GradSrc S>
+__device__ __forceinline__ void src_pair(unsigned (&o)[SrcParts<S>::n], const unsigned (&a)[SrcWords<S>::n], const unsigned (&b)[SrcWords<S>::n], int j) {
+    if constexpr (S == GradSrc::F32) {
+        split3(__uint_as_float(a[j]), __uint_as_float(b[j]), o[0], o[1], o[2]);
+    } else if constexpr (S == GradSrc::Bf16) {
+        o[0] = __byte_perm(a[j / 2], b[j / 2], j % 2 ? 0x7632 : 0x5410);
+    } else {
+        const unsigned w = __byte_perm(a[j / 4], b[j / 4], 0x0400u + (unsigned)(j % 4) * 0x0101u);   // code j of a, code j of b in bytes 0 and 2
+        o[0] = decode2<S == GradSrc::CodesSigned>(w);
+    }
+}
+
+// sum over a chunk's tokens of left[r] * src[column]: 16 * MR ranks x 64 columns per warp.  Lane (g, q) reads columns
+// 8g .. 8g+7 of token rows 4q .. 4q+3 of a 16-token step straight from memory; two rows interleave into the fragment's
+// K pairs (for codes that is the byte permutation that starts their decoding).
+template <GradSrc S, int MR>
+__device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const AdapterGradSide &sd, int block, const AdapterChunk &ch, int r0, float *smem) {
+    constexpr int W = SrcWords<S>::n, P = SrcParts<S>::n;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    const int wc = warp % p.wc, wt = warp / p.wc, ntg = kTokWarps / p.wc;
+    const int64_t c0 = ((int64_t)block * p.wc + wc) * 64;
+    const int mtr = (p.R + 15) / 16, steps = (ch.count + 15) / 16;
+    const int *perm = p.plan + PlanLayout(p.T, p.n).perm + ch.start;
+    float acc[MR][8][4];
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
+    for (int st = wt; st < steps; st += ntg) {
+        unsigned src[4][W];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int row = st * 16 + 4 * q + e;
+            load_src8<S>(src[e], sd.src, sd.ld, row < ch.count ? __ldg(perm + row) : -1, c0 + 8 * g, sd.cols, sd.vec);
+        }
+        uint4 a[MR][3];
+#pragma unroll
+        for (int m = 0; m < MR; ++m)
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                a[m][i] = r0 + m < mtr ? __ldg(sd.frag + (((int64_t)(ch.step + st) * mtr + r0 + m) * 3 + i) * 32 + lane) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            unsigned b0[P], b1[P];
+            src_pair<S>(b0, src[0], src[1], j);
+            src_pair<S>(b1, src[2], src[3], j);
+#pragma unroll
+            for (int m = 0; m < MR; ++m)
+#pragma unroll
+                for (int i = 2; i >= 0; --i)
+#pragma unroll
+                    for (int k = P - 1; k >= 0; --k)
+                        if (i + k <= 2) mma16<__nv_bfloat16>(acc[m][j], a[m][i].x, a[m][i].y, a[m][i].z, a[m][i].w, b0[k], b1[k]);
+        }
+    }
+    // the token groups' sums meet in shared memory, added in order
+    constexpr int kWarpTile = MR * 16 * 64;
+    if (ntg > 1) {
+        if (wt > 0) {
+            float *mine = smem + (size_t)((wt - 1) * p.wc + wc) * kWarpTile;
+#pragma unroll
+            for (int m = 0; m < MR; ++m)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    *reinterpret_cast<float4 *>(mine + ((m * 8 + j) * 32 + lane) * 4) = make_float4(acc[m][j][0], acc[m][j][1], acc[m][j][2], acc[m][j][3]);
+        }
+        __syncthreads();
+        if (wt > 0) return;
+        for (int o = 1; o < ntg; ++o) {
+            const float *other = smem + (size_t)((o - 1) * p.wc + wc) * kWarpTile;
+#pragma unroll
+            for (int m = 0; m < MR; ++m)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float4 f = *reinterpret_cast<const float4 *>(other + ((m * 8 + j) * 32 + lane) * 4);
+                    acc[m][j][0] += f.x;
+                    acc[m][j][1] += f.y;
+                    acc[m][j][2] += f.z;
+                    acc[m][j][3] += f.w;
+                }
+        }
+    }
+    float *out = ch.partial >= 0 ? sd.partial + (int64_t)ch.partial * p.R * sd.cols : sd.out + (int64_t)ch.adapter * p.R * sd.cols;
+    const bool vec = sd.cols % 4 == 0 && aligned16(out);
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = (r0 + m) * 16 + g + 8 * h;
+            if (r >= p.R) continue;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int j = 0; j < 8; j += 4)
+                    store4<float>(out + (int64_t)r * sd.cols, c0 + (2 * q + b) * 8 + j, sd.cols, vec,
+                                  make_float4(acc[m][j][2 * h + b], acc[m][j + 1][2 * h + b], acc[m][j + 2][2 * h + b], acc[m][j + 3][2 * h + b]));
+        }
+}
+
+// blockIdx: x = columns (side 0, then side 1), y = chunk, z = ranks beyond 16 * MR.
+template <GradSrc S0, GradSrc S1, int MR>
+__global__ void __launch_bounds__(kTokThreads, MR <= 2 ? 2 : 1) adapter_grad_kernel(const __grid_constant__ AdapterGrad p) {
+    extern __shared__ __align__(16) float smem_f[];
+    pdl_enter();
+    if ((int)blockIdx.y >= p.plan[3]) return;
+    const AdapterChunk ch = reinterpret_cast<const AdapterChunk *>(p.plan + PlanLayout(p.T, p.n).chunks)[blockIdx.y];
+    const int r0 = (int)blockIdx.z * MR;
+    if ((int)blockIdx.x < p.blocks0) adapter_grad_body<S0, MR>(p, p.side[0], (int)blockIdx.x, ch, r0, smem_f);
+    else adapter_grad_body<S1, MR>(p, p.side[1], (int)blockIdx.x - p.blocks0, ch, r0, smem_f);
+}
+
+// Adapters with several chunks: the chunks' sums, added in order; adapters without tokens: zeros.
+__global__ void __launch_bounds__(256) adapter_grad_sum_kernel(const __grid_constant__ AdapterGrad p) {
+    pdl_enter();
+    const int a = blockIdx.y;
+    const int *off = p.plan + PlanLayout(p.T, p.n).offsets + (int64_t)a * kPlanColumns;
+    const int chunks = off[kPlanColumns + 4] - off[4], first = off[5];
+    if (chunks == 1) return;
+    for (int s = 0; s < 2; ++s) {
+        const AdapterGradSide &sd = p.side[s];
+        const int64_t size = p.R * sd.cols;                    // a multiple of 8
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size / 4; i += (int64_t)gridDim.x * 256) {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int c = 0; c < chunks; ++c) {
+                const float4 o = __ldcg(reinterpret_cast<const float4 *>(sd.partial + (int64_t)(first + c) * size) + i);
+                v.x += o.x;
+                v.y += o.y;
+                v.z += o.z;
+                v.w += o.w;
+            }
+            float *dst = sd.out + a * size + 4 * i;
+            if (aligned16(dst)) {
+                *reinterpret_cast<float4 *>(dst) = v;
+            } else {
+                dst[0] = v.x;
+                dst[1] = v.y;
+                dst[2] = v.z;
+                dst[3] = v.w;
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ host side
+
+static bool rows_vec(const void *p, int64_t ld, int elem, int bytes) { return aligned(p, bytes) && (ld * elem) % bytes == 0; }
+
+constexpr int kMaxClusterCtas = 8;
+
+template <typename TX, typename TW, typename TY, int RT, int MT, bool BWD>
+static dybit_status launch_tokens(const AdapterTokens &p, int cs, cudaStream_t s) {
+    auto kern = adapter_tokens_kernel<TX, TW, TY, RT, MT, BWD>;
+    constexpr int smem = TokSmem<RT, MT>::kBytes;
+    static std::atomic<bool> ready[64];
+    int dev = 0;
+    DYBIT_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return DYBIT_ERR_CUDA;
+    if (!ready[dev].load(std::memory_order_acquire)) {
+        DYBIT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        ready[dev].store(true, std::memory_order_release);
+    }
+    const PlanLayout L(p.T, p.n);
+    const int64_t blocks = L.tiles_cap[MT == 1 ? 0 : (MT == 2 ? 1 : 2)] * cs;
+    if (blocks > 0x7fffffff) return DYBIT_ERR_UNSUPPORTED;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(kTokThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cs;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    (void)cudaLaunchKernelEx(&cfg, kern, p);
+    return launch_status();
+}
+
+template <typename TX, typename TW, typename TY, bool BWD>
+static dybit_status launch_tokens_rank(const AdapterTokens &p, cudaStream_t s) {
+    // tiles of several 16-token slices read the factors once for all of them: worth it where adapters have that many tokens
+    const bool many = p.T >= 32 * (int64_t)p.n;
+    const int cs = kMaxClusterCtas;
+    if (p.R <= 16) return many ? launch_tokens<TX, TW, TY, 16, 4, BWD>(p, cs, s) : launch_tokens<TX, TW, TY, 16, 1, BWD>(p, cs, s);
+    if (p.R <= 32) return many ? launch_tokens<TX, TW, TY, 32, 4, BWD>(p, cs, s) : launch_tokens<TX, TW, TY, 32, 1, BWD>(p, cs, s);
+    if (p.R <= 64) return many ? launch_tokens<TX, TW, TY, 64, 2, BWD>(p, cs, s) : launch_tokens<TX, TW, TY, 64, 1, BWD>(p, cs, s);
+    return launch_tokens<TX, TW, TY, 128, 1, BWD>(p, cs, s);
+}
+
+template <GradSrc S0, GradSrc S1>
+static dybit_status launch_grad(const AdapterGrad &p_in, cudaStream_t s) {
+    AdapterGrad p = p_in;
+    const PlanLayout L(p.T, p.n);
+    const int mtr = (p.R + 15) / 16, mr = mtr >= 3 ? 4 : mtr, z = (mtr + mr - 1) / mr;
+    // wide blocks read longer runs of a row and the left operand less often; narrow ones fill the device
+    p.wc = 4;
+    auto blocks = [&](int side) { return (p.side[side].cols + 64 * p.wc - 1) / (64 * p.wc); };
+    while (p.wc > 1 && (blocks(0) + blocks(1)) * L.chunks_cap * z < sm_count()) p.wc /= 2;
+    p.blocks0 = (int)blocks(0);
+    const int64_t bx = blocks(0) + blocks(1);
+    if (bx > 0x7fffffff || L.chunks_cap > 65535) return DYBIT_ERR_UNSUPPORTED;
+    const int smem = (kTokWarps - p.wc) * mr * 16 * 64 * 4;
+    auto go = [&](auto kern) {
+        DYBIT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        launch_k(kern, dim3((unsigned)bx, (unsigned)L.chunks_cap, (unsigned)z), dim3(kTokThreads), (size_t)smem, s, p);
+        return launch_status();
+    };
+    dybit_status st;
+    if (L.chunks_cap > 0) {
+        if (mr == 1) st = go(adapter_grad_kernel<S0, S1, 1>);
+        else if (mr == 2) st = go(adapter_grad_kernel<S0, S1, 2>);
+        else st = go(adapter_grad_kernel<S0, S1, 4>);
+        if (st != DYBIT_OK) return st;
+    }
+    const int64_t most = p.side[0].cols > p.side[1].cols ? p.side[0].cols : p.side[1].cols;
+    int64_t bs = (p.R * most / 4 + 255) / 256;
+    if (bs > 64) bs = 64;
+    if (bs < 1) bs = 1;
+    launch_k(adapter_grad_sum_kernel, dim3((unsigned)bs, (unsigned)p.n), dim3(256), 0, s, p);
+    return launch_status();
+}
+
+static dybit_status check_adapters(int64_t T, int64_t K, int64_t N, int R, int n, const void *A, const void *B, dybit_dtype tw,
+                                   const float *alpha, const void *plan) {
+    if (T < 0 || K < 1 || N < 1 || K > 0x7fffffff || N > 0x7fffffff || R < 8 || dybit_adapters_plan_bytes(T, n) == 0) return DYBIT_ERR_INVALID_ARG;
+    if (R % 8 != 0 || R > DYBIT_MAX_RANK) return DYBIT_ERR_UNSUPPORTED;
+    if (A == nullptr || B == nullptr || plan == nullptr) return DYBIT_ERR_INVALID_ARG;
+    if (!dtype_ok(tw)) return DYBIT_ERR_INVALID_ARG;
+    if (!aligned(A, 2) || !aligned(B, 2) || !aligned(plan, 16) || !aligned(alpha, 4)) return DYBIT_ERR_ALIGNMENT;
+    return DYBIT_OK;
+}
+
+struct BackwardWs {
+    int64_t frag_u, frag_v, partial_a, partial_b, bytes;
+    BackwardWs(int64_t T, int64_t K, int64_t N, int R, int n) {
+        const PlanLayout L(T, n);
+        const int64_t frag = L.steps_cap * ((R + 15) / 16) * 3 * 512;
+        int64_t at = 0;
+        frag_u = at, at += round_up(frag, 1024);
+        frag_v = at, at += round_up(frag, 1024);
+        partial_a = at, at += round_up(L.partials_cap * R * K * 4, 1024);
+        partial_b = at, at += round_up(L.partials_cap * R * N * 4, 1024);
+        bytes = at + 1024;
+    }
+};
+
+}  // namespace dybit
+
+extern "C" {
+
+dybit_status dybit_adapters(int64_t T, int64_t K, int64_t N, int R, const void *X, dybit_dtype tx, int64_t ldx,
+                            int n_adapters, const void *A, const void *B, dybit_dtype tw, const float *alpha,
+                            const void *plan, const void *base, int64_t ldbase, dybit_dtype ty, void *Y, int64_t ldy,
+                            float *V, void *stream) {
+    using namespace dybit;
+    dybit_status st = check_adapters(T, K, N, R, n_adapters, A, B, tw, alpha, plan);
+    if (st != DYBIT_OK) return st;
+    if (!dtype_ok(tx) || !dtype_ok(ty) || ldx < K || ldy < N || (base != nullptr && ldbase < N)) return DYBIT_ERR_INVALID_ARG;
+    if (!((tx == DYBIT_F32 && tw == DYBIT_BF16) || (tx != DYBIT_F32 && tw == tx)) || !(ty == DYBIT_F32 || ty == tx)) return DYBIT_ERR_UNSUPPORTED;
+    if (T == 0) return DYBIT_OK;
+    if (X == nullptr || Y == nullptr) return DYBIT_ERR_INVALID_ARG;
+    const int ex = dtype_bytes(tx), ey = dtype_bytes(ty);
+    if (!aligned(X, ex) || !aligned(Y, ey) || !aligned(base, ey) || !aligned(V, 16)) return DYBIT_ERR_ALIGNMENT;
+    AdapterTokens p = {};
+    p.x = X, p.ldx = ldx, p.w1 = A, p.w2 = B, p.alpha = alpha, p.plan = static_cast<const int *>(plan);
+    p.base = base, p.ldbase = ldbase, p.y = Y, p.ldy = ldy, p.v_out = V;
+    p.T = T, p.K = K, p.N = N, p.n = n_adapters, p.R = R;
+    p.vec_x = rows_vec(X, ldx, ex, 16), p.vec_w1 = rows_vec(A, K, 2, 16), p.vec_w2 = rows_vec(B, N, 2, 8);
+    p.vec_y = rows_vec(Y, ldy, ey, 4 * ey) && (base == nullptr || rows_vec(base, ldbase, ey, 4 * ey));
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (tx == DYBIT_F32) return launch_tokens_rank<float, __nv_bfloat16, float, false>(p, s);
+    if (tx == DYBIT_BF16)
+        return ty == DYBIT_F32 ? launch_tokens_rank<__nv_bfloat16, __nv_bfloat16, float, false>(p, s)
+                               : launch_tokens_rank<__nv_bfloat16, __nv_bfloat16, __nv_bfloat16, false>(p, s);
+    return ty == DYBIT_F32 ? launch_tokens_rank<__half, __half, float, false>(p, s) : launch_tokens_rank<__half, __half, __half, false>(p, s);
+}
+
+size_t dybit_adapters_backward_workspace_bytes(int64_t T, int64_t K, int64_t N, int R, int n_adapters) {
+    if (dybit_adapters_plan_bytes(T, n_adapters) == 0 || K < 1 || N < 1 || R < 8 || R % 8 != 0 || R > DYBIT_MAX_RANK) return 0;
+    return (size_t)dybit::BackwardWs(T, K, N, R, n_adapters).bytes;
+}
+
+dybit_status dybit_adapters_backward(int64_t T, int64_t K, int64_t N, int R, const void *dY, dybit_dtype tdy, int64_t lddy,
+                                     const void *codes, int64_t row_stride_bytes, dybit_fmt fmt, const float *scales,
+                                     int64_t scale_stride, int n_adapters, const void *A, const void *B,
+                                     dybit_dtype tw, const float *alpha, const void *plan, const float *V,
+                                     const void *dXbase, int64_t lddxbase, void *dX, int64_t lddx, float *dA,
+                                     float *dB, void *ws, size_t ws_bytes, void *stream) {
+    using namespace dybit;
+    dybit_status st = check_adapters(T, K, N, R, n_adapters, A, B, tw, alpha, plan);
+    if (st != DYBIT_OK) return st;
+    st = check_codes(codes, T, K, row_stride_bytes, fmt);
+    if (st != DYBIT_OK) return st;
+    if (!dtype_ok(tdy) || lddy < N || lddx < K || (dXbase != nullptr && lddxbase < K) || scale_stride < 0) return DYBIT_ERR_INVALID_ARG;
+    if (tdy == DYBIT_F16 || tw != DYBIT_BF16) return DYBIT_ERR_UNSUPPORTED;
+    if (dA == nullptr || dB == nullptr) return DYBIT_ERR_INVALID_ARG;
+    if (T > 0 && (dY == nullptr || dX == nullptr || V == nullptr || scales == nullptr)) return DYBIT_ERR_INVALID_ARG;
+    const int e = dtype_bytes(tdy);
+    if (!aligned(dY, e) || !aligned(dX, e) || !aligned(dXbase, e) || !aligned(V, 4) || !aligned(scales, 4) || !aligned(dA, 4) ||
+        !aligned(dB, 4) || !aligned(ws, 1024))
+        return DYBIT_ERR_ALIGNMENT;
+    const BackwardWs w(T, K, N, R, n_adapters);
+    if (ws == nullptr || ws_bytes < (size_t)w.bytes) return DYBIT_ERR_WORKSPACE;
+    uint8_t *base = static_cast<uint8_t *>(ws);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+
+    AdapterTokens p = {};
+    p.x = dY, p.ldx = lddy, p.w1 = B, p.w2 = A, p.alpha = alpha, p.plan = static_cast<const int *>(plan);
+    p.base = dXbase, p.ldbase = lddxbase, p.y = dX, p.ldy = lddx;
+    p.T = T, p.K = N, p.N = K, p.n = n_adapters, p.R = R;
+    p.vec_x = rows_vec(dY, lddy, e, 16), p.vec_w1 = rows_vec(B, N, 2, 16), p.vec_w2 = rows_vec(A, K, 2, 8);
+    p.vec_y = rows_vec(dX, lddx, e, 4 * e) && (dXbase == nullptr || rows_vec(dXbase, lddxbase, e, 4 * e));
+    p.v_in = V, p.scales = scales, p.scale_stride = scale_stride;
+    p.frag_u = reinterpret_cast<uint4 *>(base + w.frag_u), p.frag_v = reinterpret_cast<uint4 *>(base + w.frag_v);
+    if (T > 0) {
+        st = tdy == DYBIT_F32 ? launch_tokens_rank<float, __nv_bfloat16, float, true>(p, s)
+                              : launch_tokens_rank<__nv_bfloat16, __nv_bfloat16, __nv_bfloat16, true>(p, s);
+        if (st != DYBIT_OK) return st;
+    }
+    AdapterGrad gp = {};
+    gp.plan = p.plan, gp.T = T, gp.n = n_adapters, gp.R = R;
+    gp.side[0] = {codes, row_stride_bytes, K, p.frag_u, dA, reinterpret_cast<float *>(base + w.partial_a), 1};
+    gp.side[1] = {dY, lddy, N, p.frag_v, dB, reinterpret_cast<float *>(base + w.partial_b), rows_vec(dY, lddy, e, 16) ? 1 : 0};
+    if (fmt.is_signed)
+        return tdy == DYBIT_F32 ? launch_grad<GradSrc::CodesSigned, GradSrc::F32>(gp, s) : launch_grad<GradSrc::CodesSigned, GradSrc::Bf16>(gp, s);
+    return tdy == DYBIT_F32 ? launch_grad<GradSrc::CodesUnsigned, GradSrc::F32>(gp, s) : launch_grad<GradSrc::CodesUnsigned, GradSrc::Bf16>(gp, s);
+}
+
+}  // extern "C"

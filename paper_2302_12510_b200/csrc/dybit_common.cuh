@@ -77,8 +77,24 @@ inline ProfileEvents &profile_events() {
 }
 
 // Device status word: 0 = fine; otherwise (site << 8) | 1 of the first bounded
-// wait that expired.  Kernels only ever OR a value in.
-__device__ unsigned int g_device_status = 0;
+// wait that expired.  Kernels only ever OR a value in.  Each translation unit of the library has its own word;
+// dybit_last_device_status looks at all of them.
+static __device__ unsigned int g_device_status = 0;
+
+// Reads and clears this translation unit's word (waits for the stream).
+static inline cudaError_t take_status_word(cudaStream_t s, unsigned *word) {
+    const unsigned zero = 0;
+    *word = 0;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(word, g_device_status, sizeof(*word), 0, cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (e == cudaSuccess && *word != 0) {
+        e = cudaMemcpyToSymbolAsync(g_device_status, &zero, sizeof(zero), 0, cudaMemcpyHostToDevice, s);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    }
+    return e;
+}
+// The word of dybit_finetune.cu.
+cudaError_t take_finetune_status_word(cudaStream_t s, unsigned *word);
 
 // Range checks of the debug build (-DDYBIT_DEBUG_BOUNDS, libdybit_debug.so): global-memory stores whose extent the
 // kernel knows are wrapped in `if (DYBIT_CHECK(index condition, site))`.  A failing check skips the access and ORs

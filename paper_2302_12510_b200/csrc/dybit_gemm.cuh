@@ -18,6 +18,7 @@
 #include "dybit_host.cuh"
 #include "dybit_quantize.cuh"
 #include "dybit_sm100.cuh"
+#include "dybit_wait.cuh"
 
 namespace dybit {
 
@@ -1262,7 +1263,6 @@ constexpr int kBKBytes = 128;       // one 128-byte swizzle row of K per pipelin
 constexpr int kUmmaKBytes = 32;     // K bytes consumed by one tcgen05.mma
 constexpr int kStageBytesTotal = 192 * 1024;
 constexpr int kEpilogueWarps = 8;     // two groups of four (one warp per TMEM lane quarter in each)
-constexpr unsigned long long kWaitLimitNs = 4000000000ull;
 
 struct GemmParams {
     int M, N;                 // output extent
@@ -1292,50 +1292,6 @@ struct GemmParams {
     int split_from;           // pair kernel: tiles from this index on are worked on as two 256 x 128 halves (see pair_item)
     int64_t c_bstride;        // batched GEMM: elements between consecutive entries of C / C_raw
 };
-
-// Waits for the phase with the given parity; gives up after `limit_ns` (kWaitLimitNs in every kernel of the
-// library), records the site in the device status word and raises the CTA-wide abort flag.
-__device__ __forceinline__ bool wait_bounded(uint64_t *bar, uint32_t parity, volatile uint32_t *abort_flag,
-                                             unsigned site, unsigned long long limit_ns = kWaitLimitNs) {
-    if (mbar_try_wait(bar, parity)) return true;
-    const uint64_t t0 = global_timer_ns();
-    unsigned spins = 0;
-    for (;;) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if ((++spins & 63u) == 0u) {
-            if (*abort_flag) return false;
-            if (global_timer_ns() - t0 > limit_ns) {
-                atomicOr(&g_device_status, (site << 8) | 1u);
-                *abort_flag = 1u;
-                return false;
-            }
-        }
-    }
-}
-
-// The same wait for the MMA-issuing thread: the barrier is named by its shared-memory address and only the first
-// probe is inlined, so the common case (the stage is there already) costs three instructions.
-__device__ __noinline__ bool wait_bounded_slow(uint32_t bar_addr, uint32_t parity, volatile uint32_t *abort_flag, unsigned site) {
-    const uint64_t t0 = global_timer_ns();
-    unsigned spins = 0;
-    for (;;) {
-        if (mbar_try_wait_addr(bar_addr, parity)) return true;
-        if ((++spins & 63u) == 0u) {
-            if (*abort_flag) return false;
-            if (global_timer_ns() - t0 > kWaitLimitNs) {
-                atomicOr(&g_device_status, (site << 8) | 1u);
-                *abort_flag = 1u;
-                return false;
-            }
-        }
-    }
-}
-
-__device__ __forceinline__ bool wait_bounded_addr(uint32_t bar_addr, uint32_t parity, volatile uint32_t *abort_flag,
-                                                  unsigned site) {
-    if (mbar_try_wait_addr(bar_addr, parity)) return true;
-    return wait_bounded_slow(bar_addr, parity, abort_flag, site);
-}
 
 // Self-test of the give-up path: one thread waits, with the library's own wait_bounded, on a barrier that nothing
 // ever arrives on.  The wait runs out after limit_ns, sets the status word (site kSelftestSite) and the abort flag
@@ -1951,27 +1907,6 @@ __global__ void __launch_bounds__(320, 1) dybit_gemm_multi_kernel(const __grid_c
 }
 
 // ------------------------------------------------------------------ host side
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn encode_tiled_fn() {
-    static std::atomic<EncodeTiledFn> fn{nullptr};
-    EncodeTiledFn f = fn.load(std::memory_order_acquire);
-    if (f == nullptr) {
-        void *ptr = nullptr;
-        cudaDriverEntryPointQueryResult qres;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &qres) == cudaSuccess &&
-            qres == cudaDriverEntryPointSuccess) {
-            f = reinterpret_cast<EncodeTiledFn>(ptr);
-            fn.store(f, std::memory_order_release);
-        } else {
-            (void)cudaGetLastError();
-        }
-    }
-    return f;
-}
 
 // Byte matrix [rows][row_bytes] with row stride `stride`; box = swb bytes x box_rows, swb-byte swizzle.
 static dybit_status make_operand_map(CUtensorMap *map, const void *base, int64_t rows, int64_t row_bytes, int64_t stride,

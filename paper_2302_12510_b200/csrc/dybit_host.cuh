@@ -306,15 +306,10 @@ dybit_status dybit_profile_next_gemm_clock(unsigned long long *t2) {
 
 dybit_status dybit_last_device_status(void *stream, uint32_t *detail) {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    unsigned int word = 0, zero = 0;
-    DYBIT_CUDA_TRY(cudaMemcpyFromSymbolAsync(&word, dybit::g_device_status, sizeof(word), 0,
-                                             cudaMemcpyDeviceToHost, s));
-    DYBIT_CUDA_TRY(cudaStreamSynchronize(s));
-    if (word != 0) {
-        DYBIT_CUDA_TRY(cudaMemcpyToSymbolAsync(dybit::g_device_status, &zero, sizeof(zero), 0,
-                                               cudaMemcpyHostToDevice, s));
-        DYBIT_CUDA_TRY(cudaStreamSynchronize(s));
-    }
+    unsigned int word = 0, more = 0;
+    DYBIT_CUDA_TRY(dybit::take_status_word(s, &word));
+    DYBIT_CUDA_TRY(dybit::take_finetune_status_word(s, &more));
+    if (word == 0) word = more;
     if (detail) *detail = word;
     if (word == 0) return DYBIT_OK;
     return (word & 1u) ? DYBIT_ERR_DEVICE_TIMEOUT : DYBIT_ERR_DEVICE_BOUNDS;

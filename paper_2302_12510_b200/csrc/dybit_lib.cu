@@ -1,5 +1,5 @@
-// libdybit: single translation unit (the device status word and the kernels
-// share one module, so no relocatable device code is needed).
+// libdybit: quantize, GEMM and convolution (dybit_finetune.cu is the second translation unit; no relocatable
+// device code is needed, each has its own device status word).
 #include "dybit_host.cuh"
 #include "dybit_quantize.cuh"
 #include "dybit_gemm.cuh"
