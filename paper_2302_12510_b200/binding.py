@@ -155,17 +155,29 @@ def _load() -> C.CDLL:
 lib = _load()
 
 
+_FMT_CACHE = {}
+
+
 def _fmt(f) -> _CFmt:
     bits, sg = f
-    return _CFmt(int(bits), int(bool(sg)))
+    key = (int(bits), bool(sg))
+    c = _FMT_CACHE.get(key)
+    if c is None:
+        c = _FMT_CACHE[key] = _CFmt(key[0], int(key[1]))
+    return c
 
 
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
-def _stream(stream) -> C.c_void_p:
+_raw_stream, _raw_device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+
+
+def _stream(stream):
     if stream is None:
+        if _raw_stream is not None and _raw_device is not None:      # 0.2 us where torch.cuda.current_stream() takes 3
+            return _raw_stream(_raw_device())
         stream = torch.cuda.current_stream()
     return C.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
@@ -692,53 +704,48 @@ def dybit_search_bitwidths(lat, rmse, num_layers: int, strategy: str, constraint
 _DTYPE_CODE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
-def _matrix(x: torch.Tensor, name: str, cols: Optional[int] = None, rows: Optional[int] = None) -> int:
-    """Checks a 2-D device matrix of real numbers with contiguous rows; returns its dybit_dtype."""
-    code = _DTYPE_CODE.get(x.dtype)
-    if code is None or not x.is_cuda or x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
+def _matrix(x: torch.Tensor, name: str, rows: Optional[int] = None, cols: Optional[int] = None) -> Tuple[int, int]:
+    """Checks a 2-D device matrix of real numbers with contiguous rows; returns (dybit_dtype, row stride)."""
+    code, shape = _DTYPE_CODE.get(x.dtype), x.shape
+    if code is None or not x.is_cuda or len(shape) != 2:
         raise ValueError(f"{name} must be a 2-D float32, bfloat16 or float16 CUDA tensor with unit inner stride")
-    if (cols is not None and x.shape[1] != cols) or (rows is not None and x.shape[0] != rows):
-        raise ValueError(f"{name} has shape {tuple(x.shape)}, expected ({'any' if rows is None else rows}, {'any' if cols is None else cols})")
-    return code
+    r, c = shape
+    ld, inner = x.stride()
+    if inner != 1 and c > 1:
+        raise ValueError(f"{name} must be a 2-D float32, bfloat16 or float16 CUDA tensor with unit inner stride")
+    if (cols is not None and c != cols) or (rows is not None and r != rows):
+        raise ValueError(f"{name} has shape {(r, c)}, expected ({'any' if rows is None else rows}, {'any' if cols is None else cols})")
+    return code, (ld if r > 1 or ld > c else c)       # (torch gives a single row any stride)
 
 
-def _ld(x: torch.Tensor) -> int:
-    """Row stride of a matrix; torch gives one row any stride, which must not be below its length."""
-    return max(x.stride(0), x.shape[1]) if x.shape[0] <= 1 else x.stride(0)
-
-
-def _codes8(codes: torch.Tensor, rows: int, cols: int, scales: torch.Tensor) -> Tuple[int, int]:
-    """Checks a matrix of 8-bit codes and its scales; returns (row stride in bytes, number of scales)."""
-    if codes.dtype != torch.uint8 or not codes.is_cuda or codes.dim() != 2 or codes.shape[0] != rows or codes.shape[1] < cols or \
-            (codes.stride(1) != 1 and codes.shape[1] > 1):
+def _codes8(codes: torch.Tensor, rows: int, cols: int, scales: torch.Tensor, per_row: bool) -> Tuple[int, int]:
+    """Checks a matrix of 8-bit codes and its scales; returns (row stride in bytes, scale stride)."""
+    shape = codes.shape
+    if codes.dtype != torch.uint8 or not codes.is_cuda or len(shape) != 2 or shape[0] != rows or shape[1] < cols:
         raise ValueError("codes must be a 2-D uint8 CUDA tensor [rows][row bytes >= cols] with unit inner stride")
-    if scales.dtype != torch.float32 or not scales.is_cuda or not scales.is_contiguous():
-        raise ValueError("scales must be a contiguous float32 CUDA tensor")
-    return _ld(codes), scales.numel()
-
-
-def _scale_stride(scales: torch.Tensor, rows: int, per_row: bool) -> int:
-    if scales.numel() < (rows if per_row else 1):
-        raise ValueError("scales must hold one value per row, or the scale of the whole tensor")
-    return 1 if per_row else 0
+    ld, inner = codes.stride()
+    if inner != 1 and shape[1] > 1:
+        raise ValueError("codes must be a 2-D uint8 CUDA tensor [rows][row bytes >= cols] with unit inner stride")
+    if scales.dtype != torch.float32 or not scales.is_cuda or not scales.is_contiguous() or scales.numel() < (rows if per_row else 1):
+        raise ValueError("scales must be a contiguous float32 CUDA tensor with one value per row, or the scale of the whole tensor")
+    return (ld if rows > 1 or ld > shape[1] else shape[1]), 1 if per_row else 0
 
 
 def dybit_checkpoint_save(x: torch.Tensor, fmt, top: int = 2, codes: Optional[torch.Tensor] = None,
                           scales: Optional[torch.Tensor] = None, stream=None):
     """8-bit codes of an activation [rows][cols] with one power-of-two scale per row; the largest magnitude of a row
     lands in (2^(top-1), 2^top].  Returns (codes uint8 [rows][row bytes], scales float32 [rows])."""
-    t = _matrix(x, "x")
+    t, ld = _matrix(x, "x")
     rows, cols = x.shape
+    padded = (cols + 127) // 128 * 128
     if codes is None:
-        codes = torch.empty((rows, (cols + 127) // 128 * 128), dtype=torch.uint8, device=x.device)
+        codes = x.new_empty((rows, padded), dtype=torch.uint8)
     if scales is None:
-        scales = torch.empty(rows, dtype=torch.float32, device=x.device)
-    stride, n = _codes8(codes, rows, cols, scales)
-    if n < rows:
-        raise ValueError("scales must hold one value per row")
-    if codes.shape[1] < min(stride, (cols + 127) // 128 * 128):
+        scales = x.new_empty(rows, dtype=torch.float32)
+    stride, _ = _codes8(codes, rows, cols, scales, True)
+    if codes.shape[1] < padded and codes.shape[1] < stride:
         raise ValueError("codes must have room for the columns rounded up to 128, or to the end of its rows")
-    _check(lib.dybit_checkpoint_save(x.data_ptr(), t, rows, cols, _ld(x), _fmt(fmt), int(top), codes.data_ptr(), stride,
+    _check(lib.dybit_checkpoint_save(x.data_ptr(), t, rows, cols, ld, _fmt(fmt), top, codes.data_ptr(), stride,
                                      scales.data_ptr(), _stream(stream)), "dybit_checkpoint_save")
     return codes, scales
 
@@ -748,13 +755,12 @@ def dybit_checkpoint_load(codes: torch.Tensor, cols: int, fmt, scales: torch.Ten
     """The activation [rows][cols] that a checkpoint stands for.  per_row=False: scales is the pair {scale, 1/scale} of
     the whole tensor, as dybit_quantize_pack_2d writes it."""
     rows = codes.shape[0]
-    stride, _ = _codes8(codes, rows, cols, scales)
+    stride, scale_stride = _codes8(codes, rows, cols, scales, per_row)
     if out is None:
-        out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
-    t = _matrix(out, "out", cols, rows)
-    _check(lib.dybit_checkpoint_load(codes.data_ptr(), stride, scales.data_ptr(), _scale_stride(scales, rows, per_row), rows,
-                                     int(cols), _fmt(fmt), out.data_ptr(), t, _ld(out), _stream(stream)),
-           "dybit_checkpoint_load")
+        out = codes.new_empty((rows, cols), dtype=dtype)
+    t, ld = _matrix(out, "out", rows, cols)
+    _check(lib.dybit_checkpoint_load(codes.data_ptr(), stride, scales.data_ptr(), scale_stride, rows, cols, _fmt(fmt),
+                                     out.data_ptr(), t, ld, _stream(stream)), "dybit_checkpoint_load")
     return out
 
 
@@ -775,17 +781,17 @@ def dybit_checkpoint_wgrad(dY: torch.Tensor, codes: torch.Tensor, K: int, fmt, s
                            out: Optional[torch.Tensor] = None, per_row: bool = True,
                            ws: Optional[torch.Tensor] = None, stream=None):
     """dW [N][K] float32 = dY^T x^ with x^ [T][K] read from an 8-bit checkpoint."""
-    t = _matrix(dY, "dY")
+    t, ld = _matrix(dY, "dY")
     T, N = dY.shape
-    stride, _ = _codes8(codes, T, K, scales)
+    stride, scale_stride = _codes8(codes, T, K, scales, per_row)
     if out is None:
-        out = torch.empty((N, K), dtype=torch.float32, device=dY.device)
-    if _matrix(out, "out", K, N) != 0:
+        out = dY.new_empty((N, K), dtype=torch.float32)
+    to, ldo = _matrix(out, "out", N, K)
+    if to != 0:
         raise ValueError("out must be float32")
     at, size, ws = _workspace(lib.dybit_checkpoint_wgrad_workspace_bytes(T, N, K, t), ws, dY.device)
-    _check(lib.dybit_checkpoint_wgrad(T, N, K, dY.data_ptr(), t, _ld(dY), codes.data_ptr(), stride, _fmt(fmt),
-                                      scales.data_ptr(), _scale_stride(scales, T, per_row), out.data_ptr(), _ld(out), at, size,
-                                      _stream(stream)), "dybit_checkpoint_wgrad")
+    _check(lib.dybit_checkpoint_wgrad(T, N, K, dY.data_ptr(), t, ld, codes.data_ptr(), stride, _fmt(fmt), scales.data_ptr(),
+                                      scale_stride, out.data_ptr(), ldo, at, size, _stream(stream)), "dybit_checkpoint_wgrad")
     return out
 
 
@@ -812,16 +818,25 @@ class AdapterPlan:
     def __init__(self, ids: torch.Tensor, n_adapters: int, stream=None):
         self.T, self.n = ids.numel(), int(n_adapters)
         self.buffer = dybit_adapters_plan(ids, n_adapters, stream=stream)
+        self.address = self.buffer.data_ptr()
 
 
 def _factors(A: torch.Tensor, B: torch.Tensor, alpha: Optional[torch.Tensor], plan: AdapterPlan) -> Tuple[int, int, int, int]:
     """Checks the factors [n][R][K] and [n][R][N]; returns (R, K, N, dybit_dtype)."""
-    if A.dim() != 3 or B.dim() != 3 or A.shape[:2] != B.shape[:2] or A.shape[0] != plan.n or A.dtype != B.dtype or \
-            not (A.is_cuda and B.is_cuda and A.is_contiguous() and B.is_contiguous()) or A.dtype not in (torch.bfloat16, torch.float16):
+    a, b, dt = A.shape, B.shape, A.dtype
+    if len(a) != 3 or len(b) != 3 or a[0] != plan.n or b[0] != plan.n or a[1] != b[1] or dt != B.dtype or \
+            dt not in (torch.bfloat16, torch.float16) or not (A.is_cuda and B.is_cuda and A.is_contiguous() and B.is_contiguous()):
         raise ValueError("A and B must be contiguous 16-bit CUDA tensors [n_adapters][R][K] and [n_adapters][R][N]")
     if alpha is not None and (alpha.dtype != torch.float32 or not alpha.is_cuda or not alpha.is_contiguous() or alpha.numel() != plan.n):
         raise ValueError("alpha must be a contiguous float32 CUDA tensor with one value per adapter")
-    return A.shape[1], A.shape[2], B.shape[2], _DTYPE_CODE[A.dtype]
+    return a[1], a[2], b[2], _DTYPE_CODE[dt]
+
+
+def _dense(x: torch.Tensor, name: str, shape) -> int:
+    """Checks a dense float32 device tensor of the given shape; returns its address."""
+    if x.dtype != torch.float32 or not x.is_cuda or x.shape != shape or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 CUDA tensor {list(shape)}")
+    return x.data_ptr()
 
 
 def dybit_adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, alpha: Optional[torch.Tensor], plan: AdapterPlan,
@@ -831,22 +846,21 @@ def dybit_adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, alpha: Opt
     out may be base.  Returns (y [T][N], V [T][R] float32 or None); V is what dybit_adapters_backward takes."""
     R, K, N, tw = _factors(A, B, alpha, plan)
     T = plan.T
-    tx = _matrix(x, "x", K, T)
-    if base is not None:
-        tb = _matrix(base, "base", N, T)
+    tx, ldx = _matrix(x, "x", T, K)
+    tb, ldb = (None, 0) if base is None else _matrix(base, "base", T, N)
     if out is None:
-        out = torch.empty((T, N), dtype=base.dtype if base is not None else (out_dtype or x.dtype), device=x.device)
-    ty = _matrix(out, "out", N, T)
+        out = x.new_empty((T, N), dtype=base.dtype if base is not None else (out_dtype or x.dtype))
+        ty, ldy = _DTYPE_CODE.get(out.dtype), N
+    else:
+        ty, ldy = _matrix(out, "out", T, N)
     if base is not None and tb != ty:
         raise ValueError("base and out must have one dtype")
     if want_v and v is None:
-        v = torch.empty((T, R), dtype=torch.float32, device=x.device)
-    if v is not None and (v.dtype != torch.float32 or not v.is_cuda or not v.is_contiguous() or tuple(v.shape) != (T, R)):
-        raise ValueError("v must be a contiguous float32 CUDA tensor [T][R]")
-    _check(lib.dybit_adapters(T, K, N, R, x.data_ptr(), tx, _ld(x), plan.n, A.data_ptr(), B.data_ptr(), tw,
-                              None if alpha is None else alpha.data_ptr(), plan.buffer.data_ptr(),
-                              None if base is None else base.data_ptr(), 0 if base is None else _ld(base), ty, out.data_ptr(),
-                              _ld(out), None if v is None else v.data_ptr(), _stream(stream)), "dybit_adapters")
+        v = x.new_empty((T, R), dtype=torch.float32)
+    _check(lib.dybit_adapters(T, K, N, R, x.data_ptr(), tx, ldx, plan.n, A.data_ptr(), B.data_ptr(), tw,
+                              None if alpha is None else alpha.data_ptr(), plan.address, None if base is None else base.data_ptr(),
+                              ldb, ty, out.data_ptr(), ldy, None if v is None else _dense(v, "v", (T, R)), _stream(stream)),
+           "dybit_adapters")
     return out, v
 
 
@@ -863,26 +877,23 @@ def dybit_adapters_backward(dY: torch.Tensor, codes: torch.Tensor, fmt, scales: 
     be dx_base.  Returns (dx [T][K] like dY, dA [n][R][K] float32, dB [n][R][N] float32)."""
     R, K, N, tw = _factors(A, B, alpha, plan)
     T, n = plan.T, plan.n
-    t = _matrix(dY, "dY", N, T)
-    stride, _ = _codes8(codes, T, K, scales)
-    if v.dtype != torch.float32 or not v.is_cuda or not v.is_contiguous() or tuple(v.shape) != (T, R):
-        raise ValueError("v must be a contiguous float32 CUDA tensor [T][R]")
+    t, ldy = _matrix(dY, "dY", T, N)
+    stride, scale_stride = _codes8(codes, T, K, scales, per_row)
+    tb, ldb = (t, 0) if dx_base is None else _matrix(dx_base, "dx_base", T, K)
     if dx is None:
-        dx = torch.empty((T, K), dtype=dY.dtype, device=dY.device)
-    if _matrix(dx, "dx", K, T) != t or (dx_base is not None and _matrix(dx_base, "dx_base", K, T) != t):
+        dx = dY.new_empty((T, K))
+    tx, ldx = _matrix(dx, "dx", T, K)
+    if tx != t or tb != t:
         raise ValueError("dx and dx_base must have dY's dtype")
     if dA is None:
-        dA = torch.empty((n, R, K), dtype=torch.float32, device=dY.device)
+        dA = dY.new_empty((n, R, K), dtype=torch.float32)
     if dB is None:
-        dB = torch.empty((n, R, N), dtype=torch.float32, device=dY.device)
-    for g, like in ((dA, A), (dB, B)):
-        if g.dtype != torch.float32 or not g.is_cuda or not g.is_contiguous() or g.shape != like.shape:
-            raise ValueError("dA and dB must be contiguous float32 CUDA tensors shaped like A and B")
+        dB = dY.new_empty((n, R, N), dtype=torch.float32)
     at, size, ws = _workspace(lib.dybit_adapters_backward_workspace_bytes(T, K, N, R, n), ws, dY.device)
-    _check(lib.dybit_adapters_backward(T, K, N, R, dY.data_ptr(), t, _ld(dY), codes.data_ptr(), stride, _fmt(fmt),
-                                       scales.data_ptr(), _scale_stride(scales, T, per_row), n, A.data_ptr(), B.data_ptr(), tw,
-                                       None if alpha is None else alpha.data_ptr(), plan.buffer.data_ptr(), v.data_ptr(),
-                                       None if dx_base is None else dx_base.data_ptr(), 0 if dx_base is None else _ld(dx_base),
-                                       dx.data_ptr(), _ld(dx), dA.data_ptr(), dB.data_ptr(), at, size, _stream(stream)),
+    _check(lib.dybit_adapters_backward(T, K, N, R, dY.data_ptr(), t, ldy, codes.data_ptr(), stride, _fmt(fmt),
+                                       scales.data_ptr(), scale_stride, n, A.data_ptr(), B.data_ptr(), tw,
+                                       None if alpha is None else alpha.data_ptr(), plan.address, _dense(v, "v", (T, R)),
+                                       None if dx_base is None else dx_base.data_ptr(), ldb, dx.data_ptr(), ldx,
+                                       _dense(dA, "dA", (n, R, K)), _dense(dB, "dB", (n, R, N)), at, size, _stream(stream)),
            "dybit_adapters_backward")
     return dx, dA, dB

@@ -71,6 +71,7 @@ struct AdapterTokens {
     float *v_out;                // forward: tokens x R, or null
     int64_t T, K, N;
     int n, R;
+    int64_t perm_at, tiles_at;   // word offsets in the plan
     int vec_x, vec_w1, vec_y, vec_w2;      // rows can be moved in vectors (16 bytes; 4 elements for y and w2)
     // backward: fragments for adapter_grad_kernel
     const float *v_in;
@@ -80,53 +81,72 @@ struct AdapterTokens {
 };
 
 // Sixteen consecutive elements of a row at column k (the lane's share of a 64-column block), as raw words.
-template <typename T, int WORDS>
-__device__ __forceinline__ void load16(unsigned (&w)[WORDS], const T *row, int64_t k, int64_t K, bool vec, bool there) {
-    static_assert(WORDS == 4 * (int)sizeof(T), "sixteen elements");
-    constexpr int E = 16 / (int)sizeof(T);
+template <typename T>
+__device__ __forceinline__ void load16(unsigned (&w)[4 * sizeof(T)], const T *row) {
 #pragma unroll
-    for (int i = 0; i < WORDS / 4; ++i) {
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        const int64_t c = k + i * E;
-        if (there && c < K) {
-            if (vec && c + E <= K) {
-                v = __ldg(reinterpret_cast<const uint4 *>(row + c));
-            } else {
-                T e[E];
-#pragma unroll
-                for (int j = 0; j < E; ++j) e[j] = c + j < K ? row[c + j] : from_f32<T>(0.0f);
-                v = *reinterpret_cast<const uint4 *>(e);
-            }
-        }
+    for (int i = 0; i < (int)sizeof(T); ++i) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4 *>(row) + i);
         w[4 * i] = v.x;
         w[4 * i + 1] = v.y;
         w[4 * i + 2] = v.z;
         w[4 * i + 3] = v.w;
     }
 }
-
-// Four consecutive elements of a row as floats, zeros beyond `cols`.
+// The same where rows may start anywhere and the block may reach past column K (zeros there): element loads without
+// branches, so that all of them are in flight together.  Slot e of lane q takes column 4e + q of the block, so that
+// four lanes read neighbours; both operands of a product come in this order or both in the other.
 template <typename T>
-__device__ __forceinline__ float4 load4(const T *row, int64_t c, int64_t cols, bool vec) {
-    if (c >= cols) return make_float4(0.f, 0.f, 0.f, 0.f);
-    if (vec && c + 4 <= cols) {
-        if constexpr (sizeof(T) == 4) {
-            return *reinterpret_cast<const float4 *>(row + c);
-        } else {
-            const uint2 v = *reinterpret_cast<const uint2 *>(row + c);
-            const float2 a = unpack2<T>(v.x), b = unpack2<T>(v.y);
-            return make_float4(a.x, a.y, b.x, b.y);
-        }
-    }
-    float f[4];
+__device__ __forceinline__ void load16_any(unsigned (&w)[4 * sizeof(T)], const T *row, int64_t block, int q, int64_t K) {
+    T e[16];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) f[j] = c + j < cols ? to_f32(row[c + j]) : 0.0f;
-    return make_float4(f[0], f[1], f[2], f[3]);
+    for (int i = 0; i < 16; ++i) {
+        const int64_t c = block * 64 + 4 * i + q;
+        const T v = row[c < K ? c : K - 1];
+        e[i] = c < K ? v : from_f32<T>(0.0f);
+    }
+#pragma unroll
+    for (int i = 0; i < 4 * (int)sizeof(T); ++i) w[i] = reinterpret_cast<const unsigned *>(e)[i];
+}
+
+// Four consecutive elements of a row, raw.
+template <typename T> struct Quad { unsigned w[sizeof(T)]; };
+template <typename T>
+__device__ __forceinline__ Quad<T> load_quad(const T *p) {
+    Quad<T> o;
+    if constexpr (sizeof(T) == 4) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(p);
+        o.w[0] = v.x, o.w[1] = v.y, o.w[2] = v.z, o.w[3] = v.w;
+    } else {
+        const uint2 v = *reinterpret_cast<const uint2 *>(p);
+        o.w[0] = v.x, o.w[1] = v.y;
+    }
+    return o;
+}
+template <typename T>
+__device__ __forceinline__ Quad<T> load_quad_any(const T *row, int64_t c, int64_t cols) {
+    T e[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const T v = row[c + j < cols ? c + j : cols - 1];
+        e[j] = c + j < cols ? v : from_f32<T>(0.0f);
+    }
+    Quad<T> o;
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T); ++j) o.w[j] = reinterpret_cast<const unsigned *>(e)[j];
+    return o;
+}
+template <typename T>
+__device__ __forceinline__ float4 quad_floats(const Quad<T> &v) {
+    if constexpr (sizeof(T) == 4) {
+        return make_float4(__uint_as_float(v.w[0]), __uint_as_float(v.w[1]), __uint_as_float(v.w[2]), __uint_as_float(v.w[3]));
+    } else {
+        const float2 a = unpack2<T>(v.w[0]), b = unpack2<T>(v.w[1]);
+        return make_float4(a.x, a.y, b.x, b.y);
+    }
 }
 
 template <typename T>
 __device__ __forceinline__ void store4(T *row, int64_t c, int64_t cols, bool vec, const float4 f) {
-    if (c >= cols) return;
     if (vec && c + 4 <= cols) {
         if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(row + c) = f;
         else *reinterpret_cast<uint2 *>(row + c) = make_uint2(pack2<T>(f.x, f.y), pack2<T>(f.z, f.w));
@@ -151,6 +171,7 @@ __device__ __forceinline__ uint32_t cluster_nctarank() {
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+__device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // Fragments of a 16 (ranks) x 16 (tokens) block for adapter_grad_kernel: lane (g, q) of the reader takes ranks g, g + 8
 // and tokens 4q .. 4q + 3; three uint4 (leading, middle and last bf16 parts) of 32 lanes follow one another.
@@ -166,43 +187,71 @@ __device__ __forceinline__ void store_fragment(uint4 *frag, int lane, const floa
 
 constexpr int kTokWarps = 8;
 constexpr int kTokThreads = kTokWarps * 32;
+constexpr int kMaxClusterCtas = 8;
 
 template <int RT, int MT>
 struct TokSmem {
     static constexpr int kTile = 16 * MT * RT;                 // floats of one token tile of V
-    static constexpr int kPad = RT + 4;                        // row of the tile that feeds the second product
-    static constexpr int kBytes = (kTokWarps * kTile + kTile + 16 * MT * kPad) * 4;
+    static constexpr int kPad = RT + 4;                        // row of the tiles that feed the second product
+    static constexpr int kBytes = (kTokWarps * kTile + kTile + 2 * 16 * MT * kPad) * 4;
 };
 
 // One cluster per tile of up to 16 * MT tokens of one adapter.  Its CTAs share the columns of x in the first product
 // and those of y in the second; in between they sum up their parts of V through distributed shared memory.  RT is the
-// rank rounded up (16, 32, 64, 128); missing ranks, tokens and columns are read as zeros.
+// rank rounded up (16, 32, 64, 128); ranks and columns that are missing are read as zeros, tokens that are missing
+// repeat the tile's first one and are not stored.
 //
 // First product: a warp takes 64 columns at a time.  Lane (g = lane / 4, q = lane % 4) loads columns 16q .. 16q+15 of
 // token rows g, g + 8 and of factor rows g (+ 8 per n-tile) with 16-byte loads and uses them as the four K = 16 slices
 // of the fragment layout: the order of columns inside a sum is free as long as both operands take the same.
 // Second product: tf32, with V cut into two tf32 numbers (what is left over is below 2^-21 of V; the factors are exact
-// in tf32).  The 64 columns of a warp are dealt to fragment columns so that a lane ends up with four consecutive ones.
+// in tf32).  The 64 columns of a warp are dealt to fragment columns so that a lane ends up with four consecutive ones
+// and four lanes with sixteen.
 template <typename TX, typename TW, typename TY, int RT, int MT, bool BWD>
-__global__ void __launch_bounds__(kTokThreads, 2) adapter_tokens_kernel(const AdapterTokens p) {
+__global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_kernel(const AdapterTokens p) {
     constexpr int NT = RT / 8, TM = 16 * MT, XW = 4 * (int)sizeof(TX);
+    constexpr int XB = sizeof(TX) == 4 || RT > 16 ? 1 : (MT < 2 ? MT : 2);                // 16-token slices whose loads are in flight together
+    constexpr int WB = NT < 8 ? NT : 8;                                        // n-tiles of the factor in registers
+    constexpr bool kHoldB = RT <= 32;                                          // the second factor stays in registers across slices
     using Smem = TokSmem<RT, MT>;
     extern __shared__ __align__(16) float smem_f[];
     float *s_warp = smem_f;                                    // [warps][TM][RT]
     float *s_part = smem_f + kTokWarps * Smem::kTile;          // [TM][RT], read by the whole cluster
-    float *s_v = s_part + Smem::kTile;                         // [TM][RT + 4]
+    float *s_hi = s_part + Smem::kTile, *s_lo = s_hi + TM * Smem::kPad;        // alpha V: tf32 part and rest, [TM][RT + 4]
     __shared__ int s_token[TM];
     pdl_enter();
-    const PlanLayout L(p.T, p.n);
     const int cs = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
     const int tile_id = (int)blockIdx.x / cs;
     constexpr int kList = MT == 1 ? 0 : (MT == 2 ? 1 : 2);
     if (tile_id >= p.plan[kList]) return;                      // the whole cluster
-    const AdapterTile tile = reinterpret_cast<const AdapterTile *>(p.plan + L.tiles[kList])[tile_id];
+    const AdapterTile tile = reinterpret_cast<const AdapterTile *>(p.plan + p.tiles_at)[tile_id];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int R = p.R;
-    if (threadIdx.x < TM) s_token[threadIdx.x] = threadIdx.x < tile.count ? p.plan[L.perm + tile.start + threadIdx.x] : -1;
+    if (threadIdx.x < TM) s_token[threadIdx.x] = p.plan[p.perm_at + tile.start + ((int)threadIdx.x < tile.count ? (int)threadIdx.x : 0)];
     __syncthreads();
+
+    const int slices = tile.adapter >= 0 ? R / 8 : 0;
+    const TW *w2 = static_cast<const TW *>(p.w2) + (int64_t)max(tile.adapter, 0) * R * p.N;
+    const int groups = (int)((p.N + 63) / 64);
+    const int gcol = (g & 1) * 16 + (g >> 1) * 4;              // the lane's columns as fragment column g: + jh * 32 + jl
+    Quad<TW> bq[kHoldB ? NT : 1][2][2];                        // [8 ranks][row q, q + 4][jh]
+    auto load_b = [&](Quad<TW> (&o)[2][2], int s, int64_t n0) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int jh = 0; jh < 2; ++jh) {
+                const TW *row = w2 + (int64_t)(s * 8 + 4 * h + q) * p.N;
+                o[h][jh] = p.vec_w2 && n0 + 64 <= p.N ? load_quad<TW>(row + n0 + jh * 32 + gcol) : load_quad_any<TW>(row, n0 + jh * 32 + gcol, p.N);
+            }
+    };
+    auto load_group = [&](int gi) {
+        if constexpr (kHoldB) {
+#pragma unroll
+            for (int s = 0; s < NT; ++s)
+                if (s < slices) load_b(bq[s], s, (int64_t)gi * 64);
+        }
+    };
+    const int g_first = rank * kTokWarps + warp, g_step = cs * kTokWarps;
 
     if (tile.adapter >= 0) {
         // ---- V = x A^T over this CTA's columns, this warp's blocks of 64
@@ -217,36 +266,71 @@ __global__ void __launch_bounds__(kTokThreads, 2) adapter_tokens_kernel(const Ad
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
         for (int b = rank * per + warp; b < last; b += kTokWarps) {
-            const int64_t k = (int64_t)b * 64 + q * 16;
-            unsigned w[NT][8];
+            const bool fast = p.vec_x && p.vec_w1 && (int64_t)b * 64 + 64 <= p.K;
 #pragma unroll
-            for (int j = 0; j < NT; ++j) load16<TW, 8>(w[j], w1 + (int64_t)(j * 8 + g) * p.K, k, p.K, p.vec_w1, j * 8 + g < R);
+            for (int j0 = 0; j0 < NT; j0 += WB) {
+                unsigned w[WB][8];
+                if (fast) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                if (m * 16 >= tile.count) break;
-                const int t0 = s_token[m * 16 + g], t1 = s_token[m * 16 + g + 8];
-                unsigned x0[XW], x1[XW];
-                load16<TX, XW>(x0, static_cast<const TX *>(p.x) + (int64_t)t0 * p.ldx, k, p.K, p.vec_x, t0 >= 0);
-                load16<TX, XW>(x1, static_cast<const TX *>(p.x) + (int64_t)t1 * p.ldx, k, p.K, p.vec_x, t1 >= 0);
+                    for (int j = 0; j < WB; ++j)               // (a missing rank reads row 0: its column of V is not used)
+                        load16<TW>(w[j], w1 + (int64_t)((j0 + j) * 8 + g < R ? (j0 + j) * 8 + g : 0) * p.K + b * 64 + q * 16);
+                } else {
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    if constexpr (sizeof(TX) == 2) {
+                    for (int j = 0; j < WB; ++j)
+                        load16_any<TW>(w[j], w1 + (int64_t)((j0 + j) * 8 + g < R ? (j0 + j) * 8 + g : 0) * p.K, b, q, p.K);
+                }
 #pragma unroll
-                        for (int j = 0; j < NT; ++j)
-                            mma16<TW>(acc[m][j], x0[2 * s], x1[2 * s], x0[2 * s + 1], x1[2 * s + 1], w[j][2 * s], w[j][2 * s + 1]);
+                for (int m0 = 0; m0 < MT; m0 += XB) {
+                    if (m0 * 16 >= tile.count) break;
+                    unsigned x[XB][2][XW];
+                    if (fast) {
+#pragma unroll
+                        for (int m = 0; m < XB; ++m)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+                                load16<TX>(x[m][h], static_cast<const TX *>(p.x) + (int64_t)s_token[(m0 + m) * 16 + 8 * h + g] * p.ldx + b * 64 + q * 16);
                     } else {
-                        unsigned a[4][3];
-                        split3(__uint_as_float(x0[4 * s]), __uint_as_float(x0[4 * s + 1]), a[0][0], a[0][1], a[0][2]);
-                        split3(__uint_as_float(x1[4 * s]), __uint_as_float(x1[4 * s + 1]), a[1][0], a[1][1], a[1][2]);
-                        split3(__uint_as_float(x0[4 * s + 2]), __uint_as_float(x0[4 * s + 3]), a[2][0], a[2][1], a[2][2]);
-                        split3(__uint_as_float(x1[4 * s + 2]), __uint_as_float(x1[4 * s + 3]), a[3][0], a[3][1], a[3][2]);
 #pragma unroll
-                        for (int i = 2; i >= 0; --i)
+                        for (int m = 0; m < XB; ++m)
 #pragma unroll
-                            for (int j = 0; j < NT; ++j)
-                                mma16<TW>(acc[m][j], a[0][i], a[1][i], a[2][i], a[3][i], w[j][2 * s], w[j][2 * s + 1]);
+                            for (int h = 0; h < 2; ++h)
+                                load16_any<TX>(x[m][h], static_cast<const TX *>(p.x) + (int64_t)s_token[(m0 + m) * 16 + 8 * h + g] * p.ldx, b, q, p.K);
+                    }
+#pragma unroll
+                    for (int m = 0; m < XB; ++m) {
+                        const unsigned (&x0)[XW] = x[m][0], (&x1)[XW] = x[m][1];
+#pragma unroll
+                        for (int s = 0; s < 4; ++s) {
+                            if constexpr (sizeof(TX) == 2) {
+#pragma unroll
+                                for (int j = 0; j < WB; ++j)
+                                    mma16<TW>(acc[m0 + m][j0 + j], x0[2 * s], x1[2 * s], x0[2 * s + 1], x1[2 * s + 1], w[j][2 * s], w[j][2 * s + 1]);
+                            } else {
+                                unsigned a[4][3];
+                                split3(__uint_as_float(x0[4 * s]), __uint_as_float(x0[4 * s + 1]), a[0][0], a[0][1], a[0][2]);
+                                split3(__uint_as_float(x1[4 * s]), __uint_as_float(x1[4 * s + 1]), a[1][0], a[1][1], a[1][2]);
+                                split3(__uint_as_float(x0[4 * s + 2]), __uint_as_float(x0[4 * s + 3]), a[2][0], a[2][1], a[2][2]);
+                                split3(__uint_as_float(x1[4 * s + 2]), __uint_as_float(x1[4 * s + 3]), a[3][0], a[3][1], a[3][2]);
+#pragma unroll
+                                for (int i = 2; i >= 0; --i)
+#pragma unroll
+                                    for (int j = 0; j < WB; ++j)
+                                        mma16<TW>(acc[m0 + m][j0 + j], a[0][i], a[1][i], a[2][i], a[3][i], w[j][2 * s], w[j][2 * s + 1]);
+                            }
+                        }
                     }
                 }
+            }
+        }
+        // ---- the second product's first operands are on their way while V is summed up
+        if (g_first < groups) load_group(g_first);
+        if (p.base != nullptr && p.vec_y) {
+            constexpr int kLine = 128 / (int)sizeof(TY);       // a warp takes the lines of its first group
+            for (int row = lane; row < tile.count; row += 32) {
+                const TY *at = static_cast<const TY *>(p.base) + (int64_t)s_token[row] * p.ldbase + (int64_t)g_first * 64;
+#pragma unroll
+                for (int i = 0; i < 64; i += kLine)
+                    if ((int64_t)g_first * 64 + i < p.N) prefetch_l2(at + i);
             }
         }
         // ---- sum over the warps, then over the cluster
@@ -276,44 +360,55 @@ __global__ void __launch_bounds__(kTokThreads, 2) adapter_tokens_kernel(const Ad
         const float alpha = p.alpha != nullptr ? __ldg(p.alpha + tile.adapter) : 1.0f;
         for (int i = threadIdx.x; i < Smem::kTile / 4; i += kTokThreads) {
             const uint32_t here = smem_u32(s_part + 4 * i);
-            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int c = 0; c < cs; ++c) {
-                const float4 o = ld_cluster_f4(mapa_u32(here, (uint32_t)c));
-                s.x += o.x;
-                s.y += o.y;
-                s.z += o.z;
-                s.w += o.w;
-            }
+            float4 part[kMaxClusterCtas];
+#pragma unroll
+            for (int c = 0; c < kMaxClusterCtas; ++c)
+                if (c < cs) part[c] = ld_cluster_f4(mapa_u32(here, (uint32_t)c));
+            float4 s = part[0];
+#pragma unroll
+            for (int c = 1; c < kMaxClusterCtas; ++c)
+                if (c < cs) {
+                    s.x += part[c].x;
+                    s.y += part[c].y;
+                    s.z += part[c].z;
+                    s.w += part[c].w;
+                }
             const int row = 4 * i / RT, r = 4 * i % RT;
             if (!BWD && p.v_out != nullptr && rank == 0 && row < tile.count && r < R)
                 *reinterpret_cast<float4 *>(p.v_out + (int64_t)s_token[row] * R + r) = s;
-            *reinterpret_cast<float4 *>(s_v + row * Smem::kPad + r) = make_float4(alpha * s.x, alpha * s.y, alpha * s.z, alpha * s.w);
+            float v[4] = {alpha * s.x, alpha * s.y, alpha * s.z, alpha * s.w}, hi[4], lo[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                hi[j] = __uint_as_float(__float_as_uint(v[j]) & 0xffffe000u);
+                lo[j] = rest_of(v[j], hi[j]);
+            }
+            *reinterpret_cast<float4 *>(s_hi + row * Smem::kPad + r) = make_float4(hi[0], hi[1], hi[2], hi[3]);
+            *reinterpret_cast<float4 *>(s_lo + row * Smem::kPad + r) = make_float4(lo[0], lo[1], lo[2], lo[3]);
         }
         cluster_arrive();                                      // (waited for before the CTA leaves)
         __syncthreads();
         if constexpr (BWD) {
-            // U (times the row's scale) from CTA 0, alpha V from CTA 1 or the same
-            const int steps = (tile.count + 15) / 16, mtr = (R + 15) / 16;
-            for (int half = 0; half < 2; ++half) {
-                if (rank != half % cs) continue;
-                for (int i = warp; i < steps * mtr; i += kTokWarps) {
-                    const int st = i / mtr, m = i % mtr;
-                    float f[2][4];
+            // fragments of U (times the row's scale) and of alpha V, dealt out over the cluster
+            const int steps = (tile.count + 15) / 16, mtr = (R + 15) / 16, half_items = steps * mtr;
+            for (int i = rank + cs * warp; i < 2 * half_items; i += cs * kTokWarps) {
+                const bool is_u = i < half_items;
+                const int k = is_u ? i : i - half_items, st = k / mtr, m = k % mtr;
+                float f[2][4];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                for (int e = 0; e < 4; ++e) {
+                    const int row = st * 16 + 4 * q + e;
+                    const int64_t t = s_token[row];
+                    const float factor = is_u ? __ldg(p.scales + t * p.scale_stride) : alpha;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int row = st * 16 + 4 * q + e, r = m * 16 + g + 8 * h;
-                            float v = 0.0f;
-                            if (row < tile.count && r < R) {
-                                const int64_t t = s_token[row];
-                                if (half == 0) v = s_v[row * Smem::kPad + r] * (p.scales != nullptr ? __ldg(p.scales + t * p.scale_stride) : 1.0f);
-                                else v = alpha * __ldg(p.v_in + t * R + r);
-                            }
-                            f[h][e] = v;
-                        }
-                    store_fragment((half == 0 ? p.frag_u : p.frag_v) + ((int64_t)(tile.step + st) * mtr + m) * 96, lane, f[0], f[1]);
+                    for (int h = 0; h < 2; ++h) {
+                        const int r = m * 16 + g + 8 * h;
+                        float v = 0.0f;
+                        if (row < tile.count && r < R)
+                            v = factor * (is_u ? s_hi[row * Smem::kPad + r] + s_lo[row * Smem::kPad + r] : __ldg(p.v_in + t * R + r));
+                        f[h][e] = v;
+                    }
                 }
+                store_fragment((is_u ? p.frag_u : p.frag_v) + ((int64_t)(tile.step + st) * mtr + m) * 96, lane, f[0], f[1]);
             }
         }
     } else if (!BWD && p.v_out != nullptr && rank == 0) {
@@ -321,43 +416,53 @@ __global__ void __launch_bounds__(kTokThreads, 2) adapter_tokens_kernel(const Ad
     }
 
     // ---- y = base + V B over this CTA's groups of 64 columns
-    const TW *w2 = static_cast<const TW *>(p.w2) + (int64_t)max(tile.adapter, 0) * R * p.N;
-    const int groups = (int)((p.N + 63) / 64), slices = tile.adapter >= 0 ? R / 8 : 0;
-    const int gcol = (g & 1) * 16 + (g >> 1) * 4;              // the lane's columns as fragment column g: + jh * 32 + jl
-    for (int gi = rank * kTokWarps + warp; gi < groups; gi += cs * kTokWarps) {
+    for (int gi = g_first; gi < groups; gi += g_step) {
         const int64_t n0 = (int64_t)gi * 64;
+        const bool fast = p.vec_y && n0 + 64 <= p.N;
+        if (gi != g_first) load_group(gi);
 #pragma unroll 1
         for (int m = 0; m < MT; ++m) {
             if (m * 16 >= tile.count) break;
-            int tok[2] = {s_token[m * 16 + g], s_token[m * 16 + g + 8]};
-            float4 out[2][4];                                  // base first: [row][jh * 2 + b]
+            const int64_t tok[2] = {s_token[m * 16 + g], s_token[m * 16 + g + 8]};
+            Quad<TY> base[2][4];                               // [row][jh * 2 + b]
+            if (p.base != nullptr) {
+                const TY *r0 = static_cast<const TY *>(p.base) + tok[0] * p.ldbase, *r1 = static_cast<const TY *>(p.base) + tok[1] * p.ldbase;
+                if (fast) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                    for (int i = 0; i < 4; ++i) base[0][i] = load_quad<TY>(r0 + n0 + i * 16 + q * 4);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    out[h][i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (p.base != nullptr && tok[h] >= 0)
-                        out[h][i] = load4<TY>(static_cast<const TY *>(p.base) + (int64_t)tok[h] * p.ldbase, n0 + i * 16 + q * 4, p.N, p.vec_y);
+                    for (int i = 0; i < 4; ++i) base[1][i] = load_quad<TY>(r1 + n0 + i * 16 + q * 4);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) base[0][i] = load_quad_any<TY>(r0, n0 + i * 16 + q * 4, p.N);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) base[1][i] = load_quad_any<TY>(r1, n0 + i * 16 + q * 4, p.N);
                 }
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < (int)sizeof(TY); ++j) base[h][i].w[j] = 0u;
+            }
             float acc[8][4];
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[j][i] = 0.0f;
-#pragma unroll 2
-            for (int s = 0; s < slices; ++s) {
-                const float *row0 = s_v + (m * 16 + g) * Smem::kPad + s * 8 + q, *row1 = row0 + 8 * Smem::kPad;
-                const float av[4] = {row0[0], row1[0], row0[4], row1[4]};
+            const int at = (m * 16 + g) * Smem::kPad + q;
+            auto slice = [&](const Quad<TW> (&b)[2][2], int s) {
+                const int o = at + s * 8;
                 unsigned hi[4], lo[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    hi[i] = __float_as_uint(av[i]) & 0xffffe000u;
-                    lo[i] = __float_as_uint(rest_of(av[i], __uint_as_float(hi[i])));
+                    hi[i] = __float_as_uint(s_hi[o + (i & 1) * 8 * Smem::kPad + (i >> 1) * 4]);
+                    lo[i] = __float_as_uint(s_lo[o + (i & 1) * 8 * Smem::kPad + (i >> 1) * 4]);
                 }
-                const TW *b0 = w2 + (int64_t)(s * 8 + q) * p.N, *b1 = b0 + 4 * p.N;
 #pragma unroll
                 for (int jh = 0; jh < 2; ++jh) {
-                    const float4 f0 = load4<TW>(b0, n0 + jh * 32 + gcol, p.N, p.vec_w2), f1 = load4<TW>(b1, n0 + jh * 32 + gcol, p.N, p.vec_w2);
+                    const float4 f0 = quad_floats<TW>(b[0][jh]), f1 = quad_floats<TW>(b[1][jh]);
                     const float e0[4] = {f0.x, f0.y, f0.z, f0.w}, e1[4] = {f1.x, f1.y, f1.z, f1.w};
 #pragma unroll
                     for (int jl = 0; jl < 4; ++jl) {
@@ -365,15 +470,26 @@ __global__ void __launch_bounds__(kTokThreads, 2) adapter_tokens_kernel(const Ad
                         mma8_tf32(acc[jh * 4 + jl], hi[0], hi[1], hi[2], hi[3], __float_as_uint(e0[jl]), __float_as_uint(e1[jl]));
                     }
                 }
+            };
+            if constexpr (kHoldB) {
+#pragma unroll
+                for (int s = 0; s < NT; ++s)
+                    if (s < slices) slice(bq[s], s);
+            } else {
+#pragma unroll 2
+                for (int s = 0; s < slices; ++s) {
+                    load_b(bq[0], s, n0);
+                    slice(bq[0], s);
+                }
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (tok[h] < 0) continue;
-                TY *row = static_cast<TY *>(p.y) + (int64_t)tok[h] * p.ldy;
+                if (m * 16 + g + 8 * h >= tile.count) continue;
+                TY *row = static_cast<TY *>(p.y) + tok[h] * p.ldy;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int jh = i >> 1, b = i & 1;
-                    float4 o = out[h][i];
+                    float4 o = quad_floats<TY>(base[h][i]);
                     o.x += acc[jh * 4][2 * h + b];
                     o.y += acc[jh * 4 + 1][2 * h + b];
                     o.z += acc[jh * 4 + 2][2 * h + b];
@@ -404,38 +520,48 @@ struct AdapterGrad {
     const int *plan;
     int64_t T;
     int n, R;
+    int64_t perm_at, chunks_at, offsets_at;      // word offsets in the plan
     int blocks0;                 // blocks along x that belong to side 0
     int wc;                      // groups of 64 columns per block: 1, 2 or 4; the other warps share the tokens
+    int merge;                   // chunks that one block sums up
+    int chunk_slots;             // blocks along y that take chunks; n more look after adapters without tokens
 };
 
 // Eight columns of one token row.
 template <GradSrc S> struct SrcWords { static constexpr int n = S == GradSrc::F32 ? 8 : (S == GradSrc::Bf16 ? 4 : 2); };
 template <GradSrc S>
-__device__ __forceinline__ void load_src8(unsigned (&w)[SrcWords<S>::n], const void *src, int64_t ld, int token, int64_t c, int64_t cols, bool vec) {
+__device__ __forceinline__ void load_src8(unsigned (&w)[SrcWords<S>::n], const void *src, int64_t ld, int token, bool there, int64_t c,
+                                          int64_t cols, bool fast) {
     constexpr int W = SrcWords<S>::n;
 #pragma unroll
     for (int i = 0; i < W; ++i) w[i] = 0u;
-    if (token < 0 || c >= cols) return;
     if constexpr (W == 2) {                                    // rows of codes are padded to 16: eight are always there
-        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(src) + (int64_t)token * ld + c));
-        w[0] = v.x;
-        w[1] = v.y;
+        if (there && c < cols) {
+            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(src) + (int64_t)token * ld + c));
+            w[0] = v.x;
+            w[1] = v.y;
+        }
     } else {
         using T = typename Elem<S == GradSrc::F32 ? DYBIT_F32 : DYBIT_BF16>::type;
-        const T *row = static_cast<const T *>(src) + (int64_t)token * ld + c;
-        if (vec && c + 8 <= cols) {
+        const T *row = static_cast<const T *>(src) + (int64_t)token * ld;
+        if (fast) {
+            if (there) {
 #pragma unroll
-            for (int i = 0; i < W / 4; ++i) {
-                const uint4 v = __ldg(reinterpret_cast<const uint4 *>(row) + i);
-                w[4 * i] = v.x;
-                w[4 * i + 1] = v.y;
-                w[4 * i + 2] = v.z;
-                w[4 * i + 3] = v.w;
+                for (int i = 0; i < W / 4; ++i) {
+                    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(row + c) + i);
+                    w[4 * i] = v.x;
+                    w[4 * i + 1] = v.y;
+                    w[4 * i + 2] = v.z;
+                    w[4 * i + 3] = v.w;
+                }
             }
         } else {
             T e[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = c + j < cols ? row[j] : from_f32<T>(0.0f);
+            for (int j = 0; j < 8; ++j) {
+                const T v = row[c + j < cols ? c + j : cols - 1];
+                e[j] = there && c + j < cols ? v : from_f32<T>(0.0f);
+            }
 #pragma unroll
             for (int i = 0; i < W; ++i) w[i] = reinterpret_cast<const unsigned *>(e)[i];
         }
@@ -465,8 +591,10 @@ __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const Ad
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int wc = warp % p.wc, wt = warp / p.wc, ntg = kTokWarps / p.wc;
     const int64_t c0 = ((int64_t)block * p.wc + wc) * 64;
-    const int mtr = (p.R + 15) / 16, steps = (ch.count + 15) / 16;
-    const int *perm = p.plan + PlanLayout(p.T, p.n).perm + ch.start;
+    const int mtr = (p.R + 15) / 16, count = min(ch.rest, p.merge * kChunkTokens), steps = (count + 15) / 16;
+    const bool fast = sd.vec && c0 + 64 <= sd.cols;
+    const int *perm = p.plan + p.perm_at + ch.start;
+    const uint4 *frag = sd.frag + ((int64_t)ch.step * mtr + r0) * 96 + lane;
     float acc[MR][8][4];
 #pragma unroll
     for (int m = 0; m < MR; ++m)
@@ -474,31 +602,53 @@ __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const Ad
         for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
-    for (int st = wt; st < steps; st += ntg) {
-        unsigned src[4][W];
+    // two steps ahead: the token numbers; one step ahead: the rows
+    int tok[4];
+    unsigned src[4][W];
+    auto load_tokens = [&](int st) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int row = st * 16 + 4 * q + e;
-            load_src8<S>(src[e], sd.src, sd.ld, row < ch.count ? __ldg(perm + row) : -1, c0 + 8 * g, sd.cols, sd.vec);
+            tok[e] = row < count ? __ldg(perm + row) : -1;
         }
-        uint4 a[MR][3];
+    };
+    auto load_rows = [&]() {
 #pragma unroll
-        for (int m = 0; m < MR; ++m)
+        for (int e = 0; e < 4; ++e) load_src8<S>(src[e], sd.src, sd.ld, max(tok[e], 0), tok[e] >= 0, c0 + 8 * g, sd.cols, fast);
+    };
+    if (wt < steps && c0 < sd.cols) {
+        load_tokens(wt);
+        load_rows();
+        load_tokens(wt + ntg);
+        for (int st = wt; st < steps; st += ntg) {
+            unsigned cur[4][W];
 #pragma unroll
-            for (int i = 0; i < 3; ++i)
-                a[m][i] = r0 + m < mtr ? __ldg(sd.frag + (((int64_t)(ch.step + st) * mtr + r0 + m) * 3 + i) * 32 + lane) : make_uint4(0u, 0u, 0u, 0u);
+            for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            unsigned b0[P], b1[P];
-            src_pair<S>(b0, src[0], src[1], j);
-            src_pair<S>(b1, src[2], src[3], j);
+                for (int i = 0; i < W; ++i) cur[e][i] = src[e][i];
+            uint4 a[MR][3];
 #pragma unroll
             for (int m = 0; m < MR; ++m)
 #pragma unroll
-                for (int i = 2; i >= 0; --i)
+                for (int i = 0; i < 3; ++i)
+                    a[m][i] = MR == 1 || r0 + m < mtr ? __ldg(frag + ((int64_t)st * mtr + m) * 96 + i * 32) : make_uint4(0u, 0u, 0u, 0u);
+            if (st + ntg < steps) {
+                load_rows();
+                load_tokens(st + 2 * ntg);
+            }
 #pragma unroll
-                    for (int k = P - 1; k >= 0; --k)
-                        if (i + k <= 2) mma16<__nv_bfloat16>(acc[m][j], a[m][i].x, a[m][i].y, a[m][i].z, a[m][i].w, b0[k], b1[k]);
+            for (int j = 0; j < 8; ++j) {
+                unsigned b0[P], b1[P];
+                src_pair<S>(b0, cur[0], cur[1], j);
+                src_pair<S>(b1, cur[2], cur[3], j);
+#pragma unroll
+                for (int m = 0; m < MR; ++m)
+#pragma unroll
+                    for (int i = 2; i >= 0; --i)
+#pragma unroll
+                        for (int k = P - 1; k >= 0; --k)
+                            if (i + k <= 2) mma16<__nv_bfloat16>(acc[m][j], a[m][i].x, a[m][i].y, a[m][i].z, a[m][i].w, b0[k], b1[k]);
+            }
         }
     }
     // the token groups' sums meet in shared memory, added in order
@@ -528,7 +678,9 @@ __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const Ad
                 }
         }
     }
-    float *out = ch.partial >= 0 ? sd.partial + (int64_t)ch.partial * p.R * sd.cols : sd.out + (int64_t)ch.adapter * p.R * sd.cols;
+    const bool whole = ch.index == 0 && ch.rest <= p.merge * kChunkTokens;
+    float *out = whole ? sd.out + (int64_t)ch.adapter * p.R * sd.cols
+                       : sd.partial + (int64_t)(ch.partial + ch.index / p.merge) * p.R * sd.cols;
     const bool vec = sd.cols % 4 == 0 && aligned16(out);
 #pragma unroll
     for (int m = 0; m < MR; ++m)
@@ -540,36 +692,54 @@ __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const Ad
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int j = 0; j < 8; j += 4)
-                    store4<float>(out + (int64_t)r * sd.cols, c0 + (2 * q + b) * 8 + j, sd.cols, vec,
+                    if (c0 + (2 * q + b) * 8 + j < sd.cols)
+                        store4<float>(out + (int64_t)r * sd.cols, c0 + (2 * q + b) * 8 + j, sd.cols, vec,
                                   make_float4(acc[m][j][2 * h + b], acc[m][j + 1][2 * h + b], acc[m][j + 2][2 * h + b], acc[m][j + 3][2 * h + b]));
         }
 }
 
-// blockIdx: x = columns (side 0, then side 1), y = chunk, z = ranks beyond 16 * MR.
+// blockIdx: x = columns (side 0, then side 1), y = chunk (then adapters without tokens, whose gradients are zero),
+// z = ranks beyond 16 * MR.
 template <GradSrc S0, GradSrc S1, int MR>
-__global__ void __launch_bounds__(kTokThreads, MR <= 2 ? 2 : 1) adapter_grad_kernel(const __grid_constant__ AdapterGrad p) {
+__global__ void __launch_bounds__(kTokThreads, MR == 1 ? 2 : 1) adapter_grad_kernel(const __grid_constant__ AdapterGrad p) {
     extern __shared__ __align__(16) float smem_f[];
     pdl_enter();
-    if ((int)blockIdx.y >= p.plan[3]) return;
-    const AdapterChunk ch = reinterpret_cast<const AdapterChunk *>(p.plan + PlanLayout(p.T, p.n).chunks)[blockIdx.y];
     const int r0 = (int)blockIdx.z * MR;
-    if ((int)blockIdx.x < p.blocks0) adapter_grad_body<S0, MR>(p, p.side[0], (int)blockIdx.x, ch, r0, smem_f);
-    else adapter_grad_body<S1, MR>(p, p.side[1], (int)blockIdx.x - p.blocks0, ch, r0, smem_f);
+    const bool first = (int)blockIdx.x < p.blocks0;
+    const int block = (int)blockIdx.x - (first ? 0 : p.blocks0);
+    if ((int)blockIdx.y >= p.chunk_slots) {
+        const int a = (int)blockIdx.y - p.chunk_slots;
+        const int *off = p.plan + p.offsets_at + (int64_t)a * kPlanColumns;
+        if (off[kPlanColumns] != off[0]) return;
+        const int64_t cols = p.side[first ? 0 : 1].cols, width = 64 * p.wc;
+        float *out = p.side[first ? 0 : 1].out + (int64_t)a * p.R * cols;
+        for (int64_t i = threadIdx.x; i < 16 * MR * width; i += kTokThreads) {
+            const int64_t r = r0 * 16 + i / width, c = (int64_t)block * width + i % width;
+            if (r < p.R && c < cols) out[r * cols + c] = 0.0f;
+        }
+        return;
+    }
+    if ((int)blockIdx.y >= p.plan[3]) return;
+    const AdapterChunk ch = reinterpret_cast<const AdapterChunk *>(p.plan + p.chunks_at)[blockIdx.y];
+    if (ch.index % p.merge != 0) return;
+    if (first) adapter_grad_body<S0, MR>(p, p.side[0], block, ch, r0, smem_f);
+    else adapter_grad_body<S1, MR>(p, p.side[1], block, ch, r0, smem_f);
 }
 
-// Adapters with several chunks: the chunks' sums, added in order; adapters without tokens: zeros.
+// Adapters that several blocks worked on: their sums, added in order.
 __global__ void __launch_bounds__(256) adapter_grad_sum_kernel(const __grid_constant__ AdapterGrad p) {
     pdl_enter();
     const int a = blockIdx.y;
-    const int *off = p.plan + PlanLayout(p.T, p.n).offsets + (int64_t)a * kPlanColumns;
-    const int chunks = off[kPlanColumns + 4] - off[4], first = off[5];
-    if (chunks == 1) return;
+    const int *off = p.plan + p.offsets_at + (int64_t)a * kPlanColumns;
+    const int parts = (off[kPlanColumns + 4] - off[4] + p.merge - 1) / p.merge, first = off[5];
+    if (parts <= 1) return;
     for (int s = 0; s < 2; ++s) {
         const AdapterGradSide &sd = p.side[s];
         const int64_t size = p.R * sd.cols;                    // a multiple of 8
         for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size / 4; i += (int64_t)gridDim.x * 256) {
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int c = 0; c < chunks; ++c) {
+#pragma unroll 4
+            for (int c = 0; c < parts; ++c) {
                 const float4 o = __ldcg(reinterpret_cast<const float4 *>(sd.partial + (int64_t)(first + c) * size) + i);
                 v.x += o.x;
                 v.y += o.y;
@@ -593,10 +763,8 @@ __global__ void __launch_bounds__(256) adapter_grad_sum_kernel(const __grid_cons
 
 static bool rows_vec(const void *p, int64_t ld, int elem, int bytes) { return aligned(p, bytes) && (ld * elem) % bytes == 0; }
 
-constexpr int kMaxClusterCtas = 8;
-
 template <typename TX, typename TW, typename TY, int RT, int MT, bool BWD>
-static dybit_status launch_tokens(const AdapterTokens &p, int cs, cudaStream_t s) {
+static dybit_status launch_tokens(AdapterTokens p, int cs, cudaStream_t s) {
     auto kern = adapter_tokens_kernel<TX, TW, TY, RT, MT, BWD>;
     constexpr int smem = TokSmem<RT, MT>::kBytes;
     static std::atomic<bool> ready[64];
@@ -608,7 +776,9 @@ static dybit_status launch_tokens(const AdapterTokens &p, int cs, cudaStream_t s
         ready[dev].store(true, std::memory_order_release);
     }
     const PlanLayout L(p.T, p.n);
-    const int64_t blocks = L.tiles_cap[MT == 1 ? 0 : (MT == 2 ? 1 : 2)] * cs;
+    constexpr int kList = MT == 1 ? 0 : (MT == 2 ? 1 : 2);
+    p.perm_at = L.perm, p.tiles_at = L.tiles[kList];
+    const int64_t blocks = L.tiles_cap[kList] * cs;
     if (blocks > 0x7fffffff) return DYBIT_ERR_UNSUPPORTED;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
@@ -630,44 +800,73 @@ static dybit_status launch_tokens(const AdapterTokens &p, int cs, cudaStream_t s
 
 template <typename TX, typename TW, typename TY, bool BWD>
 static dybit_status launch_tokens_rank(const AdapterTokens &p, cudaStream_t s) {
-    // tiles of several 16-token slices read the factors once for all of them: worth it where adapters have that many tokens
-    const bool many = p.T >= 32 * (int64_t)p.n;
-    const int cs = kMaxClusterCtas;
-    if (p.R <= 16) return many ? launch_tokens<TX, TW, TY, 16, 4, BWD>(p, cs, s) : launch_tokens<TX, TW, TY, 16, 1, BWD>(p, cs, s);
-    if (p.R <= 32) return many ? launch_tokens<TX, TW, TY, 32, 4, BWD>(p, cs, s) : launch_tokens<TX, TW, TY, 32, 1, BWD>(p, cs, s);
-    if (p.R <= 64) return many ? launch_tokens<TX, TW, TY, 64, 2, BWD>(p, cs, s) : launch_tokens<TX, TW, TY, 64, 1, BWD>(p, cs, s);
-    return launch_tokens<TX, TW, TY, 128, 1, BWD>(p, cs, s);
+    const PlanLayout L(p.T, p.n);
+    // CTAs of a tile: enough of them to give every SM most of two, but at least four of the 64-column blocks to each
+    const int64_t widest = ((p.K > p.N ? p.K : p.N) + 63) / 64;
+    auto cluster = [&](int64_t tiles) {
+        int cs = 1;
+        while (cs < kMaxClusterCtas && cs * 4 < widest && tiles * cs * 4 < (int64_t)sm_count() * 7) cs *= 2;
+        return cs;
+    };
+    const int c1 = cluster(L.tiles_cap[0]), c2 = cluster(L.tiles_cap[1]), c4 = cluster(L.tiles_cap[2]);
+    // tiles of several 16-token slices read the factors once for all of them: taken where adapters have that many tokens
+    // and the tiles still fill the device
+    const bool many = p.T >= 32 * (int64_t)p.n, four = many && L.tiles_cap[2] * c4 >= sm_count(), two = many && L.tiles_cap[1] * c2 >= sm_count();
+    if (p.R <= 16) return four ? launch_tokens<TX, TW, TY, 16, 4, BWD>(p, c4, s) : launch_tokens<TX, TW, TY, 16, 1, BWD>(p, c1, s);
+    if (p.R <= 32) return two ? launch_tokens<TX, TW, TY, 32, 2, BWD>(p, c2, s) : launch_tokens<TX, TW, TY, 32, 1, BWD>(p, c1, s);
+    if (p.R <= 64) return two ? launch_tokens<TX, TW, TY, 64, 2, BWD>(p, c2, s) : launch_tokens<TX, TW, TY, 64, 1, BWD>(p, c1, s);
+    return launch_tokens<TX, TW, TY, 128, 1, BWD>(p, c1, s);
+}
+
+// Lets a kernel use `bytes` of dynamic shared memory; once per kernel and device.
+static dybit_status allow_smem(const void *kernel, int bytes, std::atomic<bool> *ready) {
+    int dev = 0;
+    DYBIT_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return DYBIT_ERR_CUDA;
+    if (!ready[dev].load(std::memory_order_acquire)) {
+        DYBIT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+        ready[dev].store(true, std::memory_order_release);
+    }
+    return DYBIT_OK;
+}
+
+template <GradSrc S0, GradSrc S1, int MR>
+static dybit_status launch_grad_ranks(const AdapterGrad &p, dim3 grid, int smem, cudaStream_t s) {
+    static std::atomic<bool> ready[64];
+    auto kern = adapter_grad_kernel<S0, S1, MR>;
+    const dybit_status st = allow_smem(reinterpret_cast<const void *>(kern), (kTokWarps - 1) * MR * 16 * 64 * 4, ready);
+    if (st != DYBIT_OK) return st;
+    launch_k(kern, grid, dim3(kTokThreads), (size_t)smem, s, p);
+    return launch_status();
 }
 
 template <GradSrc S0, GradSrc S1>
 static dybit_status launch_grad(const AdapterGrad &p_in, cudaStream_t s) {
     AdapterGrad p = p_in;
     const PlanLayout L(p.T, p.n);
+    p.perm_at = L.perm, p.chunks_at = L.chunks, p.offsets_at = L.offsets;
     const int mtr = (p.R + 15) / 16, mr = mtr >= 3 ? 4 : mtr, z = (mtr + mr - 1) / mr;
-    // wide blocks read longer runs of a row and the left operand less often; narrow ones fill the device
-    p.wc = 4;
+    // wide blocks read longer runs of a row and the left operand less often, long chunks leave fewer parts to add up; both
+    // only as far as the device stays full
+    const int64_t fill = (int64_t)sm_count() * 3 / 2, chunks = p.T / kChunkTokens + 1;
+    p.wc = 4, p.merge = 1;
     auto blocks = [&](int side) { return (p.side[side].cols + 64 * p.wc - 1) / (64 * p.wc); };
-    while (p.wc > 1 && (blocks(0) + blocks(1)) * L.chunks_cap * z < sm_count()) p.wc /= 2;
+    while (p.wc > 1 && (blocks(0) + blocks(1)) * L.chunks_cap * z < fill) p.wc /= 2;
+    while (p.merge < 8 && (blocks(0) + blocks(1)) * z * (chunks / (2 * p.merge)) >= fill) p.merge *= 2;
     p.blocks0 = (int)blocks(0);
-    const int64_t bx = blocks(0) + blocks(1);
-    if (bx > 0x7fffffff || L.chunks_cap > 65535) return DYBIT_ERR_UNSUPPORTED;
+    p.chunk_slots = (int)L.chunks_cap;
+    const int64_t bx = blocks(0) + blocks(1), by = L.chunks_cap + p.n;
+    if (bx > 0x7fffffff || by > 65535) return DYBIT_ERR_UNSUPPORTED;
     const int smem = (kTokWarps - p.wc) * mr * 16 * 64 * 4;
-    auto go = [&](auto kern) {
-        DYBIT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-        launch_k(kern, dim3((unsigned)bx, (unsigned)L.chunks_cap, (unsigned)z), dim3(kTokThreads), (size_t)smem, s, p);
-        return launch_status();
-    };
+    const dim3 grid((unsigned)bx, (unsigned)by, (unsigned)z);
     dybit_status st;
-    if (L.chunks_cap > 0) {
-        if (mr == 1) st = go(adapter_grad_kernel<S0, S1, 1>);
-        else if (mr == 2) st = go(adapter_grad_kernel<S0, S1, 2>);
-        else st = go(adapter_grad_kernel<S0, S1, 4>);
-        if (st != DYBIT_OK) return st;
-    }
+    if (mr == 1) st = launch_grad_ranks<S0, S1, 1>(p, grid, smem, s);
+    else if (mr == 2) st = launch_grad_ranks<S0, S1, 2>(p, grid, smem, s);
+    else st = launch_grad_ranks<S0, S1, 4>(p, grid, smem, s);
+    if (st != DYBIT_OK || p.T <= (int64_t)p.merge * kChunkTokens) return st;       // no adapter has several parts
     const int64_t most = p.side[0].cols > p.side[1].cols ? p.side[0].cols : p.side[1].cols;
-    int64_t bs = (p.R * most / 4 + 255) / 256;
-    if (bs > 64) bs = 64;
-    if (bs < 1) bs = 1;
+    int64_t bs = (p.R * most / 4 + 255) / 256, cap = 8 * (int64_t)sm_count() / p.n + 1;
+    if (bs > cap) bs = cap;
     launch_k(adapter_grad_sum_kernel, dim3((unsigned)bs, (unsigned)p.n), dim3(256), 0, s, p);
     return launch_status();
 }

@@ -11,13 +11,13 @@
 namespace dybit {
 
 constexpr int kPlanThreads = 1024;
-constexpr int kChunkTokens = 512;            // tokens of one adapter whose gradients one block column sums up
+constexpr int kChunkTokens = 512;            // the gradient kernel sums up one or more chunks of an adapter's tokens per block
 
 // A tile: up to 16, 32 or 64 tokens of one adapter.  `step` counts 16-token steps of assigned tokens.
 struct AdapterTile { int adapter, start, count, step; };
-// A chunk: up to kChunkTokens tokens of one adapter; `partial` is its slot among the chunks of adapters that have more
-// than one (-1 where the chunk is all of the adapter).
-struct AdapterChunk { int adapter, start, count, step, partial, pad0, pad1, pad2; };
+// A chunk: kChunkTokens tokens of one adapter, or what is left of it: `rest` tokens from its start on.  `index` counts the
+// chunks of the adapter; `partial` is the adapter's first slot among the chunks of adapters that have more than one.
+struct AdapterChunk { int adapter, start, rest, step, index, partial, pad0, pad1; };
 
 // Word offsets of a plan's parts for (T, n); the capacities bound what the device fills in.
 struct PlanLayout {
@@ -129,8 +129,7 @@ __global__ void __launch_bounds__(kPlanThreads) adapters_place_kernel(const int 
         const int chunks = (count + kChunkTokens - 1) / kChunkTokens;
         AdapterChunk *list = reinterpret_cast<AdapterChunk *>(plan + L.chunks) + off[4];
         for (int k = threadIdx.x; k < chunks; k += kPlanThreads)
-            list[k] = {a, start + k * kChunkTokens, min(kChunkTokens, count - k * kChunkTokens),
-                       step0 + k * (kChunkTokens / 16), chunks > 1 ? off[5] + k : -1, 0, 0, 0};
+            list[k] = {a, start + k * kChunkTokens, count - k * kChunkTokens, step0 + k * (kChunkTokens / 16), k, off[5], 0, 0};
     }
 }
 

@@ -48,14 +48,24 @@ __device__ __forceinline__ VecFloats<T> vec_floats(const uint4 &v) {
     return o;
 }
 
-// Largest |x| of a vector; NaN is dropped, an infinity shows as such.
+// Largest bit pattern of |x| over vectors: patterns order like the numbers, with infinities and then NaN on top.  16-bit
+// elements are compared two at a time.
 template <typename T>
-__device__ __forceinline__ float vec_absmax(const uint4 &v, float best) {
-    const VecFloats<T> o = vec_floats<T>(v);
-#pragma unroll
-    for (int i = 0; i < (sizeof(T) == 4 ? 1 : 2); ++i)
-        best = fmaxf(fmaxf(fmaxf(best, fabsf(o.f[i].x)), fabsf(o.f[i].y)), fmaxf(fabsf(o.f[i].z), fabsf(o.f[i].w)));
-    return best;
+__device__ __forceinline__ unsigned vec_absmax(const uint4 &v, unsigned best) {
+    if constexpr (sizeof(T) == 4) {
+        return max(max(max(best, v.x & 0x7fffffffu), v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu));
+    } else {
+        best = __vmaxu2(__vmaxu2(best, v.x & 0x7fff7fffu), v.y & 0x7fff7fffu);
+        return __vmaxu2(__vmaxu2(best, v.z & 0x7fff7fffu), v.w & 0x7fff7fffu);
+    }
+}
+// The pattern as that of an fp32 number (NaN stays NaN, infinity infinity).
+template <typename T>
+__device__ __forceinline__ unsigned absmax_as_f32(unsigned best) {
+    if constexpr (sizeof(T) == 4) return best;
+    const unsigned top = max(best & 0xffffu, best >> 16);
+    if constexpr (__is_same(T, __half)) return __float_as_uint(__half2float(__ushort_as_half((unsigned short)top)));
+    return top << 16;
 }
 template <typename T>
 __device__ __forceinline__ float vec_absmax_finite(const uint4 &v, float best) {
@@ -68,10 +78,13 @@ __device__ __forceinline__ float vec_absmax_finite(const uint4 &v, float best) {
 }
 
 // Codes of a vector, stored at column `col` (row strides are multiples of 16, so the store is aligned and in the row).
+// LIMIT: for rows with infinities or NaN.
 template <typename T, bool SIGNED, bool LIMIT>
 __device__ __forceinline__ void store_vec_codes(const uint4 &v, float inv, uint8_t *dst) {
     const VecFloats<T> o = vec_floats<T>(v);
-    if constexpr (sizeof(T) == 4) {
+    if constexpr (!LIMIT && __is_same(T, __nv_bfloat16)) {
+        *reinterpret_cast<uint2 *>(dst) = encode8_bf16<SIGNED>(v, (__float_as_uint(inv) >> 16) * 0x00010001u);
+    } else if constexpr (sizeof(T) == 4) {
         *reinterpret_cast<unsigned *>(dst) = encode4_8<SIGNED, LIMIT>(o.f[0], inv);
     } else {
         *reinterpret_cast<uint2 *>(dst) = make_uint2(encode4_8<SIGNED, LIMIT>(o.f[0], inv), encode4_8<SIGNED, LIMIT>(o.f[1], inv));
@@ -93,14 +106,14 @@ struct CkptSave {
 template <typename T, bool SIGNED, bool VEC, int W, bool LONG>
 __global__ void __launch_bounds__(kCkptThreads) checkpoint_save_kernel(const CkptSave p) {
     constexpr int E = 16 / (int)sizeof(T), NV = kCkptPerThread / E, TPR = W * 32;
-    __shared__ float s_best[8];
+    __shared__ unsigned s_best[8];
     pdl_enter();
     const int sub = threadIdx.x / TPR, t = threadIdx.x % TPR;
     const int64_t row = (int64_t)blockIdx.x * (8 / W) + sub;
     if (W < 8 && row >= p.rows) return;                    // whole warps; with W > 1 the row's warps meet in a named barrier
     const T *x = static_cast<const T *>(p.x) + row * p.ld;
     uint4 v[NV];
-    float best = 0.0f;
+    unsigned best = 0u;
     if constexpr (!LONG) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) v[i] = load_row_vec<T, VEC>(x, (int64_t)(i * TPR + t) * E, p.cols);
@@ -109,33 +122,34 @@ __global__ void __launch_bounds__(kCkptThreads) checkpoint_save_kernel(const Ckp
     } else {
         for (int64_t c = (int64_t)t * E; c < p.cols; c += TPR * E) best = vec_absmax<T>(load_row_vec<T, VEC>(x, c, p.cols), best);
     }
-    // maximum of the row; a row with an infinity in it takes the maximum of its finite elements instead
-    auto row_max = [&](float b) {
-        b = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(b)));
+    best = absmax_as_f32<T>(best);
+    // maximum of the row; a row with infinities or NaN takes the maximum of its finite elements instead
+    auto row_max = [&](unsigned b) {
+        b = __reduce_max_sync(0xffffffffu, b);
         if constexpr (W > 1) {
             if ((threadIdx.x & 31) == 0) s_best[threadIdx.x >> 5] = b;
             asm volatile("bar.sync %0, %1;" ::"r"(1 + sub), "n"(TPR) : "memory");
 #pragma unroll
-            for (int w = 0; w < W; ++w) b = fmaxf(b, s_best[sub * W + w]);
+            for (int w = 0; w < W; ++w) b = max(b, s_best[sub * W + w]);
         }
         return b;
     };
     best = row_max(best);
-    const bool inf = __float_as_uint(best) >= 0x7f800000u;
-    if (inf) {
-        best = 0.0f;
+    const bool special = best >= 0x7f800000u;
+    if (special) {
+        float finite = 0.0f;
         if constexpr (!LONG) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) best = vec_absmax_finite<T>(v[i], best);
+            for (int i = 0; i < NV; ++i) finite = vec_absmax_finite<T>(v[i], finite);
         } else {
             for (int64_t c = (int64_t)t * E; c < p.cols; c += TPR * E)
-                best = vec_absmax_finite<T>(load_row_vec<T, VEC>(x, c, p.cols), best);
+                finite = vec_absmax_finite<T>(load_row_vec<T, VEC>(x, c, p.cols), finite);
         }
         if constexpr (W > 1) asm volatile("bar.sync %0, %1;" ::"r"(1 + sub), "n"(TPR) : "memory");   // s_best is free again
-        best = row_max(best);
+        best = row_max(__float_as_uint(finite));
     }
     float scale, inv;
-    pow2_scale(__float_as_uint(best), p.top, &scale, &inv);
+    pow2_scale(best, p.top, &scale, &inv);
     if (t == 0 && DYBIT_CHECK(row < p.rows, 0x60)) p.scales[row] = scale;
     uint8_t *out = p.codes + row * p.stride;
     if constexpr (!LONG) {
@@ -143,7 +157,7 @@ __global__ void __launch_bounds__(kCkptThreads) checkpoint_save_kernel(const Ckp
         for (int i = 0; i < NV; ++i) {
             const int64_t c = (int64_t)(i * TPR + t) * E;
             if (c < p.width) {
-                if (inf) store_vec_codes<T, SIGNED, true>(v[i], inv, out + c);
+                if (special) store_vec_codes<T, SIGNED, true>(v[i], inv, out + c);
                 else store_vec_codes<T, SIGNED, false>(v[i], inv, out + c);
             }
         }

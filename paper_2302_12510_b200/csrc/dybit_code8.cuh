@@ -132,4 +132,31 @@ __device__ __forceinline__ unsigned encode4_8(const float4 v, const float inv) {
     return mags | (tops & (mags + 0x7f7f7f7fu) & 0x80808080u);
 }
 
+// Eight bf16 elements (raw) -> eight codes, two elements to an instruction.  A bf16 number has as many significant bits
+// as the code axis asks for, so x * 2^k, the distance to the top of the axis and both roundings fit bf16: numbers of
+// 128 .. 256 have steps of 1 there, and 128 + n ends in n.  For rows without NaN and infinities.
+template <bool SIGNED>
+__device__ __forceinline__ uint2 encode8_bf16(const uint4 &v, unsigned inv2) {
+    constexpr int M = mag_bits8(SIGNED);
+    constexpr unsigned kTop = ((unsigned)(M + 253) << 7) * 0x00010001u;
+    const __nv_bfloat162 one = as_bf162(0x3f803f80u), c128 = as_bf162(0x43004300u);
+    const __nv_bfloat162 slope = as_bf162(SIGNED ? 0x42804280u : 0x43004300u);             // 2^(M-1)
+    unsigned c[4];
+    const unsigned x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        __nv_bfloat162 t = __hmul2(as_bf162(SIGNED ? x[i] & 0x7fff7fffu : x[i]), as_bf162(inv2));
+        if constexpr (!SIGNED) t = __hmax2(t, as_bf162(0u));
+        const unsigned line = as_u32(__hfma2(__hmin2(t, one), slope, c128));
+        const unsigned dist = as_u32(__hadd2(as_bf162(kTop - as_u32(__hmax2(t, one))), c128));
+        c[i] = line + (1u << (M - 1)) * 0x00010001u - dist;    // each half is the code: no borrow
+    }
+    uint2 o = make_uint2(__byte_perm(c[0], c[1], 0x6420), __byte_perm(c[2], c[3], 0x6420));
+    if constexpr (SIGNED) {
+        o.x |= __byte_perm(x[0], x[1], 0x7531) & (o.x + 0x7f7f7f7fu) & 0x80808080u;
+        o.y |= __byte_perm(x[2], x[3], 0x7531) & (o.y + 0x7f7f7f7fu) & 0x80808080u;
+    }
+    return o;
+}
+
 }  // namespace dybit
