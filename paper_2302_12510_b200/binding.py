@@ -737,14 +737,16 @@ def dybit_checkpoint_save(x: torch.Tensor, fmt, top: int = 2, codes: Optional[to
     lands in (2^(top-1), 2^top].  Returns (codes uint8 [rows][row bytes], scales float32 [rows])."""
     t, ld = _matrix(x, "x")
     rows, cols = x.shape
-    padded = (cols + 127) // 128 * 128
+    stride = padded = (cols + 127) // 128 * 128
+    given = codes is not None or scales is not None
     if codes is None:
         codes = x.new_empty((rows, padded), dtype=torch.uint8)
     if scales is None:
         scales = x.new_empty(rows, dtype=torch.float32)
-    stride, _ = _codes8(codes, rows, cols, scales, True)
-    if codes.shape[1] < padded and codes.shape[1] < stride:
-        raise ValueError("codes must have room for the columns rounded up to 128, or to the end of its rows")
+    if given:
+        stride, _ = _codes8(codes, rows, cols, scales, True)
+        if codes.shape[1] < padded and codes.shape[1] < stride:
+            raise ValueError("codes must have room for the columns rounded up to 128, or to the end of its rows")
     _check(lib.dybit_checkpoint_save(x.data_ptr(), t, rows, cols, ld, _fmt(fmt), top, codes.data_ptr(), stride,
                                      scales.data_ptr(), _stream(stream)), "dybit_checkpoint_save")
     return codes, scales
@@ -757,8 +759,11 @@ def dybit_checkpoint_load(codes: torch.Tensor, cols: int, fmt, scales: torch.Ten
     rows = codes.shape[0]
     stride, scale_stride = _codes8(codes, rows, cols, scales, per_row)
     if out is None:
-        out = codes.new_empty((rows, cols), dtype=dtype)
-    t, ld = _matrix(out, "out", rows, cols)
+        out, t, ld = codes.new_empty((rows, cols), dtype=dtype), _DTYPE_CODE.get(dtype), cols
+        if t is None:
+            raise ValueError("dtype must be float32, bfloat16 or float16")
+    else:
+        t, ld = _matrix(out, "out", rows, cols)
     _check(lib.dybit_checkpoint_load(codes.data_ptr(), stride, scales.data_ptr(), scale_stride, rows, cols, _fmt(fmt),
                                      out.data_ptr(), t, ld, _stream(stream)), "dybit_checkpoint_load")
     return out
@@ -768,10 +773,10 @@ def dybit_checkpoint_wgrad_workspace_bytes(T: int, N: int, K: int, dtype: torch.
     return int(lib.dybit_checkpoint_wgrad_workspace_bytes(int(T), int(N), int(K), _DTYPE_CODE[dtype]))
 
 
-def _workspace(need: int, ws: Optional[torch.Tensor], device):
-    """(address, bytes, tensor to keep) of a 1024-byte aligned workspace."""
+def _workspace(need: int, ws: Optional[torch.Tensor], like: torch.Tensor):
+    """(address, bytes, tensor to keep) of a 1024-byte aligned workspace on the device of `like`."""
     if ws is None:
-        ws = torch.empty(need + 1024, dtype=torch.uint8, device=device)
+        ws = like.new_empty(need + 1024, dtype=torch.uint8)
     at = ws.data_ptr()
     off = -at % 1024
     return at + off, ws.numel() - off, ws
@@ -785,11 +790,12 @@ def dybit_checkpoint_wgrad(dY: torch.Tensor, codes: torch.Tensor, K: int, fmt, s
     T, N = dY.shape
     stride, scale_stride = _codes8(codes, T, K, scales, per_row)
     if out is None:
-        out = dY.new_empty((N, K), dtype=torch.float32)
-    to, ldo = _matrix(out, "out", N, K)
-    if to != 0:
-        raise ValueError("out must be float32")
-    at, size, ws = _workspace(lib.dybit_checkpoint_wgrad_workspace_bytes(T, N, K, t), ws, dY.device)
+        out, ldo = dY.new_empty((N, K), dtype=torch.float32), K
+    else:
+        to, ldo = _matrix(out, "out", N, K)
+        if to != 0:
+            raise ValueError("out must be float32")
+    at, size, ws = _workspace(lib.dybit_checkpoint_wgrad_workspace_bytes(T, N, K, t), ws, dY)
     _check(lib.dybit_checkpoint_wgrad(T, N, K, dY.data_ptr(), t, ld, codes.data_ptr(), stride, _fmt(fmt), scales.data_ptr(),
                                       scale_stride, out.data_ptr(), ldo, at, size, _stream(stream)), "dybit_checkpoint_wgrad")
     return out
@@ -881,15 +887,16 @@ def dybit_adapters_backward(dY: torch.Tensor, codes: torch.Tensor, fmt, scales: 
     stride, scale_stride = _codes8(codes, T, K, scales, per_row)
     tb, ldb = (t, 0) if dx_base is None else _matrix(dx_base, "dx_base", T, K)
     if dx is None:
-        dx = dY.new_empty((T, K))
-    tx, ldx = _matrix(dx, "dx", T, K)
+        dx, tx, ldx = dY.new_empty((T, K)), t, K
+    else:
+        tx, ldx = _matrix(dx, "dx", T, K)
     if tx != t or tb != t:
         raise ValueError("dx and dx_base must have dY's dtype")
     if dA is None:
         dA = dY.new_empty((n, R, K), dtype=torch.float32)
     if dB is None:
         dB = dY.new_empty((n, R, N), dtype=torch.float32)
-    at, size, ws = _workspace(lib.dybit_adapters_backward_workspace_bytes(T, K, N, R, n), ws, dY.device)
+    at, size, ws = _workspace(lib.dybit_adapters_backward_workspace_bytes(T, K, N, R, n), ws, dY)
     _check(lib.dybit_adapters_backward(T, K, N, R, dY.data_ptr(), t, ldy, codes.data_ptr(), stride, _fmt(fmt),
                                        scales.data_ptr(), scale_stride, n, A.data_ptr(), B.data_ptr(), tw,
                                        None if alpha is None else alpha.data_ptr(), plan.address, _dense(v, "v", (T, R)),

@@ -72,7 +72,7 @@ struct AdapterTokens {
     int64_t T, K, N;
     int n, R;
     int64_t perm_at, tiles_at;   // word offsets in the plan
-    int vec_x, vec_w1, vec_y, vec_w2;      // rows can be moved in vectors (16 bytes; 4 elements for y and w2)
+    int fast;                    // all rows start where vectors can be moved: 16 bytes in x and w1, four elements in w2, base and y
     // backward: fragments for adapter_grad_kernel
     const float *v_in;
     const float *scales;
@@ -80,60 +80,84 @@ struct AdapterTokens {
     uint4 *frag_u, *frag_v;
 };
 
-// Sixteen consecutive elements of a row at column k (the lane's share of a 64-column block), as raw words.
-template <typename T>
-__device__ __forceinline__ void load16(unsigned (&w)[4 * sizeof(T)], const T *row) {
+// Sixteen consecutive elements of a row at column k (the lane's share of a 64-column block), as raw words, zeros from
+// column K on.  FAST: rows start on 16-byte boundaries and hold whole vectors.  Otherwise element loads without branches,
+// so that all of them are in flight together, and slot e of lane q takes column 4e + q of the block, so that four lanes
+// read neighbours; both operands of a product come in this order or both in the other.
+template <typename T, bool FAST>
+__device__ __forceinline__ void load16(unsigned (&w)[4 * sizeof(T)], const T *row, int block, int q, int K) {
+    if constexpr (FAST) {
+        constexpr int E = 16 / (int)sizeof(T);
+        const int k = block * 64 + q * 16;
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) {
-        const uint4 v = __ldg(reinterpret_cast<const uint4 *>(row) + i);
-        w[4 * i] = v.x;
-        w[4 * i + 1] = v.y;
-        w[4 * i + 2] = v.z;
-        w[4 * i + 3] = v.w;
+        for (int i = 0; i < (int)sizeof(T); ++i) {
+            const uint4 v = k + i * E < K ? __ldg(reinterpret_cast<const uint4 *>(row + k) + i) : make_uint4(0u, 0u, 0u, 0u);
+            w[4 * i] = v.x;
+            w[4 * i + 1] = v.y;
+            w[4 * i + 2] = v.z;
+            w[4 * i + 3] = v.w;
+        }
+    } else {
+        T e[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int c = block * 64 + 4 * i + q;
+            const T v = row[min(c, K - 1)];
+            e[i] = c < K ? v : from_f32<T>(0.0f);
+        }
+#pragma unroll
+        for (int i = 0; i < 4 * (int)sizeof(T); ++i) w[i] = reinterpret_cast<const unsigned *>(e)[i];
     }
-}
-// The same where rows may start anywhere and the block may reach past column K (zeros there): element loads without
-// branches, so that all of them are in flight together.  Slot e of lane q takes column 4e + q of the block, so that
-// four lanes read neighbours; both operands of a product come in this order or both in the other.
-template <typename T>
-__device__ __forceinline__ void load16_any(unsigned (&w)[4 * sizeof(T)], const T *row, int64_t block, int q, int64_t K) {
-    T e[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int64_t c = block * 64 + 4 * i + q;
-        const T v = row[c < K ? c : K - 1];
-        e[i] = c < K ? v : from_f32<T>(0.0f);
-    }
-#pragma unroll
-    for (int i = 0; i < 4 * (int)sizeof(T); ++i) w[i] = reinterpret_cast<const unsigned *>(e)[i];
 }
 
 // Four consecutive elements of a row, raw.
 template <typename T> struct Quad { unsigned w[sizeof(T)]; };
 template <typename T>
-__device__ __forceinline__ Quad<T> load_quad(const T *p) {
+__device__ __forceinline__ Quad<T> zero_quad() {
     Quad<T> o;
-    if constexpr (sizeof(T) == 4) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(p);
-        o.w[0] = v.x, o.w[1] = v.y, o.w[2] = v.z, o.w[3] = v.w;
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T); ++j) o.w[j] = 0u;
+    return o;
+}
+// FAST: rows start on boundaries of four elements and hold whole quads.
+template <typename T, bool FAST>
+__device__ __forceinline__ Quad<T> load_quad(const T *row, int c, int cols) {
+    Quad<T> o = zero_quad<T>();
+    if constexpr (FAST) {
+        if (c < cols) {
+            if constexpr (sizeof(T) == 4) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(row + c);
+                o.w[0] = v.x, o.w[1] = v.y, o.w[2] = v.z, o.w[3] = v.w;
+            } else {
+                const uint2 v = *reinterpret_cast<const uint2 *>(row + c);
+                o.w[0] = v.x, o.w[1] = v.y;
+            }
+        }
     } else {
-        const uint2 v = *reinterpret_cast<const uint2 *>(p);
-        o.w[0] = v.x, o.w[1] = v.y;
+        T e[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const T v = row[min(c + j, cols - 1)];
+            e[j] = c + j < cols ? v : from_f32<T>(0.0f);
+        }
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(T); ++j) o.w[j] = reinterpret_cast<const unsigned *>(e)[j];
     }
     return o;
 }
-template <typename T>
-__device__ __forceinline__ Quad<T> load_quad_any(const T *row, int64_t c, int64_t cols) {
-    T e[4];
+template <typename T, bool FAST>
+__device__ __forceinline__ void store_quad(T *row, int c, int cols, const float4 f) {
+    if constexpr (FAST) {
+        if (c < cols) {
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(row + c) = f;
+            else *reinterpret_cast<uint2 *>(row + c) = make_uint2(pack2<T>(f.x, f.y), pack2<T>(f.z, f.w));
+        }
+    } else {
+        const float e[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const T v = row[c + j < cols ? c + j : cols - 1];
-        e[j] = c + j < cols ? v : from_f32<T>(0.0f);
+        for (int j = 0; j < 4; ++j)
+            if (c + j < cols) row[c + j] = from_f32<T>(e[j]);
     }
-    Quad<T> o;
-#pragma unroll
-    for (int j = 0; j < (int)sizeof(T); ++j) o.w[j] = reinterpret_cast<const unsigned *>(e)[j];
-    return o;
 }
 template <typename T>
 __device__ __forceinline__ float4 quad_floats(const Quad<T> &v) {
@@ -192,32 +216,38 @@ constexpr int kMaxClusterCtas = 8;
 template <int RT, int MT>
 struct TokSmem {
     static constexpr int kTile = 16 * MT * RT;                 // floats of one token tile of V
-    static constexpr int kPad = RT + 4;                        // row of the tiles that feed the second product
-    static constexpr int kBytes = (kTokWarps * kTile + kTile + 2 * 16 * MT * kPad) * 4;
+    static constexpr int kFrag = MT * (RT / 16) * 4 * 128;     // words of its fragments for the second product (at most four parts)
+    static constexpr int kWords = kTokWarps * kTile > kFrag ? kTokWarps * kTile : kFrag;       // the warps' sums make room for them
+    static constexpr int kBytes = (kWords + kTile + (16 * MT * RT)) * 4;
 };
 
 // One cluster per tile of up to 16 * MT tokens of one adapter.  Its CTAs share the columns of x in the first product
 // and those of y in the second; in between they sum up their parts of V through distributed shared memory.  RT is the
-// rank rounded up (16, 32, 64, 128); ranks and columns that are missing are read as zeros, tokens that are missing
-// repeat the tile's first one and are not stored.
+// rank rounded up (16, 32, 64, 128); ranks and columns that are missing are zeros, tokens that are missing repeat the
+// tile's first one and are not stored.
 //
 // First product: a warp takes 64 columns at a time.  Lane (g = lane / 4, q = lane % 4) loads columns 16q .. 16q+15 of
 // token rows g, g + 8 and of factor rows g (+ 8 per n-tile) with 16-byte loads and uses them as the four K = 16 slices
 // of the fragment layout: the order of columns inside a sum is free as long as both operands take the same.
-// Second product: tf32, with V cut into two tf32 numbers (what is left over is below 2^-21 of V; the factors are exact
-// in tf32).  The 64 columns of a warp are dealt to fragment columns so that a lane ends up with four consecutive ones
-// and four lanes with sixteen.
-template <typename TX, typename TW, typename TY, int RT, int MT, bool BWD>
+// Second product: V, scaled by alpha, is cut into three bf16 numbers that hold all of it (f16 factors: into two tf32
+// numbers, off by less than 2^-21) and kept in shared memory as fragments.  The 64 columns of a warp are dealt to
+// fragment columns so that a lane ends up with four consecutive ones and four lanes with sixteen.  The base is added in
+// the accumulators where y has 16 bits (the tensor core cuts off what RN would round), by an fp32 addition otherwise.
+template <typename TX, typename TW, typename TY, int RT, int MT, bool BWD, bool FAST>
 __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_kernel(const AdapterTokens p) {
-    constexpr int NT = RT / 8, TM = 16 * MT, XW = 4 * (int)sizeof(TX);
-    constexpr int XB = sizeof(TX) == 4 || RT > 16 ? 1 : (MT < 2 ? MT : 2);                // 16-token slices whose loads are in flight together
+    constexpr int NT = RT / 8, RB = RT / 16, TM = 16 * MT, XW = 4 * (int)sizeof(TX);
+    constexpr int XB = sizeof(TX) == 4 || RT > 16 ? 1 : (MT < 2 ? MT : 2);     // 16-token slices whose loads are in flight together
     constexpr int WB = NT < 8 ? NT : 8;                                        // n-tiles of the factor in registers
+    constexpr bool kBf16 = __is_same(TW, __nv_bfloat16);
     constexpr bool kHoldB = RT <= 32;                                          // the second factor stays in registers across slices
+    constexpr int PARTS = kBf16 ? 3 : 4;                                       // fragments per 16 ranks
+    constexpr int BREGS = kBf16 ? 2 : 4;                                       // registers of the second factor per n-tile and 16 ranks
     using Smem = TokSmem<RT, MT>;
     extern __shared__ __align__(16) float smem_f[];
     float *s_warp = smem_f;                                    // [warps][TM][RT]
-    float *s_part = smem_f + kTokWarps * Smem::kTile;          // [TM][RT], read by the whole cluster
-    float *s_hi = s_part + Smem::kTile, *s_lo = s_hi + TM * Smem::kPad;        // alpha V: tf32 part and rest, [TM][RT + 4]
+    unsigned *s_frag = reinterpret_cast<unsigned *>(smem_f);   // the same words later: [MT][RB][PARTS][lane][4]
+    float *s_part = smem_f + Smem::kWords;                     // [TM][RT], read by the whole cluster
+    float *s_v = s_part + Smem::kTile;                         // [TM][RT]: alpha V (backward)
     __shared__ int s_token[TM];
     pdl_enter();
     const int cs = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
@@ -226,37 +256,53 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
     if (tile_id >= p.plan[kList]) return;                      // the whole cluster
     const AdapterTile tile = reinterpret_cast<const AdapterTile *>(p.plan + p.tiles_at)[tile_id];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int R = p.R;
+    const int R = p.R, K = (int)p.K, N = (int)p.N;
     if (threadIdx.x < TM) s_token[threadIdx.x] = p.plan[p.perm_at + tile.start + ((int)threadIdx.x < tile.count ? (int)threadIdx.x : 0)];
     __syncthreads();
 
-    const int slices = tile.adapter >= 0 ? R / 8 : 0;
-    const TW *w2 = static_cast<const TW *>(p.w2) + (int64_t)max(tile.adapter, 0) * R * p.N;
-    const int groups = (int)((p.N + 63) / 64);
+    const int rblocks = tile.adapter >= 0 ? (R + 15) / 16 : 0;
+    const TW *w2 = static_cast<const TW *>(p.w2) + (int64_t)max(tile.adapter, 0) * R * N;
+    const int groups = (N + 63) / 64;
     const int gcol = (g & 1) * 16 + (g >> 1) * 4;              // the lane's columns as fragment column g: + jh * 32 + jl
-    Quad<TW> bq[kHoldB ? NT : 1][2][2];                        // [8 ranks][row q, q + 4][jh]
-    auto load_b = [&](Quad<TW> (&o)[2][2], int s, int64_t n0) {
+    unsigned bq[kHoldB ? RB : 1][8][BREGS];                    // [16 ranks][n-tile jh * 4 + jl][fragment registers]
+    auto load_b = [&](unsigned (&o)[8][BREGS], int rb, int n0) {
+        // bf16: ranks 2q, 2q + 1, 2q + 8, 2q + 9 in pairs; f16: ranks q, q + 4, q + 8, q + 12 as floats
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int jh = 0; jh < 2; ++jh) {
+            Quad<TW> r[4];
 #pragma unroll
-            for (int jh = 0; jh < 2; ++jh) {
-                const TW *row = w2 + (int64_t)(s * 8 + 4 * h + q) * p.N;
-                o[h][jh] = p.vec_w2 && n0 + 64 <= p.N ? load_quad<TW>(row + n0 + jh * 32 + gcol) : load_quad_any<TW>(row, n0 + jh * 32 + gcol, p.N);
+            for (int i = 0; i < 4; ++i) {
+                const int rank_row = rb * 16 + (kBf16 ? 2 * q + (i & 1) + 8 * (i >> 1) : q + 4 * i);
+                r[i] = rank_row < R ? load_quad<TW, FAST>(w2 + (int64_t)rank_row * N, n0 + jh * 32 + gcol, N) : zero_quad<TW>();
             }
+#pragma unroll
+            for (int jl = 0; jl < 4; ++jl) {
+                if constexpr (kBf16) {
+                    o[jh * 4 + jl][0] = __byte_perm(r[0].w[jl / 2], r[1].w[jl / 2], jl % 2 ? 0x7632 : 0x5410);
+                    o[jh * 4 + jl][1] = __byte_perm(r[2].w[jl / 2], r[3].w[jl / 2], jl % 2 ? 0x7632 : 0x5410);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 f = unpack2<TW>(r[i].w[jl / 2]);
+                        o[jh * 4 + jl][i] = __float_as_uint(jl % 2 ? f.y : f.x);
+                    }
+                }
+            }
+        }
     };
     auto load_group = [&](int gi) {
         if constexpr (kHoldB) {
 #pragma unroll
-            for (int s = 0; s < NT; ++s)
-                if (s < slices) load_b(bq[s], s, (int64_t)gi * 64);
+            for (int rb = 0; rb < RB; ++rb)
+                if (rb < rblocks) load_b(bq[rb], rb, gi * 64);
         }
     };
     const int g_first = rank * kTokWarps + warp, g_step = cs * kTokWarps;
 
     if (tile.adapter >= 0) {
         // ---- V = x A^T over this CTA's columns, this warp's blocks of 64
-        const TW *w1 = static_cast<const TW *>(p.w1) + (int64_t)tile.adapter * R * p.K;
-        const int blocks = (int)((p.K + 63) / 64), per = (blocks + cs - 1) / cs;
+        const TW *w1 = static_cast<const TW *>(p.w1) + (int64_t)tile.adapter * R * K;
+        const int blocks = (K + 63) / 64, per = (blocks + cs - 1) / cs;
         const int last = min(blocks, (rank + 1) * per);
         float acc[MT][NT][4];
 #pragma unroll
@@ -266,36 +312,23 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
         for (int b = rank * per + warp; b < last; b += kTokWarps) {
-            const bool fast = p.vec_x && p.vec_w1 && (int64_t)b * 64 + 64 <= p.K;
 #pragma unroll
             for (int j0 = 0; j0 < NT; j0 += WB) {
                 unsigned w[WB][8];
-                if (fast) {
 #pragma unroll
-                    for (int j = 0; j < WB; ++j)               // (a missing rank reads row 0: its column of V is not used)
-                        load16<TW>(w[j], w1 + (int64_t)((j0 + j) * 8 + g < R ? (j0 + j) * 8 + g : 0) * p.K + b * 64 + q * 16);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < WB; ++j)
-                        load16_any<TW>(w[j], w1 + (int64_t)((j0 + j) * 8 + g < R ? (j0 + j) * 8 + g : 0) * p.K, b, q, p.K);
+                for (int j = 0; j < WB; ++j) {                 // (a missing rank reads row 0: its column of V is not used)
+                    const int r = (j0 + j) * 8 + g;
+                    load16<TW, FAST>(w[j], w1 + (int64_t)(r < R ? r : 0) * K, b, q, K);
                 }
 #pragma unroll
                 for (int m0 = 0; m0 < MT; m0 += XB) {
                     if (m0 * 16 >= tile.count) break;
                     unsigned x[XB][2][XW];
-                    if (fast) {
 #pragma unroll
-                        for (int m = 0; m < XB; ++m)
+                    for (int m = 0; m < XB; ++m)
 #pragma unroll
-                            for (int h = 0; h < 2; ++h)
-                                load16<TX>(x[m][h], static_cast<const TX *>(p.x) + (int64_t)s_token[(m0 + m) * 16 + 8 * h + g] * p.ldx + b * 64 + q * 16);
-                    } else {
-#pragma unroll
-                        for (int m = 0; m < XB; ++m)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h)
-                                load16_any<TX>(x[m][h], static_cast<const TX *>(p.x) + (int64_t)s_token[(m0 + m) * 16 + 8 * h + g] * p.ldx, b, q, p.K);
-                    }
+                        for (int h = 0; h < 2; ++h)
+                            load16<TX, FAST>(x[m][h], static_cast<const TX *>(p.x) + (int64_t)s_token[(m0 + m) * 16 + 8 * h + g] * p.ldx, b, q, K);
 #pragma unroll
                     for (int m = 0; m < XB; ++m) {
                         const unsigned (&x0)[XW] = x[m][0], (&x1)[XW] = x[m][1];
@@ -324,14 +357,15 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
         }
         // ---- the second product's first operands are on their way while V is summed up
         if (g_first < groups) load_group(g_first);
-        if (p.base != nullptr && p.vec_y) {
-            constexpr int kLine = 128 / (int)sizeof(TY);       // a warp takes the lines of its first group
-            for (int row = lane; row < tile.count; row += 32) {
-                const TY *at = static_cast<const TY *>(p.base) + (int64_t)s_token[row] * p.ldbase + (int64_t)g_first * 64;
+        if (FAST && p.base != nullptr) {
+            constexpr int kLine = 128 / (int)sizeof(TY);
+            for (int gi = g_first; gi < groups; gi += g_step)
+                for (int row = lane; row < tile.count; row += 32) {
+                    const TY *at = static_cast<const TY *>(p.base) + (int64_t)s_token[row] * p.ldbase + gi * 64;
 #pragma unroll
-                for (int i = 0; i < 64; i += kLine)
-                    if ((int64_t)g_first * 64 + i < p.N) prefetch_l2(at + i);
-            }
+                    for (int i = 0; i < 64; i += kLine)
+                        if (gi * 64 + i < N) prefetch_l2(at + i);
+                }
         }
         // ---- sum over the warps, then over the cluster
         float *mine = s_warp + warp * Smem::kTile;
@@ -376,19 +410,35 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
             const int row = 4 * i / RT, r = 4 * i % RT;
             if (!BWD && p.v_out != nullptr && rank == 0 && row < tile.count && r < R)
                 *reinterpret_cast<float4 *>(p.v_out + (int64_t)s_token[row] * R + r) = s;
-            float v[4] = {alpha * s.x, alpha * s.y, alpha * s.z, alpha * s.w}, hi[4], lo[4];
+            if (r >= R) s = make_float4(0.f, 0.f, 0.f, 0.f);
+            const float v[4] = {alpha * s.x, alpha * s.y, alpha * s.z, alpha * s.w};
+            if (BWD) *reinterpret_cast<float4 *>(s_v + row * RT + r) = make_float4(v[0], v[1], v[2], v[3]);
+            unsigned *frag = s_frag + ((row / 16) * RB + r / 16) * (PARTS * 128);
+            if constexpr (kBf16) {
+                // register (row & 8) / 8 + 2 * (r & 8) / 8 of lane 4 * (row % 8) + (r % 8) / 2
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                hi[j] = __uint_as_float(__float_as_uint(v[j]) & 0xffffe000u);
-                lo[j] = rest_of(v[j], hi[j]);
+                for (int j = 0; j < 4; j += 2) {
+                    unsigned part3[3];
+                    split3(v[j], v[j + 1], part3[0], part3[1], part3[2]);
+                    unsigned *at = frag + ((row & 7) * 4 + ((r + j) & 7) / 2) * 4 + ((row >> 3) & 1) + 2 * ((r >> 3) & 1);
+#pragma unroll
+                    for (int c = 0; c < 3; ++c) at[c * 128] = part3[c];
+                }
+            } else {
+                // part 2 * (slice of 8 ranks) + (0: leading, 1: rest); register (row & 8) / 8 + 2 * (r & 4) / 4 of lane 4 * (row % 8) + r % 4
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float hi = __uint_as_float(__float_as_uint(v[j]) & 0xffffe000u);
+                    unsigned *at = frag + ((r >> 3) & 1) * 256 + ((row & 7) * 4 + j) * 4 + ((row >> 3) & 1) + 2 * ((r >> 2) & 1);
+                    at[0] = __float_as_uint(hi);
+                    at[128] = __float_as_uint(rest_of(v[j], hi));
+                }
             }
-            *reinterpret_cast<float4 *>(s_hi + row * Smem::kPad + r) = make_float4(hi[0], hi[1], hi[2], hi[3]);
-            *reinterpret_cast<float4 *>(s_lo + row * Smem::kPad + r) = make_float4(lo[0], lo[1], lo[2], lo[3]);
         }
         cluster_arrive();                                      // (waited for before the CTA leaves)
         __syncthreads();
         if constexpr (BWD) {
-            // fragments of U (times the row's scale) and of alpha V, dealt out over the cluster
+            // fragments of U (times the row's scale) and of alpha V for the other gradients, dealt out over the cluster
             const int steps = (tile.count + 15) / 16, mtr = (R + 15) / 16, half_items = steps * mtr;
             for (int i = rank + cs * warp; i < 2 * half_items; i += cs * kTokWarps) {
                 const bool is_u = i < half_items;
@@ -403,8 +453,7 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
                     for (int h = 0; h < 2; ++h) {
                         const int r = m * 16 + g + 8 * h;
                         float v = 0.0f;
-                        if (row < tile.count && r < R)
-                            v = factor * (is_u ? s_hi[row * Smem::kPad + r] + s_lo[row * Smem::kPad + r] : __ldg(p.v_in + t * R + r));
+                        if (row < tile.count && r < R) v = factor * (is_u ? s_v[row * RT + r] : __ldg(p.v_in + t * R + r));
                         f[h][e] = v;
                     }
                 }
@@ -416,70 +465,55 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
     }
 
     // ---- y = base + V B over this CTA's groups of 64 columns
+    constexpr bool kBaseInAcc = sizeof(TY) == 2;
     for (int gi = g_first; gi < groups; gi += g_step) {
-        const int64_t n0 = (int64_t)gi * 64;
-        const bool fast = p.vec_y && n0 + 64 <= p.N;
+        const int n0 = gi * 64;
         if (gi != g_first) load_group(gi);
 #pragma unroll 1
         for (int m = 0; m < MT; ++m) {
             if (m * 16 >= tile.count) break;
             const int64_t tok[2] = {s_token[m * 16 + g], s_token[m * 16 + g + 8]};
             Quad<TY> base[2][4];                               // [row][jh * 2 + b]
-            if (p.base != nullptr) {
-                const TY *r0 = static_cast<const TY *>(p.base) + tok[0] * p.ldbase, *r1 = static_cast<const TY *>(p.base) + tok[1] * p.ldbase;
-                if (fast) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) base[0][i] = load_quad<TY>(r0 + n0 + i * 16 + q * 4);
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) base[1][i] = load_quad<TY>(r1 + n0 + i * 16 + q * 4);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) base[0][i] = load_quad_any<TY>(r0, n0 + i * 16 + q * 4, p.N);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) base[1][i] = load_quad_any<TY>(r1, n0 + i * 16 + q * 4, p.N);
-                }
-            } else {
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int j = 0; j < (int)sizeof(TY); ++j) base[h][i].w[j] = 0u;
-            }
+                for (int i = 0; i < 4; ++i)
+                    base[h][i] = p.base != nullptr ? load_quad<TY, FAST>(static_cast<const TY *>(p.base) + tok[h] * p.ldbase, n0 + i * 16 + q * 4, N)
+                                                   : zero_quad<TY>();
             float acc[8][4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[j][i] = 0.0f;
-            const int at = (m * 16 + g) * Smem::kPad + q;
-            auto slice = [&](const Quad<TW> (&b)[2][2], int s) {
-                const int o = at + s * 8;
-                unsigned hi[4], lo[4];
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    hi[i] = __float_as_uint(s_hi[o + (i & 1) * 8 * Smem::kPad + (i >> 1) * 4]);
-                    lo[i] = __float_as_uint(s_lo[o + (i & 1) * 8 * Smem::kPad + (i >> 1) * 4]);
+                    const float4 o = kBaseInAcc ? quad_floats<TY>(base[h][i]) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    const int jh = i >> 1, b = i & 1;
+                    acc[jh * 4][2 * h + b] = o.x;
+                    acc[jh * 4 + 1][2 * h + b] = o.y;
+                    acc[jh * 4 + 2][2 * h + b] = o.z;
+                    acc[jh * 4 + 3][2 * h + b] = o.w;
                 }
+            auto ranks16 = [&](const unsigned (&b)[8][BREGS], int rb) {
+                const uint4 *frag = reinterpret_cast<const uint4 *>(s_frag + (m * RB + rb) * (PARTS * 128)) + lane;
+                uint4 a[PARTS];
 #pragma unroll
-                for (int jh = 0; jh < 2; ++jh) {
-                    const float4 f0 = quad_floats<TW>(b[0][jh]), f1 = quad_floats<TW>(b[1][jh]);
-                    const float e0[4] = {f0.x, f0.y, f0.z, f0.w}, e1[4] = {f1.x, f1.y, f1.z, f1.w};
+                for (int c = 0; c < PARTS; ++c) a[c] = frag[c * 32];
 #pragma unroll
-                    for (int jl = 0; jl < 4; ++jl) {
-                        mma8_tf32(acc[jh * 4 + jl], lo[0], lo[1], lo[2], lo[3], __float_as_uint(e0[jl]), __float_as_uint(e1[jl]));
-                        mma8_tf32(acc[jh * 4 + jl], hi[0], hi[1], hi[2], hi[3], __float_as_uint(e0[jl]), __float_as_uint(e1[jl]));
+                for (int c = PARTS - 1; c >= 0; --c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        if constexpr (kBf16) mma16<__nv_bfloat16>(acc[j], a[c].x, a[c].y, a[c].z, a[c].w, b[j][0], b[j][1]);
+                        else mma8_tf32(acc[j], a[c].x, a[c].y, a[c].z, a[c].w, b[j][2 * (c / 2)], b[j][2 * (c / 2) + 1]);
                     }
-                }
             };
             if constexpr (kHoldB) {
 #pragma unroll
-                for (int s = 0; s < NT; ++s)
-                    if (s < slices) slice(bq[s], s);
+                for (int rb = 0; rb < RB; ++rb)
+                    if (rb < rblocks) ranks16(bq[rb], rb);
             } else {
-#pragma unroll 2
-                for (int s = 0; s < slices; ++s) {
-                    load_b(bq[0], s, n0);
-                    slice(bq[0], s);
+#pragma unroll 1
+                for (int rb = 0; rb < rblocks; ++rb) {
+                    load_b(bq[0], rb, n0);
+                    ranks16(bq[0], rb);
                 }
             }
 #pragma unroll
@@ -489,12 +523,15 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int jh = i >> 1, b = i & 1;
-                    float4 o = quad_floats<TY>(base[h][i]);
-                    o.x += acc[jh * 4][2 * h + b];
-                    o.y += acc[jh * 4 + 1][2 * h + b];
-                    o.z += acc[jh * 4 + 2][2 * h + b];
-                    o.w += acc[jh * 4 + 3][2 * h + b];
-                    store4<TY>(row, n0 + i * 16 + q * 4, p.N, p.vec_y, o);
+                    float4 o = make_float4(acc[jh * 4][2 * h + b], acc[jh * 4 + 1][2 * h + b], acc[jh * 4 + 2][2 * h + b], acc[jh * 4 + 3][2 * h + b]);
+                    if constexpr (!kBaseInAcc) {
+                        const float4 f = quad_floats<TY>(base[h][i]);
+                        o.x += f.x;
+                        o.y += f.y;
+                        o.z += f.z;
+                        o.w += f.w;
+                    }
+                    store_quad<TY, FAST>(row, n0 + i * 16 + q * 4, N, o);
                 }
             }
         }
@@ -761,20 +798,27 @@ __global__ void __launch_bounds__(256) adapter_grad_sum_kernel(const __grid_cons
 
 // ------------------------------------------------------------------ host side
 
-static bool rows_vec(const void *p, int64_t ld, int elem, int bytes) { return aligned(p, bytes) && (ld * elem) % bytes == 0; }
-
-template <typename TX, typename TW, typename TY, int RT, int MT, bool BWD>
-static dybit_status launch_tokens(AdapterTokens p, int cs, cudaStream_t s) {
-    auto kern = adapter_tokens_kernel<TX, TW, TY, RT, MT, BWD>;
-    constexpr int smem = TokSmem<RT, MT>::kBytes;
-    static std::atomic<bool> ready[64];
+// Lets a kernel use `bytes` of dynamic shared memory; once per kernel and device.
+static dybit_status allow_smem(const void *kernel, int bytes, std::atomic<bool> *ready) {
     int dev = 0;
     DYBIT_CUDA_TRY(cudaGetDevice(&dev));
     if (dev < 0 || dev >= 64) return DYBIT_ERR_CUDA;
     if (!ready[dev].load(std::memory_order_acquire)) {
-        DYBIT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        DYBIT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
         ready[dev].store(true, std::memory_order_release);
     }
+    return DYBIT_OK;
+}
+
+static bool rows_vec(const void *p, int64_t ld, int elem, int bytes) { return aligned(p, bytes) && (ld * elem) % bytes == 0; }
+
+template <typename TX, typename TW, typename TY, int RT, int MT, bool BWD, bool FAST>
+static dybit_status launch_tokens_inst(AdapterTokens p, int cs, cudaStream_t s) {
+    auto kern = adapter_tokens_kernel<TX, TW, TY, RT, MT, BWD, FAST>;
+    constexpr int smem = TokSmem<RT, MT>::kBytes;
+    static std::atomic<bool> ready[64];
+    const dybit_status st = allow_smem(reinterpret_cast<const void *>(kern), smem, ready);
+    if (st != DYBIT_OK) return st;
     const PlanLayout L(p.T, p.n);
     constexpr int kList = MT == 1 ? 0 : (MT == 2 ? 1 : 2);
     p.perm_at = L.perm, p.tiles_at = L.tiles[kList];
@@ -798,6 +842,11 @@ static dybit_status launch_tokens(AdapterTokens p, int cs, cudaStream_t s) {
     return launch_status();
 }
 
+template <typename TX, typename TW, typename TY, int RT, int MT, bool BWD>
+static dybit_status launch_tokens(const AdapterTokens &p, int cs, cudaStream_t s) {
+    return p.fast ? launch_tokens_inst<TX, TW, TY, RT, MT, BWD, true>(p, cs, s) : launch_tokens_inst<TX, TW, TY, RT, MT, BWD, false>(p, cs, s);
+}
+
 template <typename TX, typename TW, typename TY, bool BWD>
 static dybit_status launch_tokens_rank(const AdapterTokens &p, cudaStream_t s) {
     const PlanLayout L(p.T, p.n);
@@ -816,18 +865,6 @@ static dybit_status launch_tokens_rank(const AdapterTokens &p, cudaStream_t s) {
     if (p.R <= 32) return two ? launch_tokens<TX, TW, TY, 32, 2, BWD>(p, c2, s) : launch_tokens<TX, TW, TY, 32, 1, BWD>(p, c1, s);
     if (p.R <= 64) return two ? launch_tokens<TX, TW, TY, 64, 2, BWD>(p, c2, s) : launch_tokens<TX, TW, TY, 64, 1, BWD>(p, c1, s);
     return launch_tokens<TX, TW, TY, 128, 1, BWD>(p, c1, s);
-}
-
-// Lets a kernel use `bytes` of dynamic shared memory; once per kernel and device.
-static dybit_status allow_smem(const void *kernel, int bytes, std::atomic<bool> *ready) {
-    int dev = 0;
-    DYBIT_CUDA_TRY(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= 64) return DYBIT_ERR_CUDA;
-    if (!ready[dev].load(std::memory_order_acquire)) {
-        DYBIT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-        ready[dev].store(true, std::memory_order_release);
-    }
-    return DYBIT_OK;
 }
 
 template <GradSrc S0, GradSrc S1, int MR>
@@ -916,8 +953,8 @@ dybit_status dybit_adapters(int64_t T, int64_t K, int64_t N, int R, const void *
     p.x = X, p.ldx = ldx, p.w1 = A, p.w2 = B, p.alpha = alpha, p.plan = static_cast<const int *>(plan);
     p.base = base, p.ldbase = ldbase, p.y = Y, p.ldy = ldy, p.v_out = V;
     p.T = T, p.K = K, p.N = N, p.n = n_adapters, p.R = R;
-    p.vec_x = rows_vec(X, ldx, ex, 16), p.vec_w1 = rows_vec(A, K, 2, 16), p.vec_w2 = rows_vec(B, N, 2, 8);
-    p.vec_y = rows_vec(Y, ldy, ey, 4 * ey) && (base == nullptr || rows_vec(base, ldbase, ey, 4 * ey));
+    p.fast = rows_vec(X, ldx, ex, 16) && rows_vec(A, K, 2, 16) && rows_vec(B, N, 2, 8) && rows_vec(Y, ldy, ey, 4 * ey) &&
+             (base == nullptr || rows_vec(base, ldbase, ey, 4 * ey));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (tx == DYBIT_F32) return launch_tokens_rank<float, __nv_bfloat16, float, false>(p, s);
     if (tx == DYBIT_BF16)
@@ -959,8 +996,8 @@ dybit_status dybit_adapters_backward(int64_t T, int64_t K, int64_t N, int R, con
     p.x = dY, p.ldx = lddy, p.w1 = B, p.w2 = A, p.alpha = alpha, p.plan = static_cast<const int *>(plan);
     p.base = dXbase, p.ldbase = lddxbase, p.y = dX, p.ldy = lddx;
     p.T = T, p.K = N, p.N = K, p.n = n_adapters, p.R = R;
-    p.vec_x = rows_vec(dY, lddy, e, 16), p.vec_w1 = rows_vec(B, N, 2, 16), p.vec_w2 = rows_vec(A, K, 2, 8);
-    p.vec_y = rows_vec(dX, lddx, e, 4 * e) && (dXbase == nullptr || rows_vec(dXbase, lddxbase, e, 4 * e));
+    p.fast = rows_vec(dY, lddy, e, 16) && rows_vec(B, N, 2, 16) && rows_vec(A, K, 2, 8) && rows_vec(dX, lddx, e, 4 * e) &&
+             (dXbase == nullptr || rows_vec(dXbase, lddxbase, e, 4 * e));
     p.v_in = V, p.scales = scales, p.scale_stride = scale_stride;
     p.frag_u = reinterpret_cast<uint4 *>(base + w.frag_u), p.frag_v = reinterpret_cast<uint4 *>(base + w.frag_v);
     if (T > 0) {
