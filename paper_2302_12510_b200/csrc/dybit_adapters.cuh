@@ -25,18 +25,18 @@ using namespace sm100;
 template <typename TW>
 __device__ __forceinline__ void mma16(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
     if constexpr (sizeof(TW) == 2 && __is_same(TW, __half)) {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     } else {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     }
 }
 
 __device__ __forceinline__ void mma8_tf32(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
-    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -73,6 +73,7 @@ struct AdapterTokens {
     int n, R;
     int64_t perm_at, tiles_at;   // word offsets in the plan
     int fast;                    // all rows start where vectors can be moved: 16 bytes in x and w1, four elements in w2, base and y
+    int wide;                    // 16-bit y: rows of base and y start on 16-byte boundaries and hold whole vectors
     // backward: fragments for adapter_grad_kernel
     const float *v_in;
     const float *scales;
@@ -80,22 +81,28 @@ struct AdapterTokens {
     uint4 *frag_u, *frag_v;
 };
 
-// Sixteen consecutive elements of a row at column k (the lane's share of a 64-column block), as raw words, zeros from
-// column K on.  FAST: rows start on 16-byte boundaries and hold whole vectors.  Otherwise element loads without branches,
-// so that all of them are in flight together, and slot e of lane q takes column 4e + q of the block, so that four lanes
-// read neighbours; both operands of a product come in this order or both in the other.
-template <typename T, bool FAST>
+// A lane's sixteen elements of a 64-column block of a row, as raw words, zeros from column K on.  The order of columns
+// inside a sum is free as long as both operands take the same: lane q takes runs of G elements, four lanes side by side
+// (column (4i + q) * G + j of the block), with G the elements of x in 16 bytes.  FAST: rows start on 16-byte boundaries and
+// hold whole runs.  Otherwise (G = 1) element loads without branches, so that all of them are in flight together.
+template <typename T, int G, bool FAST>
 __device__ __forceinline__ void load16(unsigned (&w)[4 * sizeof(T)], const T *row, int block, int q, int K) {
     if constexpr (FAST) {
-        constexpr int E = 16 / (int)sizeof(T);
-        const int k = block * 64 + q * 16;
+        constexpr int kWords = G * (int)sizeof(T) / 4;         // of a run: 4, or 2 for a 16-bit factor beside an fp32 x
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T); ++i) {
-            const uint4 v = k + i * E < K ? __ldg(reinterpret_cast<const uint4 *>(row + k) + i) : make_uint4(0u, 0u, 0u, 0u);
-            w[4 * i] = v.x;
-            w[4 * i + 1] = v.y;
-            w[4 * i + 2] = v.z;
-            w[4 * i + 3] = v.w;
+        for (int i = 0; i < 16 / G; ++i) {
+            const int c = block * 64 + (4 * i + q) * G;
+            if constexpr (kWords == 4) {
+                const uint4 v = c < K ? __ldg(reinterpret_cast<const uint4 *>(row + c)) : make_uint4(0u, 0u, 0u, 0u);
+                w[4 * i] = v.x;
+                w[4 * i + 1] = v.y;
+                w[4 * i + 2] = v.z;
+                w[4 * i + 3] = v.w;
+            } else {
+                const uint2 v = c < K ? __ldg(reinterpret_cast<const uint2 *>(row + c)) : make_uint2(0u, 0u);
+                w[2 * i] = v.x;
+                w[2 * i + 1] = v.y;
+            }
         }
     } else {
         T e[16];
@@ -198,7 +205,7 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 __device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // Fragments of a 16 (ranks) x 16 (tokens) block for adapter_grad_kernel: lane (g, q) of the reader takes ranks g, g + 8
-// and tokens 4q .. 4q + 3; three uint4 (leading, middle and last bf16 parts) of 32 lanes follow one another.
+// and tokens q, 4 + q, 8 + q, 12 + q; three uint4 (leading, middle and last bf16 parts) of 32 lanes follow one another.
 __device__ __forceinline__ void store_fragment(uint4 *frag, int lane, const float (&f0)[4], const float (&f1)[4]) {
     uint4 part[3];
     split3(f0[0], f0[1], part[0].x, part[1].x, part[2].x);
@@ -226,12 +233,13 @@ struct TokSmem {
 // rank rounded up (16, 32, 64, 128); ranks and columns that are missing are zeros, tokens that are missing repeat the
 // tile's first one and are not stored.
 //
-// First product: a warp takes 64 columns at a time.  Lane (g = lane / 4, q = lane % 4) loads columns 16q .. 16q+15 of
-// token rows g, g + 8 and of factor rows g (+ 8 per n-tile) with 16-byte loads and uses them as the four K = 16 slices
-// of the fragment layout: the order of columns inside a sum is free as long as both operands take the same.
+// First product: a warp takes 64 columns at a time.  Lane (g = lane / 4, q = lane % 4) loads sixteen columns of token rows
+// g, g + 8 and of factor rows g (+ 8 per n-tile) straight from memory and uses them as the four K = 16 slices of the
+// fragment layout.
 // Second product: V, scaled by alpha, is cut into three bf16 numbers that hold all of it (f16 factors: into two tf32
-// numbers, off by less than 2^-21) and kept in shared memory as fragments.  The 64 columns of a warp are dealt to
-// fragment columns so that a lane ends up with four consecutive ones and four lanes with sixteen.  The base is added in
+// numbers, off by less than 2^-21; a bf16 y takes the first two, off by less than 2^-15 of V where y itself is rounded
+// to 2^-9) and kept in shared memory as fragments.  The 64 columns of a warp are dealt to
+// fragment columns so that a lane ends up with 16 bytes of consecutive ones and four lanes with 64.  The base is added in
 // the accumulators where y has 16 bits (the tensor core cuts off what RN would round), by an fp32 addition otherwise.
 template <typename TX, typename TW, typename TY, int RT, int MT, bool BWD, bool FAST>
 __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_kernel(const AdapterTokens p) {
@@ -240,7 +248,7 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
     constexpr int WB = NT < 8 ? NT : 8;                                        // n-tiles of the factor in registers
     constexpr bool kBf16 = __is_same(TW, __nv_bfloat16);
     constexpr bool kHoldB = RT <= 32;                                          // the second factor stays in registers across slices
-    constexpr int PARTS = kBf16 ? 3 : 4;                                       // fragments per 16 ranks
+    constexpr int PARTS = kBf16 ? (sizeof(TY) == 2 ? 2 : 3) : 4;               // fragments per 16 ranks
     constexpr int BREGS = kBf16 ? 2 : 4;                                       // registers of the second factor per n-tile and 16 ranks
     using Smem = TokSmem<RT, MT>;
     extern __shared__ __align__(16) float smem_f[];
@@ -263,7 +271,11 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
     const int rblocks = tile.adapter >= 0 ? (R + 15) / 16 : 0;
     const TW *w2 = static_cast<const TW *>(p.w2) + (int64_t)max(tile.adapter, 0) * R * N;
     const int groups = (N + 63) / 64;
-    const int gcol = (g & 1) * 16 + (g >> 1) * 4;              // the lane's columns as fragment column g: + jh * 32 + jl
+    // n-tile j = jh * 4 + jl, fragment column 2q' + b stands for column jh * 32 + b * 16 + q' * 4 + jl (y of 32 bits) or
+    // b * 32 + q' * 8 + jh * 4 + jl (16 bits)
+    constexpr bool kWide = sizeof(TY) == 2;
+    constexpr int kJh = kWide ? 4 : 32, kCb = kWide ? 32 : 16, kCq = kWide ? 8 : 4;
+    const int gcol = (g & 1) * kCb + (g >> 1) * kCq;           // the lane's columns as fragment column g: + jh * kJh + jl
     unsigned bq[kHoldB ? RB : 1][8][BREGS];                    // [16 ranks][n-tile jh * 4 + jl][fragment registers]
     auto load_b = [&](unsigned (&o)[8][BREGS], int rb, int n0) {
         // bf16: ranks 2q, 2q + 1, 2q + 8, 2q + 9 in pairs; f16: ranks q, q + 4, q + 8, q + 12 as floats
@@ -273,7 +285,7 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int rank_row = rb * 16 + (kBf16 ? 2 * q + (i & 1) + 8 * (i >> 1) : q + 4 * i);
-                r[i] = rank_row < R ? load_quad<TW, FAST>(w2 + (int64_t)rank_row * N, n0 + jh * 32 + gcol, N) : zero_quad<TW>();
+                r[i] = rank_row < R ? load_quad<TW, FAST>(w2 + (int64_t)rank_row * N, n0 + jh * kJh + gcol, N) : zero_quad<TW>();
             }
 #pragma unroll
             for (int jl = 0; jl < 4; ++jl) {
@@ -318,7 +330,7 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
 #pragma unroll
                 for (int j = 0; j < WB; ++j) {                 // (a missing rank reads row 0: its column of V is not used)
                     const int r = (j0 + j) * 8 + g;
-                    load16<TW, FAST>(w[j], w1 + (int64_t)(r < R ? r : 0) * K, b, q, K);
+                    load16<TW, 16 / (int)sizeof(TX), FAST>(w[j], w1 + (int64_t)(r < R ? r : 0) * K, b, q, K);
                 }
 #pragma unroll
                 for (int m0 = 0; m0 < MT; m0 += XB) {
@@ -328,7 +340,7 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
                     for (int m = 0; m < XB; ++m)
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
-                            load16<TX, FAST>(x[m][h], static_cast<const TX *>(p.x) + (int64_t)s_token[(m0 + m) * 16 + 8 * h + g] * p.ldx, b, q, K);
+                            load16<TX, 16 / (int)sizeof(TX), FAST>(x[m][h], static_cast<const TX *>(p.x) + (int64_t)s_token[(m0 + m) * 16 + 8 * h + g] * p.ldx, b, q, K);
 #pragma unroll
                     for (int m = 0; m < XB; ++m) {
                         const unsigned (&x0)[XW] = x[m][0], (&x1)[XW] = x[m][1];
@@ -422,7 +434,7 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
                     split3(v[j], v[j + 1], part3[0], part3[1], part3[2]);
                     unsigned *at = frag + ((row & 7) * 4 + ((r + j) & 7) / 2) * 4 + ((row >> 3) & 1) + 2 * ((r >> 3) & 1);
 #pragma unroll
-                    for (int c = 0; c < 3; ++c) at[c * 128] = part3[c];
+                    for (int c = 0; c < PARTS; ++c) at[c * 128] = part3[c];
                 }
             } else {
                 // part 2 * (slice of 8 ranks) + (0: leading, 1: rest); register (row & 8) / 8 + 2 * (r & 4) / 4 of lane 4 * (row % 8) + r % 4
@@ -446,7 +458,7 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
                 float f[2][4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int row = st * 16 + 4 * q + e;
+                    const int row = st * 16 + 4 * e + q;
                     const int64_t t = s_token[row];
                     const float factor = is_u ? __ldg(p.scales + t * p.scale_stride) : alpha;
 #pragma unroll
@@ -466,6 +478,7 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
 
     // ---- y = base + V B over this CTA's groups of 64 columns
     constexpr bool kBaseInAcc = sizeof(TY) == 2;
+    const bool wide_rows = p.wide != 0;
     for (int gi = g_first; gi < groups; gi += g_step) {
         const int n0 = gi * 64;
         if (gi != g_first) load_group(gi);
@@ -475,11 +488,28 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
             const int64_t tok[2] = {s_token[m * 16 + g], s_token[m * 16 + g + 8]};
             Quad<TY> base[2][4];                               // [row][jh * 2 + b]
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h) {
+                const TY *row = static_cast<const TY *>(p.base) + tok[h] * p.ldbase;
+                if (p.base == nullptr) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    base[h][i] = p.base != nullptr ? load_quad<TY, FAST>(static_cast<const TY *>(p.base) + tok[h] * p.ldbase, n0 + i * 16 + q * 4, N)
-                                                   : zero_quad<TY>();
+                    for (int i = 0; i < 4; ++i) base[h][i] = zero_quad<TY>();
+                } else if constexpr (kWide && FAST) {          // two quads side by side in one load
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int c = n0 + b * kCb + q * kCq;
+                        if (wide_rows) {
+                            const uint4 v = c < N ? *reinterpret_cast<const uint4 *>(row + c) : make_uint4(0u, 0u, 0u, 0u);
+                            base[h][b].w[0] = v.x, base[h][b].w[1] = v.y, base[h][2 + b].w[0] = v.z, base[h][2 + b].w[1] = v.w;
+                        } else {
+                            base[h][b] = load_quad<TY, FAST>(row, c, N);
+                            base[h][2 + b] = load_quad<TY, FAST>(row, c + kJh, N);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) base[h][i] = load_quad<TY, FAST>(row, n0 + (i >> 1) * kJh + (i & 1) * kCb + q * kCq, N);
+                }
+            }
             float acc[8][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -520,6 +550,18 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
             for (int h = 0; h < 2; ++h) {
                 if (m * 16 + g + 8 * h >= tile.count) continue;
                 TY *row = static_cast<TY *>(p.y) + tok[h] * p.ldy;
+                if constexpr (kWide && FAST) {
+                    if (wide_rows) {
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            const int c = n0 + b * kCb + q * kCq, i = 2 * h + b;
+                            if (c < N)
+                                *reinterpret_cast<uint4 *>(row + c) = make_uint4(pack2<TY>(acc[0][i], acc[1][i]), pack2<TY>(acc[2][i], acc[3][i]),
+                                                                                 pack2<TY>(acc[4][i], acc[5][i]), pack2<TY>(acc[6][i], acc[7][i]));
+                        }
+                        continue;
+                    }
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int jh = i >> 1, b = i & 1;
@@ -531,7 +573,7 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
                         o.z += f.z;
                         o.w += f.w;
                     }
-                    store_quad<TY, FAST>(row, n0 + i * 16 + q * 4, N, o);
+                    store_quad<TY, FAST>(row, n0 + jh * kJh + b * kCb + q * kCq, N, o);
                 }
             }
         }
@@ -564,44 +606,53 @@ struct AdapterGrad {
     int chunk_slots;             // blocks along y that take chunks; n more look after adapters without tokens
 };
 
-// Eight columns of one token row.
+// Eight columns of one token row as raw words: columns 8g .. 8g+7 of the warp's 64, for fp32 4g .. 4g+3 and 32 more.
 template <GradSrc S> struct SrcWords { static constexpr int n = S == GradSrc::F32 ? 8 : (S == GradSrc::Bf16 ? 4 : 2); };
 template <GradSrc S>
-__device__ __forceinline__ void load_src8(unsigned (&w)[SrcWords<S>::n], const void *src, int64_t ld, int token, bool there, int64_t c,
-                                          int64_t cols, bool fast) {
-    constexpr int W = SrcWords<S>::n;
+struct SrcRing {
+    static constexpr int kElem = S == GradSrc::F32 ? 4 : (S == GradSrc::Bf16 ? 2 : 1);
+    static constexpr int kPitch = 64 * kElem + 32;             // bytes of a row: the reads below meet no bank twice
+    static constexpr int kStage = 16 * kPitch;
+    static constexpr int kStages = S == GradSrc::F32 ? 3 : 4;
+    static constexpr int kBytes = kTokWarps * kStages * kStage;
+};
+template <GradSrc S>
+__device__ __forceinline__ void read_src8(unsigned (&w)[SrcWords<S>::n], const uint8_t *row, int g) {
+    if constexpr (S == GradSrc::F32) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) w[i] = 0u;
+        for (int i = 0; i < 2; ++i) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(row + g * 16 + i * 128);
+            w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+        }
+    } else if constexpr (S == GradSrc::Bf16) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(row + g * 16);
+        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    } else {
+        const uint2 v = *reinterpret_cast<const uint2 *>(row + g * 8);
+        w[0] = v.x, w[1] = v.y;
+    }
+}
+// The same from memory where the row may be missing, end before the 64 columns or start anywhere: zeros for what is not there.
+template <GradSrc S>
+__device__ __forceinline__ void load_src8_any(unsigned (&w)[SrcWords<S>::n], const uint8_t *row, bool there, int64_t c0, int g, int64_t cols) {
+    constexpr int W = SrcWords<S>::n;
     if constexpr (W == 2) {                                    // rows of codes are padded to 16: eight are always there
-        if (there && c < cols) {
-            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(src) + (int64_t)token * ld + c));
-            w[0] = v.x;
-            w[1] = v.y;
+        w[0] = w[1] = 0u;
+        if (there && c0 + 8 * g < cols) {
+            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(row + c0 + 8 * g));
+            w[0] = v.x, w[1] = v.y;
         }
     } else {
         using T = typename Elem<S == GradSrc::F32 ? DYBIT_F32 : DYBIT_BF16>::type;
-        const T *row = static_cast<const T *>(src) + (int64_t)token * ld;
-        if (fast) {
-            if (there) {
+        T e[8];
 #pragma unroll
-                for (int i = 0; i < W / 4; ++i) {
-                    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(row + c) + i);
-                    w[4 * i] = v.x;
-                    w[4 * i + 1] = v.y;
-                    w[4 * i + 2] = v.z;
-                    w[4 * i + 3] = v.w;
-                }
-            }
-        } else {
-            T e[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const T v = row[c + j < cols ? c + j : cols - 1];
-                e[j] = there && c + j < cols ? v : from_f32<T>(0.0f);
-            }
-#pragma unroll
-            for (int i = 0; i < W; ++i) w[i] = reinterpret_cast<const unsigned *>(e)[i];
+        for (int j = 0; j < 8; ++j) {
+            const int64_t c = c0 + (S == GradSrc::F32 ? j / 4 * 32 + 4 * g + j % 4 : 8 * g + j);
+            const T v = reinterpret_cast<const T *>(row)[c < cols ? c : cols - 1];
+            e[j] = there && c < cols ? v : from_f32<T>(0.0f);
         }
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i] = reinterpret_cast<const unsigned *>(e)[i];
     }
 }
 
@@ -614,14 +665,15 @@ __device__ __forceinline__ void src_pair(unsigned (&o)[SrcParts<S>::n], const un
     } else if constexpr (S == GradSrc::Bf16) {
         o[0] = __byte_perm(a[j / 2], b[j / 2], j % 2 ? 0x7632 : 0x5410);
     } else {
-        const unsigned w = __byte_perm(a[j / 4], b[j / 4], 0x0400u + (unsigned)(j % 4) * 0x0101u);   // code j of a, code j of b in bytes 0 and 2
+        const unsigned w = __byte_perm(a[j / 4], b[j / 4], 0x4400u + (unsigned)(j % 4) * 0x1111u);   // code j of a twice, code j of b twice
         o[0] = decode2<S == GradSrc::CodesSigned>(w);
     }
 }
 
-// sum over a chunk's tokens of left[r] * src[column]: 16 * MR ranks x 64 columns per warp.  Lane (g, q) reads columns
-// 8g .. 8g+7 of token rows 4q .. 4q+3 of a 16-token step straight from memory; two rows interleave into the fragment's
-// K pairs (for codes that is the byte permutation that starts their decoding).
+// sum over a chunk's tokens of left[r] * src[column]: 16 * MR ranks x 64 columns per warp.  The rows of a 16-token step
+// travel by cp.async through a ring of the warp's own in shared memory, several steps ahead.  Lane (g, q) reads eight
+// columns of rows q, 4 + q, 8 + q, 12 + q; two rows interleave into the fragment's K pairs (for codes that is the byte
+// permutation that starts their decoding).
 template <GradSrc S, int MR>
 __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const AdapterGradSide &sd, int block, const AdapterChunk &ch, int r0, float *smem) {
     constexpr int W = SrcWords<S>::n, P = SrcParts<S>::n;
@@ -639,58 +691,108 @@ __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const Ad
         for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
-    // two steps ahead: the token numbers; one step ahead: the rows
-    int tok[4];
-    unsigned src[4][W];
-    auto load_tokens = [&](int st) {
+    using Ring = SrcRing<S>;
+    constexpr int kRuns = 16 * 4 * Ring::kElem / 32;           // 16-byte runs of a step per lane
+    const int row_bytes = (int)(sd.ld * Ring::kElem);
+    const uint8_t *rows = static_cast<const uint8_t *>(sd.src);
+    uint8_t *ring = reinterpret_cast<uint8_t *>(smem) + warp * (Ring::kStages * Ring::kStage);
+    constexpr bool kFragAhead = MR <= 2;                       // (four blocks of ranks leave no registers for it)
+    uint4 a[kFragAhead ? 2 : 1][MR][3];
+    auto load_left = [&](int st, uint4 (&f)[MR][3]) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int row = st * 16 + 4 * q + e;
-            tok[e] = row < count ? __ldg(perm + row) : -1;
+        for (int m = 0; m < MR; ++m)
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                f[m][i] = MR == 1 || r0 + m < mtr ? __ldg(frag + (st * mtr + m) * 96 + i * 32) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    // the products that go into one accumulator follow each other at a distance: a matrix instruction takes dozens of clocks
+    constexpr int JG = P == 1 ? 8 : 4;
+    auto multiply = [&](const unsigned (&x)[4][W], const uint4 (&f)[MR][3]) {
+#pragma unroll
+        for (int j0 = 0; j0 < 8; j0 += JG) {
+            unsigned b0[JG][P], b1[JG][P];
+#pragma unroll
+            for (int j = 0; j < JG; ++j) {
+                src_pair<S>(b0[j], x[0], x[1], j0 + j);
+                src_pair<S>(b1[j], x[2], x[3], j0 + j);
+            }
+#pragma unroll
+            for (int i = 2; i >= 0; --i)
+#pragma unroll
+                for (int k = P - 1; k >= 0; --k)
+#pragma unroll
+                    for (int m = 0; m < MR; ++m)
+#pragma unroll
+                        for (int j = 0; j < JG; ++j)
+                            if (i + k <= 2) mma16<__nv_bfloat16>(acc[m][j0 + j], f[m][i].x, f[m][i].y, f[m][i].z, f[m][i].w, b0[j][k], b1[j][k]);
         }
     };
-    auto load_rows = [&]() {
+    const int mine = wt < steps && c0 < sd.cols ? (steps - wt + ntg - 1) / ntg : 0;      // this warp's steps: wt, wt + ntg, ...
+    if (fast) {
+        // lane l holds the token of row l % 16 of the step that is fetched next; missing rows are zero-filled
+        auto token = [&](int i) {
+            const int row = (wt + i * ntg) * 16 + (lane & 15);
+            return i < mine && row < count ? __ldg(perm + row) : -1;
+        };
+        auto fetch = [&](int i, int tok) {
+            uint8_t *stage = ring + i % Ring::kStages * Ring::kStage;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) load_src8<S>(src[e], sd.src, sd.ld, max(tok[e], 0), tok[e] >= 0, c0 + 8 * g, sd.cols, fast);
-    };
-    if (wt < steps && c0 < sd.cols) {
-        load_tokens(wt);
-        load_rows();
-        load_tokens(wt + ntg);
-        for (int st = wt; st < steps; st += ntg) {
-            unsigned cur[4][W];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int i = 0; i < W; ++i) cur[e][i] = src[e][i];
-            uint4 a[MR][3];
-#pragma unroll
-            for (int m = 0; m < MR; ++m)
-#pragma unroll
-                for (int i = 0; i < 3; ++i)
-                    a[m][i] = MR == 1 || r0 + m < mtr ? __ldg(frag + ((int64_t)st * mtr + m) * 96 + i * 32) : make_uint4(0u, 0u, 0u, 0u);
-            if (st + ntg < steps) {
-                load_rows();
-                load_tokens(st + 2 * ntg);
+            for (int k = 0; k < kRuns; ++k) {
+                const int id = k * 32 + lane, row = id / (4 * Ring::kElem), run = id % (4 * Ring::kElem);
+                const int t = __shfl_sync(0xffffffffu, tok, row);
+                if (i < mine)
+                    cp_async_16(smem_u32(stage + row * Ring::kPitch + run * 16), rows + (int64_t)max(t, 0) * row_bytes + c0 * Ring::kElem + run * 16,
+                                t >= 0 ? 16u : 0u);
             }
+            cp_async_commit();
+        };
+        int tok = token(0);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                unsigned b0[P], b1[P];
-                src_pair<S>(b0, cur[0], cur[1], j);
-                src_pair<S>(b1, cur[2], cur[3], j);
-#pragma unroll
-                for (int m = 0; m < MR; ++m)
-#pragma unroll
-                    for (int i = 2; i >= 0; --i)
-#pragma unroll
-                        for (int k = P - 1; k >= 0; --k)
-                            if (i + k <= 2) mma16<__nv_bfloat16>(acc[m][j], a[m][i].x, a[m][i].y, a[m][i].z, a[m][i].w, b0[k], b1[k]);
+        for (int i = 0; i < Ring::kStages - 1; ++i) {
+            const int next = token(i + 1);
+            fetch(i, tok);
+            tok = next;
+        }
+        if (kFragAhead && mine > 0) load_left(wt, a[0]);
+        auto step = [&](int i, uint4 (&f)[MR][3], uint4 (&ahead)[MR][3]) {
+            cp_async_wait_group<Ring::kStages - 2>();
+            __syncwarp();                                      // the other lanes' copies too, and nobody still reads the stage refilled below
+            const int next = token(i + Ring::kStages);
+            fetch(i + Ring::kStages - 1, tok);
+            tok = next;
+            if (kFragAhead) {
+                if (i + 1 < mine) load_left(wt + (i + 1) * ntg, ahead);
+            } else {
+                load_left(wt + i * ntg, f);
             }
+            const uint8_t *stage = ring + i % Ring::kStages * Ring::kStage;
+            unsigned x[4][W];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) read_src8<S>(x[e], stage + (4 * e + q) * Ring::kPitch, g);
+            multiply(x, f);
+        };
+        for (int i = 0; i < mine; i += 2) {
+            step(i, a[0], a[kFragAhead]);
+            if (i + 1 < mine) step(i + 1, a[kFragAhead], a[0]);
+        }
+        cp_async_wait_group<0>();
+    } else {
+        for (int i = 0; i < mine; ++i) {
+            const int st = wt + i * ntg;
+            unsigned x[4][W];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int row = st * 16 + 4 * e + q, t = row < count ? __ldg(perm + row) : -1;
+                load_src8_any<S>(x[e], rows + (int64_t)max(t, 0) * row_bytes, t >= 0, c0, g, sd.cols);
+            }
+            load_left(st, a[0]);
+            multiply(x, a[0]);
         }
     }
     // the token groups' sums meet in shared memory, added in order
     constexpr int kWarpTile = MR * 16 * 64;
     if (ntg > 1) {
+        __syncthreads();                                       // the rings make room
         if (wt > 0) {
             float *mine = smem + (size_t)((wt - 1) * p.wc + wc) * kWarpTile;
 #pragma unroll
@@ -728,10 +830,12 @@ __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const Ad
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int j = 0; j < 8; j += 4)
-                    if (c0 + (2 * q + b) * 8 + j < sd.cols)
-                        store4<float>(out + (int64_t)r * sd.cols, c0 + (2 * q + b) * 8 + j, sd.cols, vec,
+                for (int j = 0; j < 8; j += 4) {
+                    const int64_t c = c0 + (S == GradSrc::F32 ? j * 8 + (2 * q + b) * 4 : (2 * q + b) * 8 + j);
+                    if (c < sd.cols)
+                        store4<float>(out + (int64_t)r * sd.cols, c, sd.cols, vec,
                                   make_float4(acc[m][j][2 * h + b], acc[m][j + 1][2 * h + b], acc[m][j + 2][2 * h + b], acc[m][j + 3][2 * h + b]));
+                }
         }
 }
 
@@ -867,11 +971,13 @@ static dybit_status launch_tokens_rank(const AdapterTokens &p, cudaStream_t s) {
     return launch_tokens<TX, TW, TY, 128, 1, BWD>(p, c1, s);
 }
 
+constexpr int kMaxGradSmem = (kTokWarps - 1) * 4 * 16 * 64 * 4;      // four blocks of ranks, one group of columns
+
 template <GradSrc S0, GradSrc S1, int MR>
 static dybit_status launch_grad_ranks(const AdapterGrad &p, dim3 grid, int smem, cudaStream_t s) {
     static std::atomic<bool> ready[64];
     auto kern = adapter_grad_kernel<S0, S1, MR>;
-    const dybit_status st = allow_smem(reinterpret_cast<const void *>(kern), (kTokWarps - 1) * MR * 16 * 64 * 4, ready);
+    const dybit_status st = allow_smem(reinterpret_cast<const void *>(kern), kMaxGradSmem, ready);
     if (st != DYBIT_OK) return st;
     launch_k(kern, grid, dim3(kTokThreads), (size_t)smem, s, p);
     return launch_status();
@@ -883,18 +989,19 @@ static dybit_status launch_grad(const AdapterGrad &p_in, cudaStream_t s) {
     const PlanLayout L(p.T, p.n);
     p.perm_at = L.perm, p.chunks_at = L.chunks, p.offsets_at = L.offsets;
     const int mtr = (p.R + 15) / 16, mr = mtr >= 3 ? 4 : mtr, z = (mtr + mr - 1) / mr;
-    // wide blocks read longer runs of a row and the left operand less often, long chunks leave fewer parts to add up; both
-    // only as far as the device stays full
+    // wide blocks read longer runs of a row and the left operand less often, as far as the device stays full; long chunks
+    // leave fewer parts to add up, as far as the last of many waves does not count
     const int64_t fill = (int64_t)sm_count() * 3 / 2, chunks = p.T / kChunkTokens + 1;
     p.wc = 4, p.merge = 1;
     auto blocks = [&](int side) { return (p.side[side].cols + 64 * p.wc - 1) / (64 * p.wc); };
     while (p.wc > 1 && (blocks(0) + blocks(1)) * L.chunks_cap * z < fill) p.wc /= 2;
-    while (p.merge < 8 && (blocks(0) + blocks(1)) * z * (chunks / (2 * p.merge)) >= fill) p.merge *= 2;
+    while (p.merge < 8 && (blocks(0) + blocks(1)) * z * (chunks / (2 * p.merge)) >= 8 * fill) p.merge *= 2;
     p.blocks0 = (int)blocks(0);
     p.chunk_slots = (int)L.chunks_cap;
     const int64_t bx = blocks(0) + blocks(1), by = L.chunks_cap + p.n;
     if (bx > 0x7fffffff || by > 65535) return DYBIT_ERR_UNSUPPORTED;
-    const int smem = (kTokWarps - p.wc) * mr * 16 * 64 * 4;
+    constexpr int kRing = SrcRing<S1>::kBytes > SrcRing<S0>::kBytes ? SrcRing<S1>::kBytes : SrcRing<S0>::kBytes;
+    const int sums = (kTokWarps - p.wc) * mr * 16 * 64 * 4, smem = sums > kRing ? sums : kRing;
     const dim3 grid((unsigned)bx, (unsigned)by, (unsigned)z);
     dybit_status st;
     if (mr == 1) st = launch_grad_ranks<S0, S1, 1>(p, grid, smem, s);
@@ -955,6 +1062,7 @@ dybit_status dybit_adapters(int64_t T, int64_t K, int64_t N, int R, const void *
     p.T = T, p.K = K, p.N = N, p.n = n_adapters, p.R = R;
     p.fast = rows_vec(X, ldx, ex, 16) && rows_vec(A, K, 2, 16) && rows_vec(B, N, 2, 8) && rows_vec(Y, ldy, ey, 4 * ey) &&
              (base == nullptr || rows_vec(base, ldbase, ey, 4 * ey));
+    p.wide = N % 8 == 0 && rows_vec(Y, ldy, ey, 16) && (base == nullptr || rows_vec(base, ldbase, ey, 16));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (tx == DYBIT_F32) return launch_tokens_rank<float, __nv_bfloat16, float, false>(p, s);
     if (tx == DYBIT_BF16)
@@ -981,6 +1089,7 @@ dybit_status dybit_adapters_backward(int64_t T, int64_t K, int64_t N, int R, con
     if (st != DYBIT_OK) return st;
     if (!dtype_ok(tdy) || lddy < N || lddx < K || (dXbase != nullptr && lddxbase < K) || scale_stride < 0) return DYBIT_ERR_INVALID_ARG;
     if (tdy == DYBIT_F16 || tw != DYBIT_BF16) return DYBIT_ERR_UNSUPPORTED;
+    if (row_stride_bytes > 0x7fffffff || lddy > 0x7fffffff / dtype_bytes(tdy)) return DYBIT_ERR_UNSUPPORTED;
     if (dA == nullptr || dB == nullptr) return DYBIT_ERR_INVALID_ARG;
     if (T > 0 && (dY == nullptr || dX == nullptr || V == nullptr || scales == nullptr)) return DYBIT_ERR_INVALID_ARG;
     const int e = dtype_bytes(tdy);
@@ -998,6 +1107,7 @@ dybit_status dybit_adapters_backward(int64_t T, int64_t K, int64_t N, int R, con
     p.T = T, p.K = N, p.N = K, p.n = n_adapters, p.R = R;
     p.fast = rows_vec(dY, lddy, e, 16) && rows_vec(B, N, 2, 16) && rows_vec(A, K, 2, 8) && rows_vec(dX, lddx, e, 4 * e) &&
              (dXbase == nullptr || rows_vec(dXbase, lddxbase, e, 4 * e));
+    p.wide = K % 8 == 0 && rows_vec(dX, lddx, e, 16) && (dXbase == nullptr || rows_vec(dXbase, lddxbase, e, 16));
     p.v_in = V, p.scales = scales, p.scale_stride = scale_stride;
     p.frag_u = reinterpret_cast<uint4 *>(base + w.frag_u), p.frag_v = reinterpret_cast<uint4 *>(base + w.frag_v);
     if (T > 0) {
