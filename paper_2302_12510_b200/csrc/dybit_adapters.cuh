@@ -730,45 +730,60 @@ __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const Ad
     const int mine = wt < steps && c0 < sd.cols ? (steps - wt + ntg - 1) / ntg : 0;      // this warp's steps: wt, wt + ntg, ...
     if (fast) {
         // lane l holds the token of row l % 16 of the step that is fetched next; missing rows are zero-filled
-        auto token = [&](int i) {
-            const int row = (wt + i * ntg) * 16 + (lane & 15);
-            return i < mine && row < count ? __ldg(perm + row) : -1;
+        constexpr int kRowRuns = 4 * Ring::kElem;              // 16-byte runs of a row
+        const int lane_row = lane / kRowRuns;
+        const uint8_t *from = rows + c0 * Ring::kElem + lane % kRowRuns * 16;
+        const uint32_t into = smem_u32(ring) + lane_row * Ring::kPitch + lane % kRowRuns * 16;
+        const int *look = perm + wt * 16 + (lane & 15);        // of the step whose tokens are looked up next
+        int look_rows = count - wt * 16, fill_rows = 0, fill = 0;
+        auto token = [&]() {
+            const int t = (lane & 15) < look_rows ? __ldg(look) : 0;
+            look += ntg * 16;
+            fill_rows = look_rows;
+            look_rows -= ntg * 16;
+            return t;
         };
-        auto fetch = [&](int i, int tok) {
-            uint8_t *stage = ring + i % Ring::kStages * Ring::kStage;
+        auto fetch = [&](int tok, int present) {
+            if (present >= 16) {
 #pragma unroll
-            for (int k = 0; k < kRuns; ++k) {
-                const int id = k * 32 + lane, row = id / (4 * Ring::kElem), run = id % (4 * Ring::kElem);
-                const int t = __shfl_sync(0xffffffffu, tok, row);
-                if (i < mine)
-                    cp_async_16(smem_u32(stage + row * Ring::kPitch + run * 16), rows + (int64_t)max(t, 0) * row_bytes + c0 * Ring::kElem + run * 16,
-                                t >= 0 ? 16u : 0u);
+                for (int k = 0; k < kRuns; ++k)
+                    cp_async_16_full(into + fill + k * (32 / kRowRuns) * Ring::kPitch,
+                                     from + (int64_t)__shfl_sync(0xffffffffu, tok, k * (32 / kRowRuns) + lane_row) * row_bytes);
+            } else if (present > 0) {
+#pragma unroll
+                for (int k = 0; k < kRuns; ++k)
+                    cp_async_16(into + fill + k * (32 / kRowRuns) * Ring::kPitch,
+                                from + (int64_t)__shfl_sync(0xffffffffu, tok, k * (32 / kRowRuns) + lane_row) * row_bytes,
+                                k * (32 / kRowRuns) + lane_row < present ? 16u : 0u);
             }
             cp_async_commit();
+            fill = fill == (Ring::kStages - 1) * Ring::kStage ? 0 : fill + Ring::kStage;
         };
-        int tok = token(0);
+        int tok = token(), present = fill_rows;
 #pragma unroll
         for (int i = 0; i < Ring::kStages - 1; ++i) {
-            const int next = token(i + 1);
-            fetch(i, tok);
-            tok = next;
+            const int next = token(), next_rows = fill_rows;
+            fetch(tok, present);
+            tok = next, present = next_rows;
         }
+        int drained = 0;
         if (kFragAhead && mine > 0) load_left(wt, a[0]);
         auto step = [&](int i, uint4 (&f)[MR][3], uint4 (&ahead)[MR][3]) {
             cp_async_wait_group<Ring::kStages - 2>();
             __syncwarp();                                      // the other lanes' copies too, and nobody still reads the stage refilled below
-            const int next = token(i + Ring::kStages);
-            fetch(i + Ring::kStages - 1, tok);
-            tok = next;
+            const int next = token(), next_rows = fill_rows;
+            fetch(tok, present);
+            tok = next, present = next_rows;
             if (kFragAhead) {
                 if (i + 1 < mine) load_left(wt + (i + 1) * ntg, ahead);
             } else {
                 load_left(wt + i * ntg, f);
             }
-            const uint8_t *stage = ring + i % Ring::kStages * Ring::kStage;
+            const uint8_t *stage = ring + drained + q * Ring::kPitch;
+            drained = drained == (Ring::kStages - 1) * Ring::kStage ? 0 : drained + Ring::kStage;
             unsigned x[4][W];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) read_src8<S>(x[e], stage + (4 * e + q) * Ring::kPitch, g);
+            for (int e = 0; e < 4; ++e) read_src8<S>(x[e], stage + 4 * e * Ring::kPitch, g);
             multiply(x, f);
         };
         for (int i = 0; i < mine; i += 2) {

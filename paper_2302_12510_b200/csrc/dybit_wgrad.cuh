@@ -128,6 +128,11 @@ constexpr int kWgStages = 6;
 constexpr int kWgStoreStage = 128 * 128;     // 128 rows x 32 fp32 columns
 constexpr int kWgSmem = kWgStages * kWgStageBytes + 2 * kWgStoreStage + 512 + 1024;
 constexpr int kWgThreads = 320;
+// The tensor core cuts off what an addition to its fp32 accumulator cannot hold, so its error grows with the length of the
+// sum (3.4e-6 of the result over 8192 tokens).  After this many stages (1024 tokens) the epilogue warps take the
+// accumulator and add it to sums of their own in registers, rounded to nearest, while the next one fills
+// (8192 tokens: 4e-7, as a product in plain fp32).
+constexpr int kWgSegment = 16;
 
 struct WgradParams {
     int N, K;                    // extent of dW
@@ -268,25 +273,28 @@ dybit_wgrad_kernel(const __grid_constant__ CUtensorMap tmap_dy, const __grid_con
             constexpr uint32_t idesc_half = umma_idesc(1u, 1u, 256, 128) | kMnMajor;
             uint32_t it = 0, lt = 0;
             bool ok = true;
-            for (int item = pair; item < items && ok; item += num_pairs, ++lt) {
+            for (int item = pair; item < items && ok; item += num_pairs) {
                 const WgradItem w = wgrad_item(item, p);
                 const uint32_t idesc = w.width == kWgTile ? idesc_whole : idesc_half;
-                const uint32_t as = lt & 1u, aph = (lt >> 1) & 1u;
-                if (!wait_bounded(&acc_empty[as], aph ^ 1u, abort_flag, 0x62)) { ok = false; break; }
-                tc_fence_after_sync();
-                const uint32_t d = tmem_base + as * kWgTile;
-                for (int b = w.first; b < w.last; ++b, ++it) {
-                    const int s = it % kWgStages;
-                    if (!wait_bounded(&full[s], (it / kWgStages) & 1u, abort_flag, 0x63)) { ok = false; break; }
+                for (int b0 = w.first; b0 < w.last && ok; b0 += kWgSegment, ++lt) {
+                    const uint32_t as = lt & 1u, aph = (lt >> 1) & 1u;
+                    if (!wait_bounded(&acc_empty[as], aph ^ 1u, abort_flag, 0x62)) { ok = false; break; }
                     tc_fence_after_sync();
-                    const uint64_t adesc = umma_desc_mnmajor(smem_u32(smem + s * kWgStageBytes));
-                    const uint64_t bdesc = umma_desc_mnmajor(smem_u32(smem + s * kWgStageBytes + 2 * kWgBox));
+                    const uint32_t d = tmem_base + as * kWgTile;
+                    const int b1 = min(w.last, b0 + kWgSegment);
+                    for (int b = b0; b < b1; ++b, ++it) {
+                        const int s = it % kWgStages;
+                        if (!wait_bounded(&full[s], (it / kWgStages) & 1u, abort_flag, 0x63)) { ok = false; break; }
+                        tc_fence_after_sync();
+                        const uint64_t adesc = umma_desc_mnmajor(smem_u32(smem + s * kWgStageBytes));
+                        const uint64_t bdesc = umma_desc_mnmajor(smem_u32(smem + s * kWgStageBytes + 2 * kWgBox));
 #pragma unroll
-                    for (int k = 0; k < kWgTokens / 16; ++k)                   // 16 contraction rows are 2048 bytes
-                        umma_pair<Kind::F16>(d, adesc + (uint64_t)(k * 128), bdesc + (uint64_t)(k * 128), idesc, (uint32_t)(b != w.first || k != 0));
-                    umma_commit_pair(&empty[s], (uint16_t)3);
+                        for (int k = 0; k < kWgTokens / 16; ++k)               // 16 contraction rows are 2048 bytes
+                            umma_pair<Kind::F16>(d, adesc + (uint64_t)(k * 128), bdesc + (uint64_t)(k * 128), idesc, (uint32_t)(b != b0 || k != 0));
+                        umma_commit_pair(&empty[s], (uint16_t)3);
+                    }
+                    if (ok) umma_commit_pair(&acc_full[as], (uint16_t)3);
                 }
-                if (ok) umma_commit_pair(&acc_full[as], (uint16_t)3);
             }
         }
     } else {
@@ -295,24 +303,47 @@ dybit_wgrad_kernel(const __grid_constant__ CUtensorMap tmap_dy, const __grid_con
         const bool issuer = (threadIdx.x & 127) == 64;
         const float alpha = p.scale != nullptr ? __ldg(p.scale) : 1.0f;
         uint32_t lt = 0;
-        for (int item = pair; item < items; item += num_pairs, ++lt) {
+        bool ok = true;
+        for (int item = pair; item < items && ok; item += num_pairs) {
             const WgradItem w = wgrad_item(item, p);
-            const uint32_t as = lt & 1u, aph = (lt >> 1) & 1u;
-            const bool ok = named_barrier_and(1 + group, 128, wait_bounded(&acc_full[as], aph, abort_flag, 0x64));
-            if (!ok) break;
-            tc_fence_after_sync();
-            const int row0 = w.n_blk * kWgTile + (int)rank * 128;
-            const uint32_t taddr = tmem_base + as * kWgTile + ((uint32_t)(q * 32) << 16);
-#pragma unroll 1
-            for (int cc = group; cc < w.width / 32; cc += 2) {
-                const int col0 = w.k_blk * kWgTile + w.k_off + cc * 32;
-                if (col0 >= p.K || row0 >= p.N) break;
-                uint32_t r[32];
-                tmem_ld_32x32(taddr + cc * 32, r);
-                tmem_ld_wait();
-                float f[32];
+            const int row0 = w.n_blk * kWgTile + (int)rank * 128, tile_col = w.k_blk * kWgTile + w.k_off;
+            float f[4][32];                                    // chunks group, group + 2, ... of 32 columns
 #pragma unroll
-                for (int j = 0; j < 32; ++j) f[j] = __fmul_rn(__uint_as_float(r[j]), alpha);
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) f[c][j] = 0.0f;
+            for (int b0 = w.first; b0 < w.last; b0 += kWgSegment, ++lt) {
+                const uint32_t as = lt & 1u, aph = (lt >> 1) & 1u;
+                ok = named_barrier_and(1 + group, 128, wait_bounded(&acc_full[as], aph, abort_flag, 0x64));
+                if (!ok) break;
+                tc_fence_after_sync();
+                const uint32_t taddr = tmem_base + as * kWgTile + ((uint32_t)(q * 32) << 16);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int cc = group + 2 * c;
+                    if (cc * 32 >= w.width) continue;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t r[16];
+                        tmem_ld_32x16(taddr + cc * 32 + h * 16, r);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) f[c][h * 16 + j] = __fadd_rn(f[c][h * 16 + j], __uint_as_float(r[j]));
+                    }
+                }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(mapa_u32(smem_u32(&acc_empty[as]), 0u));
+            }
+            if (!ok) break;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int col0 = tile_col + (group + 2 * c) * 32;
+                if ((group + 2 * c) * 32 >= w.width || col0 >= p.K || row0 >= p.N) continue;
+                if (p.scale != nullptr) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) f[c][j] = __fmul_rn(f[c][j], alpha);
+                }
                 if (p.tma_store) {
                     uint8_t *stage = out_stages + group * kWgStoreStage;
                     if (issuer) bulk_wait_group_read<0>();
@@ -321,7 +352,7 @@ dybit_wgrad_kernel(const __grid_constant__ CUtensorMap tmap_dy, const __grid_con
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
                         *reinterpret_cast<float4 *>(srow + ((j ^ (row_in_tile & 7)) << 4)) =
-                            make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+                            make_float4(f[c][4 * j], f[c][4 * j + 1], f[c][4 * j + 2], f[c][4 * j + 3]);
                     fence_proxy_async_smem();
                     named_barrier(1 + group, 128);
                     if (issuer) {
@@ -333,12 +364,9 @@ dybit_wgrad_kernel(const __grid_constant__ CUtensorMap tmap_dy, const __grid_con
                     float *row = p.out + w.split * p.part + (int64_t)(row0 + row_in_tile) * p.ld;
 #pragma unroll
                     for (int j = 0; j < 32; ++j)
-                        if (col0 + j < p.K) row[col0 + j] = f[j];
+                        if (col0 + j < p.K) row[col0 + j] = f[c][j];
                 }
             }
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(mapa_u32(smem_u32(&acc_empty[as]), 0u));
         }
         if (issuer) bulk_wait_group_read<0>();
     }
