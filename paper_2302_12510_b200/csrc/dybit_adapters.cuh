@@ -202,7 +202,6 @@ __device__ __forceinline__ uint32_t cluster_nctarank() {
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-__device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // Fragments of a 16 (ranks) x 16 (tokens) block for adapter_grad_kernel: lane (g, q) of the reader takes ranks g, g + 8
 // and tokens q, 4 + q, 8 + q, 12 + q; three uint4 (leading, middle and last bf16 parts) of 32 lanes follow one another.
@@ -369,16 +368,6 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
         }
         // ---- the second product's first operands are on their way while V is summed up
         if (g_first < groups) load_group(g_first);
-        if (FAST && p.base != nullptr) {
-            constexpr int kLine = 128 / (int)sizeof(TY);
-            for (int gi = g_first; gi < groups; gi += g_step)
-                for (int row = lane; row < tile.count; row += 32) {
-                    const TY *at = static_cast<const TY *>(p.base) + (int64_t)s_token[row] * p.ldbase + gi * 64;
-#pragma unroll
-                    for (int i = 0; i < 64; i += kLine)
-                        if (gi * 64 + i < N) prefetch_l2(at + i);
-                }
-        }
         // ---- sum over the warps, then over the cluster
         float *mine = s_warp + warp * Smem::kTile;
 #pragma unroll
@@ -479,37 +468,40 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
     // ---- y = base + V B over this CTA's groups of 64 columns
     constexpr bool kBaseInAcc = sizeof(TY) == 2;
     const bool wide_rows = p.wide != 0;
+    Quad<TY> base[2][4];                                       // [row][jh * 2 + b]
+    auto load_base = [&](int n0, int m) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const TY *row = static_cast<const TY *>(p.base) + (int64_t)s_token[m * 16 + g + 8 * h] * p.ldbase;
+            if (p.base == nullptr) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) base[h][i] = zero_quad<TY>();
+            } else if constexpr (kWide && FAST) {              // two quads side by side in one load
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int c = n0 + b * kCb + q * kCq;
+                    if (wide_rows) {
+                        const uint4 v = c < N ? *reinterpret_cast<const uint4 *>(row + c) : make_uint4(0u, 0u, 0u, 0u);
+                        base[h][b].w[0] = v.x, base[h][b].w[1] = v.y, base[h][2 + b].w[0] = v.z, base[h][2 + b].w[1] = v.w;
+                    } else {
+                        base[h][b] = load_quad<TY, FAST>(row, c, N);
+                        base[h][2 + b] = load_quad<TY, FAST>(row, c + kJh, N);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) base[h][i] = load_quad<TY, FAST>(row, n0 + (i >> 1) * kJh + (i & 1) * kCb + q * kCq, N);
+            }
+        }
+    };
+    if (kBaseInAcc && g_first < groups) load_base(g_first * 64, 0);
     for (int gi = g_first; gi < groups; gi += g_step) {
         const int n0 = gi * 64;
         if (gi != g_first) load_group(gi);
 #pragma unroll 1
         for (int m = 0; m < MT; ++m) {
             if (m * 16 >= tile.count) break;
-            const int64_t tok[2] = {s_token[m * 16 + g], s_token[m * 16 + g + 8]};
-            Quad<TY> base[2][4];                               // [row][jh * 2 + b]
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const TY *row = static_cast<const TY *>(p.base) + tok[h] * p.ldbase;
-                if (p.base == nullptr) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) base[h][i] = zero_quad<TY>();
-                } else if constexpr (kWide && FAST) {          // two quads side by side in one load
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const int c = n0 + b * kCb + q * kCq;
-                        if (wide_rows) {
-                            const uint4 v = c < N ? *reinterpret_cast<const uint4 *>(row + c) : make_uint4(0u, 0u, 0u, 0u);
-                            base[h][b].w[0] = v.x, base[h][b].w[1] = v.y, base[h][2 + b].w[0] = v.z, base[h][2 + b].w[1] = v.w;
-                        } else {
-                            base[h][b] = load_quad<TY, FAST>(row, c, N);
-                            base[h][2 + b] = load_quad<TY, FAST>(row, c + kJh, N);
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) base[h][i] = load_quad<TY, FAST>(row, n0 + (i >> 1) * kJh + (i & 1) * kCb + q * kCq, N);
-                }
-            }
+            if (!kBaseInAcc) load_base(n0, m);
             float acc[8][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -522,6 +514,10 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
                     acc[jh * 4 + 2][2 * h + b] = o.z;
                     acc[jh * 4 + 3][2 * h + b] = o.w;
                 }
+            if (kBaseInAcc) {                                  // its registers are free again: the next base is on its way
+                if (m + 1 < MT && (m + 1) * 16 < tile.count) load_base(n0, m + 1);
+                else if (gi + g_step < groups) load_base((gi + g_step) * 64, 0);
+            }
             auto ranks16 = [&](const unsigned (&b)[8][BREGS], int rb) {
                 const uint4 *frag = reinterpret_cast<const uint4 *>(s_frag + (m * RB + rb) * (PARTS * 128)) + lane;
                 uint4 a[PARTS];
@@ -549,7 +545,7 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if (m * 16 + g + 8 * h >= tile.count) continue;
-                TY *row = static_cast<TY *>(p.y) + tok[h] * p.ldy;
+                TY *row = static_cast<TY *>(p.y) + (int64_t)s_token[m * 16 + g + 8 * h] * p.ldy;
                 if constexpr (kWide && FAST) {
                     if (wide_rows) {
 #pragma unroll
@@ -1004,13 +1000,13 @@ static dybit_status launch_grad(const AdapterGrad &p_in, cudaStream_t s) {
     const PlanLayout L(p.T, p.n);
     p.perm_at = L.perm, p.chunks_at = L.chunks, p.offsets_at = L.offsets;
     const int mtr = (p.R + 15) / 16, mr = mtr >= 3 ? 4 : mtr, z = (mtr + mr - 1) / mr;
-    // wide blocks read longer runs of a row and the left operand less often, as far as the device stays full; long chunks
-    // leave fewer parts to add up, as far as the last of many waves does not count
+    // wide blocks read longer runs of a row and the left operand less often, long chunks leave fewer parts to add up and
+    // fewer pipelines to fill; both only as far as the device stays full
     const int64_t fill = (int64_t)sm_count() * 3 / 2, chunks = p.T / kChunkTokens + 1;
     p.wc = 4, p.merge = 1;
     auto blocks = [&](int side) { return (p.side[side].cols + 64 * p.wc - 1) / (64 * p.wc); };
     while (p.wc > 1 && (blocks(0) + blocks(1)) * L.chunks_cap * z < fill) p.wc /= 2;
-    while (p.merge < 8 && (blocks(0) + blocks(1)) * z * (chunks / (2 * p.merge)) >= 8 * fill) p.merge *= 2;
+    while (p.merge < 8 && (blocks(0) + blocks(1)) * z * (chunks / (2 * p.merge)) >= fill) p.merge *= 2;
     p.blocks0 = (int)blocks(0);
     p.chunk_slots = (int)L.chunks_cap;
     const int64_t bx = blocks(0) + blocks(1), by = L.chunks_cap + p.n;
