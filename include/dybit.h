@@ -431,7 +431,7 @@ typedef enum {
  *     scales[row] = 2^(e - top)     (exponent clamped to -126..126; 1 for a row without a finite non-zero value)
  *     code        = encode(x / scales[row])    the encoder of dybit_quantize_pack
  * so the row's largest magnitude lands in (2^(top-1), 2^top] of the format's value axis.  Values near 1 are held most
- * finely: top = 2 keeps most of a bell-shaped row in the linear part (relative error of the row near 2^-7), larger
+ * finely: top = 2 keeps most of a bell-shaped row in the linear part (relative error of the row about 1 %), larger
  * values suit rows with strong outliers.  The power of two makes the division and the product scale * value exact.
  * NaN -> code 0; infinities and what exceeds the format's range saturate.
  *   x      [dev]  rows x cols, row stride ld >= cols (elements)

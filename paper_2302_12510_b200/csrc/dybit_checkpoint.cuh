@@ -190,6 +190,18 @@ __global__ void __launch_bounds__(kCkptThreads) checkpoint_load_kernel(const Ckp
     T *out = static_cast<T *>(p.y) + row * p.ld;
     const float scale = __ldg(p.scales + row * p.scale_stride);
     const int64_t c0 = chunk * (NV * 32 * E) + lane * E;
+    if constexpr (!VEC) {
+        // rows of y that start anywhere: neighbouring lanes take neighbouring elements, so their stores fill whole sectors
+        const int64_t first = chunk * (NV * 32 * E) + lane;
+        unsigned code[NV * E];
+#pragma unroll
+        for (int i = 0; i < NV * E; ++i) code[i] = first + i * 32 < p.cols ? __ldg(in + first + i * 32) : 0u;
+#pragma unroll
+        for (int i = 0; i < NV * E; ++i)
+            if (first + i * 32 < p.cols)
+                out[first + i * 32] = from_f32<T>(__fmul_rn(__uint_as_float(decode2<SIGNED>(code[i] * 0x0101u) << 16), scale));
+        return;
+    }
     uint2 w[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
