@@ -598,7 +598,6 @@ struct AdapterGrad {
     int64_t perm_at, chunks_at, offsets_at;      // word offsets in the plan
     int blocks0;                 // blocks along x that belong to side 0
     int wc;                      // groups of 64 columns per block: 1, 2 or 4; the other warps share the tokens
-    int merge;                   // chunks that one block sums up
     int chunk_slots;             // blocks along y that take chunks; n more look after adapters without tokens
 };
 
@@ -676,7 +675,7 @@ __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const Ad
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int wc = warp % p.wc, wt = warp / p.wc, ntg = kTokWarps / p.wc;
     const int64_t c0 = ((int64_t)block * p.wc + wc) * 64;
-    const int mtr = (p.R + 15) / 16, count = min(ch.rest, p.merge * kChunkTokens), steps = (count + 15) / 16;
+    const int mtr = (p.R + 15) / 16, count = min(ch.rest, kChunkTokens), steps = (count + 15) / 16;
     const bool fast = sd.vec && c0 + 64 <= sd.cols;
     const int *perm = p.plan + p.perm_at + ch.start;
     const uint4 *frag = sd.frag + ((int64_t)ch.step * mtr + r0) * 96 + lane;
@@ -828,9 +827,9 @@ __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const Ad
                 }
         }
     }
-    const bool whole = ch.index == 0 && ch.rest <= p.merge * kChunkTokens;
+    const bool whole = ch.index == 0 && ch.rest <= kChunkTokens;
     float *out = whole ? sd.out + (int64_t)ch.adapter * p.R * sd.cols
-                       : sd.partial + (int64_t)(ch.partial + ch.index / p.merge) * p.R * sd.cols;
+                       : sd.partial + (int64_t)(ch.partial + ch.index) * p.R * sd.cols;
     const bool vec = sd.cols % 4 == 0 && aligned16(out);
 #pragma unroll
     for (int m = 0; m < MR; ++m)
@@ -873,7 +872,6 @@ __global__ void __launch_bounds__(kTokThreads, MR == 1 ? 2 : 1) adapter_grad_ker
     }
     if ((int)blockIdx.y >= p.plan[3]) return;
     const AdapterChunk ch = reinterpret_cast<const AdapterChunk *>(p.plan + p.chunks_at)[blockIdx.y];
-    if (ch.index % p.merge != 0) return;
     if (first) adapter_grad_body<S0, MR>(p, p.side[0], block, ch, r0, smem_f);
     else adapter_grad_body<S1, MR>(p, p.side[1], block, ch, r0, smem_f);
 }
@@ -883,7 +881,7 @@ __global__ void __launch_bounds__(256) adapter_grad_sum_kernel(const __grid_cons
     pdl_enter();
     const int a = blockIdx.y;
     const int *off = p.plan + p.offsets_at + (int64_t)a * kPlanColumns;
-    const int parts = (off[kPlanColumns + 4] - off[4] + p.merge - 1) / p.merge, first = off[5];
+    const int parts = off[kPlanColumns + 4] - off[4], first = off[5];
     if (parts <= 1) return;
     for (int s = 0; s < 2; ++s) {
         const AdapterGradSide &sd = p.side[s];
@@ -1000,13 +998,11 @@ static dybit_status launch_grad(const AdapterGrad &p_in, cudaStream_t s) {
     const PlanLayout L(p.T, p.n);
     p.perm_at = L.perm, p.chunks_at = L.chunks, p.offsets_at = L.offsets;
     const int mtr = (p.R + 15) / 16, mr = mtr >= 3 ? 4 : mtr, z = (mtr + mr - 1) / mr;
-    // wide blocks read longer runs of a row and the left operand less often, long chunks leave fewer parts to add up and
-    // fewer pipelines to fill; both only as far as the device stays full
-    const int64_t fill = (int64_t)sm_count() * 3 / 2, chunks = p.T / kChunkTokens + 1;
-    p.wc = 4, p.merge = 1;
+    // wide blocks read longer runs of a row and the left operand less often, as far as the device stays full
+    const int64_t fill = (int64_t)sm_count() * 3 / 2;
+    p.wc = 4;
     auto blocks = [&](int side) { return (p.side[side].cols + 64 * p.wc - 1) / (64 * p.wc); };
     while (p.wc > 1 && (blocks(0) + blocks(1)) * L.chunks_cap * z < fill) p.wc /= 2;
-    while (p.merge < 8 && (blocks(0) + blocks(1)) * z * (chunks / (2 * p.merge)) >= fill) p.merge *= 2;
     p.blocks0 = (int)blocks(0);
     p.chunk_slots = (int)L.chunks_cap;
     const int64_t bx = blocks(0) + blocks(1), by = L.chunks_cap + p.n;
@@ -1018,7 +1014,7 @@ static dybit_status launch_grad(const AdapterGrad &p_in, cudaStream_t s) {
     if (mr == 1) st = launch_grad_ranks<S0, S1, 1>(p, grid, smem, s);
     else if (mr == 2) st = launch_grad_ranks<S0, S1, 2>(p, grid, smem, s);
     else st = launch_grad_ranks<S0, S1, 4>(p, grid, smem, s);
-    if (st != DYBIT_OK || p.T <= (int64_t)p.merge * kChunkTokens) return st;       // no adapter has several parts
+    if (st != DYBIT_OK || p.T <= kChunkTokens) return st;       // no adapter has several parts
     const int64_t most = p.side[0].cols > p.side[1].cols ? p.side[0].cols : p.side[1].cols;
     int64_t bs = (p.R * most / 4 + 255) / 256, cap = 8 * (int64_t)sm_count() / p.n + 1;
     if (bs > cap) bs = cap;

@@ -11,7 +11,8 @@
 namespace dybit {
 
 constexpr int kPlanThreads = 1024;
-constexpr int kChunkTokens = 512;            // the gradient kernel sums up one or more chunks of an adapter's tokens per block
+constexpr int kChunkTokens = 512;            // of one adapter that a block of the gradient kernel sums up (longer sums: the tensor core's
+                                             // cut-off additions show, over 1e-6 of the result for 1024 tokens of which 2 us are gained)
 
 // A tile: up to 16, 32 or 64 tokens of one adapter.  `step` counts 16-token steps of assigned tokens.
 struct AdapterTile { int adapter, start, count, step; };
