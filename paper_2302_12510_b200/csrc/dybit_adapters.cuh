@@ -45,6 +45,13 @@ __device__ __forceinline__ void mma8_tf32(float (&c)[4], unsigned a0, unsigned a
 __device__ __forceinline__ float rest_of(float x, float head) {
     return fabsf(x) == __uint_as_float(0x7f800000u) ? 0.0f : __fsub_rn(x, head);
 }
+// The nearest number of eleven significant bits (tf32); the largest fp32 numbers, whose nearest is an infinity, are cut off.
+__device__ __forceinline__ float round_tf32(float x) {
+    unsigned r;
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
+    const float cut = __uint_as_float(__float_as_uint(x) & 0xffffe000u);
+    return fabsf(x) > 3.4e38f && fabsf(x) < __uint_as_float(0x7f800000u) ? cut : __uint_as_float(r);
+}
 __device__ __forceinline__ float top16(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
 
 // Two fp32 numbers as three pairs of bf16 whose sums they are: eight significand bits each, cut off, so 24 in all and
@@ -235,11 +242,12 @@ struct TokSmem {
 // First product: a warp takes 64 columns at a time.  Lane (g = lane / 4, q = lane % 4) loads sixteen columns of token rows
 // g, g + 8 and of factor rows g (+ 8 per n-tile) straight from memory and uses them as the four K = 16 slices of the
 // fragment layout.
-// Second product: V, scaled by alpha, is cut into three bf16 numbers that hold all of it (f16 factors: into two tf32
-// numbers, off by less than 2^-21; a bf16 y takes the first two, off by less than 2^-15 of V where y itself is rounded
-// to 2^-9) and kept in shared memory as fragments.  The 64 columns of a warp are dealt to
-// fragment columns so that a lane ends up with 16 bytes of consecutive ones and four lanes with 64.  The base is added in
-// the accumulators where y has 16 bits (the tensor core cuts off what RN would round), by an fp32 addition otherwise.
+// Second product: V, scaled by alpha, enters it as an fp32 number whatever the type of y: three bf16 numbers that hold all
+// of it, for f16 factors two tf32 numbers rounded to nearest (off by at most 2^-24 of V, as an fp32 number is itself).
+// They are kept in shared memory as fragments.  The 64 columns of a warp are dealt to fragment columns so that a lane ends
+// up with 16 bytes of consecutive ones and four lanes with 64.  The base is added to the finished sum by an fp32 addition
+// rounded to nearest (in the accumulators the tensor core would cut it off); one of 16 bits is fetched a step ahead, one
+// of 32 bits while the products run.
 template <typename TX, typename TW, typename TY, int RT, int MT, bool BWD, bool FAST>
 __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_kernel(const AdapterTokens p) {
     constexpr int NT = RT / 8, RB = RT / 16, TM = 16 * MT, XW = 4 * (int)sizeof(TX);
@@ -247,7 +255,7 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
     constexpr int WB = NT < 8 ? NT : 8;                                        // n-tiles of the factor in registers
     constexpr bool kBf16 = __is_same(TW, __nv_bfloat16);
     constexpr bool kHoldB = RT <= 32;                                          // the second factor stays in registers across slices
-    constexpr int PARTS = kBf16 ? (sizeof(TY) == 2 ? 2 : 3) : 4;               // fragments per 16 ranks
+    constexpr int PARTS = kBf16 ? 3 : 4;                                       // fragments per 16 ranks
     constexpr int BREGS = kBf16 ? 2 : 4;                                       // registers of the second factor per n-tile and 16 ranks
     using Smem = TokSmem<RT, MT>;
     extern __shared__ __align__(16) float smem_f[];
@@ -429,10 +437,10 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
                 // part 2 * (slice of 8 ranks) + (0: leading, 1: rest); register (row & 8) / 8 + 2 * (r & 4) / 4 of lane 4 * (row % 8) + r % 4
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float hi = __uint_as_float(__float_as_uint(v[j]) & 0xffffe000u);
+                    const float hi = round_tf32(v[j]);
                     unsigned *at = frag + ((r >> 3) & 1) * 256 + ((row & 7) * 4 + j) * 4 + ((row >> 3) & 1) + 2 * ((r >> 2) & 1);
                     at[0] = __float_as_uint(hi);
-                    at[128] = __float_as_uint(rest_of(v[j], hi));
+                    at[128] = __float_as_uint(round_tf32(rest_of(v[j], hi)));
                 }
             }
         }
@@ -466,7 +474,7 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
     }
 
     // ---- y = base + V B over this CTA's groups of 64 columns
-    constexpr bool kBaseInAcc = sizeof(TY) == 2;
+    constexpr bool kBaseAhead = sizeof(TY) == 2;
     const bool wide_rows = p.wide != 0;
     Quad<TY> base[2][4];                                       // [row][jh * 2 + b]
     auto load_base = [&](int n0, int m) {
@@ -494,30 +502,28 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
             }
         }
     };
-    if (kBaseInAcc && g_first < groups) load_base(g_first * 64, 0);
+    if (kBaseAhead && g_first < groups) load_base(g_first * 64, 0);
     for (int gi = g_first; gi < groups; gi += g_step) {
         const int n0 = gi * 64;
         if (gi != g_first) load_group(gi);
 #pragma unroll 1
         for (int m = 0; m < MT; ++m) {
             if (m * 16 >= tile.count) break;
-            if (!kBaseInAcc) load_base(n0, m);
-            float acc[8][4];
+            if (!kBaseAhead) load_base(n0, m);
+            Quad<TY> mine[2][4];                               // 16 bits: this step's base, while the next one is on its way
+            if constexpr (kBaseAhead) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float4 o = kBaseInAcc ? quad_floats<TY>(base[h][i]) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    const int jh = i >> 1, b = i & 1;
-                    acc[jh * 4][2 * h + b] = o.x;
-                    acc[jh * 4 + 1][2 * h + b] = o.y;
-                    acc[jh * 4 + 2][2 * h + b] = o.z;
-                    acc[jh * 4 + 3][2 * h + b] = o.w;
-                }
-            if (kBaseInAcc) {                                  // its registers are free again: the next base is on its way
+                    for (int i = 0; i < 4; ++i) mine[h][i] = base[h][i];
                 if (m + 1 < MT && (m + 1) * 16 < tile.count) load_base(n0, m + 1);
                 else if (gi + g_step < groups) load_base((gi + g_step) * 64, 0);
             }
+            float acc[8][4];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[j][i] = -0.0f;   // (a token without an adapter keeps its base bit for bit)
             auto ranks16 = [&](const unsigned (&b)[8][BREGS], int rb) {
                 const uint4 *frag = reinterpret_cast<const uint4 *>(s_frag + (m * RB + rb) * (PARTS * 128)) + lane;
                 uint4 a[PARTS];
@@ -546,31 +552,28 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
             for (int h = 0; h < 2; ++h) {
                 if (m * 16 + g + 8 * h >= tile.count) continue;
                 TY *row = static_cast<TY *>(p.y) + (int64_t)s_token[m * 16 + g + 8 * h] * p.ldy;
+                float4 o[4];                                   // [jh * 2 + b]
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = (i >> 1) * 4, k = 2 * h + (i & 1);
+                    const float4 f = quad_floats<TY>(kBaseAhead ? mine[h][i] : base[h][i]);
+                    o[i] = make_float4(__fadd_rn(f.x, acc[j][k]), __fadd_rn(f.y, acc[j + 1][k]), __fadd_rn(f.z, acc[j + 2][k]),
+                                       __fadd_rn(f.w, acc[j + 3][k]));
+                }
                 if constexpr (kWide && FAST) {
                     if (wide_rows) {
 #pragma unroll
                         for (int b = 0; b < 2; ++b) {
-                            const int c = n0 + b * kCb + q * kCq, i = 2 * h + b;
+                            const int c = n0 + b * kCb + q * kCq;
                             if (c < N)
-                                *reinterpret_cast<uint4 *>(row + c) = make_uint4(pack2<TY>(acc[0][i], acc[1][i]), pack2<TY>(acc[2][i], acc[3][i]),
-                                                                                 pack2<TY>(acc[4][i], acc[5][i]), pack2<TY>(acc[6][i], acc[7][i]));
+                                *reinterpret_cast<uint4 *>(row + c) = make_uint4(pack2<TY>(o[b].x, o[b].y), pack2<TY>(o[b].z, o[b].w),
+                                                                                 pack2<TY>(o[2 + b].x, o[2 + b].y), pack2<TY>(o[2 + b].z, o[2 + b].w));
                         }
                         continue;
                     }
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int jh = i >> 1, b = i & 1;
-                    float4 o = make_float4(acc[jh * 4][2 * h + b], acc[jh * 4 + 1][2 * h + b], acc[jh * 4 + 2][2 * h + b], acc[jh * 4 + 3][2 * h + b]);
-                    if constexpr (!kBaseInAcc) {
-                        const float4 f = quad_floats<TY>(base[h][i]);
-                        o.x += f.x;
-                        o.y += f.y;
-                        o.z += f.z;
-                        o.w += f.w;
-                    }
-                    store_quad<TY, FAST>(row, n0 + jh * kJh + b * kCb + q * kCq, N, o);
-                }
+                for (int i = 0; i < 4; ++i) store_quad<TY, FAST>(row, n0 + (i >> 1) * kJh + (i & 1) * kCb + q * kCq, N, o[i]);
             }
         }
     }
