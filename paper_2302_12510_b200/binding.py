@@ -187,6 +187,15 @@ def _check(status: int, where: str):
         raise DybitError(status, where)
 
 
+def _ws_span(ws: torch.Tensor, like: torch.Tensor) -> Tuple[int, int]:
+    """(address, bytes) of the part of a workspace from its first 1024-byte boundary on; 0 bytes where it ends before."""
+    if not (ws.is_cuda and ws.device == like.device and ws.is_contiguous()):
+        raise ValueError("ws must be a contiguous CUDA tensor on the device of the operands")
+    at = ws.data_ptr()
+    off = -at % 1024
+    return at + off, max(0, ws.numel() * ws.element_size() - off)
+
+
 def _dev_f32(x: torch.Tensor, name: str) -> torch.Tensor:
     if not (x.is_cuda and x.dtype == torch.float32 and x.is_contiguous()):
         raise ValueError(f"{name} must be a contiguous float32 CUDA tensor")
@@ -311,10 +320,9 @@ def dybit_gemm(M: int, N: int, K: int, A: torch.Tensor, fa, scale_a: torch.Tenso
         C_raw = torch.empty((M, N), dtype=torch.int32, device=A.device)
     if ws is None:
         ws = torch.empty(dybit_gemm_workspace_bytes(M, N, K, fa, fb) + 1024, dtype=torch.uint8, device=A.device)
-    off = (-ws.data_ptr()) % 1024
-    ws_ptr = C.c_void_p(ws.data_ptr() + off)
+    ws_ptr, ws_bytes = _ws_span(ws, A)
     _check(lib.dybit_gemm(M, N, K, _ptr(A), _fmt(fa), _ptr(scale_a), lda, _ptr(B), _fmt(fb), _ptr(scale_b), ldb,
-                          _ptr(C_out), C_out.stride(0), _ptr(C_raw), ws_ptr, ws.numel() - off, _stream(stream)),
+                          _ptr(C_out), C_out.stride(0), _ptr(C_raw), ws_ptr, ws_bytes, _stream(stream)),
            "dybit_gemm")
     return C_out, C_raw
 
@@ -332,11 +340,10 @@ def dybit_conv2d(desc: ConvDesc, X: torch.Tensor, fx, scale_x: torch.Tensor,
         Y_raw = torch.empty((desc.n, oh, ow, desc.k), dtype=torch.int32, device=X.device)
     if ws is None:
         ws = torch.empty(dybit_conv2d_workspace_bytes(desc, fx, fw) + 1024, dtype=torch.uint8, device=X.device)
-    off = (-ws.data_ptr()) % 1024
-    ws_ptr = C.c_void_p(ws.data_ptr() + off)
+    ws_ptr, ws_bytes = _ws_span(ws, X)
     cd = _cdesc(desc)
     _check(lib.dybit_conv2d(C.byref(cd), _ptr(X), _fmt(fx), _ptr(scale_x), _ptr(W), _fmt(fw), _ptr(scale_w), ldw,
-                            _ptr(Y), _ptr(Y_raw), ws_ptr, ws.numel() - off, _stream(stream)), "dybit_conv2d")
+                            _ptr(Y), _ptr(Y_raw), ws_ptr, ws_bytes, _stream(stream)), "dybit_conv2d")
     return Y, Y_raw
 
 
@@ -409,11 +416,6 @@ def dybit_gemm_static_ws(M: int, N: int, K: int, A: torch.Tensor, fa, scale_a: t
     return C_out, C_raw
 
 
-def _ws_ptr(ws: torch.Tensor):
-    off = (-ws.data_ptr()) % 1024
-    return C.c_void_p(ws.data_ptr() + off), ws.numel() - off
-
-
 def _bias_ptr(bias, n):
     if bias is None:
         return None
@@ -433,7 +435,7 @@ def dybit_gemm_requant(M: int, N: int, K: int, A: torch.Tensor, fa, scale_a: tor
         Q = torch.zeros((M, ldq_bytes), dtype=torch.uint8, device=A.device)
     if ws is None:
         ws = torch.empty(dybit_gemm_workspace_bytes(M, N, K, fa, fb) + 1024, dtype=torch.uint8, device=A.device)
-    wp, wn = _ws_ptr(ws)
+    wp, wn = _ws_span(ws, A)
     _check(lib.dybit_gemm_requant(M, N, K, _ptr(A), _fmt(fa), _ptr(scale_a), A.stride(0), _ptr(B), _fmt(fb),
                                   _ptr(scale_b), B.stride(0), _fmt(fq), _ptr(scale_q), _bias_ptr(bias, N), int(bool(relu)),
                                   _ptr(Q), ldq_bytes, wp, wn, _stream(stream)), "dybit_gemm_requant")
@@ -449,7 +451,7 @@ def dybit_conv2d_requant(desc: ConvDesc, X: torch.Tensor, fx, scale_x: torch.Ten
         Q = torch.zeros(dybit_packed_bytes(desc.n * oh * ow * desc.k, fq[0]), dtype=torch.uint8, device=X.device)
     if ws is None:
         ws = torch.empty(dybit_conv2d_workspace_bytes(desc, fx, fw) + 1024, dtype=torch.uint8, device=X.device)
-    wp, wn = _ws_ptr(ws)
+    wp, wn = _ws_span(ws, X)
     cd = _cdesc(desc)
     _check(lib.dybit_conv2d_requant(C.byref(cd), _ptr(X), _fmt(fx), _ptr(scale_x), _ptr(W), _fmt(fw), _ptr(scale_w),
                                     W.stride(0), _fmt(fq), _ptr(scale_q), _bias_ptr(bias, desc.k), int(bool(relu)),
@@ -477,7 +479,7 @@ def dybit_quantize_conv2d_requant(desc: ConvDesc, X: torch.Tensor, fx, W: torch.
         scale_out = torch.empty(2, dtype=torch.float32, device=X.device)
     if ws is None:
         ws = torch.empty(dybit_conv2d_workspace_bytes(desc, fx, fw) + 1024, dtype=torch.uint8, device=X.device)
-    wp, wn = _ws_ptr(ws)
+    wp, wn = _ws_span(ws, X)
     cd = _cdesc(desc)
     _check(lib.dybit_quantize_conv2d_requant(C.byref(cd), _ptr(X), _fmt(fx), _ptr(scale_x), _ptr(scale_out), _ptr(packed),
                                              _ptr(W), _fmt(fw), _ptr(scale_w), W.stride(0), _fmt(fq), _ptr(scale_q),
@@ -508,7 +510,7 @@ def dybit_gemm_batched(M: int, N: int, K: int, A: torch.Tensor, fa, scale_a: tor
     if ws is None:
         ws = torch.empty(dybit_gemm_batched_workspace_bytes(batch, M, N, K, fa, fb) + 1024, dtype=torch.uint8,
                          device=A.device)
-    wp, wn = _ws_ptr(ws)
+    wp, wn = _ws_span(ws, A)
     _check(lib.dybit_gemm_batched(batch, M, N, K, _ptr(A), _fmt(fa), _ptr(scale_a), A.stride(1), A.stride(0),
                                   _ptr(B), _fmt(fb), _ptr(scale_b), B.stride(1), B.stride(0),
                                   _ptr(C), C.stride(1), C.stride(0), _ptr(raw), wp, wn, _stream(stream)),
@@ -535,7 +537,7 @@ def dybit_quantize_conv2d(desc: ConvDesc, X: torch.Tensor, fx, W: torch.Tensor, 
         scale_out = torch.empty(2, dtype=torch.float32, device=X.device)
     if ws is None:
         ws = torch.empty(dybit_conv2d_workspace_bytes(desc, fx, fw) + 1024, dtype=torch.uint8, device=X.device)
-    wp, wn = _ws_ptr(ws)
+    wp, wn = _ws_span(ws, X)
     cd = _cdesc(desc)
     _check(lib.dybit_quantize_conv2d(C.byref(cd), _ptr(X), _fmt(fx), _ptr(scale_x), _ptr(scale_out), _ptr(packed),
                                      _ptr(W), _fmt(fw), _ptr(scale_w), W.stride(0), _ptr(Y), _ptr(raw), wp, wn,
@@ -580,14 +582,14 @@ class ConvLayers:
             ws = a.get("ws")
             if ws is None:
                 ws = torch.empty(dybit_conv2d_workspace_bytes(desc, fx, fw) + 1024, dtype=torch.uint8, device=X.device)
-            wp, wn = _ws_ptr(ws)
+            wp, wn = _ws_span(ws, X)
             c = self.array[i]
             c.desc = _cdesc(desc)
             addr = lambda t: None if t is None else t.data_ptr()
             c.X, c.fx, c.scale_x = addr(X), _fmt(fx), addr(a.get("scale_x"))
             c.scale_x_out, c.X_packed = addr(scale_out), addr(packed)
             c.W, c.fw, c.scale_w, c.ldw_bytes = addr(W), _fmt(fw), addr(a["scale_w"]), W.stride(0)
-            c.Y, c.Y_raw, c.ws, c.ws_bytes = addr(Y), addr(raw), wp.value, wn
+            c.Y, c.Y_raw, c.ws, c.ws_bytes = addr(Y), addr(raw), wp, wn
             if requant:
                 bias = a.get("bias")
                 c.Q, c.fq, c.scale_q, c.relu = addr(Q), _fmt(a["fq"]), addr(a["scale_q"]), int(bool(a.get("relu")))
@@ -777,9 +779,7 @@ def _workspace(need: int, ws: Optional[torch.Tensor], like: torch.Tensor):
     """(address, bytes, tensor to keep) of a 1024-byte aligned workspace on the device of `like`."""
     if ws is None:
         ws = like.new_empty(need + 1024, dtype=torch.uint8)
-    at = ws.data_ptr()
-    off = -at % 1024
-    return at + off, ws.numel() - off, ws
+    return (*_ws_span(ws, like), ws)
 
 
 def dybit_checkpoint_wgrad(dY: torch.Tensor, codes: torch.Tensor, K: int, fmt, scales: torch.Tensor,
