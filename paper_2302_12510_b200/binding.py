@@ -3,6 +3,12 @@
 Function names follow include/dybit.h.  torch supplies device memory and the
 current stream; every computation happens inside the library's kernels.
 There is no fallback: if libdybit.so is absent the import fails.
+
+Every device call takes `stream` (a torch stream or a stream's handle; default:
+the current stream).  What it allocates itself belongs to that stream.  What it
+is given follows torch's own rule: the stream has to wait for whatever filled
+it, and a tensor of another stream's that is dropped before the call has run
+needs record_stream.
 """
 from __future__ import annotations
 
@@ -187,6 +193,31 @@ def _check(status: int, where: str):
         raise DybitError(status, where)
 
 
+def _torch_stream(stream, device) -> torch.cuda.Stream:
+    """The torch stream of a call's `stream` argument: a torch stream, or the handle of one (0: the default stream)."""
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    return torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+
+
+def _new(like: torch.Tensor, shape, dtype: torch.dtype, stream, zero: bool = False, returned: bool = True) -> torch.Tensor:
+    """A tensor that a call allocates on the device of `like`.  It belongs to the stream that the call runs on, so its memory
+    is neither still in use by earlier work of another stream nor handed on before that stream is done with it.  One that
+    is returned stays alive for the work that the caller's current stream does with it, too."""
+    make = like.new_zeros if zero else like.new_empty
+    if stream is None:
+        return make(shape, dtype=dtype)
+    s, current = _torch_stream(stream, like.device), torch.cuda.current_stream(like.device)
+    if s == current:
+        return make(shape, dtype=dtype)
+    with torch.cuda.stream(s):
+        t = make(shape, dtype=dtype)
+    if returned:
+        t.record_stream(current)
+    return t
+
+
 def _ws_span(ws: torch.Tensor, like: torch.Tensor) -> Tuple[int, int]:
     """(address, bytes) of the part of a workspace from its first 1024-byte boundary on; 0 bytes where it ends before."""
     if not (ws.is_cuda and ws.device == like.device and ws.is_contiguous()):
@@ -194,6 +225,13 @@ def _ws_span(ws: torch.Tensor, like: torch.Tensor) -> Tuple[int, int]:
     at = ws.data_ptr()
     off = -at % 1024
     return at + off, max(0, ws.numel() * ws.element_size() - off)
+
+
+def _workspace(need: int, ws: Optional[torch.Tensor], like: torch.Tensor, stream=None):
+    """(address, bytes, tensor to keep) of a 1024-byte aligned workspace on the device of `like`."""
+    if ws is None:
+        ws = _new(like, need + 1024, torch.uint8, stream, returned=False)
+    return (*_ws_span(ws, like), ws)
 
 
 def _dev_f32(x: torch.Tensor, name: str) -> torch.Tensor:
@@ -254,7 +292,7 @@ def dybit_conv2d_out_hw(desc: ConvDesc) -> Tuple[int, int]:
 def dybit_absmax_scale(x: torch.Tensor, fmt, scale_out: Optional[torch.Tensor] = None, stream=None):
     _dev_f32(x, "x")
     if scale_out is None:
-        scale_out = torch.empty(2, dtype=torch.float32, device=x.device)
+        scale_out = _new(x, 2, torch.float32, stream)
     _check(lib.dybit_absmax_scale(_ptr(x), x.numel(), _fmt(fmt), _ptr(scale_out), _stream(stream)),
            "dybit_absmax_scale")
     return scale_out
@@ -267,9 +305,9 @@ def dybit_quantize_pack(x: torch.Tensor, fmt, scale: Optional[torch.Tensor] = No
     _dev_f32(x, "x")
     n = x.numel()
     if packed is None:
-        packed = torch.empty(dybit_packed_bytes(n, fmt[0]), dtype=torch.uint8, device=x.device)
+        packed = _new(x, dybit_packed_bytes(n, fmt[0]), torch.uint8, stream)
     if scale is None and scale_out is None:
-        scale_out = torch.empty(2, dtype=torch.float32, device=x.device)
+        scale_out = _new(x, 2, torch.float32, stream)
     _check(lib.dybit_quantize_pack(_ptr(x), n, _fmt(fmt), _ptr(scale), _ptr(packed), _ptr(scale_out),
                                    _stream(stream)), "dybit_quantize_pack")
     return packed, (scale if scale is not None else scale_out)
@@ -288,9 +326,9 @@ def dybit_quantize_pack_2d(x: torch.Tensor, fmt, scale: Optional[torch.Tensor] =
     if row_stride_bytes is None:
         row_stride_bytes = dybit_row_stride_bytes(cols, fmt[0])
     if packed is None:
-        packed = torch.empty((rows, row_stride_bytes), dtype=torch.uint8, device=x.device)
+        packed = _new(x, (rows, row_stride_bytes), torch.uint8, stream)
     if scale is None and scale_out is None:
-        scale_out = torch.empty(2, dtype=torch.float32, device=x.device)
+        scale_out = _new(x, 2, torch.float32, stream)
     _check(lib.dybit_quantize_pack_2d(_ptr(x), rows, cols, ld, _fmt(fmt), _ptr(scale), _ptr(packed),
                                       row_stride_bytes, _ptr(scale_out), _stream(stream)),
            "dybit_quantize_pack_2d")
@@ -300,7 +338,7 @@ def dybit_quantize_pack_2d(x: torch.Tensor, fmt, scale: Optional[torch.Tensor] =
 def dybit_decode(packed: torch.Tensor, n: int, fmt, scale: Optional[torch.Tensor] = None,
                  out: Optional[torch.Tensor] = None, stream=None):
     if out is None:
-        out = torch.empty(n, dtype=torch.float32, device=packed.device)
+        out = _new(packed, n, torch.float32, stream)
     _check(lib.dybit_decode(_ptr(packed), int(n), _fmt(fmt), _ptr(scale), _ptr(out), _stream(stream)),
            "dybit_decode")
     return out
@@ -315,12 +353,10 @@ def dybit_gemm(M: int, N: int, K: int, A: torch.Tensor, fa, scale_a: torch.Tenso
     lda = A.stride(0) if lda_bytes is None else lda_bytes
     ldb = B.stride(0) if ldb_bytes is None else ldb_bytes
     if C_out is None:
-        C_out = torch.empty((M, N), dtype=torch.float32, device=A.device)
+        C_out = _new(A, (M, N), torch.float32, stream)
     if want_raw and C_raw is None:
-        C_raw = torch.empty((M, N), dtype=torch.int32, device=A.device)
-    if ws is None:
-        ws = torch.empty(dybit_gemm_workspace_bytes(M, N, K, fa, fb) + 1024, dtype=torch.uint8, device=A.device)
-    ws_ptr, ws_bytes = _ws_span(ws, A)
+        C_raw = _new(A, (M, N), torch.int32, stream)
+    ws_ptr, ws_bytes, ws = _workspace(dybit_gemm_workspace_bytes(M, N, K, fa, fb), ws, A, stream)
     _check(lib.dybit_gemm(M, N, K, _ptr(A), _fmt(fa), _ptr(scale_a), lda, _ptr(B), _fmt(fb), _ptr(scale_b), ldb,
                           _ptr(C_out), C_out.stride(0), _ptr(C_raw), ws_ptr, ws_bytes, _stream(stream)),
            "dybit_gemm")
@@ -335,12 +371,10 @@ def dybit_conv2d(desc: ConvDesc, X: torch.Tensor, fx, scale_x: torch.Tensor,
     oh, ow = dybit_conv2d_out_hw(desc)
     ldw = W.stride(0) if ldw_bytes is None else ldw_bytes
     if Y is None:
-        Y = torch.empty((desc.n, oh, ow, desc.k), dtype=torch.float32, device=X.device)
+        Y = _new(X, (desc.n, oh, ow, desc.k), torch.float32, stream)
     if want_raw and Y_raw is None:
-        Y_raw = torch.empty((desc.n, oh, ow, desc.k), dtype=torch.int32, device=X.device)
-    if ws is None:
-        ws = torch.empty(dybit_conv2d_workspace_bytes(desc, fx, fw) + 1024, dtype=torch.uint8, device=X.device)
-    ws_ptr, ws_bytes = _ws_span(ws, X)
+        Y_raw = _new(X, (desc.n, oh, ow, desc.k), torch.int32, stream)
+    ws_ptr, ws_bytes, ws = _workspace(dybit_conv2d_workspace_bytes(desc, fx, fw), ws, X, stream)
     cd = _cdesc(desc)
     _check(lib.dybit_conv2d(C.byref(cd), _ptr(X), _fmt(fx), _ptr(scale_x), _ptr(W), _fmt(fw), _ptr(scale_w), ldw,
                             _ptr(Y), _ptr(Y_raw), ws_ptr, ws_bytes, _stream(stream)), "dybit_conv2d")
@@ -432,10 +466,8 @@ def dybit_gemm_requant(M: int, N: int, K: int, A: torch.Tensor, fa, scale_a: tor
     if ldq_bytes is None:
         ldq_bytes = N * fq[0] // 8
     if Q is None:
-        Q = torch.zeros((M, ldq_bytes), dtype=torch.uint8, device=A.device)
-    if ws is None:
-        ws = torch.empty(dybit_gemm_workspace_bytes(M, N, K, fa, fb) + 1024, dtype=torch.uint8, device=A.device)
-    wp, wn = _ws_span(ws, A)
+        Q = _new(A, (M, ldq_bytes), torch.uint8, stream, zero=True)
+    wp, wn, ws = _workspace(dybit_gemm_workspace_bytes(M, N, K, fa, fb), ws, A, stream)
     _check(lib.dybit_gemm_requant(M, N, K, _ptr(A), _fmt(fa), _ptr(scale_a), A.stride(0), _ptr(B), _fmt(fb),
                                   _ptr(scale_b), B.stride(0), _fmt(fq), _ptr(scale_q), _bias_ptr(bias, N), int(bool(relu)),
                                   _ptr(Q), ldq_bytes, wp, wn, _stream(stream)), "dybit_gemm_requant")
@@ -448,10 +480,8 @@ def dybit_conv2d_requant(desc: ConvDesc, X: torch.Tensor, fx, scale_x: torch.Ten
     """Convolution whose result is the dense NHWK stream of packed codes (the next layer's X).  Returns Q (1-D uint8)."""
     oh, ow = dybit_conv2d_out_hw(desc)
     if Q is None:
-        Q = torch.zeros(dybit_packed_bytes(desc.n * oh * ow * desc.k, fq[0]), dtype=torch.uint8, device=X.device)
-    if ws is None:
-        ws = torch.empty(dybit_conv2d_workspace_bytes(desc, fx, fw) + 1024, dtype=torch.uint8, device=X.device)
-    wp, wn = _ws_span(ws, X)
+        Q = _new(X, dybit_packed_bytes(desc.n * oh * ow * desc.k, fq[0]), torch.uint8, stream, zero=True)
+    wp, wn, ws = _workspace(dybit_conv2d_workspace_bytes(desc, fx, fw), ws, X, stream)
     cd = _cdesc(desc)
     _check(lib.dybit_conv2d_requant(C.byref(cd), _ptr(X), _fmt(fx), _ptr(scale_x), _ptr(W), _fmt(fw), _ptr(scale_w),
                                     W.stride(0), _fmt(fq), _ptr(scale_q), _bias_ptr(bias, desc.k), int(bool(relu)),
@@ -472,14 +502,12 @@ def dybit_quantize_conv2d_requant(desc: ConvDesc, X: torch.Tensor, fx, W: torch.
         raise ValueError("X does not match the descriptor")
     oh, ow = dybit_conv2d_out_hw(desc)
     if Q is None:
-        Q = torch.zeros(dybit_packed_bytes(desc.n * oh * ow * desc.k, fq[0]), dtype=torch.uint8, device=X.device)
+        Q = _new(X, dybit_packed_bytes(desc.n * oh * ow * desc.k, fq[0]), torch.uint8, stream, zero=True)
     if packed is None:
-        packed = torch.empty(dybit_packed_bytes(X.numel(), fx[0]), dtype=torch.uint8, device=X.device)
+        packed = _new(X, dybit_packed_bytes(X.numel(), fx[0]), torch.uint8, stream)
     if scale_out is None:
-        scale_out = torch.empty(2, dtype=torch.float32, device=X.device)
-    if ws is None:
-        ws = torch.empty(dybit_conv2d_workspace_bytes(desc, fx, fw) + 1024, dtype=torch.uint8, device=X.device)
-    wp, wn = _ws_span(ws, X)
+        scale_out = _new(X, 2, torch.float32, stream)
+    wp, wn, ws = _workspace(dybit_conv2d_workspace_bytes(desc, fx, fw), ws, X, stream)
     cd = _cdesc(desc)
     _check(lib.dybit_quantize_conv2d_requant(C.byref(cd), _ptr(X), _fmt(fx), _ptr(scale_x), _ptr(scale_out), _ptr(packed),
                                              _ptr(W), _fmt(fw), _ptr(scale_w), W.stride(0), _fmt(fq), _ptr(scale_q),
@@ -503,14 +531,11 @@ def dybit_gemm_batched(M: int, N: int, K: int, A: torch.Tensor, fa, scale_a: tor
         raise ValueError("rows of A and B must be contiguous")
     batch = A.shape[0]
     if C is None:
-        C = torch.empty((batch, M, N), dtype=torch.float32, device=A.device)
-    raw = torch.empty(C.shape, dtype=torch.int32, device=A.device) if want_raw else None
+        C = _new(A, (batch, M, N), torch.float32, stream)
+    raw = _new(A, C.shape, torch.int32, stream) if want_raw else None
     if raw is not None and not C.is_contiguous():
         raise ValueError("want_raw needs a contiguous C")
-    if ws is None:
-        ws = torch.empty(dybit_gemm_batched_workspace_bytes(batch, M, N, K, fa, fb) + 1024, dtype=torch.uint8,
-                         device=A.device)
-    wp, wn = _ws_span(ws, A)
+    wp, wn, ws = _workspace(dybit_gemm_batched_workspace_bytes(batch, M, N, K, fa, fb), ws, A, stream)
     _check(lib.dybit_gemm_batched(batch, M, N, K, _ptr(A), _fmt(fa), _ptr(scale_a), A.stride(1), A.stride(0),
                                   _ptr(B), _fmt(fb), _ptr(scale_b), B.stride(1), B.stride(0),
                                   _ptr(C), C.stride(1), C.stride(0), _ptr(raw), wp, wn, _stream(stream)),
@@ -529,15 +554,13 @@ def dybit_quantize_conv2d(desc: ConvDesc, X: torch.Tensor, fx, W: torch.Tensor, 
         raise ValueError("X does not match the descriptor")
     oh, ow = dybit_conv2d_out_hw(desc)
     if Y is None:
-        Y = torch.empty((desc.n, oh, ow, desc.k), dtype=torch.float32, device=X.device)
-    raw = torch.empty(Y.shape, dtype=torch.int32, device=X.device) if want_raw else None
+        Y = _new(X, (desc.n, oh, ow, desc.k), torch.float32, stream)
+    raw = _new(X, Y.shape, torch.int32, stream) if want_raw else None
     if packed is None:
-        packed = torch.empty(dybit_packed_bytes(X.numel(), fx[0]), dtype=torch.uint8, device=X.device)
+        packed = _new(X, dybit_packed_bytes(X.numel(), fx[0]), torch.uint8, stream)
     if scale_out is None:
-        scale_out = torch.empty(2, dtype=torch.float32, device=X.device)
-    if ws is None:
-        ws = torch.empty(dybit_conv2d_workspace_bytes(desc, fx, fw) + 1024, dtype=torch.uint8, device=X.device)
-    wp, wn = _ws_span(ws, X)
+        scale_out = _new(X, 2, torch.float32, stream)
+    wp, wn, ws = _workspace(dybit_conv2d_workspace_bytes(desc, fx, fw), ws, X, stream)
     cd = _cdesc(desc)
     _check(lib.dybit_quantize_conv2d(C.byref(cd), _ptr(X), _fmt(fx), _ptr(scale_x), _ptr(scale_out), _ptr(packed),
                                      _ptr(W), _fmt(fw), _ptr(scale_w), W.stride(0), _ptr(Y), _ptr(raw), wp, wn,
@@ -551,7 +574,8 @@ class ConvLayers:
     arguments of dybit_quantize_conv2d (desc, X, fx, W, fw, scale_w and optionally scale_x, scale_out, packed, Y,
     want_raw, ws) or, with fq and scale_q given, of dybit_quantize_conv2d_requant (relu, bias, Q): that layer then
     leaves as packed codes in self.Q[i] instead of fp32 in self.Y[i].  Missing outputs and workspaces are allocated
-    here, one workspace per layer."""
+    here, on the current stream, one workspace per layer; they live as long as this object, which has to outlive the
+    calls that use it."""
 
     def __init__(self, layers):
         self.n = len(layers)
@@ -626,7 +650,7 @@ def dybit_depthwise_conv2d(desc: ConvDesc, X: torch.Tensor, fx, scale_x: torch.T
     (dybit_quantize_pack_2d of the [c][r*s] filter matrix).  Returns Y [n][oh][ow][c] float32."""
     oh, ow = dybit_conv2d_out_hw(desc)
     if Y is None:
-        Y = torch.empty((desc.n, oh, ow, desc.c), dtype=torch.float32, device=X.device)
+        Y = _new(X, (desc.n, oh, ow, desc.c), torch.float32, stream)
     cd = _cdesc(desc)
     _check(lib.dybit_depthwise_conv2d(C.byref(cd), _ptr(X), _fmt(fx), _ptr(scale_x), _ptr(W), _fmt(fw), _ptr(scale_w),
                                       W.stride(0), _ptr(Y), _stream(stream)), "dybit_depthwise_conv2d")
@@ -637,7 +661,7 @@ def dybit_rmse(x: torch.Tensor, fmt, scale: torch.Tensor, out: Optional[torch.Te
     """Eq. 2.  Returns a float64 device tensor {RMSE, sigma, mse, n}."""
     _dev_f32(x, "x")
     if out is None:
-        out = torch.empty(4, dtype=torch.float64, device=x.device)
+        out = _new(x, 4, torch.float64, stream)
     _check(lib.dybit_rmse(_ptr(x), x.numel(), _fmt(fmt), _ptr(scale), _ptr(out), _stream(stream)), "dybit_rmse")
     return out
 
@@ -651,8 +675,8 @@ def dybit_rmse_sweep(x: torch.Tensor, fmts, scales: torch.Tensor, stream=None):
     if not (scales.is_cuda and scales.dtype == torch.float32 and scales.is_contiguous() and scales.numel() == 2 * nc):
         raise ValueError("scales must be a contiguous float32 device tensor with two values per candidate")
     arr = (_CFmt * max(nc, 1))(*[_fmt(f) for f in fmts])
-    out = torch.empty((nc, 4), dtype=torch.float64, device=x.device)
-    best = torch.empty(1, dtype=torch.int32, device=x.device)
+    out = _new(x, (nc, 4), torch.float64, stream)
+    best = _new(x, 1, torch.int32, stream)
     _check(lib.dybit_rmse_sweep(_ptr(x), x.numel(), nc, arr, _ptr(scales), _ptr(out), _ptr(best), _stream(stream)),
            "dybit_rmse_sweep")
     return out, best
@@ -662,7 +686,7 @@ def dybit_fake_quant(x: torch.Tensor, fmt, scale: torch.Tensor, out: Optional[to
     """Quantize-dequantize image of x (QAT forward) in one pass; returns a float32 tensor shaped like x."""
     _dev_f32(x, "x")
     if out is None:
-        out = torch.empty_like(x)
+        out = _new(x, x.shape, x.dtype, stream)
     _dev_f32(out, "out")
     _check(lib.dybit_fake_quant(_ptr(x), x.numel(), _fmt(fmt), _ptr(scale), _ptr(out), _stream(stream)),
            "dybit_fake_quant")
@@ -677,7 +701,7 @@ def dybit_fake_quant_backward(x: torch.Tensor, grad_out: torch.Tensor, fmt, scal
     if grad_out.numel() != x.numel():
         raise ValueError("grad_out must have as many elements as x")
     if out is None:
-        out = torch.empty_like(x)
+        out = _new(x, x.shape, x.dtype, stream)
     _dev_f32(out, "out")
     _check(lib.dybit_fake_quant_backward(_ptr(x), _ptr(grad_out), x.numel(), _fmt(fmt), _ptr(scale), _ptr(out),
                                          _stream(stream)), "dybit_fake_quant_backward")
@@ -742,9 +766,9 @@ def dybit_checkpoint_save(x: torch.Tensor, fmt, top: int = 2, codes: Optional[to
     stride = padded = (cols + 127) // 128 * 128
     given = codes is not None or scales is not None
     if codes is None:
-        codes = x.new_empty((rows, padded), dtype=torch.uint8)
+        codes = _new(x, (rows, padded), torch.uint8, stream)
     if scales is None:
-        scales = x.new_empty(rows, dtype=torch.float32)
+        scales = _new(x, rows, torch.float32, stream)
     if given:
         stride, _ = _codes8(codes, rows, cols, scales, True)
         if codes.shape[1] < padded and codes.shape[1] < stride:
@@ -761,7 +785,7 @@ def dybit_checkpoint_load(codes: torch.Tensor, cols: int, fmt, scales: torch.Ten
     rows = codes.shape[0]
     stride, scale_stride = _codes8(codes, rows, cols, scales, per_row)
     if out is None:
-        out, t, ld = codes.new_empty((rows, cols), dtype=dtype), _DTYPE_CODE.get(dtype), cols
+        out, t, ld = _new(codes, (rows, cols), dtype, stream), _DTYPE_CODE.get(dtype), cols
         if t is None:
             raise ValueError("dtype must be float32, bfloat16 or float16")
     else:
@@ -775,13 +799,6 @@ def dybit_checkpoint_wgrad_workspace_bytes(T: int, N: int, K: int, dtype: torch.
     return int(lib.dybit_checkpoint_wgrad_workspace_bytes(int(T), int(N), int(K), _DTYPE_CODE[dtype]))
 
 
-def _workspace(need: int, ws: Optional[torch.Tensor], like: torch.Tensor):
-    """(address, bytes, tensor to keep) of a 1024-byte aligned workspace on the device of `like`."""
-    if ws is None:
-        ws = like.new_empty(need + 1024, dtype=torch.uint8)
-    return (*_ws_span(ws, like), ws)
-
-
 def dybit_checkpoint_wgrad(dY: torch.Tensor, codes: torch.Tensor, K: int, fmt, scales: torch.Tensor,
                            out: Optional[torch.Tensor] = None, per_row: bool = True,
                            ws: Optional[torch.Tensor] = None, stream=None):
@@ -790,12 +807,12 @@ def dybit_checkpoint_wgrad(dY: torch.Tensor, codes: torch.Tensor, K: int, fmt, s
     T, N = dY.shape
     stride, scale_stride = _codes8(codes, T, K, scales, per_row)
     if out is None:
-        out, ldo = dY.new_empty((N, K), dtype=torch.float32), K
+        out, ldo = _new(dY, (N, K), torch.float32, stream), K
     else:
         to, ldo = _matrix(out, "out", N, K)
         if to != 0:
             raise ValueError("out must be float32")
-    at, size, ws = _workspace(lib.dybit_checkpoint_wgrad_workspace_bytes(T, N, K, t), ws, dY)
+    at, size, ws = _workspace(lib.dybit_checkpoint_wgrad_workspace_bytes(T, N, K, t), ws, dY, stream)
     _check(lib.dybit_checkpoint_wgrad(T, N, K, dY.data_ptr(), t, ld, codes.data_ptr(), stride, _fmt(fmt), scales.data_ptr(),
                                       scale_stride, out.data_ptr(), ldo, at, size, _stream(stream)), "dybit_checkpoint_wgrad")
     return out
@@ -812,14 +829,15 @@ def dybit_adapters_plan(ids: torch.Tensor, n_adapters: int, plan: Optional[torch
         raise ValueError("ids must be a contiguous 1-D int32 CUDA tensor")
     T = ids.numel()
     if plan is None:
-        plan = torch.empty(dybit_adapters_plan_bytes(T, n_adapters), dtype=torch.uint8, device=ids.device)
+        plan = _new(ids, dybit_adapters_plan_bytes(T, n_adapters), torch.uint8, stream)
     _check(lib.dybit_adapters_plan(T, ids.data_ptr(), int(n_adapters), plan.data_ptr(), plan.numel(), _stream(stream)),
            "dybit_adapters_plan")
     return plan
 
 
 class AdapterPlan:
-    """The plan of one batch of tokens, for every call with the same tokens (dybit_adapters_plan)."""
+    """The plan of one batch of tokens, for every call with the same tokens (dybit_adapters_plan).  It has to outlive the
+    calls that use it (or take buffer.record_stream), as any tensor that is used on another stream than its own."""
 
     def __init__(self, ids: torch.Tensor, n_adapters: int, stream=None):
         self.T, self.n = ids.numel(), int(n_adapters)
@@ -855,14 +873,14 @@ def dybit_adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, alpha: Opt
     tx, ldx = _matrix(x, "x", T, K)
     tb, ldb = (None, 0) if base is None else _matrix(base, "base", T, N)
     if out is None:
-        out = x.new_empty((T, N), dtype=base.dtype if base is not None else (out_dtype or x.dtype))
+        out = _new(x, (T, N), base.dtype if base is not None else (out_dtype or x.dtype), stream)
         ty, ldy = _DTYPE_CODE.get(out.dtype), N
     else:
         ty, ldy = _matrix(out, "out", T, N)
     if base is not None and tb != ty:
         raise ValueError("base and out must have one dtype")
     if want_v and v is None:
-        v = x.new_empty((T, R), dtype=torch.float32)
+        v = _new(x, (T, R), torch.float32, stream)
     _check(lib.dybit_adapters(T, K, N, R, x.data_ptr(), tx, ldx, plan.n, A.data_ptr(), B.data_ptr(), tw,
                               None if alpha is None else alpha.data_ptr(), plan.address, None if base is None else base.data_ptr(),
                               ldb, ty, out.data_ptr(), ldy, None if v is None else _dense(v, "v", (T, R)), _stream(stream)),
@@ -887,16 +905,16 @@ def dybit_adapters_backward(dY: torch.Tensor, codes: torch.Tensor, fmt, scales: 
     stride, scale_stride = _codes8(codes, T, K, scales, per_row)
     tb, ldb = (t, 0) if dx_base is None else _matrix(dx_base, "dx_base", T, K)
     if dx is None:
-        dx, tx, ldx = dY.new_empty((T, K)), t, K
+        dx, tx, ldx = _new(dY, (T, K), dY.dtype, stream), t, K
     else:
         tx, ldx = _matrix(dx, "dx", T, K)
     if tx != t or tb != t:
         raise ValueError("dx and dx_base must have dY's dtype")
     if dA is None:
-        dA = dY.new_empty((n, R, K), dtype=torch.float32)
+        dA = _new(dY, (n, R, K), torch.float32, stream)
     if dB is None:
-        dB = dY.new_empty((n, R, N), dtype=torch.float32)
-    at, size, ws = _workspace(lib.dybit_adapters_backward_workspace_bytes(T, K, N, R, n), ws, dY)
+        dB = _new(dY, (n, R, N), torch.float32, stream)
+    at, size, ws = _workspace(lib.dybit_adapters_backward_workspace_bytes(T, K, N, R, n), ws, dY, stream)
     _check(lib.dybit_adapters_backward(T, K, N, R, dY.data_ptr(), t, ldy, codes.data_ptr(), stride, _fmt(fmt),
                                        scales.data_ptr(), scale_stride, n, A.data_ptr(), B.data_ptr(), tw,
                                        None if alpha is None else alpha.data_ptr(), plan.address, _dense(v, "v", (T, R)),
