@@ -668,13 +668,95 @@ __device__ __forceinline__ void src_pair(unsigned (&o)[SrcParts<S>::n], const un
     }
 }
 
+// A pair of bf16 with zeros in the place of infinities and NaN.
+__device__ __forceinline__ unsigned finite_pair(unsigned w) {
+    return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
+}
+
+// acc += left (16 * MR ranks x 16 tokens) * src (16 tokens x 64 columns).  The products of two lower parts whose sum of places is
+// above 2 are left out, each less than 2^-22 of the whole product.  The products that go into one accumulator follow each other at a
+// distance: a matrix instruction takes dozens of clocks.
+// APART: an infinity would meet the other side's lower parts as well, which may be 0, and 0 * infinity is NaN.  Leading parts
+// that are not finite are multiplied with leading parts only (the lower parts of an infinity are 0).
+template <GradSrc S, int MR, bool APART>
+__device__ __forceinline__ void grad_multiply(float (&acc)[MR][8][4], const unsigned (&x)[4][SrcWords<S>::n], const uint4 (&f)[MR][3]) {
+    constexpr int P = SrcParts<S>::n, JG = P == 1 ? 8 : 4;
+#pragma unroll
+    for (int j0 = 0; j0 < 8; j0 += JG) {
+        unsigned b0[JG][P], b1[JG][P];
+#pragma unroll
+        for (int j = 0; j < JG; ++j) {
+            src_pair<S>(b0[j], x[0], x[1], j0 + j);
+            src_pair<S>(b1[j], x[2], x[3], j0 + j);
+        }
+#pragma unroll
+        for (int i = 2; i >= 0; --i)
+#pragma unroll
+            for (int k = P - 1; k >= 0; --k)
+#pragma unroll
+                for (int m = 0; m < MR; ++m)
+#pragma unroll
+                    for (int j = 0; j < JG; ++j) {
+                        if (i + k > 2) continue;
+                        uint4 l = f[m][i];
+                        unsigned r0 = b0[j][k], r1 = b1[j][k];
+                        if (APART && i == 0 && k > 0) l = make_uint4(finite_pair(l.x), finite_pair(l.y), finite_pair(l.z), finite_pair(l.w));
+                        if (APART && i > 0 && k == 0) r0 = finite_pair(r0), r1 = finite_pair(r1);
+                        mma16<__nv_bfloat16>(acc[m][j0 + j], l.x, l.y, l.z, l.w, r0, r1);
+                    }
+    }
+}
+
+// Rows `row`, 4 + row, 8 + row, 12 + row of a chunk from memory.
+template <GradSrc S>
+__device__ __forceinline__ void load_step_any(unsigned (&x)[4][SrcWords<S>::n], const uint8_t *rows, int row_bytes, const int *perm, int row, int count,
+                                              int64_t c0, int g, int64_t cols) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int t = row + 4 * e < count ? __ldg(perm + row + 4 * e) : -1;
+        load_src8_any<S>(x[e], rows + (int64_t)max(t, 0) * row_bytes, t >= 0, c0, g, cols);
+    }
+}
+
+// A warp's sums once more, infinities kept apart: taken where the first ones are not all finite.
+template <GradSrc S, int MR>
+__device__ __noinline__ void adapter_grad_apart(float (&out)[MR][8][4], const uint8_t *rows, int row_bytes, const int *perm, int wt, int mine, int ntg,
+                                                int count, int64_t c0, int64_t cols, const uint4 *frag, int r0, int mtr) {
+    const int lane = threadIdx.x & 31;
+    float acc[MR][8][4];
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
+    for (int i = 0; i < mine; ++i) {
+        const int st = wt + i * ntg;
+        unsigned x[4][SrcWords<S>::n];
+        load_step_any<S>(x, rows, row_bytes, perm, st * 16 + (lane & 3), count, c0, lane >> 2, cols);
+        uint4 f[MR][3];
+#pragma unroll
+        for (int m = 0; m < MR; ++m)
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+                f[m][k] = MR == 1 || r0 + m < mtr ? __ldg(frag + (st * mtr + m) * 96 + k * 32) : make_uint4(0u, 0u, 0u, 0u);
+        grad_multiply<S, MR, true>(acc, x, f);
+    }
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out[m][j][i] = acc[m][j][i];
+}
+
 // sum over a chunk's tokens of left[r] * src[column]: 16 * MR ranks x 64 columns per warp.  The rows of a 16-token step
 // travel by cp.async through a ring of the warp's own in shared memory, several steps ahead.  Lane (g, q) reads eight
 // columns of rows q, 4 + q, 8 + q, 12 + q; two rows interleave into the fragment's K pairs (for codes that is the byte
 // permutation that starts their decoding).
 template <GradSrc S, int MR>
 __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const AdapterGradSide &sd, int block, const AdapterChunk &ch, int r0, float *smem) {
-    constexpr int W = SrcWords<S>::n, P = SrcParts<S>::n;
+    constexpr int W = SrcWords<S>::n;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int wc = warp % p.wc, wt = warp / p.wc, ntg = kTokWarps / p.wc;
     const int64_t c0 = ((int64_t)block * p.wc + wc) * 64;
@@ -702,28 +784,6 @@ __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const Ad
 #pragma unroll
             for (int i = 0; i < 3; ++i)
                 f[m][i] = MR == 1 || r0 + m < mtr ? __ldg(frag + (st * mtr + m) * 96 + i * 32) : make_uint4(0u, 0u, 0u, 0u);
-    };
-    // the products that go into one accumulator follow each other at a distance: a matrix instruction takes dozens of clocks
-    constexpr int JG = P == 1 ? 8 : 4;
-    auto multiply = [&](const unsigned (&x)[4][W], const uint4 (&f)[MR][3]) {
-#pragma unroll
-        for (int j0 = 0; j0 < 8; j0 += JG) {
-            unsigned b0[JG][P], b1[JG][P];
-#pragma unroll
-            for (int j = 0; j < JG; ++j) {
-                src_pair<S>(b0[j], x[0], x[1], j0 + j);
-                src_pair<S>(b1[j], x[2], x[3], j0 + j);
-            }
-#pragma unroll
-            for (int i = 2; i >= 0; --i)
-#pragma unroll
-                for (int k = P - 1; k >= 0; --k)
-#pragma unroll
-                    for (int m = 0; m < MR; ++m)
-#pragma unroll
-                        for (int j = 0; j < JG; ++j)
-                            if (i + k <= 2) mma16<__nv_bfloat16>(acc[m][j0 + j], f[m][i].x, f[m][i].y, f[m][i].z, f[m][i].w, b0[j][k], b1[j][k]);
-        }
     };
     const int mine = wt < steps && c0 < sd.cols ? (steps - wt + ntg - 1) / ntg : 0;      // this warp's steps: wt, wt + ntg, ...
     if (fast) {
@@ -782,24 +842,40 @@ __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const Ad
             unsigned x[4][W];
 #pragma unroll
             for (int e = 0; e < 4; ++e) read_src8<S>(x[e], stage + 4 * e * Ring::kPitch, g);
-            multiply(x, f);
+            grad_multiply<S, MR, false>(acc, x, f);
         };
         for (int i = 0; i < mine; i += 2) {
             step(i, a[0], a[kFragAhead]);
             if (i + 1 < mine) step(i + 1, a[kFragAhead], a[0]);
         }
         cp_async_wait_group<0>();
-    } else {
+    }
+    if (!fast) {
         for (int i = 0; i < mine; ++i) {
             const int st = wt + i * ntg;
             unsigned x[4][W];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int row = st * 16 + 4 * e + q, t = row < count ? __ldg(perm + row) : -1;
-                load_src8_any<S>(x[e], rows + (int64_t)max(t, 0) * row_bytes, t >= 0, c0, g, sd.cols);
-            }
+            load_step_any<S>(x, rows, row_bytes, perm, st * 16 + q, count, c0, g, sd.cols);
             load_left(st, a[0]);
-            multiply(x, a[0]);
+            grad_multiply<S, MR, false>(acc, x, a[0]);
+        }
+    }
+    if constexpr (S == GradSrc::F32 || S == GradSrc::Bf16) {   // (codes are finite and have one part)
+        bool finite = true;
+#pragma unroll
+        for (int m = 0; m < MR; ++m)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) finite = finite && fabsf(acc[m][j][i]) < __uint_as_float(0x7f800000u);
+        if (__any_sync(0xffffffffu, !finite)) {
+            float again[MR][8][4];
+            adapter_grad_apart<S, MR>(again, rows, row_bytes, perm, wt, mine, ntg, count, c0, sd.cols, frag, r0, mtr);
+#pragma unroll
+            for (int m = 0; m < MR; ++m)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m][j][i] = again[m][j][i];
         }
     }
     // the token groups' sums meet in shared memory, added in order
