@@ -54,13 +54,13 @@ __device__ __forceinline__ float round_tf32(float x) {
 }
 __device__ __forceinline__ float top16(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
 
-// Two fp32 numbers as three pairs of bf16 whose sums they are: eight significand bits each, cut off, so 24 in all and
-// nothing is lost (down to bf16's smallest numbers).
+// Two fp32 numbers as three pairs of bf16 whose sums they are (down to bf16's smallest numbers): eight significand bits cut
+// off, the 16 that are left rounded to eight, and what that leaves, of either sign, which has no more than eight.
 __device__ __forceinline__ void split3(float x, float y, unsigned &hi, unsigned &mid, unsigned &lo) {
     hi = __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632);
     const float x1 = rest_of(x, top16(x)), y1 = rest_of(y, top16(y));
-    mid = __byte_perm(__float_as_uint(x1), __float_as_uint(y1), 0x7632);
-    lo = pack_bf16(__fsub_rn(x1, top16(x1)), __fsub_rn(y1, top16(y1)));
+    mid = pack_bf16(x1, y1);
+    lo = pack_bf16(__fsub_rn(x1, __uint_as_float(mid << 16)), __fsub_rn(y1, top16(__uint_as_float(mid))));
 }
 
 // ------------------------------------------------------------------ tokens -> tokens
@@ -674,7 +674,8 @@ __device__ __forceinline__ unsigned finite_pair(unsigned w) {
 }
 
 // acc += left (16 * MR ranks x 16 tokens) * src (16 tokens x 64 columns).  The products of two lower parts whose sum of places is
-// above 2 are left out, each less than 2^-22 of the whole product.  The products that go into one accumulator follow each other at a
+// above 2 are left out: each is below 2^-23 of the whole product, and since the last part has either sign they do not add up
+// to a bias (a product's own rounding in fp32 is 2^-24).  The products that go into one accumulator follow each other at a
 // distance: a matrix instruction takes dozens of clocks.
 // APART: an infinity would meet the other side's lower parts as well, which may be 0, and 0 * infinity is NaN.  Leading parts
 // that are not finite are multiplied with leading parts only (the lower parts of an infinity are 0).

@@ -77,3 +77,20 @@ def test_token_without_adapter_keeps_its_base_bit_for_bit(ty):
     y, _ = dy.dybit_adapters(x, A, B, None, plan, base)
     bits = torch.int32 if ty == F else torch.int16
     assert torch.equal(y.view(bits), base.view(bits))
+
+
+def test_gradient_products_of_fp32_numbers():
+    # one token, so dB is one product of two fp32 numbers, each in three bf16 parts.  Numbers 1 + n * 2^-23 for every n below
+    # 2^16: their leading part is 1, the rest is all in the lower parts.  Bound, relative to the product (which is at least 1):
+    # two products of lower parts that are left out, 2^-23 each, and additions that may cut off, 2^-23 in the last and less than
+    # a 64th of it in the others
+    N, R = 1 << 16, 8
+    dY = (1 + torch.arange(N, device=DEV).double() * 2.0 ** -23).float()[None]
+    v = (1 + torch.tensor([0xffff, 0x8000, 0xff80, 0x7f80, 0x0080, 0x7fff, 0xff7f, 0x5555], device=DEV).double() * 2.0 ** -23).float()[None]
+    plan = dy.AdapterPlan(torch.zeros(1, dtype=torch.int32, device=DEV), 1)
+    codes, scales = dy.dybit_checkpoint_save(torch.ones((1, 64), device=DEV), (8, True))
+    A, B = torch.zeros((1, R, 64), dtype=BF, device=DEV), torch.zeros((1, R, N), dtype=BF, device=DEV)
+    _, _, dB = dy.dybit_adapters_backward(dY, codes, (8, True), scales, A, B, None, plan, v)
+    want = v[0].double()[:, None] * dY[0].double()[None, :]
+    err = ((dB[0].double() - want) / want).abs()
+    assert float(err.max()) <= (2 + 1 + 2.0 ** -6) * 2.0 ** -23, float(err.max()) * 2.0 ** 23
