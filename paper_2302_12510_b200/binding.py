@@ -231,6 +231,8 @@ def _workspace(need: int, ws: Optional[torch.Tensor], like: torch.Tensor, stream
     """(address, bytes, tensor to keep) of a 1024-byte aligned workspace on the device of `like`."""
     if ws is None:
         ws = _new(like, need + 1024, torch.uint8, stream, returned=False)
+        at = ws.data_ptr()
+        return at + -at % 1024, need + 1024 - -at % 1024, ws
     return (*_ws_span(ws, like), ws)
 
 
