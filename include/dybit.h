@@ -508,6 +508,7 @@ dybit_status dybit_adapters(int64_t T, int64_t K, int64_t N, int R, const void *
  *   V      [dev]  T x R floats, from dybit_adapters
  *   dA, dB [dev]  n_adapters x R x K and n_adapters x R x N floats, overwritten
  *   ws     [dev]  dybit_adapters_backward_workspace_bytes(...) bytes, 1024-byte aligned
+ * T / 512 + min(T, n_adapters) + n_adapters above 65535 (over 29 million tokens): DYBIT_ERR_UNSUPPORTED.
  * The order of the sums is fixed by the arguments: equal calls give equal bits. */
 size_t dybit_adapters_backward_workspace_bytes(int64_t T, int64_t K, int64_t N, int R, int n_adapters);
 dybit_status dybit_adapters_backward(int64_t T, int64_t K, int64_t N, int R, const void *dY, dybit_dtype tdy, int64_t lddy,

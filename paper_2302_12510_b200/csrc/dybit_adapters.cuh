@@ -1060,6 +1060,12 @@ static dybit_status launch_tokens_rank(const AdapterTokens &p, cudaStream_t s) {
     return launch_tokens<TX, TW, TY, 128, 1, BWD>(p, c1, s);
 }
 
+// Whether the gradient kernel's grid can hold the problem: chunks and adapters along y, at most blocks of 64 columns along x.
+// Asked before anything is launched.
+inline bool grad_grid_ok(int64_t T, int64_t K, int64_t N, int n) {
+    return PlanLayout(T, n).chunks_cap + n <= 65535 && (K + 63) / 64 + (N + 63) / 64 <= 0x7fffffff;
+}
+
 constexpr int kMaxGradSmem = (kTokWarps - 1) * 4 * 16 * 64 * 4;      // four blocks of ranks, one group of columns
 
 template <GradSrc S0, GradSrc S1, int MR>
@@ -1085,8 +1091,7 @@ static dybit_status launch_grad(const AdapterGrad &p_in, cudaStream_t s) {
     while (p.wc > 1 && (blocks(0) + blocks(1)) * L.chunks_cap * z < fill) p.wc /= 2;
     p.blocks0 = (int)blocks(0);
     p.chunk_slots = (int)L.chunks_cap;
-    const int64_t bx = blocks(0) + blocks(1), by = L.chunks_cap + p.n;
-    if (bx > 0x7fffffff || by > 65535) return DYBIT_ERR_UNSUPPORTED;
+    const int64_t bx = blocks(0) + blocks(1), by = L.chunks_cap + p.n;      // (within the grid's limits: grad_grid_ok)
     constexpr int kRing = SrcRing<S1>::kBytes > SrcRing<S0>::kBytes ? SrcRing<S1>::kBytes : SrcRing<S0>::kBytes;
     const int sums = (kTokWarps - p.wc) * mr * 16 * 64 * 4, smem = sums > kRing ? sums : kRing;
     const dim3 grid((unsigned)bx, (unsigned)by, (unsigned)z);
@@ -1176,7 +1181,7 @@ dybit_status dybit_adapters_backward(int64_t T, int64_t K, int64_t N, int R, con
     if (st != DYBIT_OK) return st;
     if (!dtype_ok(tdy) || lddy < N || lddx < K || (dXbase != nullptr && lddxbase < K) || scale_stride < 0) return DYBIT_ERR_INVALID_ARG;
     if (tdy == DYBIT_F16 || tw != DYBIT_BF16) return DYBIT_ERR_UNSUPPORTED;
-    if (row_stride_bytes > 0x7fffffff || lddy > 0x7fffffff / dtype_bytes(tdy)) return DYBIT_ERR_UNSUPPORTED;
+    if (row_stride_bytes > 0x7fffffff || lddy > 0x7fffffff / dtype_bytes(tdy) || !grad_grid_ok(T, K, N, n_adapters)) return DYBIT_ERR_UNSUPPORTED;
     if (dA == nullptr || dB == nullptr) return DYBIT_ERR_INVALID_ARG;
     if (T > 0 && (dY == nullptr || dX == nullptr || V == nullptr || scales == nullptr)) return DYBIT_ERR_INVALID_ARG;
     const int e = dtype_bytes(tdy);
