@@ -79,6 +79,7 @@ struct AdapterTokens {
     int64_t T, K, N;
     int n, R;
     int64_t perm_at, tiles_at;   // word offsets in the plan
+    int64_t tiles_cap, steps_cap;                // what the plan's list and the fragments' buffers hold (range checks)
     int fast;                    // all rows start where vectors can be moved: 16 bytes in x and w1, four elements in w2, base and y
     int wide;                    // 16-bit y: rows of base and y start on 16-byte boundaries and hold whole vectors
     // backward: fragments for adapter_grad_kernel
@@ -162,7 +163,7 @@ __device__ __forceinline__ Quad<T> load_quad(const T *row, int c, int cols) {
 template <typename T, bool FAST>
 __device__ __forceinline__ void store_quad(T *row, int c, int cols, const float4 f) {
     if constexpr (FAST) {
-        if (c < cols) {
+        if (c < cols && DYBIT_CHECK(c + 4 <= cols, 0x78)) {
             if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(row + c) = f;
             else *reinterpret_cast<uint2 *>(row + c) = make_uint2(pack2<T>(f.x, f.y), pack2<T>(f.z, f.w));
         }
@@ -268,12 +269,16 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
     const int cs = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
     const int tile_id = (int)blockIdx.x / cs;
     constexpr int kList = MT == 1 ? 0 : (MT == 2 ? 1 : 2);
-    if (tile_id >= p.plan[kList]) return;                      // the whole cluster
+    if (tile_id >= p.plan[kList] || !DYBIT_CHECK(tile_id < p.tiles_cap, 0x73)) return;       // the whole cluster
     const AdapterTile tile = reinterpret_cast<const AdapterTile *>(p.plan + p.tiles_at)[tile_id];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int R = p.R, K = (int)p.K, N = (int)p.N;
+    if (!DYBIT_CHECK(tile.adapter < p.n && tile.start >= 0 && tile.count >= 1 && tile.count <= TM && (int64_t)tile.start + tile.count <= p.T, 0x74)) return;
     if (threadIdx.x < TM) s_token[threadIdx.x] = p.plan[p.perm_at + tile.start + ((int)threadIdx.x < tile.count ? (int)threadIdx.x : 0)];
     __syncthreads();
+#ifdef DYBIT_DEBUG_BOUNDS
+    if (__syncthreads_or(threadIdx.x < TM && !DYBIT_CHECK((unsigned)s_token[threadIdx.x] < p.T, 0x75))) return;      // the whole cluster: all see the same
+#endif
 
     const int rblocks = tile.adapter >= 0 ? (R + 15) / 16 : 0;
     const TW *w2 = static_cast<const TW *>(p.w2) + (int64_t)max(tile.adapter, 0) * R * N;
@@ -466,7 +471,8 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
                         f[h][e] = v;
                     }
                 }
-                store_fragment((is_u ? p.frag_u : p.frag_v) + ((int64_t)(tile.step + st) * mtr + m) * 96, lane, f[0], f[1]);
+                if (DYBIT_CHECK(tile.step >= 0 && tile.step + st < p.steps_cap, 0x76))
+                    store_fragment((is_u ? p.frag_u : p.frag_v) + ((int64_t)(tile.step + st) * mtr + m) * 96, lane, f[0], f[1]);
             }
         }
     } else if (!BWD && p.v_out != nullptr && rank == 0) {
@@ -565,7 +571,7 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
 #pragma unroll
                         for (int b = 0; b < 2; ++b) {
                             const int c = n0 + b * kCb + q * kCq;
-                            if (c < N)
+                            if (c < N && DYBIT_CHECK(c + 8 <= N, 0x77))
                                 *reinterpret_cast<uint4 *>(row + c) = make_uint4(pack2<TY>(o[b].x, o[b].y), pack2<TY>(o[b].z, o[b].w),
                                                                                  pack2<TY>(o[2 + b].x, o[2 + b].y), pack2<TY>(o[2 + b].z, o[2 + b].w));
                         }
@@ -599,6 +605,7 @@ struct AdapterGrad {
     int64_t T;
     int n, R;
     int64_t perm_at, chunks_at, offsets_at;      // word offsets in the plan
+    int64_t steps_cap, partials_cap;             // what the fragments' and the partial sums' buffers hold (range checks)
     int blocks0;                 // blocks along x that belong to side 0
     int wc;                      // groups of 64 columns per block: 1, 2 or 4; the other warps share the tokens
     int chunk_slots;             // blocks along y that take chunks; n more look after adapters without tokens
@@ -710,19 +717,20 @@ __device__ __forceinline__ void grad_multiply(float (&acc)[MR][8][4], const unsi
 
 // Rows `row`, 4 + row, 8 + row, 12 + row of a chunk from memory.
 template <GradSrc S>
-__device__ __forceinline__ void load_step_any(unsigned (&x)[4][SrcWords<S>::n], const uint8_t *rows, int row_bytes, const int *perm, int row, int count,
-                                              int64_t c0, int g, int64_t cols) {
+__device__ __forceinline__ void load_step_any(unsigned (&x)[4][SrcWords<S>::n], const uint8_t *rows, int row_bytes, const int *perm, int64_t T, int row,
+                                              int count, int64_t c0, int g, int64_t cols) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const int t = row + 4 * e < count ? __ldg(perm + row + 4 * e) : -1;
+        int t = row + 4 * e < count ? __ldg(perm + row + 4 * e) : -1;
+        if (!DYBIT_CHECK(t < T, 0x7a)) t = -1;
         load_src8_any<S>(x[e], rows + (int64_t)max(t, 0) * row_bytes, t >= 0, c0, g, cols);
     }
 }
 
 // A warp's sums once more, infinities kept apart: taken where the first ones are not all finite.
 template <GradSrc S, int MR>
-__device__ __noinline__ void adapter_grad_apart(float (&out)[MR][8][4], const uint8_t *rows, int row_bytes, const int *perm, int wt, int mine, int ntg,
-                                                int count, int64_t c0, int64_t cols, const uint4 *frag, int r0, int mtr) {
+__device__ __noinline__ void adapter_grad_apart(float (&out)[MR][8][4], const uint8_t *rows, int row_bytes, const int *perm, int64_t T, int wt, int mine,
+                                                int ntg, int count, int64_t c0, int64_t cols, const uint4 *frag, int r0, int mtr) {
     const int lane = threadIdx.x & 31;
     float acc[MR][8][4];
 #pragma unroll
@@ -734,7 +742,7 @@ __device__ __noinline__ void adapter_grad_apart(float (&out)[MR][8][4], const ui
     for (int i = 0; i < mine; ++i) {
         const int st = wt + i * ntg;
         unsigned x[4][SrcWords<S>::n];
-        load_step_any<S>(x, rows, row_bytes, perm, st * 16 + (lane & 3), count, c0, lane >> 2, cols);
+        load_step_any<S>(x, rows, row_bytes, perm, T, st * 16 + (lane & 3), count, c0, lane >> 2, cols);
         uint4 f[MR][3];
 #pragma unroll
         for (int m = 0; m < MR; ++m)
@@ -796,7 +804,8 @@ __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const Ad
         const int *look = perm + wt * 16 + (lane & 15);        // of the step whose tokens are looked up next
         int look_rows = count - wt * 16, fill_rows = 0, fill = 0;
         auto token = [&]() {
-            const int t = (lane & 15) < look_rows ? __ldg(look) : 0;
+            int t = (lane & 15) < look_rows ? __ldg(look) : 0;
+            if (!DYBIT_CHECK((unsigned)t < p.T, 0x7a)) t = 0;
             look += ntg * 16;
             fill_rows = look_rows;
             look_rows -= ntg * 16;
@@ -855,7 +864,7 @@ __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const Ad
         for (int i = 0; i < mine; ++i) {
             const int st = wt + i * ntg;
             unsigned x[4][W];
-            load_step_any<S>(x, rows, row_bytes, perm, st * 16 + q, count, c0, g, sd.cols);
+            load_step_any<S>(x, rows, row_bytes, perm, p.T, st * 16 + q, count, c0, g, sd.cols);
             load_left(st, a[0]);
             grad_multiply<S, MR, false>(acc, x, a[0]);
         }
@@ -870,7 +879,7 @@ __device__ __forceinline__ void adapter_grad_body(const AdapterGrad &p, const Ad
                 for (int i = 0; i < 4; ++i) finite = finite && fabsf(acc[m][j][i]) < __uint_as_float(0x7f800000u);
         if (__any_sync(0xffffffffu, !finite)) {
             float again[MR][8][4];
-            adapter_grad_apart<S, MR>(again, rows, row_bytes, perm, wt, mine, ntg, count, c0, sd.cols, frag, r0, mtr);
+            adapter_grad_apart<S, MR>(again, rows, row_bytes, perm, p.T, wt, mine, ntg, count, c0, sd.cols, frag, r0, mtr);
 #pragma unroll
             for (int m = 0; m < MR; ++m)
 #pragma unroll
@@ -952,6 +961,10 @@ __global__ void __launch_bounds__(kTokThreads, MR == 1 ? 2 : 1) adapter_grad_ker
     }
     if ((int)blockIdx.y >= p.plan[3]) return;
     const AdapterChunk ch = reinterpret_cast<const AdapterChunk *>(p.plan + p.chunks_at)[blockIdx.y];
+    if (!DYBIT_CHECK((unsigned)ch.adapter < (unsigned)p.n && ch.start >= 0 && ch.rest >= 1 && (int64_t)ch.start + min(ch.rest, kChunkTokens) <= p.T &&
+                         ch.step >= 0 && ch.step + (min(ch.rest, kChunkTokens) + 15) / 16 <= p.steps_cap &&
+                         ((ch.index == 0 && ch.rest <= kChunkTokens) || (ch.index >= 0 && ch.partial >= 0 && ch.partial + ch.index < p.partials_cap)), 0x79))
+        return;
     if (first) adapter_grad_body<S0, MR>(p, p.side[0], block, ch, r0, smem_f);
     else adapter_grad_body<S1, MR>(p, p.side[1], block, ch, r0, smem_f);
 }
@@ -962,7 +975,7 @@ __global__ void __launch_bounds__(256) adapter_grad_sum_kernel(const __grid_cons
     const int a = blockIdx.y;
     const int *off = p.plan + p.offsets_at + (int64_t)a * kPlanColumns;
     const int parts = off[kPlanColumns + 4] - off[4], first = off[5];
-    if (parts <= 1) return;
+    if (parts <= 1 || !DYBIT_CHECK(first >= 0 && first + parts <= p.partials_cap, 0x7b)) return;
     for (int s = 0; s < 2; ++s) {
         const AdapterGradSide &sd = p.side[s];
         const int64_t size = p.R * sd.cols;                    // a multiple of 8
@@ -1014,7 +1027,7 @@ static dybit_status launch_tokens_inst(AdapterTokens p, int cs, cudaStream_t s) 
     if (st != DYBIT_OK) return st;
     const PlanLayout L(p.T, p.n);
     constexpr int kList = MT == 1 ? 0 : (MT == 2 ? 1 : 2);
-    p.perm_at = L.perm, p.tiles_at = L.tiles[kList];
+    p.perm_at = L.perm, p.tiles_at = L.tiles[kList], p.tiles_cap = L.tiles_cap[kList], p.steps_cap = L.steps_cap;
     const int64_t blocks = L.tiles_cap[kList] * cs;
     if (blocks > 0x7fffffff) return DYBIT_ERR_UNSUPPORTED;
     cudaLaunchConfig_t cfg = {};
@@ -1082,7 +1095,7 @@ template <GradSrc S0, GradSrc S1>
 static dybit_status launch_grad(const AdapterGrad &p_in, cudaStream_t s) {
     AdapterGrad p = p_in;
     const PlanLayout L(p.T, p.n);
-    p.perm_at = L.perm, p.chunks_at = L.chunks, p.offsets_at = L.offsets;
+    p.perm_at = L.perm, p.chunks_at = L.chunks, p.offsets_at = L.offsets, p.steps_cap = L.steps_cap, p.partials_cap = L.partials_cap;
     const int mtr = (p.R + 15) / 16, mr = mtr >= 3 ? 4 : mtr, z = (mtr + mr - 1) / mr;
     // wide blocks read longer runs of a row and the left operand less often, as far as the device stays full
     const int64_t fill = (int64_t)sm_count() * 3 / 2;

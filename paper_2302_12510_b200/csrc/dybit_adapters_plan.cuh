@@ -115,7 +115,8 @@ __global__ void __launch_bounds__(kPlanThreads) adapters_place_kernel(const int 
         int before = lane < warp ? s_warp[lane] : 0, all = s_warp[lane];
         before = __reduce_add_sync(0xffffffffu, before);
         all = __reduce_add_sync(0xffffffffu, all);
-        if (is) perm[done + before + __popc(votes & ((1u << lane) - 1u))] = (int)t;
+        const int at = done + before + __popc(votes & ((1u << lane) - 1u));
+        if (is && DYBIT_CHECK(at < count && start + at < T, 0x70)) perm[at] = (int)t;
         done += all;
         __syncthreads();
     }
@@ -124,13 +125,13 @@ __global__ void __launch_bounds__(kPlanThreads) adapters_place_kernel(const int 
         const int size = 16 << i, tiles = (count + size - 1) / size;
         AdapterTile *list = reinterpret_cast<AdapterTile *>(plan + L.tiles[i]) + off[1 + i];
         for (int k = threadIdx.x; k < tiles; k += kPlanThreads)
-            list[k] = {a < n ? a : -1, start + k * size, min(size, count - k * size), step0 + k * (size / 16)};
+            if (DYBIT_CHECK(off[1 + i] + k < L.tiles_cap[i], 0x71)) list[k] = {a < n ? a : -1, start + k * size, min(size, count - k * size), step0 + k * (size / 16)};
     }
     if (a < n) {
         const int chunks = (count + kChunkTokens - 1) / kChunkTokens;
         AdapterChunk *list = reinterpret_cast<AdapterChunk *>(plan + L.chunks) + off[4];
         for (int k = threadIdx.x; k < chunks; k += kPlanThreads)
-            list[k] = {a, start + k * kChunkTokens, count - k * kChunkTokens, step0 + k * (kChunkTokens / 16), k, off[5], 0, 0};
+            if (DYBIT_CHECK(off[4] + k < L.chunks_cap, 0x72)) list[k] = {a, start + k * kChunkTokens, count - k * kChunkTokens, step0 + k * (kChunkTokens / 16), k, off[5], 0, 0};
     }
 }
 

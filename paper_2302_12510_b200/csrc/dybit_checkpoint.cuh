@@ -156,14 +156,15 @@ __global__ void __launch_bounds__(kCkptThreads) checkpoint_save_kernel(const Ckp
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int64_t c = (int64_t)(i * TPR + t) * E;
-            if (c < p.width) {
+            if (c < p.width && DYBIT_CHECK(row < p.rows && c + E <= p.stride, 0x65)) {
                 if (special) store_vec_codes<T, SIGNED, true>(v[i], inv, out + c);
                 else store_vec_codes<T, SIGNED, false>(v[i], inv, out + c);
             }
         }
     } else {
         for (int64_t c = (int64_t)t * E; c < p.width; c += TPR * E)
-            store_vec_codes<T, SIGNED, true>(load_row_vec<T, VEC>(x, c, p.cols), inv, out + c);
+            if (DYBIT_CHECK(row < p.rows && c + E <= p.stride, 0x65))
+                store_vec_codes<T, SIGNED, true>(load_row_vec<T, VEC>(x, c, p.cols), inv, out + c);
     }
 }
 
@@ -207,7 +208,7 @@ __global__ void __launch_bounds__(kCkptThreads) checkpoint_load_kernel(const Ckp
     for (int i = 0; i < NV; ++i) {
         const int64_t c = c0 + i * (32 * E);
         w[i] = make_uint2(0u, 0u);
-        if (c < p.cols) {                                  // rows of codes are padded to 16: the whole vector is there
+        if (c < p.cols && DYBIT_CHECK(c + E <= p.stride, 0x66)) {      // rows of codes are padded to 16: the whole vector is there
             if constexpr (E == 4) w[i].x = __ldg(reinterpret_cast<const unsigned *>(in + c));
             else w[i] = __ldg(reinterpret_cast<const uint2 *>(in + c));
         }

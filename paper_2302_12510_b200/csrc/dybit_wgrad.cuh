@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(kExpandThreads) wgrad_expand_kernel(const Wgra
 #pragma unroll
         for (int i = 0; i < kExpandUnroll; ++i) {
             const int64_t c = c0 + i * 256;
-            if (c >= p.K) break;
+            if (c >= p.K || !DYBIT_CHECK(c + 8 <= p.ldx && c + 8 <= p.stride, 0x67)) break;
             const float4 a = decode4<SIGNED>(w[i].x), b = decode4<SIGNED>(w[i].y);
             *reinterpret_cast<uint4 *>(p.xe + t * p.ldx + c) =
                 make_uint4(pack_bf16(__fmul_rn(a.x, scale), __fmul_rn(a.y, scale)), pack_bf16(__fmul_rn(a.z, scale), __fmul_rn(a.w, scale)),
@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(kExpandThreads) wgrad_expand_kernel(const Wgra
 #pragma unroll
         for (int i = 0; i < kExpandUnroll; ++i) {
             const int64_t c = c0 + i * 256;
-            if (c >= p.N) break;
+            if (c >= p.N || !DYBIT_CHECK(c + 8 <= p.ldn, 0x68)) break;
             float f[8];
             load8f<T>(f, in, c, p.N, VEC);
 #pragma unroll
@@ -364,7 +364,7 @@ dybit_wgrad_kernel(const __grid_constant__ CUtensorMap tmap_dy, const __grid_con
                     float *row = p.out + w.split * p.part + (int64_t)(row0 + row_in_tile) * p.ld;
 #pragma unroll
                     for (int j = 0; j < 32; ++j)
-                        if (col0 + j < p.K) row[col0 + j] = f[c][j];
+                        if (col0 + j < p.K && DYBIT_CHECK(w.split < p.splits && col0 + j < p.ld, 0x69)) row[col0 + j] = f[c][j];
                 }
             }
         }
@@ -387,6 +387,7 @@ __global__ void __launch_bounds__(256) wgrad_sum_kernel(const float *__restrict_
     const int64_t cols4 = (K + 3) / 4;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < N * cols4; i += (int64_t)gridDim.x * 256) {
         const int64_t n = i / cols4, c = (i - n * cols4) * 4;
+        if (!DYBIT_CHECK(c + 4 <= ld && (n + 1) * ld <= part, 0x6a)) continue;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int k = 0; k < splits; ++k) {
             const float4 v = __ldcg(reinterpret_cast<const float4 *>(parts + k * part + n * ld + c));
