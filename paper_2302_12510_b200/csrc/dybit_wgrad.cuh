@@ -131,7 +131,7 @@ constexpr int kWgThreads = 320;
 // The tensor core cuts off what an addition to its fp32 accumulator cannot hold, so its error grows with the length of the
 // sum (3.4e-6 of the result over 8192 tokens).  After this many stages (1024 tokens) the epilogue warps take the
 // accumulator and add it to sums of their own in registers, rounded to nearest, while the next one fills
-// (8192 tokens: 4e-7, as a product in plain fp32).
+// (8192 tokens: 2.4e-7; a product in plain fp32 has 3.3e-7).
 constexpr int kWgSegment = 16;
 
 struct WgradParams {
@@ -430,7 +430,8 @@ struct WgradPlan {
         blocks_per_term = (T + kWgTokens - 1) / kWgTokens;
         blocks = blocks_per_term * terms;
         // a product of few tiles is cut along the contraction until the pairs of SMs have work, with at least eight stages
-        // to each part
+        // to each part.  The pairs are counted as the B200 has them, not asked of the device: the workspace's size depends on
+        // the parts, and is the same wherever it is asked for.  Fewer resident pairs work the same parts off in more rounds.
         const int64_t tiles = (int64_t)n_tiles * k_tiles, pairs = 74;
         splits = 1;
         while (tiles * splits * 2 <= pairs && blocks / (splits * 2) >= 8 && splits < 16) splits *= 2;
