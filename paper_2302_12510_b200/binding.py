@@ -804,7 +804,8 @@ def dybit_checkpoint_wgrad_workspace_bytes(T: int, N: int, K: int, dtype: torch.
 def dybit_checkpoint_wgrad(dY: torch.Tensor, codes: torch.Tensor, K: int, fmt, scales: torch.Tensor,
                            out: Optional[torch.Tensor] = None, per_row: bool = True,
                            ws: Optional[torch.Tensor] = None, stream=None):
-    """dW [N][K] float32 = dY^T x^ with x^ [T][K] read from an 8-bit checkpoint."""
+    """dW [N][K] float32 = dY^T x^ with x^ [T][K] read from an 8-bit checkpoint.  x^ takes part as bf16 numbers: exact for the
+    scales of dybit_checkpoint_save (powers of two) and with per_row=False, rounded to nearest for other row scales."""
     t, ld = _matrix(dY, "dY")
     T, N = dY.shape
     stride, scale_stride = _codes8(codes, T, K, scales, per_row)
