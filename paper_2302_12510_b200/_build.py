@@ -32,15 +32,41 @@ def _deps():
             glob.glob(os.path.join(_ROOT, "include", "*.h")))
 
 
+def _flags(debug_bounds: bool) -> list:
+    """The options that decide what the compiler makes of a source."""
+    return NVCC_FLAGS + (["-DDYBIT_DEBUG_BOUNDS"] if debug_bounds else [])
+
+
+def _flags_file(path: str) -> str:
+    """Where the options are kept that an object or a library was built with."""
+    return os.path.join(_OBJECTS, os.path.basename(path) + ".flags")
+
+
+def _built_with(path: str, flags: list) -> bool:
+    try:
+        with open(_flags_file(path)) as f:
+            return f.read() == "\n".join(flags)
+    except OSError:
+        return False
+
+
+def _record_flags(path: str, flags: list) -> None:
+    with open(_flags_file(path), "w") as f:
+        f.write("\n".join(flags))
+
+
 def is_stale(path: str = LIB_PATH) -> bool:
-    if not os.path.exists(path):
+    if not os.path.exists(path) or not _built_with(path, _flags(path == DEBUG_LIB_PATH)):
         return True
     t = os.path.getmtime(path)
     return any(os.path.getmtime(p) > t for p in _deps())
 
 
-def _object_is_stale(obj: str) -> bool:
-    """Whether a file that the object was compiled from (nvcc's list of dependencies beside it) is newer than it."""
+def _object_is_stale(obj: str, flags: list) -> bool:
+    """Whether the object was built with other options, or a file that it was compiled from (nvcc's list of dependencies
+    beside it) is newer than it."""
+    if not _built_with(obj, flags):
+        return True
     try:
         t = os.path.getmtime(obj)
         with open(obj + ".d") as f:
@@ -58,13 +84,14 @@ def build_library(force: bool = False, verbose: bool = False, debug_bounds: bool
     if not force and not is_stale(out):
         return out
     os.makedirs(_OBJECTS, exist_ok=True)
-    flags = NVCC_FLAGS + (["-DDYBIT_DEBUG_BOUNDS"] if debug_bounds else []) + (["-Xptxas", "-v"] if verbose else []) + [
+    options = _flags(debug_bounds)
+    flags = options + (["-Xptxas", "-v"] if verbose else []) + [
         "-I", os.path.join(_ROOT, "include"), "-I", os.path.join(_PKG, "csrc")]
     objects, jobs = [], []
     for src in _SOURCES:
         obj = os.path.join(_OBJECTS, os.path.basename(src) + (".debug.o" if debug_bounds else ".o"))
         objects.append(obj)
-        if force or _object_is_stale(obj):
+        if force or _object_is_stale(obj, options):
             tmp = obj + ".tmp%d" % os.getpid()
             cmd = [_nvcc()] + flags + ["-c", "-MD", "-MF", obj + ".d", "-o", tmp, src]
             jobs.append((obj, tmp, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
@@ -75,11 +102,13 @@ def build_library(force: bool = False, verbose: bool = False, debug_bounds: bool
         if verbose:
             print(log)
         os.replace(tmp, obj)
+        _record_flags(obj, options)
     tmp = out + ".tmp%d" % os.getpid()
     proc = subprocess.run([_nvcc()] + NVCC_FLAGS + ["-shared", "-o", tmp] + objects, capture_output=True, text=True)
     if proc.returncode != 0:
         raise RuntimeError("nvcc failed:\n" + proc.stdout + proc.stderr)
     os.replace(tmp, out)
+    _record_flags(out, options)
     return out
 
 
