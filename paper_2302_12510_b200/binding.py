@@ -787,9 +787,9 @@ def dybit_checkpoint_load(codes: torch.Tensor, cols: int, fmt, scales: torch.Ten
     rows = codes.shape[0]
     stride, scale_stride = _codes8(codes, rows, cols, scales, per_row)
     if out is None:
-        out, t, ld = _new(codes, (rows, cols), dtype, stream), _DTYPE_CODE.get(dtype), cols
-        if t is None:
+        if dtype not in _DTYPE_CODE:
             raise ValueError("dtype must be float32, bfloat16 or float16")
+        out, t, ld = _new(codes, (rows, cols), dtype, stream), _DTYPE_CODE[dtype], cols
     else:
         t, ld = _matrix(out, "out", rows, cols)
     _check(lib.dybit_checkpoint_load(codes.data_ptr(), stride, scales.data_ptr(), scale_stride, rows, cols, _fmt(fmt),
@@ -798,6 +798,8 @@ def dybit_checkpoint_load(codes: torch.Tensor, cols: int, fmt, scales: torch.Ten
 
 
 def dybit_checkpoint_wgrad_workspace_bytes(T: int, N: int, K: int, dtype: torch.dtype) -> int:
+    if dtype not in _DTYPE_CODE:
+        raise ValueError("dtype must be float32, bfloat16 or float16")
     return int(lib.dybit_checkpoint_wgrad_workspace_bytes(int(T), int(N), int(K), _DTYPE_CODE[dtype]))
 
 
@@ -876,8 +878,10 @@ def dybit_adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, alpha: Opt
     tx, ldx = _matrix(x, "x", T, K)
     tb, ldb = (None, 0) if base is None else _matrix(base, "base", T, N)
     if out is None:
-        out = _new(x, (T, N), base.dtype if base is not None else (out_dtype or x.dtype), stream)
-        ty, ldy = _DTYPE_CODE.get(out.dtype), N
+        dtype = base.dtype if base is not None else (out_dtype or x.dtype)
+        if dtype not in _DTYPE_CODE:
+            raise ValueError("out_dtype must be float32, bfloat16 or float16")
+        out, ty, ldy = _new(x, (T, N), dtype, stream), _DTYPE_CODE[dtype], N
     else:
         ty, ldy = _matrix(out, "out", T, N)
     if base is not None and tb != ty:

@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 import paper_2302_12510_b200 as dy
 
@@ -23,3 +24,19 @@ def test_backward_of_more_tokens_than_its_grid_holds(T, n):
                                    P(64), P(64), P(1024), need, None)
     assert st == UNSUPPORTED
     assert dy.dybit_launch_count() == launches
+
+
+def test_types_that_the_operators_do_not_have():
+    with pytest.raises(ValueError):
+        dy.dybit_checkpoint_wgrad_workspace_bytes(32, 64, 64, torch.float64)
+
+
+@pytest.mark.gpu
+def test_output_types_that_the_operators_do_not_have():
+    x, f = torch.zeros((4, 64), device="cuda"), torch.zeros((2, 8, 64), dtype=torch.bfloat16, device="cuda")
+    plan = dy.AdapterPlan(torch.zeros(4, dtype=torch.int32, device="cuda"), 2)
+    with pytest.raises(ValueError):
+        dy.dybit_adapters(x, f, f, None, plan, out_dtype=torch.float64)
+    codes, scales = dy.dybit_checkpoint_save(x, (8, 1))
+    with pytest.raises(ValueError):
+        dy.dybit_checkpoint_load(codes, 64, (8, 1), scales, dtype=torch.float64)
