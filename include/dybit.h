@@ -447,7 +447,8 @@ dybit_status dybit_checkpoint_save(const void *x, dybit_dtype tx, int64_t rows, 
 
 /* Reads it back: y = round_to_ty(fmul_rn(scale of the row, value(code))).  The scale of row r is
  * scales[r * scale_stride]: 1 for the scales of dybit_checkpoint_save, 0 for one scale of the whole tensor (the
- * pair that dybit_quantize_pack_2d writes). */
+ * pair that dybit_quantize_pack_2d writes).  y is an infinity where the nearest code stands for more than ty holds: f16
+ * elements from about 64500 on may come back as 65536, f32 and bf16 elements as close to their largest as 2^128. */
 dybit_status dybit_checkpoint_load(const void *codes, int64_t row_stride_bytes, const float *scales, int64_t scale_stride,
                                    int64_t rows, int64_t cols, dybit_fmt fmt, void *y, dybit_dtype ty, int64_t ld,
                                    void *stream);
@@ -490,7 +491,10 @@ dybit_status dybit_adapters_plan(int64_t T, const int32_t *ids, int n_adapters, 
  *   base  [dev]  T x N, row stride ldbase, or NULL for 0;  Y [dev] T x N, row stride ldy, may be base itself
  *   ty    type of base and Y: f32, or tx
  *   V     [dev]  T x R floats, dense, 16-byte aligned, or NULL: what dybit_adapters_backward wants of the forward pass
- * R is a multiple of 8 up to DYBIT_MAX_RANK (an adapter of lower rank has zero rows in A and B). */
+ * R is a multiple of 8 up to DYBIT_MAX_RANK (an adapter of lower rank has zero rows in A and B).
+ * V enters the second product as an fp32 number (f16 factors: off by at most 2^-24 of it).  A row of X that is not finite
+ * makes its own V and y not finite, as the formula has it, and no other.  Elements of A and B are finite: an infinite one
+ * makes what it enters not finite, but NaN where the formula may have an infinity. */
 #define DYBIT_MAX_RANK 128
 dybit_status dybit_adapters(int64_t T, int64_t K, int64_t N, int R, const void *X, dybit_dtype tx, int64_t ldx,
                             int n_adapters, const void *A, const void *B, dybit_dtype tw, const float *alpha,
@@ -501,7 +505,8 @@ dybit_status dybit_adapters(int64_t T, int64_t K, int64_t N, int R, const void *
  *     U[t]  = alpha_a * B_a dY[t]                  fp32
  *     dX[t] = dXbase[t] + sum_r U[t][r] A_a[r]
  *     dA_a  = sum_{t of a} U[t]^T x^[t],   dB_a = alpha_a * sum_{t of a} V[t]^T dY[t]
- * dX[t] = dXbase[t] for a token without an adapter; dA_a = dB_a = 0 for an adapter without tokens.
+ * dX[t] = dXbase[t] for a token without an adapter; dA_a = dB_a = 0 for an adapter without tokens.  Infinities and NaN in dY
+ * and V make those of the formula; tokens without an adapter have no part in dA and dB, whatever they hold.
  *   dY     [dev]  T x N, row stride lddy;  dXbase (or NULL), dX [dev] T x K, dX may be dXbase
  *   tdy    type of dY, dXbase and dX: f32 or bf16 (f16: DYBIT_ERR_UNSUPPORTED);  A and B are bf16
  *   codes, row_stride_bytes, fmt, scales, scale_stride: the checkpoint of X, T rows of K codes
