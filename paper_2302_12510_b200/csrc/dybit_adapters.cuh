@@ -247,8 +247,9 @@ struct TokSmem {
 // of it, for f16 factors two tf32 numbers rounded to nearest (off by at most 2^-24 of V, as an fp32 number is itself).
 // They are kept in shared memory as fragments.  The 64 columns of a warp are dealt to fragment columns so that a lane ends
 // up with 16 bytes of consecutive ones and four lanes with 64.  The base is added to the finished sum by an fp32 addition
-// rounded to nearest (in the accumulators the tensor core would cut it off); one of 16 bits is fetched a step ahead, one
-// of 32 bits while the products run.
+// rounded to nearest (in the accumulators the tensor core would cut it off).  It is fetched while the products run; one of 16
+// bits in a tile of several slices, where a warp has many steps, a step ahead (8192 tokens bf16, four slices: 45.5 us; tiles of
+// one slice are better off without the second set of registers: 256 tokens of 64 adapters 8.3 us, with it 8.8).
 template <typename TX, typename TW, typename TY, int RT, int MT, bool BWD, bool FAST>
 __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_kernel(const AdapterTokens p) {
     constexpr int NT = RT / 8, RB = RT / 16, TM = 16 * MT, XW = 4 * (int)sizeof(TX);
@@ -480,7 +481,7 @@ __global__ void __launch_bounds__(kTokThreads, RT <= 32 ? 2 : 1) adapter_tokens_
     }
 
     // ---- y = base + V B over this CTA's groups of 64 columns
-    constexpr bool kBaseAhead = sizeof(TY) == 2;
+    constexpr bool kBaseAhead = sizeof(TY) == 2 && MT > 1;
     const bool wide_rows = p.wide != 0;
     Quad<TY> base[2][4];                                       // [row][jh * 2 + b]
     auto load_base = [&](int n0, int m) {
