@@ -523,6 +523,88 @@ dybit_status dybit_adapters_backward(int64_t T, int64_t K, int64_t N, int R, con
                                      const void *dXbase, int64_t lddxbase, void *dX, int64_t lddx, float *dA,
                                      float *dB, void *ws, size_t ws_bytes, void *stream);
 
+/* ---------------------------------------------------------------- key-value cache in 8-bit codes
+ *
+ * The keys and values of a transformer's past tokens as signed 8-bit codes.  The cache is a pool of pages.  A page holds
+ * `page` consecutive tokens of one sequence, head by head:
+ *     codes  [pages][heads][page][dim]      one byte each, for keys and for values
+ *     scales [pages][heads]                 powers of two, likewise
+ *     element = scale * value(code)
+ * and a scale of 0 stands for a block whose elements are all 0.  Position p of sequence b lies on page
+ * table[b * table_stride + p / page], at its token p % page.  An entry outside 0 .. pages-1 is a page that is not there:
+ * its tokens are not written, read as zeros, and are seen by no query.
+ *   dim    a multiple of 16 up to 128;  page  16, 32, 64 or 128;  others: DYBIT_ERR_UNSUPPORTED
+ *   k_codes, v_codes [dev] 16-byte aligned;  pages * heads < 2^31 - 1 */
+typedef struct {
+    void *k_codes, *v_codes;
+    float *k_scales, *v_scales;
+    int64_t pages;
+    int page, heads, dim;
+} dybit_cache;
+
+/* A batch of sequences.  Its arrays of queries, keys, values and outputs have `tokens` rows; rows starts[b] ..
+ * starts[b + 1] - 1 are the last, new tokens of sequence b, which has lengths[b] tokens with them.  So row starts[b] + i
+ * is position lengths[b] - (starts[b + 1] - starts[b]) + i.  Rows that belong to no sequence are left as they are.
+ *   starts  sequences + 1 int32 that do not decrease, the last at most `tokens`
+ *   lengths at most max_pages * page (what is beyond is cut off); a sequence of fewer tokens than new rows is one whose
+ *           first rows lie in front of position 0: they are not written, read as zeros and see no key
+ *   max_new no sequence has more new tokens (what is beyond is left out); at most `tokens`
+ *   q_heads query heads of the attention, a multiple of cache.heads, up to 128 to a key head
+ *   table   [dev] sequences rows of max_pages entries, row stride table_stride */
+typedef struct {
+    int sequences;
+    int64_t tokens;
+    int max_new, q_heads;
+    const int32_t *table;
+    int64_t table_stride;
+    int max_pages;
+} dybit_cache_batch;
+
+/* Lists of the work of a batch: which pages its new tokens go to, the tiles of its queries, and how the keys of long
+ * sequences are cut.  Made once for a batch; every layer's calls with the same batch go by it, on caches of the same
+ * pages' size and heads, several calls at once if wanted (they only read it).
+ *   starts, lengths  [dev] int32
+ *   plan    [dev] dybit_cache_plan_bytes(...) bytes, 16-byte aligned, overwritten.  0 bytes: the arguments are refused */
+size_t dybit_cache_plan_bytes(const dybit_cache *cache, const dybit_cache_batch *batch);
+dybit_status dybit_cache_plan(const dybit_cache *cache, const dybit_cache_batch *batch, const int32_t *starts, const int32_t *lengths, void *plan,
+                              size_t plan_bytes, void *stream);
+
+/* Stores the keys and values of a batch's new tokens.  Per page and head, keys and values apart, with amax the largest
+ * finite magnitude of the new tokens that go there:
+ *     need  = 2^(ceil(log2(amax)) - top)         (exponent clamped to -126..126; 0 without a finite non-zero value)
+ *     scale = need                               where the new tokens open the page (one of them is its first)
+ *             max(need, the scale it has)        otherwise
+ *     code  = encode(x / scale)                  the encoder of dybit_quantize_pack; 0 for scale 0
+ * Where a begun page's scale grows, its older codes are encoded again, x being what they stand for: each time by half a
+ * step at most.  NaN -> code 0; infinities saturate.  Two sequences of a batch must not write to the same page (they may share pages that they read).
+ *   k, v  [dev]  tokens x heads x dim, unit inner stride, strides in elements.  (16-byte aligned rows run fastest.)
+ *   top   0 .. 6; 2 keeps most of a bell-shaped block where codes are finest */
+dybit_status dybit_cache_write(const dybit_cache *cache, const dybit_cache_batch *batch, const void *plan, const void *k, int64_t k_token_stride,
+                               int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride, dybit_dtype t, int top,
+                               void *stream);
+
+/* Reads the tokens of a batch back: k, v [dev] tokens x heads x dim, round_to_t(scale * value(code)).  (A batch whose
+ * new tokens are all tokens of its sequences reads the sequences whole.) */
+dybit_status dybit_cache_read(const dybit_cache *cache, const dybit_cache_batch *batch, const void *plan, void *k, int64_t k_token_stride,
+                              int64_t k_head_stride, void *v, int64_t v_token_stride, int64_t v_head_stride, dybit_dtype t, void *stream);
+
+/* Attention of a batch's new tokens over their sequences' caches (the new tokens' own keys and values have been
+ * written).  For the token at position i and query head h, over the keys j of head h / (q_heads / heads):
+ *     x_j = scale * q . k_j,   y = sum_j exp(x_j) v_j / sum_j exp(x_j),   lse = log(sum_j exp(x_j))
+ *     j <= i                 if causal, every j < lengths[b] otherwise
+ *     j >  i - window        if window > 0 (causal only): the last `window` keys, its own among them
+ * A row that sees no key is 0, its lse minus infinity.  Sums, maxima and statistics are fp32; q meets the keys as it is,
+ * probabilities meet the values as f16 numbers (2^-12 off at most, relative to the row's largest), y is rounded once.
+ * A row of q that is not finite makes its own y and lse not finite, and no other's.  The scales of the values that a row
+ * sees lie within 2^100 of each other.
+ *   q, y [dev]  tokens x q_heads x dim, unit inner stride, strides in elements;  t  bf16 or f16 (f32: DYBIT_ERR_UNSUPPORTED)
+ *   lse  [dev]  tokens x q_heads floats, dense, or NULL
+ *   ws   [dev]  dybit_cache_attention_workspace_bytes(...) bytes, 1024-byte aligned; calls that run at once need one each */
+size_t dybit_cache_attention_workspace_bytes(const dybit_cache *cache, const dybit_cache_batch *batch);
+dybit_status dybit_cache_attention(const dybit_cache *cache, const dybit_cache_batch *batch, const void *plan, const void *q, dybit_dtype t,
+                                   int64_t q_token_stride, int64_t q_head_stride, void *y, int64_t y_token_stride, int64_t y_head_stride, float *lse,
+                                   float scale, int causal, int window, void *ws, size_t ws_bytes, void *stream);
+
 /* Reads and clears the device status word of the current device.  Blocks
  * until `stream` has drained.  DYBIT_ERR_DEVICE_TIMEOUT means a kernel gave
  * up on a bounded wait (results of that call are invalid); DYBIT_OK

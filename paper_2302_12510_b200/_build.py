@@ -10,7 +10,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 LIB_PATH = os.path.join(_PKG, "libdybit.so")
 DEBUG_LIB_PATH = os.path.join(_PKG, "libdybit_debug.so")     # the same sources with -DDYBIT_DEBUG_BOUNDS (range checks)
-_SOURCES = [os.path.join(_PKG, "csrc", f) for f in ("dybit_lib.cu", "dybit_finetune.cu")]
+_SOURCES = [os.path.join(_PKG, "csrc", f) for f in ("dybit_lib.cu", "dybit_finetune.cu", "dybit_cache.cu")]
 _OBJECTS = os.path.join(_PKG, "build")
 
 NVCC_FLAGS = [

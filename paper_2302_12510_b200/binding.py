@@ -35,6 +35,8 @@ __all__ = [
     "dybit_checkpoint_save", "dybit_checkpoint_load", "dybit_checkpoint_wgrad", "dybit_checkpoint_wgrad_workspace_bytes",
     "AdapterPlan", "dybit_adapters_plan", "dybit_adapters_plan_bytes", "dybit_adapters", "dybit_adapters_backward",
     "dybit_adapters_backward_workspace_bytes",
+    "KVCache", "CachePlan", "dybit_cache_plan", "dybit_cache_plan_bytes", "dybit_cache_write", "dybit_cache_read", "dybit_cache_attention",
+    "dybit_cache_attention_workspace_bytes",
 ]
 
 
@@ -57,6 +59,16 @@ class _CConvLayer(C.Structure):
                 ("scale_w", C.c_void_p), ("ldw_bytes", C.c_int64), ("Y", C.c_void_p), ("Y_raw", C.c_void_p),
                 ("ws", C.c_void_p), ("ws_bytes", C.c_size_t), ("Q", C.c_void_p), ("fq", _CFmt),
                 ("scale_q", C.c_void_p), ("bias", C.c_void_p), ("relu", C.c_int)]
+
+
+class _CCache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+                ("pages", C.c_int64), ("page", C.c_int), ("heads", C.c_int), ("dim", C.c_int)]
+
+
+class _CCacheBatch(C.Structure):
+    _fields_ = [("sequences", C.c_int), ("tokens", C.c_int64), ("max_new", C.c_int), ("q_heads", C.c_int), ("table", C.c_void_p),
+                ("table_stride", C.c_int64), ("max_pages", C.c_int)]
 
 
 class ConvDesc(NamedTuple):
@@ -154,6 +166,15 @@ def _load() -> C.CDLL:
     lib.dybit_adapters_backward_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
     lib.dybit_adapters_backward.argtypes = [i64, i64, i64, i32, vp, i32, i64, vp, i64, _CFmt, vp, i64, i32, vp, vp, i32,
                                             vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+    cache, batch = C.POINTER(_CCache), C.POINTER(_CCacheBatch)
+    lib.dybit_cache_plan_bytes.restype = sz
+    lib.dybit_cache_plan_bytes.argtypes = [cache, batch]
+    lib.dybit_cache_plan.argtypes = [cache, batch, vp, vp, vp, sz, vp]
+    lib.dybit_cache_write.argtypes = [cache, batch, vp, vp, i64, i64, vp, i64, i64, i32, i32, vp]
+    lib.dybit_cache_read.argtypes = [cache, batch, vp, vp, i64, i64, vp, i64, i64, i32, vp]
+    lib.dybit_cache_attention_workspace_bytes.restype = sz
+    lib.dybit_cache_attention_workspace_bytes.argtypes = [cache, batch]
+    lib.dybit_cache_attention.argtypes = [cache, batch, vp, vp, i32, i64, i64, vp, i64, i64, vp, C.c_float, i32, i32, vp, sz, vp]
     lib.dybit_gemm_static_ws.argtypes = [i64, i64, i64, vp, _CFmt, vp, i64, vp, _CFmt, vp, i64, vp, i64, vp, vp]
     return lib
 
@@ -929,3 +950,156 @@ def dybit_adapters_backward(dY: torch.Tensor, codes: torch.Tensor, fmt, scales: 
                                        _dense(dA, "dA", (n, R, K)), _dense(dB, "dB", (n, R, N)), at, size, _stream(stream)),
            "dybit_adapters_backward")
     return dx, dA, dB
+
+
+# ---------------------------------------------------------------- key-value cache in 8-bit codes
+
+class KVCache:
+    """A pool of `pages` pages for the keys and values of `heads` heads of `dim` elements, `page` tokens to a page: codes
+    uint8 [pages][heads][page][dim] and scales float32 [pages][heads], for keys and for values.  Buffers that are not given
+    are allocated on `device`, on the current stream; a new pool reads as zeros."""
+
+    def __init__(self, pages: int, page: int, heads: int, dim: int, device=None, k_codes: Optional[torch.Tensor] = None,
+                 v_codes: Optional[torch.Tensor] = None, k_scales: Optional[torch.Tensor] = None, v_scales: Optional[torch.Tensor] = None):
+        self.pages, self.page, self.heads, self.dim = int(pages), int(page), int(heads), int(dim)
+        given = next((t for t in (k_codes, v_codes, k_scales, v_scales) if t is not None), None)
+        device = given.device if given is not None else device or torch.device("cuda", torch.cuda.current_device())
+
+        def buffer(t, name, shape, dtype):
+            if t is None:
+                return torch.zeros(shape, dtype=dtype, device=device) if dtype == torch.float32 else torch.empty(shape, dtype=dtype, device=device)
+            if not (t.is_cuda and t.device == given.device and t.dtype == dtype and tuple(t.shape) == shape and t.is_contiguous()):
+                raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor {list(shape)}, all on one device")
+            return t
+
+        codes, scales = (self.pages, self.heads, self.page, self.dim), (self.pages, self.heads)
+        self.k_codes, self.v_codes = buffer(k_codes, "k_codes", codes, torch.uint8), buffer(v_codes, "v_codes", codes, torch.uint8)
+        self.k_scales, self.v_scales = buffer(k_scales, "k_scales", scales, torch.float32), buffer(v_scales, "v_scales", scales, torch.float32)
+        self.c = _CCache(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(), self.v_scales.data_ptr(),
+                         self.pages, self.page, self.heads, self.dim)
+        self.ref = C.byref(self.c)
+
+
+def _cache_ints(t: torch.Tensor, name: str, n: int):
+    if not (t.dtype == torch.int32 and t.is_cuda and t.dim() == 1 and t.is_contiguous() and t.numel() == n):
+        raise ValueError(f"{name} must be a contiguous int32 CUDA tensor of {n} entries")
+
+
+def _cache_batch(cache: KVCache, table: torch.Tensor, tokens: int, q_heads: Optional[int], max_new: Optional[int]) -> _CCacheBatch:
+    if not (table.dtype == torch.int32 and table.is_cuda and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] <= 1)):
+        raise ValueError("table must be a 2-D int32 CUDA tensor [sequences][pages] with unit inner stride")
+    B, most = table.shape
+    return _CCacheBatch(B, int(tokens), int(tokens if max_new is None else min(max_new, tokens)), cache.heads if q_heads is None else int(q_heads),
+                        table.data_ptr(), max(table.stride(0), most) if B > 1 else most, most)
+
+
+def dybit_cache_plan_bytes(cache: KVCache, table: torch.Tensor, tokens: int, q_heads: Optional[int] = None, max_new: Optional[int] = None) -> int:
+    return int(lib.dybit_cache_plan_bytes(cache.ref, C.byref(_cache_batch(cache, table, tokens, q_heads, max_new))))
+
+
+def dybit_cache_plan(cache: KVCache, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, tokens: int, q_heads: Optional[int] = None,
+                     max_new: Optional[int] = None, plan: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Lists of the work of a batch (see CachePlan).  Returns the plan's buffer (uint8)."""
+    batch = _cache_batch(cache, table, tokens, q_heads, max_new)
+    _cache_ints(starts, "starts", batch.sequences + 1)
+    _cache_ints(lengths, "lengths", batch.sequences)
+    need = int(lib.dybit_cache_plan_bytes(cache.ref, C.byref(batch)))
+    if plan is None:
+        plan = _new(table, max(need, 16), torch.uint8, stream)
+    elif not (plan.is_cuda and plan.is_contiguous()):
+        raise ValueError("plan must be a contiguous CUDA tensor")
+    _check(lib.dybit_cache_plan(cache.ref, C.byref(batch), starts.data_ptr(), lengths.data_ptr(), plan.data_ptr(), plan.numel() * plan.element_size(),
+                                _stream(stream)), "dybit_cache_plan")
+    return plan
+
+
+class CachePlan:
+    """The plan of one batch of sequences, for every call on caches of the same pages' size and heads: table int32
+    [sequences][pages] with the page of every `page` tokens, starts int32 [sequences + 1] with the rows of each sequence's
+    new tokens among the batch's `tokens` rows, lengths int32 [sequences] with the tokens of each sequence, new ones
+    included.  max_new bounds the new tokens of one sequence (default: tokens); the smaller, the less is launched.  The
+    plan and its table have to outlive the calls that use them."""
+
+    def __init__(self, cache: KVCache, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, tokens: int, q_heads: Optional[int] = None,
+                 max_new: Optional[int] = None, buffer: Optional[torch.Tensor] = None, stream=None):
+        self.table, self.T = table, int(tokens)
+        self.batch = _cache_batch(cache, table, tokens, q_heads, max_new)
+        self.q_heads, self.page, self.heads = self.batch.q_heads, cache.page, cache.heads
+        self.buffer = dybit_cache_plan(cache, table, starts, lengths, tokens, q_heads, max_new, buffer, stream)
+        self.address, self.ref = self.buffer.data_ptr(), C.byref(self.batch)
+        self._ws_bytes = {}
+
+    def _for(self, cache: KVCache):
+        if cache.page != self.page or cache.heads != self.heads:
+            raise ValueError("the plan was made for a cache of other pages or heads")
+
+    def _workspace_bytes(self, cache: KVCache) -> int:
+        need = self._ws_bytes.get(cache.dim)
+        if need is None:
+            need = self._ws_bytes[cache.dim] = int(lib.dybit_cache_attention_workspace_bytes(cache.ref, self.ref))
+        return need
+
+
+def _heads3(x: torch.Tensor, name: str, T: int, heads: int, dim: int, code: Optional[int] = None) -> Tuple[int, int, int]:
+    """Checks a tensor [T][heads][dim] with unit inner stride; returns (dybit_dtype, token stride, head stride)."""
+    t = _DTYPE_CODE.get(x.dtype)
+    if t is None or not x.is_cuda or tuple(x.shape) != (T, heads, dim) or x.stride(2) != 1 or (code is not None and t != code):
+        raise ValueError(f"{name} must be a CUDA tensor [{T}][{heads}][{dim}] with unit inner stride, of float32, bfloat16 or float16 as its fellows")
+    st, sh, _ = x.stride()
+    if (T > 1 and st < dim) or (heads > 1 and sh < dim):
+        raise ValueError(f"the tokens and heads of {name} must not overlap")
+    # (torch gives an axis of one entry any stride)
+    return t, (st if T > 1 else heads * dim), (sh if heads > 1 else dim)
+
+
+def dybit_cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, plan: CachePlan, top: int = 2, stream=None) -> None:
+    """Stores the keys and values [tokens][heads][dim] of a batch's new tokens in the pages of the plan's table."""
+    plan._for(cache)
+    t, kt, kh = _heads3(k, "k", plan.T, cache.heads, cache.dim)
+    _, vt, vh = _heads3(v, "v", plan.T, cache.heads, cache.dim, t)
+    _check(lib.dybit_cache_write(cache.ref, plan.ref, plan.address, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, t, top, _stream(stream)),
+           "dybit_cache_write")
+
+
+def dybit_cache_read(cache: KVCache, plan: CachePlan, dtype: torch.dtype = torch.float32, k: Optional[torch.Tensor] = None,
+                     v: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The keys and values [tokens][heads][dim] that the cache holds for a batch's new tokens.  Rows of no sequence are
+    left as they are."""
+    plan._for(cache)
+    if dtype not in _DTYPE_CODE:
+        raise ValueError("dtype must be float32, bfloat16 or float16")
+    shape = (plan.T, cache.heads, cache.dim)
+    if k is None:
+        k = _new(cache.k_codes, shape, dtype if v is None else v.dtype, stream)
+    if v is None:
+        v = _new(cache.k_codes, shape, k.dtype, stream)
+    t, kt, kh = _heads3(k, "k", *shape)
+    _, vt, vh = _heads3(v, "v", *shape, t)
+    _check(lib.dybit_cache_read(cache.ref, plan.ref, plan.address, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, t, _stream(stream)),
+           "dybit_cache_read")
+    return k, v
+
+
+def dybit_cache_attention_workspace_bytes(cache: KVCache, plan: CachePlan) -> int:
+    return plan._workspace_bytes(cache)
+
+
+def dybit_cache_attention(q: torch.Tensor, cache: KVCache, plan: CachePlan, scale: Optional[float] = None, causal: bool = True, window: int = 0,
+                          out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """Attention of a batch's new tokens q [tokens][q_heads][dim] (bfloat16 or float16) over their sequences' caches; scale
+    defaults to dim ** -0.5, window > 0 lets a token see the last `window` keys, its own among them.  Returns the outputs
+    [tokens][q_heads][dim]; lse, float32 [tokens][q_heads], receives the logarithms of the rows' sums where it is given."""
+    plan._for(cache)
+    t, qt, qh = _heads3(q, "q", plan.T, plan.q_heads, cache.dim)
+    if t == 0:
+        raise ValueError("q must be bfloat16 or float16")
+    if out is None:
+        out, yt, yh = _new(q, q.shape, q.dtype, stream), plan.q_heads * cache.dim, cache.dim
+    else:
+        _, yt, yh = _heads3(out, "out", plan.T, plan.q_heads, cache.dim, t)
+    at, size, ws = _workspace(plan._workspace_bytes(cache), ws, q, stream)
+    _check(lib.dybit_cache_attention(cache.ref, plan.ref, plan.address, q.data_ptr(), t, qt, qh, out.data_ptr(), yt, yh,
+                                     None if lse is None else _dense(lse, "lse", (plan.T, plan.q_heads)),
+                                     cache.dim ** -0.5 if scale is None else scale, int(bool(causal)), int(window), at, size, _stream(stream)),
+           "dybit_cache_attention")
+    return out

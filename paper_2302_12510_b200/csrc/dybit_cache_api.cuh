@@ -1,0 +1,305 @@
+// Host side of the key-value cache: checks of arguments, sizes, launches.
+#pragma once
+
+#include <limits.h>
+
+#include "dybit_cache_attention.cuh"
+
+namespace dybit {
+
+constexpr int kCacheMaxDim = 128, kCacheMaxGroup = 128;
+
+static dybit_status check_cache(const dybit_cache *c) {
+    if (c == nullptr) return DYBIT_ERR_INVALID_ARG;
+    if (c->pages < 0 || c->heads < 1 || c->dim < 1 || c->page < 1) return DYBIT_ERR_INVALID_ARG;
+    if (c->dim % 16 != 0 || c->dim > kCacheMaxDim || (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128)) return DYBIT_ERR_UNSUPPORTED;
+    if (c->heads > 4096 || c->pages * c->heads > 0x7ffffffe) return DYBIT_ERR_UNSUPPORTED;
+    return DYBIT_OK;
+}
+
+// The cache's memory, which the plan does not look at.
+static dybit_status check_cache_memory(const dybit_cache *c) {
+    if (c->pages == 0) return DYBIT_OK;
+    if (c->k_codes == nullptr || c->v_codes == nullptr || c->k_scales == nullptr || c->v_scales == nullptr) return DYBIT_ERR_INVALID_ARG;
+    if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16) || !aligned(c->k_scales, 4) || !aligned(c->v_scales, 4)) return DYBIT_ERR_ALIGNMENT;
+    return DYBIT_OK;
+}
+
+static dybit_status check_batch(const dybit_cache *c, const dybit_cache_batch *b) {
+    if (b == nullptr) return DYBIT_ERR_INVALID_ARG;
+    if (b->sequences < 0 || b->tokens < 0 || b->max_new < 0 || b->q_heads < 1 || b->max_pages < 0 || b->table_stride < b->max_pages) return DYBIT_ERR_INVALID_ARG;
+    if (b->q_heads % c->heads != 0) return DYBIT_ERR_INVALID_ARG;
+    if (b->q_heads / c->heads > kCacheMaxGroup || b->sequences > (1 << 20) || b->tokens > (1 << 26)) return DYBIT_ERR_UNSUPPORTED;
+    if (b->tokens * (int64_t)b->q_heads > (1 << 30) || (int64_t)b->max_pages * c->page > INT_MAX - 256) return DYBIT_ERR_UNSUPPORTED;
+    return DYBIT_OK;
+}
+
+// The longest run of new tokens that small tiles take: four tiles' worth of rows.  See cache_prefill_tile for the other side.
+static CacheShape cache_shape(const dybit_cache *c, const dybit_cache_batch *b) {
+    CacheShape s = {};
+    s.T = b->tokens;
+    s.B = b->sequences;
+    s.page = c->page;
+    s.heads = c->heads;
+    s.group = b->q_heads / c->heads;
+    s.max_new = (int)std::min<int64_t>(b->max_new, b->tokens);
+    s.max_pages = b->max_pages;
+    s.small_tokens = INT_MAX;
+    return s;
+}
+
+static dybit_status check_plan(const dybit_cache *c, const dybit_cache_batch *b, const void *plan) {
+    dybit_status st = check_cache(c);
+    if (st == DYBIT_OK) st = check_cache_memory(c);
+    if (st == DYBIT_OK) st = check_batch(c, b);
+    if (st != DYBIT_OK) return st;
+    if (plan == nullptr || (b->table == nullptr && b->sequences > 0 && b->max_pages > 0)) return DYBIT_ERR_INVALID_ARG;
+    return aligned(plan, 16) && aligned(b->table, 4) ? DYBIT_OK : DYBIT_ERR_ALIGNMENT;
+}
+
+static int log2_of(int v) {
+    int s = 0;
+    while ((1 << s) < v) ++s;
+    return s;
+}
+
+// Tokens x heads x dim with unit inner stride.
+static dybit_status check_heads(const void *x, dybit_dtype t, int64_t token, int64_t head, int64_t T, int heads, int dim) {
+    if (x == nullptr) return DYBIT_ERR_INVALID_ARG;
+    if ((heads > 1 && head < dim) || (T > 1 && token < dim)) return DYBIT_ERR_INVALID_ARG;
+    return aligned(x, dtype_bytes(t)) ? DYBIT_OK : DYBIT_ERR_ALIGNMENT;
+}
+static bool heads_aligned(const void *x, dybit_dtype t, int64_t token, int64_t head, int bytes) {
+    return aligned(x, bytes) && token * dtype_bytes(t) % bytes == 0 && head * dtype_bytes(t) % bytes == 0;
+}
+
+template <typename T, bool VEC>
+static dybit_status launch_cache_write(const CacheWrite &p, int64_t items, int most, cudaStream_t s) {
+    const int64_t tiles = items * 2 * p.heads;
+    auto go = [&](auto kernel, int tiles_per_block) {
+        const int64_t blocks = (tiles + tiles_per_block - 1) / tiles_per_block;
+        if (blocks > kMaxGridX) return DYBIT_ERR_UNSUPPORTED;
+        launch_k(kernel, dim3((unsigned)blocks), dim3(kCkptThreads), 0, s, p);
+        return launch_status();
+    };
+    // warps to a page and head: as many as hold the new tokens of one in registers
+    const int vectors = most * p.vpr;
+    if (vectors <= 256) return go(cache_write_kernel<T, VEC, 1>, 8);
+    if (vectors <= 512) return go(cache_write_kernel<T, VEC, 2>, 4);
+    if (vectors <= 1024) return go(cache_write_kernel<T, VEC, 4>, 2);
+    return go(cache_write_kernel<T, VEC, 8>, 1);
+}
+
+template <typename F>
+static dybit_status with_type(dybit_dtype t, bool vec, F &&f) {
+    switch (t) {
+        case DYBIT_F32: return vec ? f.template operator()<float, true>() : f.template operator()<float, false>();
+        case DYBIT_BF16: return vec ? f.template operator()<__nv_bfloat16, true>() : f.template operator()<__nv_bfloat16, false>();
+        default: return vec ? f.template operator()<__half, true>() : f.template operator()<__half, false>();
+    }
+}
+
+struct CacheWriteLauncher {
+    const CacheWrite &p;
+    int64_t items;
+    int most;
+    cudaStream_t s;
+    template <typename T, bool VEC> dybit_status operator()() const { return launch_cache_write<T, VEC>(p, items, most, s); }
+};
+struct CacheReadLauncher {
+    const CacheRead &p;
+    int64_t items;
+    int threads;
+    cudaStream_t s;
+    template <typename T, bool VEC> dybit_status operator()() const {
+        const int64_t blocks = items * 2 * p.heads;
+        if (blocks > kMaxGridX) return DYBIT_ERR_UNSUPPORTED;
+        launch_k(cache_read_kernel<T, VEC>, dim3((unsigned)blocks), dim3((unsigned)threads), 0, s, p);
+        return launch_status();
+    }
+};
+
+// Codes [pages * heads][page][dim] of bytes, boxes of `rows` keys x DP bytes; what lies beyond dim reads as code 0.
+static bool make_cache_map(CUtensorMap *map, const void *codes, const dybit_cache *c, int rows, int dp) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (fn == nullptr) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)c->dim, (cuuint64_t)c->page, (cuuint64_t)(c->pages * c->heads)};
+    cuuint64_t strides[2] = {(cuuint64_t)c->dim, (cuuint64_t)c->dim * c->page};
+    cuuint32_t box[3] = {(cuuint32_t)dp, (cuuint32_t)rows, 1}, estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(codes), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              dp == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Parts of the attention's workspace: outputs and {maximum, sum, exponent} of the parts of cut tiles.
+struct CacheWorkspace {
+    int64_t small_y, small_ml, large_y, large_ml, bytes;
+    CacheWorkspace(const CacheShape &s, int dim) {
+        const CachePlanLayout L(s);
+        int64_t at = 0;
+        small_y = at, at += round_up(L.small_slots * s.heads * kSmallRows * dim * 4, 1024);
+        small_ml = at, at += round_up(L.small_slots * s.heads * kSmallRows * 16, 1024);
+        large_y = at, at += round_up(L.large_slots * s.heads * kLargeRows * dim * 4, 1024);
+        large_ml = at, at += round_up(L.large_slots * s.heads * kLargeRows * 16, 1024);
+        bytes = at;
+    }
+};
+
+template <typename T, int DP>
+static dybit_status launch_cache_small(const CUtensorMap &mk, const CUtensorMap &mv, const CacheAttn &p, int64_t items, cudaStream_t s) {
+    static std::atomic<int> ready[64];
+    int dev = 0;
+    DYBIT_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return DYBIT_ERR_CUDA;
+    if (ready[dev].load(std::memory_order_acquire) == 0) {
+        DYBIT_CUDA_TRY(cudaFuncSetAttribute(cache_small_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem_bytes<DP>()));
+        ready[dev].store(1, std::memory_order_release);
+    }
+    const int64_t blocks = items * p.heads;
+    if (blocks > kMaxGridX) return DYBIT_ERR_UNSUPPORTED;
+    launch_k(cache_small_kernel<T, DP>, dim3((unsigned)blocks), dim3(kSmThreads), small_smem_bytes<DP>(), s, mk, mv, p);
+    return launch_status();
+}
+
+template <typename T>
+static dybit_status run_cache_attention(const dybit_cache *c, const CacheShape &shape, CacheAttn p, uint8_t *ws, int *plan, cudaStream_t s) {
+    const CachePlanLayout L(shape);
+    const CacheWorkspace w(shape, c->dim);
+    const int dp = c->dim <= 64 ? 64 : 128;
+    CUtensorMap mk, mv;
+    if (!make_cache_map(&mk, c->k_codes, c, 16, dp) || !make_cache_map(&mv, c->v_codes, c, 16, dp)) return DYBIT_ERR_CUDA;
+    p.tiles = reinterpret_cast<const CacheTile *>(plan + L.small);
+    p.comb = reinterpret_cast<const CacheTile *>(plan + L.small_comb);
+    p.part_y = reinterpret_cast<float *>(ws + w.small_y);
+    p.part_ml = reinterpret_cast<float4 *>(ws + w.small_ml);
+    dybit_status st = dp == 64 ? launch_cache_small<T, 64>(mk, mv, p, L.small_cap, s) : launch_cache_small<T, 128>(mk, mv, p, L.small_cap, s);
+    if (st != DYBIT_OK) return st;
+    // a sequence of at most one part's least length is never cut
+    if (L.small_comb_cap > 0 && (int64_t)shape.max_pages * shape.page > kSmallLeast * kSmallUnit) {
+        launch_k(cache_join_kernel<T, kSmallRows>, dim3((unsigned)(L.small_comb_cap * p.heads)), dim3(128), 0, s, p);
+        st = launch_status();
+    }
+    return st;
+}
+
+}  // namespace dybit
+
+extern "C" {
+
+size_t dybit_cache_plan_bytes(const dybit_cache *cache, const dybit_cache_batch *batch) {
+    using namespace dybit;
+    if (check_cache(cache) != DYBIT_OK || check_batch(cache, batch) != DYBIT_OK) return 0;
+    return (size_t)round_up(CachePlanLayout(cache_shape(cache, batch)).words * 4, 16);
+}
+
+dybit_status dybit_cache_plan(const dybit_cache *cache, const dybit_cache_batch *batch, const int32_t *starts, const int32_t *lengths, void *plan,
+                              size_t plan_bytes, void *stream) {
+    using namespace dybit;
+    dybit_status st = check_cache(cache);
+    if (st == DYBIT_OK) st = check_batch(cache, batch);
+    if (st != DYBIT_OK) return st;
+    if (plan == nullptr || (batch->sequences > 0 && (starts == nullptr || lengths == nullptr))) return DYBIT_ERR_INVALID_ARG;
+    if (!aligned(plan, 16) || !aligned(starts, 4) || !aligned(lengths, 4)) return DYBIT_ERR_ALIGNMENT;
+    if (plan_bytes < dybit_cache_plan_bytes(cache, batch)) return DYBIT_ERR_WORKSPACE;
+    const CachePlanArgs a = {cache_shape(cache, batch), starts, lengths, static_cast<int *>(plan)};
+    launch_k(cache_plan_kernel, dim3(1), dim3(kCachePlanThreads), 0, static_cast<cudaStream_t>(stream), a);
+    return launch_status();
+}
+
+dybit_status dybit_cache_write(const dybit_cache *cache, const dybit_cache_batch *batch, const void *plan, const void *k, int64_t k_token_stride,
+                               int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride, dybit_dtype t, int top,
+                               void *stream) {
+    using namespace dybit;
+    dybit_status st = check_plan(cache, batch, plan);
+    if (st != DYBIT_OK) return st;
+    if (!dtype_ok(t) || top < 0 || top > 6) return DYBIT_ERR_INVALID_ARG;
+    if (batch->tokens == 0 || batch->sequences == 0 || batch->max_new == 0) return DYBIT_OK;
+    st = check_heads(k, t, k_token_stride, k_head_stride, batch->tokens, cache->heads, cache->dim);
+    if (st == DYBIT_OK) st = check_heads(v, t, v_token_stride, v_head_stride, batch->tokens, cache->heads, cache->dim);
+    if (st != DYBIT_OK) return st;
+    const CacheShape shape = cache_shape(cache, batch);
+    const CachePlanLayout L(shape);
+    const int *words = static_cast<const int *>(plan);
+    CacheWrite p = {};
+    p.plan = words, p.items = reinterpret_cast<const CacheItem *>(words + L.items);
+    p.table = batch->table, p.table_stride = batch->table_stride;
+    p.pages = cache->pages, p.page = cache->page, p.heads = cache->heads, p.dim = cache->dim;
+    p.vpr = cache->dim * dtype_bytes(t) / 16, p.vpr_mul = ((1 << 20) + p.vpr - 1) / p.vpr;
+    p.x[0] = k, p.x[1] = v;
+    p.token_stride[0] = k_token_stride, p.token_stride[1] = v_token_stride;
+    p.head_stride[0] = k_head_stride, p.head_stride[1] = v_head_stride;
+    p.codes[0] = static_cast<uint8_t *>(cache->k_codes), p.codes[1] = static_cast<uint8_t *>(cache->v_codes);
+    p.scales[0] = cache->k_scales, p.scales[1] = cache->v_scales;
+    p.top = top;
+    const bool vec = heads_aligned(k, t, k_token_stride, k_head_stride, 16) && heads_aligned(v, t, v_token_stride, v_head_stride, 16);
+    return with_type(t, vec, CacheWriteLauncher{p, L.items_cap, std::min(cache->page, shape.max_new), static_cast<cudaStream_t>(stream)});
+}
+
+dybit_status dybit_cache_read(const dybit_cache *cache, const dybit_cache_batch *batch, const void *plan, void *k, int64_t k_token_stride,
+                              int64_t k_head_stride, void *v, int64_t v_token_stride, int64_t v_head_stride, dybit_dtype t, void *stream) {
+    using namespace dybit;
+    dybit_status st = check_plan(cache, batch, plan);
+    if (st != DYBIT_OK) return st;
+    if (!dtype_ok(t)) return DYBIT_ERR_INVALID_ARG;
+    if (batch->tokens == 0 || batch->sequences == 0 || batch->max_new == 0) return DYBIT_OK;
+    st = check_heads(k, t, k_token_stride, k_head_stride, batch->tokens, cache->heads, cache->dim);
+    if (st == DYBIT_OK) st = check_heads(v, t, v_token_stride, v_head_stride, batch->tokens, cache->heads, cache->dim);
+    if (st != DYBIT_OK) return st;
+    const CacheShape shape = cache_shape(cache, batch);
+    const CachePlanLayout L(shape);
+    const int *words = static_cast<const int *>(plan);
+    CacheRead p = {};
+    p.plan = words, p.items = reinterpret_cast<const CacheItem *>(words + L.items);
+    p.table = batch->table, p.table_stride = batch->table_stride;
+    p.pages = cache->pages, p.page = cache->page, p.heads = cache->heads, p.dim = cache->dim;
+    p.vpr = cache->dim * dtype_bytes(t) / 16, p.vpr_mul = ((1 << 20) + p.vpr - 1) / p.vpr;
+    p.y[0] = k, p.y[1] = v;
+    p.token_stride[0] = k_token_stride, p.token_stride[1] = v_token_stride;
+    p.head_stride[0] = k_head_stride, p.head_stride[1] = v_head_stride;
+    p.codes[0] = static_cast<const uint8_t *>(cache->k_codes), p.codes[1] = static_cast<const uint8_t *>(cache->v_codes);
+    p.scales[0] = cache->k_scales, p.scales[1] = cache->v_scales;
+    const bool vec = heads_aligned(k, t, k_token_stride, k_head_stride, 16) && heads_aligned(v, t, v_token_stride, v_head_stride, 16);
+    const int vectors = std::min(cache->page, shape.max_new) * p.vpr, threads = (int)std::min<int64_t>(kCkptThreads, round_up((vectors + 3) / 4, 32));
+    return with_type(t, vec, CacheReadLauncher{p, L.items_cap, threads, static_cast<cudaStream_t>(stream)});
+}
+
+size_t dybit_cache_attention_workspace_bytes(const dybit_cache *cache, const dybit_cache_batch *batch) {
+    using namespace dybit;
+    if (check_cache(cache) != DYBIT_OK || check_batch(cache, batch) != DYBIT_OK) return 0;
+    return (size_t)CacheWorkspace(cache_shape(cache, batch), cache->dim).bytes;
+}
+
+dybit_status dybit_cache_attention(const dybit_cache *cache, const dybit_cache_batch *batch, const void *plan, const void *q, dybit_dtype t,
+                                   int64_t q_token_stride, int64_t q_head_stride, void *y, int64_t y_token_stride, int64_t y_head_stride, float *lse,
+                                   float scale, int causal, int window, void *ws, size_t ws_bytes, void *stream) {
+    using namespace dybit;
+    dybit_status st = check_plan(cache, batch, plan);
+    if (st != DYBIT_OK) return st;
+    if (!dtype_ok(t) || window < 0 || (window > 0 && !causal) || !(scale >= 0.0f) || scale > 3.0e38f) return DYBIT_ERR_INVALID_ARG;
+    if (t == DYBIT_F32) return DYBIT_ERR_UNSUPPORTED;
+    if (batch->tokens == 0 || batch->sequences == 0 || batch->max_new == 0) return DYBIT_OK;
+    st = check_heads(q, t, q_token_stride, q_head_stride, batch->tokens, batch->q_heads, cache->dim);
+    if (st == DYBIT_OK) st = check_heads(y, t, y_token_stride, y_head_stride, batch->tokens, batch->q_heads, cache->dim);
+    if (st != DYBIT_OK) return st;
+    if (!aligned(lse, 4) || !aligned(ws, 1024)) return DYBIT_ERR_ALIGNMENT;
+    if (ws == nullptr || ws_bytes < dybit_cache_attention_workspace_bytes(cache, batch)) return DYBIT_ERR_WORKSPACE;
+    if (cache->pages == 0) return DYBIT_ERR_INVALID_ARG;
+    CacheAttn p = {};
+    p.plan = static_cast<const int *>(plan);
+    p.table = batch->table, p.table_stride = batch->table_stride;
+    p.pages = cache->pages, p.page_shift = log2_of(cache->page), p.heads = cache->heads, p.group = batch->q_heads / cache->heads, p.dim = cache->dim;
+    p.k_scales = cache->k_scales, p.v_scales = cache->v_scales;
+    p.q = q, p.q_token = q_token_stride, p.q_head = q_head_stride;
+    p.y = y, p.y_token = y_token_stride, p.y_head = y_head_stride;
+    p.lse = lse;
+    p.scale_log2 = scale * kLog2e;
+    p.causal = causal != 0, p.window = window > 0 ? window : INT_MAX;
+    p.q_vec = heads_aligned(q, t, q_token_stride, q_head_stride, 8), p.y_vec = heads_aligned(y, t, y_token_stride, y_head_stride, 8);
+    const CacheShape shape = cache_shape(cache, batch);
+    uint8_t *base = static_cast<uint8_t *>(ws);
+    int *words = static_cast<int *>(const_cast<void *>(plan));
+    if (t == DYBIT_BF16) return run_cache_attention<__nv_bfloat16>(cache, shape, p, base, words, static_cast<cudaStream_t>(stream));
+    return run_cache_attention<__half>(cache, shape, p, base, words, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

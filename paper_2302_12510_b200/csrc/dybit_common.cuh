@@ -93,8 +93,9 @@ static inline cudaError_t take_status_word(cudaStream_t s, unsigned *word) {
     }
     return e;
 }
-// The word of dybit_finetune.cu.
+// The words of dybit_finetune.cu and dybit_cache.cu.
 cudaError_t take_finetune_status_word(cudaStream_t s, unsigned *word);
+cudaError_t take_cache_status_word(cudaStream_t s, unsigned *word);
 
 // Range checks of the debug build (-DDYBIT_DEBUG_BOUNDS, libdybit_debug.so): global-memory stores whose extent the
 // kernel knows are wrapped in `if (DYBIT_CHECK(index condition, site))`.  A failing check skips the access and ORs

@@ -310,6 +310,8 @@ dybit_status dybit_last_device_status(void *stream, uint32_t *detail) {
     DYBIT_CUDA_TRY(dybit::take_status_word(s, &word));
     DYBIT_CUDA_TRY(dybit::take_finetune_status_word(s, &more));
     if (word == 0) word = more;
+    DYBIT_CUDA_TRY(dybit::take_cache_status_word(s, &more));
+    if (word == 0) word = more;
     if (detail) *detail = word;
     if (word == 0) return DYBIT_OK;
     return (word & 1u) ? DYBIT_ERR_DEVICE_TIMEOUT : DYBIT_ERR_DEVICE_BOUNDS;

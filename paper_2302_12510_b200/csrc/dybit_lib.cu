@@ -1,5 +1,5 @@
-// libdybit: quantize, GEMM and convolution (dybit_finetune.cu is the second translation unit; no relocatable
-// device code is needed, each has its own device status word).
+// libdybit: quantize, GEMM and convolution (dybit_finetune.cu and dybit_cache.cu are the other translation units; no
+// relocatable device code is needed, each has its own device status word).
 #include "dybit_host.cuh"
 #include "dybit_quantize.cuh"
 #include "dybit_gemm.cuh"
