@@ -3,7 +3,7 @@
 
 #include <limits.h>
 
-#include "dybit_cache_attention.cuh"
+#include "dybit_cache_prefill.cuh"
 
 namespace dybit {
 
@@ -34,7 +34,9 @@ static dybit_status check_batch(const dybit_cache *c, const dybit_cache_batch *b
     return DYBIT_OK;
 }
 
-// The longest run of new tokens that small tiles take: four tiles' worth of rows.  See cache_prefill_tile for the other side.
+// Rows of a sequence that small tiles take: four tiles.  A large tile costs its keys as much whether it is full or not,
+// about what four small ones do.
+constexpr int kSmallMost = 64;
 static CacheShape cache_shape(const dybit_cache *c, const dybit_cache_batch *b) {
     CacheShape s = {};
     s.T = b->tokens;
@@ -44,7 +46,7 @@ static CacheShape cache_shape(const dybit_cache *c, const dybit_cache_batch *b) 
     s.group = b->q_heads / c->heads;
     s.max_new = (int)std::min<int64_t>(b->max_new, b->tokens);
     s.max_pages = b->max_pages;
-    s.small_tokens = INT_MAX;
+    s.small_tokens = std::max(1, kSmallMost / s.group);
     return s;
 }
 
@@ -161,6 +163,23 @@ static dybit_status launch_cache_small(const CUtensorMap &mk, const CUtensorMap 
     return launch_status();
 }
 
+template <typename T, int DP>
+static dybit_status launch_cache_large(const dybit_cache *c, const CacheAttn &p, int64_t items, cudaStream_t s) {
+    static std::atomic<int> ready[64];
+    int dev = 0;
+    DYBIT_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return DYBIT_ERR_CUDA;
+    if (ready[dev].load(std::memory_order_acquire) == 0) {
+        DYBIT_CUDA_TRY(cudaFuncSetAttribute(cache_large_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, large_smem_bytes<DP>()));
+        ready[dev].store(1, std::memory_order_release);
+    }
+    const int64_t blocks = items * p.heads;
+    if (blocks > kMaxGridX) return DYBIT_ERR_UNSUPPORTED;
+    launch_k(cache_large_kernel<T, DP>, dim3((unsigned)blocks), dim3(kLgThreads), large_smem_bytes<DP>(), s,
+             static_cast<const uint8_t *>(c->k_codes), static_cast<const uint8_t *>(c->v_codes), p);
+    return launch_status();
+}
+
 template <typename T>
 static dybit_status run_cache_attention(const dybit_cache *c, const CacheShape &shape, CacheAttn p, uint8_t *ws, int *plan, cudaStream_t s) {
     const CachePlanLayout L(shape);
@@ -168,15 +187,31 @@ static dybit_status run_cache_attention(const dybit_cache *c, const CacheShape &
     const int dp = c->dim <= 64 ? 64 : 128;
     CUtensorMap mk, mv;
     if (!make_cache_map(&mk, c->k_codes, c, 16, dp) || !make_cache_map(&mv, c->v_codes, c, 16, dp)) return DYBIT_ERR_CUDA;
-    p.tiles = reinterpret_cast<const CacheTile *>(plan + L.small);
-    p.comb = reinterpret_cast<const CacheTile *>(plan + L.small_comb);
-    p.part_y = reinterpret_cast<float *>(ws + w.small_y);
-    p.part_ml = reinterpret_cast<float4 *>(ws + w.small_ml);
-    dybit_status st = dp == 64 ? launch_cache_small<T, 64>(mk, mv, p, L.small_cap, s) : launch_cache_small<T, 128>(mk, mv, p, L.small_cap, s);
+    CacheAttn small = p, large = p;
+    small.tiles = reinterpret_cast<const CacheTile *>(plan + L.small);
+    small.comb = reinterpret_cast<const CacheTile *>(plan + L.small_comb);
+    small.part_y = reinterpret_cast<float *>(ws + w.small_y);
+    small.part_ml = reinterpret_cast<float4 *>(ws + w.small_ml);
+    large.tiles = reinterpret_cast<const CacheTile *>(plan + L.large);
+    large.comb = reinterpret_cast<const CacheTile *>(plan + L.large_comb);
+    large.part_y = reinterpret_cast<float *>(ws + w.large_y);
+    large.part_ml = reinterpret_cast<float4 *>(ws + w.large_ml);
+    const int64_t most = (int64_t)shape.max_pages * shape.page;      // keys of a sequence
+    dybit_status st = DYBIT_OK;
+    if (L.large_cap > 0) {
+        st = dp == 64 ? launch_cache_large<T, 64>(c, large, L.large_cap, s) : launch_cache_large<T, 128>(c, large, L.large_cap, s);
+        if (st != DYBIT_OK) return st;
+    }
+    st = dp == 64 ? launch_cache_small<T, 64>(mk, mv, small, L.small_cap, s) : launch_cache_small<T, 128>(mk, mv, small, L.small_cap, s);
     if (st != DYBIT_OK) return st;
     // a sequence of at most one part's least length is never cut
-    if (L.small_comb_cap > 0 && (int64_t)shape.max_pages * shape.page > kSmallLeast * kSmallUnit) {
-        launch_k(cache_join_kernel<T, kSmallRows>, dim3((unsigned)(L.small_comb_cap * p.heads)), dim3(128), 0, s, p);
+    if (L.large_comb_cap > 0 && most > kLargeLeast * kLargeUnit) {
+        launch_k(cache_join_kernel<T, kLargeRows>, dim3((unsigned)(L.large_comb_cap * p.heads), kLargeRows / 16), dim3(128), 0, s, large);
+        st = launch_status();
+        if (st != DYBIT_OK) return st;
+    }
+    if (most > kSmallLeast * kSmallUnit) {
+        launch_k(cache_join_kernel<T, kSmallRows>, dim3((unsigned)(L.small_comb_cap * p.heads)), dim3(128), 0, s, small);
         st = launch_status();
     }
     return st;
@@ -294,7 +329,8 @@ dybit_status dybit_cache_attention(const dybit_cache *cache, const dybit_cache_b
     p.lse = lse;
     p.scale_log2 = scale * kLog2e;
     p.causal = causal != 0, p.window = window > 0 ? window : INT_MAX;
-    p.q_vec = heads_aligned(q, t, q_token_stride, q_head_stride, 8), p.y_vec = heads_aligned(y, t, y_token_stride, y_head_stride, 8);
+    p.q_vec = heads_aligned(q, t, q_token_stride, q_head_stride, 8), p.q_vec16 = heads_aligned(q, t, q_token_stride, q_head_stride, 16);
+    p.y_vec = heads_aligned(y, t, y_token_stride, y_head_stride, 8);
     const CacheShape shape = cache_shape(cache, batch);
     uint8_t *base = static_cast<uint8_t *>(ws);
     int *words = static_cast<int *>(const_cast<void *>(plan));

@@ -41,8 +41,7 @@ struct CacheAttn {
     int causal, window;          // window: keys that a row sees, its own the last; INT_MAX for all
     float *part_y;               // [slot][head][rows][dim] of parts
     float4 *part_ml;             // [slot][head][rows]: {m + E0, l, E0, -}
-    int q_vec, y_vec;            // rows can be moved in 8-byte pieces
-    int first_wait;              // this launch is the first of its call: it waits for what came before
+    int q_vec, q_vec16, y_vec;   // rows can be moved in pieces of 8 (16) bytes
 };
 
 __device__ __forceinline__ float ex2(float x) {
