@@ -52,6 +52,11 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r
         "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
         : "memory");
 }
+__device__ __forceinline__ void tmem_st_32x8(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr)
+                 : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Two fp32 operations to an instruction.
@@ -76,13 +81,147 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
     return d;
 }
 
+// What the decoding warps need to know of their tile.
+struct LargeDecode {
+    const int *table;
+    int len, head, first, last;
+    volatile uint32_t *abort_flag;
+};
+
+// Page of the 16 keys from `key` on, or -1.
+__device__ __forceinline__ int large_page(const CacheAttn &p, const int *table, int len, int key) {
+    const int pg = key < len ? __ldg(table + (key >> p.page_shift)) : -1;
+    return (unsigned)pg < (uint64_t)p.pages ? pg : -1;
+}
+
+// Four warps turn the codes of a block's keys (or values) into 16-bit numbers of type T in the operand's layout, a unit
+// of 16 codes to a thread and pass.  The codes of the next half block are on their way while one is decoded.
+template <typename T, int DP, bool VALUES>
+__device__ __forceinline__ void large_decode(const CacheAttn &p, const LargeDecode &t, const uint8_t *__restrict__ codes, uint8_t *tiles, uint64_t *full,
+                                             uint64_t *empty) {
+    constexpr int UNITS = DP / 16, ROWS = 128 / UNITS, PASSES = kLgKeys / ROWS, HALF = PASSES / 2, PANEL = large_panel_bytes<DP>();
+    const int lane = threadIdx.x & 31, i = threadIdx.x & 127, u = i % UNITS, row0 = i / UNITS;
+    const bool in_dim = u * 16 < p.dim;
+    const int page_mask = (1 << p.page_shift) - 1;
+    const int64_t page_bytes = (int64_t)p.heads * p.dim << p.page_shift;
+    const uint8_t *base = codes + ((int64_t)t.head * p.dim << p.page_shift) + u * 16;
+    auto load = [&](int key, int pg) {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (pg >= 0 && in_dim) v = __ldg(reinterpret_cast<const uint4 *>(base + pg * page_bytes + (key & page_mask) * p.dim));
+        return v;
+    };
+    auto page_at = [&](int b) { return b < t.last ? large_page(p, t.table, t.len, b * kLgKeys + 16 * (lane & 7)) : -1; };
+    // values whose scale is 0 are zeros whatever their codes
+    auto held = [&](int pg) { return !VALUES || (pg >= 0 && __ldg(p.v_scales + (int64_t)pg * p.heads + t.head) > 0.0f); };
+    // lane k < 8 has the page of 16 keys k of a block
+    int page_now = page_at(t.first), page_next = page_at(t.first + 1);
+    bool held_now = held(page_now);
+    uint4 c[HALF];
+#pragma unroll
+    for (int s = 0; s < HALF; ++s) {
+        const int key = row0 + s * ROWS;
+        c[s] = load(key, __shfl_sync(0xffffffffu, page_now, key >> 4));
+    }
+    // threads of the second panel store their second half first: eight lanes then fill eight different 16-byte columns
+    const bool swap = DP == 128 && (u & 4) != 0;
+    const int chunk = 2 * (u & 3) + (swap ? 1 : 0);
+    uint8_t *const dst0 = tiles + (u >> 2) * PANEL + row0 * 128;
+    for (int b = t.first, n = 0; b < t.last; ++b, ++n) {
+        const int stage = n % kLgStages;
+        const int page_after = page_at(b + 2);
+        const bool held_next = held(page_next);
+        if (!__all_sync(0xffffffffu, wait_bounded(&empty[stage], ((n / kLgStages) & 1u) ^ 1u, t.abort_flag, 0x82))) break;
+        const uint32_t holds = __ballot_sync(0xffffffffu, held_now);
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+            uint8_t *dst = dst0 + stage * large_tile_bytes<DP>() + h * (HALF * ROWS * 128);
+            const int ahead = h == 0 ? page_now : page_next;
+#pragma unroll
+            for (int s = 0; s < HALF; ++s) {
+                const int key = row0 + (h * HALF + s) * ROWS, next = row0 + ((h ^ 1) * HALF + s) * ROWS;
+                uint4 w = c[s];
+                if (VALUES && !((holds >> (key >> 4)) & 1u)) w = make_uint4(0u, 0u, 0u, 0u);
+                c[s] = load(next, __shfl_sync(0xffffffffu, ahead, next >> 4));
+                const unsigned a0 = swap ? w.z : w.x, a1 = swap ? w.w : w.y, a2 = swap ? w.x : w.z, a3 = swap ? w.y : w.w;
+                auto pair = [&](unsigned x, int sel) { return decode_pair<T>(__byte_perm(x, 0u, sel)); };
+                const uint4 lo = make_uint4(pair(a0, 0x1100), pair(a0, 0x3322), pair(a1, 0x1100), pair(a1, 0x3322));
+                const uint4 hi = make_uint4(pair(a2, 0x1100), pair(a2, 0x3322), pair(a3, 0x1100), pair(a3, 0x3322));
+                uint8_t *row = dst + s * (ROWS * 128);
+                *reinterpret_cast<uint4 *>(row + ((chunk ^ (key & 7)) << 4)) = lo;
+                *reinterpret_cast<uint4 *>(row + (((chunk ^ 1) ^ (key & 7)) << 4)) = hi;
+            }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&full[stage]);
+        page_now = page_next, page_next = page_after, held_now = held_next;
+    }
+}
+
+// The largest of a row's 128 scores (TMEM address ts), times 16 keys' factor plus their exponent.
+template <bool EDGE>
+__device__ __forceinline__ float large_row_max(uint32_t ts, const float4 *blk, int lo, int hi) {
+    float top = -INFINITY;
+#pragma unroll 2
+    for (int c = 0; c < 8; ++c) {
+        uint32_t v[16];
+        tmem_ld_32x16(ts + c * 16, v);
+        const float4 f = blk[c];
+        tmem_ld_wait();
+        if (EDGE) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float x = __fmaf_rn(__uint_as_float(v[j]), f.x, f.y);
+                top = c * 16 + j >= lo && c * 16 + j < hi ? fmaxf(top, x) : top;
+            }
+        } else {                                           // the factor is not negative: the largest product has the largest x
+            float a = __uint_as_float(v[0]);
+#pragma unroll
+            for (int j = 1; j < 15; j += 2) a = fmaxf(fmaxf(a, __uint_as_float(v[j])), __uint_as_float(v[j + 1]));
+            a = fmaxf(a, __uint_as_float(v[15]));
+            top = fmaxf(top, __fmaf_rn(a, f.x, f.y));
+        }
+    }
+    return top;
+}
+
+// The row's probabilities at maximum um, written over its scores; returns l with their sum.
+template <bool EDGE>
+__device__ __forceinline__ float large_row_exp(uint32_t ts, const float4 *blk, int lo, int hi, float um, float l) {
+#pragma unroll 2
+    for (int c = 0; c < 8; ++c) {
+        uint32_t v[16], pr[8];
+        tmem_ld_32x16(ts + c * 16, v);
+        const float4 f = blk[c];
+        const float shift = f.y - um;
+        const uint64_t cc = pack_f32x2(f.x, f.x), ss = pack_f32x2(shift, shift);
+        uint64_t sum = 0;
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float2 x = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), cc, ss));
+            if (EDGE) {
+                if (c * 16 + 2 * j < lo || c * 16 + 2 * j >= hi) x.x = -INFINITY;
+                if (c * 16 + 2 * j + 1 < lo || c * 16 + 2 * j + 1 >= hi) x.y = -INFINITY;
+            }
+            x.x = ex2(x.x), x.y = ex2(x.y);
+            sum = j == 0 ? pack_f32x2(x.x, x.y) : add_f32x2(sum, pack_f32x2(x.x, x.y));
+            pr[j] = pack_f16(x.x, x.y);
+        }
+        const float2 s = unpack_f32x2(sum);
+        l = __fmaf_rn(s.x + s.y, f.z, l);
+        tmem_st_32x8(ts + c * 8, pr);
+    }
+    return l;
+}
+
 // A tile's own blocks: those between the first and the last key that a row of its half sees, within the part's range.
 struct LargeHalf { int first, last; };
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kLgThreads, 1)
 cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restrict__ v_codes, const CacheAttn p) {
-    constexpr int KS = DP / 16, UNITS = DP / 16, PASSES = kLgKeys * UNITS / 128, PANEL = large_panel_bytes<DP>(), TILE = large_tile_bytes<DP>();
+    constexpr int KS = DP / 16, PANEL = large_panel_bytes<DP>(), TILE = large_tile_bytes<DP>();
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *s_q = smem, *s_k = smem + 2 * TILE, *s_v = s_k + kLgStages * TILE;
@@ -130,11 +269,7 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
     const int b_first = half0.first == half0.last ? half1.first : half1.first == half1.last ? half0.first : min(half0.first, half1.first);
     const int b_last = half0.first == half0.last ? half1.last : half1.first == half1.last ? half0.last : max(half0.last, half1.last);
     const int *table = p.table + tile.seq * p.table_stride;
-    // page of the 16 keys from `key` on, or -1
-    auto page_at = [&](int key) {
-        const int pg = key < tile.len ? __ldg(table + (key >> p.page_shift)) : -1;
-        return (unsigned)pg < (uint64_t)p.pages ? pg : -1;
-    };
+    auto page_at = [&](int key) { return large_page(p, table, tile.len, key); };
 
     if (warp < 8 && there) {
         // a thread loads its row of queries
@@ -168,66 +303,9 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
 
     if (warp >= 8 && warp < 16) {
         // ------------------------------------------------ decode: warps 8 .. 11 keys, 12 .. 15 values
-        const bool values = warp >= 12;
-        const uint8_t *codes = values ? v_codes : k_codes;
-        uint64_t *full = values ? v_full : k_full, *empty = values ? v_empty : k_empty;
-        const int i = threadIdx.x & 127, u = i % UNITS, row0 = i / UNITS;
-        constexpr int ROWS = 128 / UNITS;                  // keys of a pass
-        const bool in_dim = u * 16 < p.dim;
-        uint4 c[PASSES];
-        auto load = [&](int b, int pass, int pg) {
-            const int key = row0 + pass * ROWS;
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (pg >= 0 && in_dim)
-                v = __ldg(reinterpret_cast<const uint4 *>(codes + (((int64_t)pg * p.heads + head) << p.page_shift) * p.dim +
-                                                          (((b * kLgKeys + key) & ((1 << p.page_shift) - 1)) * p.dim + u * 16)));
-            return v;
-        };
-        // lane k < 8 has the page of 16 keys k of a block
-        int page_now = -1;
-        if (b_first < b_last) page_now = page_at(b_first * kLgKeys + 16 * (lane & 7));
-        int page_next = b_first + 1 < b_last ? page_at((b_first + 1) * kLgKeys + 16 * (lane & 7)) : -1;
-        // values whose scale is 0 are zeros whatever their codes
-        auto held = [&](int pg) { return !values || (pg >= 0 && __ldg(p.v_scales + (int64_t)pg * p.heads + head) > 0.0f); };
-        bool held_now = held(page_now);
-#pragma unroll
-        for (int s = 0; s < PASSES; ++s) {
-            const int pg = __shfl_sync(0xffffffffu, page_now, (row0 + s * ROWS) >> 4);
-            if (b_first < b_last) c[s] = load(b_first, s, pg);
-        }
-        for (int b = b_first, n = 0; b < b_last; ++b, ++n) {
-            const int stage = n % kLgStages;
-            const int page_after = b + 2 < b_last ? page_at((b + 2) * kLgKeys + 16 * (lane & 7)) : -1;
-            const bool held_next = b + 1 < b_last ? held(page_next) : false;
-            if (!__all_sync(0xffffffffu, wait_bounded(&empty[stage], ((n / kLgStages) & 1u) ^ 1u, &s_abort, 0x82))) break;
-            uint8_t *dst = (values ? s_v : s_k) + stage * TILE;
-            const uint32_t holds = __ballot_sync(0xffffffffu, held_now);
-#pragma unroll
-            for (int s = 0; s < PASSES; ++s) {
-                const int key = row0 + s * ROWS;
-                uint4 w = c[s];
-                if (!((holds >> (key >> 4)) & 1u)) w = make_uint4(0u, 0u, 0u, 0u);
-                const int pg = __shfl_sync(0xffffffffu, page_next, key >> 4);
-                if (b + 1 < b_last) c[s] = load(b + 1, s, pg);
-                // lanes of the second panel store their second half first: eight lanes then fill eight different banks' worth
-                const bool swap = DP == 128 && (u & 4) != 0;
-                const unsigned a0 = swap ? w.z : w.x, a1 = swap ? w.w : w.y, a2 = swap ? w.x : w.z, a3 = swap ? w.y : w.w;
-                auto pair = [&](unsigned x, int sel) {
-                    const unsigned d = __byte_perm(x, 0u, sel);
-                    return values ? decode2_f16(d) : decode_pair<T>(d);
-                };
-                const uint4 lo = make_uint4(pair(a0, 0x1100), pair(a0, 0x3322), pair(a1, 0x1100), pair(a1, 0x3322));
-                const uint4 hi = make_uint4(pair(a2, 0x1100), pair(a2, 0x3322), pair(a3, 0x1100), pair(a3, 0x3322));
-                uint8_t *row = dst + (u >> 2) * PANEL + key * 128;
-                const int chunk = 2 * (u & 3) + (swap ? 1 : 0);
-                *reinterpret_cast<uint4 *>(row + ((chunk ^ (key & 7)) << 4)) = lo;
-                *reinterpret_cast<uint4 *>(row + (((chunk ^ 1) ^ (key & 7)) << 4)) = hi;
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&full[stage]);
-            page_now = page_next, page_next = page_after, held_now = held_next;
-        }
+        const LargeDecode d = {table, tile.len, head, b_first, b_last, &s_abort};
+        if (warp < 12) large_decode<T, DP, false>(p, d, k_codes, s_k, k_full, k_empty);
+        else large_decode<__half, DP, true>(p, d, v_codes, s_v, v_full, v_empty);
     } else if (warp == 16) {
         // ------------------------------------------------ issue
         if (lane == 0 && b_first < b_last) {
@@ -337,38 +415,13 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
             tc_fence_after_sync();
             const int key0 = b * kLgKeys;
             const bool edge = key0 < all_lo || key0 + kLgKeys > all_hi;
-            // the row's maximum
-            float top = -INFINITY;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t v[32];
-                tmem_ld_32x32(ts + c * 32, v);
-                tmem_ld_wait();
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float4 f = blk[2 * c + h];
-                    if (edge) {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const int key = key0 + c * 32 + h * 16 + j;
-                            const float x = __fmaf_rn(__uint_as_float(v[h * 16 + j]), f.x, f.y);
-                            top = key >= keys.lo && key < keys.hi ? fmaxf(top, x) : top;
-                        }
-                    } else {                               // the factor is not negative: the largest product has the largest x
-                        float a = __uint_as_float(v[h * 16]);
-#pragma unroll
-                        for (int j = 1; j < 15; j += 2) a = fmaxf(fmaxf(a, __uint_as_float(v[h * 16 + j])), __uint_as_float(v[h * 16 + j + 1]));
-                        a = fmaxf(a, __uint_as_float(v[h * 16 + 15]));
-                        top = fmaxf(top, __fmaf_rn(a, f.x, f.y));
-                    }
-                }
-            }
+            const float top = edge ? large_row_max<true>(ts, blk, keys.lo - key0, keys.hi - key0) : large_row_max<false>(ts, blk, 0, 0);
             if (__any_sync(0xffffffffu, top > m + kRaise)) {
                 const float raised = fmaxf(m, top), f = m == raised ? 1.0f : ex2(m - raised);
                 m = raised;
                 l *= f;
                 if (n > 0) {                               // the products up to the last block have ended: s_full comes behind them
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < DP / 16; ++c) {
                         uint32_t v[16];
                         tmem_ld_32x16(to + c * 16, v);
@@ -380,35 +433,7 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
                 }
             }
             const float um = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t v[32], pr[16];
-                tmem_ld_32x32(ts + c * 32, v);
-                tmem_ld_wait();
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float4 f = blk[2 * c + h];
-                    const float shift = f.y - um;
-                    const uint64_t cc = pack_f32x2(f.x, f.x), ss = pack_f32x2(shift, shift);
-                    uint64_t sum = 0;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const uint64_t x2 = fma_f32x2(pack_f32x2(__uint_as_float(v[h * 16 + 2 * j]), __uint_as_float(v[h * 16 + 2 * j + 1])), cc, ss);
-                        float2 x = unpack_f32x2(x2);
-                        if (edge) {
-                            const int key = key0 + c * 32 + h * 16 + 2 * j;
-                            if (key < keys.lo || key >= keys.hi) x.x = -INFINITY;
-                            if (key + 1 < keys.lo || key + 1 >= keys.hi) x.y = -INFINITY;
-                        }
-                        x.x = ex2(x.x), x.y = ex2(x.y);
-                        sum = j == 0 ? pack_f32x2(x.x, x.y) : add_f32x2(sum, pack_f32x2(x.x, x.y));
-                        pr[h * 8 + j] = pack_f16(x.x, x.y);
-                    }
-                    const float2 s = unpack_f32x2(sum);
-                    l = __fmaf_rn(s.x + s.y, f.z, l);
-                }
-                tmem_st_32x16(ts + c * 16, pr);
-            }
+            l = edge ? large_row_exp<true>(ts, blk, keys.lo - key0, keys.hi - key0, um, l) : large_row_exp<false>(ts, blk, 0, 0, um, l);
             tmem_st_wait();
             tc_fence_before_sync();
             __syncwarp();
@@ -421,7 +446,7 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
         const bool any = half.first < half.last && ok;
         if (128 * t + 32 * w4 < rows) {                    // whole warps
             const int64_t at = ((int64_t)tile.slot * p.heads + head) * kLargeRows + r;
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < DP / 16; ++c) {
                 uint32_t v[16];
                 if (any) {
