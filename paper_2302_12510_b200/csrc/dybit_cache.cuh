@@ -17,7 +17,8 @@ __device__ __forceinline__ void named_tile_sync(int sub) {
 }
 
 constexpr int kCachePlanThreads = 1024;
-constexpr int kSmallRows = 16;               // query rows (token x query head of one key head) of a small tile: one matrix instruction's
+constexpr int kSmallRows = 16;               // query rows (token x query head of one key head) of a small tile at most; half of them
+                                             // where no sequence of the batch has more
 constexpr int kLargeRows = 256;              // rows of a large tile: two accumulators of 128
 constexpr int kSmallUnit = 64, kLargeUnit = 128;     // keys in which a split of the key axis is counted
 // CTAs that the key axis is cut for.  Counted as the B200 has them, not asked of the device: the sizes of plans and
@@ -35,7 +36,8 @@ struct CacheSeq { int row, n, len, items, small_tiles, large_tiles; };
 struct CacheShape {
     int64_t T;
     int B, page, heads, group, max_new, max_pages;
-    int small_tokens;            // a sequence with more new tokens than this takes large tiles (INT_MAX: none does)
+    int small_tokens;            // a sequence with more new tokens than this takes large tiles
+    int small_rows;              // of a small tile: 8 or kSmallRows
 };
 
 // Word offsets of a plan's parts; the capacities bound what the device fills in.
@@ -48,7 +50,7 @@ struct CachePlanLayout {
         items_cap = lesser(T, T / s.page + 3 * B);
         // new tokens that small tiles take: all of a sequence of at most small_tokens
         const int64_t few = s.small_tokens >= s.max_new ? T : lesser(T, B * (int64_t)s.small_tokens);
-        const int64_t small_tiles = lesser(few * s.group, few * s.group / kSmallRows + B);
+        const int64_t small_tiles = lesser(few * s.group, few * s.group / s.small_rows + B);
         const int64_t large_tiles = s.max_new > s.small_tokens ? lesser(T, T * s.group / kLargeRows + B) : 0;
         const int64_t small_parts = kSmallTarget / s.heads + 1, large_parts = kLargeTarget / s.heads + 1;
         small_cap = small_tiles + small_parts;
@@ -86,7 +88,7 @@ __device__ __forceinline__ CacheSeq cache_seq(const CachePlanArgs &a, int b) {
     q.items = cache_div_up(outside, a.s.page) + (inside > 0 ? (q.len - 1) / a.s.page - p0 / a.s.page + 1 : 0);
     const int rows = q.n * a.s.group;
     const bool small = q.n <= a.s.small_tokens;
-    q.small_tiles = small ? cache_div_up(rows, kSmallRows) : 0;
+    q.small_tiles = small ? cache_div_up(rows, a.s.small_rows) : 0;
     q.large_tiles = small ? 0 : cache_div_up(rows, kLargeRows);
     return q;
 }

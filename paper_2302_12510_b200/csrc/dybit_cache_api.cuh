@@ -47,6 +47,7 @@ static CacheShape cache_shape(const dybit_cache *c, const dybit_cache_batch *b) 
     s.max_new = (int)std::min<int64_t>(b->max_new, b->tokens);
     s.max_pages = b->max_pages;
     s.small_tokens = std::max(1, kSmallMost / s.group);
+    s.small_rows = (int64_t)s.max_new * s.group <= 8 ? 8 : kSmallRows;
     return s;
 }
 
@@ -139,27 +140,27 @@ struct CacheWorkspace {
     CacheWorkspace(const CacheShape &s, int dim) {
         const CachePlanLayout L(s);
         int64_t at = 0;
-        small_y = at, at += round_up(L.small_slots * s.heads * kSmallRows * dim * 4, 1024);
-        small_ml = at, at += round_up(L.small_slots * s.heads * kSmallRows * 16, 1024);
+        small_y = at, at += round_up(L.small_slots * s.heads * s.small_rows * dim * 4, 1024);
+        small_ml = at, at += round_up(L.small_slots * s.heads * s.small_rows * 16, 1024);
         large_y = at, at += round_up(L.large_slots * s.heads * kLargeRows * dim * 4, 1024);
         large_ml = at, at += round_up(L.large_slots * s.heads * kLargeRows * 16, 1024);
         bytes = at;
     }
 };
 
-template <typename T, int DP>
+template <typename T, int DP, int NQ>
 static dybit_status launch_cache_small(const CUtensorMap &mk, const CUtensorMap &mv, const CacheAttn &p, int64_t items, cudaStream_t s) {
     static std::atomic<int> ready[64];
     int dev = 0;
     DYBIT_CUDA_TRY(cudaGetDevice(&dev));
     if (dev < 0 || dev >= 64) return DYBIT_ERR_CUDA;
     if (ready[dev].load(std::memory_order_acquire) == 0) {
-        DYBIT_CUDA_TRY(cudaFuncSetAttribute(cache_small_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem_bytes<DP>()));
+        DYBIT_CUDA_TRY(cudaFuncSetAttribute(cache_small_kernel<T, DP, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem_bytes<DP>()));
         ready[dev].store(1, std::memory_order_release);
     }
     const int64_t blocks = items * p.heads;
     if (blocks > kMaxGridX) return DYBIT_ERR_UNSUPPORTED;
-    launch_k(cache_small_kernel<T, DP>, dim3((unsigned)blocks), dim3(kSmThreads), small_smem_bytes<DP>(), s, mk, mv, p);
+    launch_k(cache_small_kernel<T, DP, NQ>, dim3((unsigned)blocks), dim3(kSmThreads), small_smem_bytes<DP>(), s, mk, mv, p);
     return launch_status();
 }
 
@@ -202,16 +203,20 @@ static dybit_status run_cache_attention(const dybit_cache *c, const CacheShape &
         st = dp == 64 ? launch_cache_large<T, 64>(c, large, L.large_cap, s) : launch_cache_large<T, 128>(c, large, L.large_cap, s);
         if (st != DYBIT_OK) return st;
     }
-    st = dp == 64 ? launch_cache_small<T, 64>(mk, mv, small, L.small_cap, s) : launch_cache_small<T, 128>(mk, mv, small, L.small_cap, s);
+    const bool few = shape.small_rows == 8;
+    if (dp == 64) st = few ? launch_cache_small<T, 64, 1>(mk, mv, small, L.small_cap, s) : launch_cache_small<T, 64, 2>(mk, mv, small, L.small_cap, s);
+    else st = few ? launch_cache_small<T, 128, 1>(mk, mv, small, L.small_cap, s) : launch_cache_small<T, 128, 2>(mk, mv, small, L.small_cap, s);
     if (st != DYBIT_OK) return st;
     // a sequence of at most one part's least length is never cut
     if (L.large_comb_cap > 0 && most > kLargeLeast * kLargeUnit) {
-        launch_k(cache_join_kernel<T, kLargeRows>, dim3((unsigned)(L.large_comb_cap * p.heads), kLargeRows / 16), dim3(128), 0, s, large);
+        launch_k(cache_join_kernel<T, kLargeRows>, dim3((unsigned)(L.large_comb_cap * p.heads), kLargeRows / kSmallRows), dim3(128), 0, s, large);
         st = launch_status();
         if (st != DYBIT_OK) return st;
     }
     if (most > kSmallLeast * kSmallUnit) {
-        launch_k(cache_join_kernel<T, kSmallRows>, dim3((unsigned)(L.small_comb_cap * p.heads)), dim3(128), 0, s, small);
+        const dim3 grid((unsigned)(L.small_comb_cap * p.heads));
+        if (few) launch_k(cache_join_kernel<T, 8>, grid, dim3(128), 0, s, small);
+        else launch_k(cache_join_kernel<T, kSmallRows>, grid, dim3(128), 0, s, small);
         st = launch_status();
     }
     return st;

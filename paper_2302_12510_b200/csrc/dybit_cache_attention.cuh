@@ -3,7 +3,7 @@
 //     x[i][j] = scale * q_i . k_j  (keys j that row i sees),   y_i = sum_j softmax_j(x[i]) v_j,   k_j = s_K(page) * value(code)
 //
 // Rows are (new token, query head) pairs of one key head: the heads of a group share every key that is fetched.  Two
-// kernels: this one for tiles of up to 16 rows, bound by the one pass over the codes, and dybit_cache_prefill.cuh for
+// kernels: this one for tiles of 8 or 16 rows, bound by the one pass over the codes, and dybit_cache_prefill.cuh for
 // tiles of 256 rows, bound by the tensor cores.
 //
 // What both have in common.  The running maximum of a row goes over x + log2 of the values' scale (base 2), so
@@ -64,17 +64,25 @@ template <typename T> __device__ __forceinline__ unsigned decode_pair(unsigned w
 template <> __device__ __forceinline__ unsigned decode_pair<__nv_bfloat16>(unsigned w) { return decode2<true>(w); }
 template <> __device__ __forceinline__ unsigned decode_pair<__half>(unsigned w) { return decode2_f16(w); }
 
+// d (16 x 8, fp32) += a (16 x 16) * b (16 x 8) on the legacy tensor path: sixteen rows of codes against eight queries.
 template <typename T>
-__device__ __forceinline__ void mma_16816(float (&d)[4], const unsigned (&a)[4], unsigned b0, unsigned b1) {
+__device__ __forceinline__ void mma_16816(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, const unsigned (&b)[2]) {
     if constexpr (__is_same(T, __half)) {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
     } else {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
     }
+}
+
+// An 8 x 8 matrix of 16-bit elements, two to a lane, with rows and columns exchanged.
+__device__ __forceinline__ unsigned transpose8(unsigned a) {
+    unsigned d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
 }
 
 // Row r of a sequence: its token's position, and which keys [lo, hi) it sees.  Rows that are not there see none.
@@ -120,7 +128,7 @@ __device__ __forceinline__ void store_attention_row(const CacheAttn &p, const Ca
         p.lse[(int64_t)(tile.row + token) * (p.heads * p.group) + h] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
-// ------------------------------------------------------------------ tiles of 16 rows
+// ------------------------------------------------------------------ tiles of 8 or 16 rows
 
 constexpr int kSmThreads = 128, kSmWarps = 4;
 constexpr int kSmKeys = 32;                  // keys of a stage: two boxes of 16
@@ -134,21 +142,24 @@ template <int DP> __host__ __device__ constexpr int small_smem_bytes() { return 
 struct KeyBlock { float c, e, f; int z, zv; };   // x's factor, values' exponent, 2^-e; coordinates page * heads + head of keys and values
 
 // Four warps share a part's keys, 32 at a time each, with a ring of their own that the TMA fills; they meet at the end.
-// A stage is read straight into the fragments of mma.sync: the contraction over head elements and the one over keys may
-// run in any order, so a lane takes 16 consecutive codes of its key, and the keys of a block are ordered so that the
-// swizzled reads of a quarter warp hit different banks (key_row).  Bound by HBM, then by instruction issue: a pair of
-// codes takes 7 instructions and there is little else.
-template <typename T, int DP>
+// Both products have the codes as their left operand, sixteen rows of them, and 8 * NQ query rows as their right one:
+//     S^T = K Q^T (keys x rows),   Y^T += V^T P^T (head elements x rows)
+// so that an instruction takes twice the codes that it would with the queries on the left.  A stage is read straight into
+// the fragments: contractions over head elements and over keys may run in any order, so a lane takes 16 consecutive codes of
+// its key, and the keys of a block are ordered so that the swizzled reads of a quarter warp hit different banks (key_row).
+// Bound by HBM, then by instruction issue: a pair of codes takes 7 instructions and there is little else.
+template <typename T, int DP, int NQ>
 __global__ void __launch_bounds__(kSmThreads, 3)
 cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const CacheAttn p) {
     constexpr int KS = DP / 16;                            // matrix instructions along a head
-    constexpr int X = DP / 8;                              // head elements of a lane's value column, and n-tiles of the output
+    constexpr int X = DP / 8;                              // head elements of a lane's value column
+    constexpr int ROWS = 8 * NQ;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ KeyBlock s_block[kSmSegment / 16];
     __shared__ uint64_t s_full[kSmWarps][kSmStages];
     __shared__ uint32_t s_abort;
-    __shared__ float s_m[kSmWarps][16], s_l[kSmWarps][16];
+    __shared__ float s_m[kSmWarps][ROWS], s_l[kSmWarps][ROWS];
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int item = (int)(blockIdx.x / (unsigned)p.heads), head = (int)(blockIdx.x - (unsigned)item * (unsigned)p.heads);
@@ -163,41 +174,40 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     pdl_enter();
     if (item >= p.plan[1]) return;
     const CacheTile tile = p.tiles[item];
-    const int r0 = tile.tile * kSmallRows, rows = min(kSmallRows, tile.n * p.group - r0);
-    const KeyRange range = tile_keys(p, tile, r0, kSmallRows, kSmKeys);
+    const int r0 = tile.tile * ROWS, rows = min(ROWS, tile.n * p.group - r0);
+    const KeyRange range = tile_keys(p, tile, r0, ROWS, kSmKeys);
     const int *table = p.table + tile.seq * p.table_stride;
-    const RowKeys k0 = row_keys(p, tile, r0 + g), k1 = row_keys(p, tile, r0 + g + 8);
+    // this lane's scores are those of rows 8 * q + 2t and 8 * q + 2t + 1
+    RowKeys seen[NQ][2];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) seen[q][h] = row_keys(p, tile, r0 + 8 * q + 2 * t + h);
     // keys between these two are seen by every row that is there
     const int all_lo = row_keys(p, tile, r0 + rows - 1).lo, all_hi = row_keys(p, tile, r0).hi;
 
-    // queries as fragments: k index 2t, 2t+1 (8+2t, 8+2t+1) of step j is element 16 * (t + 4 * (j / 4)) + 4 * (j % 4) + 0, 1 (2, 3)
-    unsigned qf[KS][4];
-    {
-        const int ra = r0 + g, rb = ra + 8;
-        auto row_at = [&](int r) {
-            const int token = r / p.group, h = head * p.group + (r - token * p.group);
-            return static_cast<const T *>(p.q) + (tile.row + token) * p.q_token + h * p.q_head;
-        };
-        const T *qa = g < rows ? row_at(ra) : nullptr, *qb = g + 8 < rows ? row_at(rb) : nullptr;
-        auto four = [&](const T *q, int d) {
-            uint2 v = make_uint2(0u, 0u);
-            if (q != nullptr && d < p.dim) {
-                if (p.q_vec) {
-                    v = __ldg(reinterpret_cast<const uint2 *>(q + d));
-                } else {
-                    T e[4];
+    // queries as right-hand fragments: row 8 * q + g; k index 2t, 2t+1 (8+2t, 8+2t+1) of step j is head element
+    // 16 * (t + 4 * (j / 4)) + 4 * (j % 4) + 0, 1 (2, 3)
+    unsigned qf[NQ][KS][2];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) e[i] = q[d + i];
-                    memcpy(&v, e, 8);
-                }
-            }
-            return v;
-        };
+    for (int q = 0; q < NQ; ++q) {
+        const int r = r0 + 8 * q + g, token = r / p.group, h = head * p.group + (r - token * p.group);
+        const T *at = 8 * q + g < rows ? static_cast<const T *>(p.q) + (tile.row + token) * p.q_token + h * p.q_head : nullptr;
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
             const int d = 16 * (t + 4 * (j / 4)) + 4 * (j % 4);
-            const uint2 a = four(qa, d), b = four(qb, d);
-            qf[j][0] = a.x, qf[j][1] = b.x, qf[j][2] = a.y, qf[j][3] = b.y;
+            uint2 v = make_uint2(0u, 0u);
+            if (at != nullptr && d < p.dim) {
+                if (p.q_vec) {
+                    v = __ldg(reinterpret_cast<const uint2 *>(at + d));
+                } else {
+                    T e[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) e[i] = at[d + i];
+                    memcpy(&v, e, 8);
+                }
+            }
+            qf[q][j][0] = v.x, qf[q][j][1] = v.y;
         }
     }
 
@@ -210,12 +220,17 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     }
 
     uint8_t *ring = smem + warp * (kSmStages * small_stage_bytes<DP>());
-    float o[X][4];
+    // output i: head elements X * g + 2i (o[0], o[1]) and X * g + 2i + 1 (o[2], o[3]) of rows 8q + 2t and 8q + 2t + 1
+    float o[NQ][X / 2][4], m[NQ][2], l[NQ][2];
 #pragma unroll
-    for (int i = 0; i < X; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
-    // n index g of a block of eight keys is key key_row(g): two neighbours lie four (DP 64: an odd number of) rows apart and
-    // the rows of the even ones differ above their lowest bit, which makes both kinds of reads free of bank conflicts
+    for (int q = 0; q < NQ; ++q) {
+#pragma unroll
+        for (int i = 0; i < X / 2; ++i) o[q][i][0] = o[q][i][1] = o[q][i][2] = o[q][i][3] = 0.0f;
+        m[q][0] = m[q][1] = -INFINITY;
+        l[q][0] = l[q][1] = 0.0f;
+    }
+    // row i of a group of eight keys is key key_row(i): two neighbours lie four (DP 64: an odd number of) rows apart and the rows
+    // of the even ones differ above their lowest bit, which makes both kinds of reads free of bank conflicts
     auto key_row = [](int i) {
         if constexpr (DP == 128) {
             const int h = i >> 1;
@@ -271,116 +286,123 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             ok = __all_sync(0xffffffffu, wait_bounded(&s_full[warp][stage], (it / kSmStages) & 1u, &s_abort, 0x81));
             if (!ok) break;
             const uint8_t *ks = ring + stage * small_stage_bytes<DP>(), *vs = ks + kSmKeys * DP;
-            const KeyBlock b0 = s_block[2 * i], b1 = s_block[2 * i + 1];
-            float x[4][4];
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const int row = n * 8 + kr;
-                uint4 w[DP / 64];
-                if constexpr (DP == 128) {
-                    w[0] = *reinterpret_cast<const uint4 *>(ks + row * 128 + ((t ^ (row & 7)) << 4));
-                    w[1] = *reinterpret_cast<const uint4 *>(ks + row * 128 + (((t + 4) ^ (row & 7)) << 4));
-                } else {
-                    w[0] = *reinterpret_cast<const uint4 *>(ks + row * 64 + ((t ^ ((row >> 1) & 3)) << 4));
-                }
-                x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.0f;
-#pragma unroll
-                for (int j = 0; j < KS; ++j) {
-                    const uint4 &q4 = w[j / 4];
-                    const unsigned c = j % 4 == 0 ? q4.x : j % 4 == 1 ? q4.y : j % 4 == 2 ? q4.z : q4.w;
-                    mma_16816<T>(x[n], qf[j], decode_pair<T>(__byte_perm(c, 0u, 0x1100)), decode_pair<T>(__byte_perm(c, 0u, 0x3322)));
-                }
-            }
-            // x[n][0], x[n][1]: row g, keys key_row(2t), key_row(2t + 1) of block n; x[n][2], x[n][3]: row g + 8
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const float c = n < 2 ? b0.c : b1.c, e = n < 2 ? b0.e : b1.e;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) x[n][k] = __fmaf_rn(x[n][k], c, e);
-            }
-            const int first = seg + kSmKeys * i;
-            if (first < all_lo || first + kSmKeys > all_hi) {
-#pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const int ka = first + n * 8 + kv0, kb = first + n * 8 + kv1;
-                    if (ka < k0.lo || ka >= k0.hi) x[n][0] = -INFINITY;
-                    if (kb < k0.lo || kb >= k0.hi) x[n][1] = -INFINITY;
-                    if (ka < k1.lo || ka >= k1.hi) x[n][2] = -INFINITY;
-                    if (kb < k1.lo || kb >= k1.hi) x[n][3] = -INFINITY;
-                }
-            }
-            float a0 = x[0][0], a1 = x[0][2];
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                a0 = fmaxf(a0, fmaxf(x[n][0], x[n][1]));
-                a1 = fmaxf(a1, fmaxf(x[n][2], x[n][3]));
-            }
-#pragma unroll
-            for (int d = 1; d < 4; d <<= 1) {
-                a0 = fmaxf(a0, __shfl_xor_sync(0xffffffffu, a0, d));
-                a1 = fmaxf(a1, __shfl_xor_sync(0xffffffffu, a1, d));
-            }
-            if (__any_sync(0xffffffffu, a0 > m0 + kRaise || a1 > m1 + kRaise)) {
-                const float n0 = fmaxf(m0, a0), n1 = fmaxf(m1, a1);
-                const float f0 = m0 == n0 ? 1.0f : ex2(m0 - n0), f1 = m1 == n1 ? 1.0f : ex2(m1 - n1);
-                m0 = n0, m1 = n1;
-                l0 *= f0, l1 *= f1;
-#pragma unroll
-                for (int d = 0; d < X; ++d) o[d][0] *= f0, o[d][1] *= f0, o[d][2] *= f1, o[d][3] *= f1;
-            }
-            const float u0 = m0 == -INFINITY ? 0.0f : m0, u1 = m1 == -INFINITY ? 0.0f : m1;
+            // x[b][q][0], [1]: key key_row(g) of block b, rows 8q + 2t and 8q + 2t + 1; [2], [3]: key 8 + key_row(g)
+            float x[2][NQ][4];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                unsigned pf[4];
-                float s0 = 0.0f, s1 = 0.0f;
+                uint4 w[2][DP / 64];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float(&v)[4] = x[2 * b + h];
-                    v[0] = ex2(v[0] - u0), v[1] = ex2(v[1] - u0), v[2] = ex2(v[2] - u1), v[3] = ex2(v[3] - u1);
-                    s0 += v[0] + v[1];
-                    s1 += v[2] + v[3];
-                    pf[2 * h] = pack_f16(v[0], v[1]);
-                    pf[2 * h + 1] = pack_f16(v[2], v[3]);
+                    const int row = b * 16 + h * 8 + kr;
+                    if constexpr (DP == 128) {
+                        w[h][0] = *reinterpret_cast<const uint4 *>(ks + row * 128 + ((t ^ (row & 7)) << 4));
+                        w[h][1] = *reinterpret_cast<const uint4 *>(ks + row * 128 + (((t + 4) ^ (row & 7)) << 4));
+                    } else {
+                        w[h][0] = *reinterpret_cast<const uint4 *>(ks + row * 64 + ((t ^ ((row >> 1) & 3)) << 4));
+                    }
                 }
-                const float f = b == 0 ? b0.f : b1.f;
-                l0 = __fmaf_rn(s0, f, l0), l1 = __fmaf_rn(s1, f, l1);
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) x[b][q][0] = x[b][q][1] = x[b][q][2] = x[b][q][3] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < KS; ++j) {
+                    unsigned c[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint4 &q4 = w[h][j / 4];
+                        c[h] = j % 4 == 0 ? q4.x : j % 4 == 1 ? q4.y : j % 4 == 2 ? q4.z : q4.w;
+                    }
+                    const unsigned a0 = decode_pair<T>(__byte_perm(c[0], 0u, 0x1100)), a1 = decode_pair<T>(__byte_perm(c[1], 0u, 0x1100)),
+                                   a2 = decode_pair<T>(__byte_perm(c[0], 0u, 0x3322)), a3 = decode_pair<T>(__byte_perm(c[1], 0u, 0x3322));
+#pragma unroll
+                    for (int q = 0; q < NQ; ++q) mma_16816<T>(x[b][q], a0, a1, a2, a3, qf[q][j]);
+                }
+            }
+            const int first = seg + kSmKeys * i;
+            const bool edge = first < all_lo || first + kSmKeys > all_hi;
+            float f[2];
+            float top[NQ][2];
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) top[q][0] = top[q][1] = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const KeyBlock kb = s_block[2 * i + b];
+                f[b] = kb.f;
+#pragma unroll
+                for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[b][q][k] = __fmaf_rn(x[b][q][k], kb.c, kb.e);
+                if (edge) {
+                    const int ka = first + b * 16 + kr;
+#pragma unroll
+                    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int key = ka + (k >> 1) * 8;
+                            if (key < seen[q][k & 1].lo || key >= seen[q][k & 1].hi) x[b][q][k] = -INFINITY;
+                        }
+                }
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) {
+                    top[q][0] = fmaxf(top[q][0], fmaxf(x[b][q][0], x[b][q][2]));
+                    top[q][1] = fmaxf(top[q][1], fmaxf(x[b][q][1], x[b][q][3]));
+                }
+            }
+            bool raise = false;
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) raise |= top[q][0] > m[q][0] + kRaise || top[q][1] > m[q][1] + kRaise;
+            if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+                for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {          // the row's maximum over the eight lanes that share it
+                        float a = top[q][h];
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
+                        const float n = fmaxf(m[q][h], a), s = m[q][h] == n ? 1.0f : ex2(m[q][h] - n);
+                        m[q][h] = n;
+                        l[q][h] *= s;
+#pragma unroll
+                        for (int d = 0; d < X / 2; ++d) o[q][d][h] *= s, o[q][d][2 + h] *= s;
+                    }
+            }
+            unsigned pf[2][NQ][2];
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) {
+                const float u0 = m[q][0] == -INFINITY ? 0.0f : m[q][0], u1 = m[q][1] == -INFINITY ? 0.0f : m[q][1];
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    float(&v)[4] = x[b][q];
+                    v[0] = ex2(v[0] - u0), v[1] = ex2(v[1] - u1), v[2] = ex2(v[2] - u0), v[3] = ex2(v[3] - u1);
+                    l[q][0] = __fmaf_rn(v[0] + v[2], f[b], l[q][0]);
+                    l[q][1] = __fmaf_rn(v[1] + v[3], f[b], l[q][1]);
+                    // keys x rows -> rows x keys
+                    pf[b][q][0] = transpose8(pack_f16(v[0], v[1]));
+                    pf[b][q][1] = transpose8(pack_f16(v[2], v[3]));
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
                 const int ra = b * 16 + kv0, rb = b * 16 + kv1;
-                if constexpr (DP == 128) {
-                    uint4 v[4];
+                unsigned v[4][DP / 32];                    // rows of keys 2t, 2t + 1, 8 + 2t, 8 + 2t + 1
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int row = (k & 1 ? rb : ra) + (k >> 1) * 8;
-                        v[k] = *reinterpret_cast<const uint4 *>(vs + row * 128 + ((g ^ (row & 7)) << 4));
+                for (int k = 0; k < 4; ++k) {
+                    const int row = (k & 1 ? rb : ra) + (k >> 1) * 8;
+                    if constexpr (DP == 128) {
+                        const uint4 c = *reinterpret_cast<const uint4 *>(vs + row * 128 + ((g ^ (row & 7)) << 4));
+                        v[k][0] = c.x, v[k][1] = c.y, v[k][2] = c.z, v[k][3] = c.w;
+                    } else {
+                        const uint2 c = *reinterpret_cast<const uint2 *>(vs + row * 64 + (((g >> 1) ^ ((row >> 1) & 3)) << 4) + (g & 1) * 8);
+                        v[k][0] = c.x, v[k][1] = c.y;
                     }
+                }
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        unsigned c[4];
+                for (int i2 = 0; i2 < X / 2; ++i2) {
+                    const int w = i2 / 2;
+                    const unsigned s0 = 0x4400u + 0x1111u * (2 * (i2 & 1)), s1 = s0 + 0x1111u;
+                    const unsigned a0 = decode2_f16(__byte_perm(v[0][w], v[1][w], s0)), a1 = decode2_f16(__byte_perm(v[0][w], v[1][w], s1)),
+                                   a2 = decode2_f16(__byte_perm(v[2][w], v[3][w], s0)), a3 = decode2_f16(__byte_perm(v[2][w], v[3][w], s1));
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) c[k] = w == 0 ? v[k].x : w == 1 ? v[k].y : w == 2 ? v[k].z : v[k].w;
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            const unsigned sel = 0x4400u + 0x1111u * y;
-                            mma_16816<__half>(o[4 * w + y], pf, decode2_f16(__byte_perm(c[0], c[1], sel)), decode2_f16(__byte_perm(c[2], c[3], sel)));
-                        }
-                    }
-                } else {
-                    uint2 v[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int row = (k & 1 ? rb : ra) + (k >> 1) * 8;
-                        v[k] = *reinterpret_cast<const uint2 *>(vs + row * 64 + (((g >> 1) ^ ((row >> 1) & 3)) << 4) + (g & 1) * 8);
-                    }
-#pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        unsigned c[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) c[k] = w == 0 ? v[k].x : v[k].y;
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            const unsigned sel = 0x4400u + 0x1111u * y;
-                            mma_16816<__half>(o[4 * w + y], pf, decode2_f16(__byte_perm(c[0], c[1], sel)), decode2_f16(__byte_perm(c[2], c[3], sel)));
-                        }
-                    }
+                    for (int q = 0; q < NQ; ++q) mma_16816<__half>(o[q][i2], a0, a1, a2, a3, pf[b][q]);
                 }
             }
             __syncwarp();
@@ -393,56 +415,57 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 
     // the four warps' parts: maxima first, then the sums at the common maximum
 #pragma unroll
-    for (int d = 1; d < 4; d <<= 1) {
-        l0 += __shfl_xor_sync(0xffffffffu, l0, d);
-        l1 += __shfl_xor_sync(0xffffffffu, l1, d);
-    }
-    if (t == 0) {
-        s_m[warp][g] = m0, s_m[warp][g + 8] = m1;
-        s_l[warp][g] = l0, s_l[warp][g + 8] = l1;
-    }
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) l[q][h] += __shfl_xor_sync(0xffffffffu, l[q][h], d);
+            if (g == 0) {
+                s_m[warp][8 * q + 2 * t + h] = m[q][h];
+                s_l[warp][8 * q + 2 * t + h] = l[q][h];
+            }
+        }
     __syncthreads();
     auto common = [&](int r) {
-        float m = s_m[0][r];
+        float v = s_m[0][r];
 #pragma unroll
-        for (int w = 1; w < kSmWarps; ++w) m = fmaxf(m, s_m[w][r]);
-        return m;
+        for (int w = 1; w < kSmWarps; ++w) v = fmaxf(v, s_m[w][r]);
+        return v;
     };
     constexpr int LD = DP + 4;
-    float *sum = reinterpret_cast<float *>(smem) + warp * 8 * LD;
+    float *const all = reinterpret_cast<float *>(smem);
     const int vecs = p.dim / 4;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {                 // rows 0 .. 7, then 8 .. 15: the ring holds one half of four warps
-        if (half * 8 >= rows) break;
-        const float m = common(g + 8 * half), mine = half == 0 ? m0 : m1;
-        const float f = mine == -INFINITY ? 0.0f : ex2(mine - m);
-        if (half == 1) __syncthreads();
+    for (int q = 0; q < NQ; ++q) {                         // eight rows at a time: the ring holds those of four warps
+        if (q * 8 >= rows) break;
+        if (q > 0) __syncthreads();
 #pragma unroll
-        for (int i = 0; i < X; i += 4) {
-            *reinterpret_cast<float4 *>(sum + g * LD + 2 * t * X + i) =
-                make_float4(o[i][2 * half] * f, o[i + 1][2 * half] * f, o[i + 2][2 * half] * f, o[i + 3][2 * half] * f);
-            *reinterpret_cast<float4 *>(sum + g * LD + (2 * t + 1) * X + i) =
-                make_float4(o[i][2 * half + 1] * f, o[i + 1][2 * half + 1] * f, o[i + 2][2 * half + 1] * f, o[i + 3][2 * half + 1] * f);
+        for (int h = 0; h < 2; ++h) {
+            const float top = common(8 * q + 2 * t + h), f = m[q][h] == -INFINITY ? 0.0f : ex2(m[q][h] - top);
+            float *row = all + (warp * 8 + 2 * t + h) * LD + g * X;
+#pragma unroll
+            for (int i = 0; i < X / 2; i += 2)
+                *reinterpret_cast<float4 *>(row + 2 * i) = make_float4(o[q][i][h] * f, o[q][i][2 + h] * f, o[q][i + 1][h] * f, o[q][i + 1][2 + h] * f);
         }
         __syncthreads();
         for (int i = threadIdx.x; i < 8 * vecs; i += kSmThreads) {
-            const int lr = i / vecs, d = (i - lr * vecs) * 4, r = half * 8 + lr;
+            const int lr = i / vecs, d = (i - lr * vecs) * 4, r = q * 8 + lr;
             if (r >= rows) break;
             float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-            float l = 0.0f;
-            const float mr = common(r);
+            float sum = 0.0f;
+            const float top = common(r);
 #pragma unroll
             for (int w = 0; w < kSmWarps; ++w) {
-                const float4 v = *reinterpret_cast<const float4 *>(reinterpret_cast<float *>(smem) + (w * 8 + lr) * LD + d);
+                const float4 v = *reinterpret_cast<const float4 *>(all + (w * 8 + lr) * LD + d);
                 s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-                l += s_m[w][r] == -INFINITY ? s_l[w][r] : s_l[w][r] * ex2(s_m[w][r] - mr);
+                sum += s_m[w][r] == -INFINITY ? s_l[w][r] : s_l[w][r] * ex2(s_m[w][r] - top);
             }
             if (tile.splits > 1) {
-                const int64_t at = ((int64_t)tile.slot * p.heads + head) * kSmallRows + r;
+                const int64_t at = ((int64_t)tile.slot * p.heads + head) * ROWS + r;
                 *reinterpret_cast<float4 *>(p.part_y + at * p.dim + d) = s;
-                if (d == 0) p.part_ml[at] = make_float4(mr + e0, l, e0, 0.0f);
+                if (d == 0) p.part_ml[at] = make_float4(top + e0, sum, e0, 0.0f);
             } else {
-                store_attention_row<T>(p, tile, head, r0 + r, d, s, l, mr, e0);
+                store_attention_row<T>(p, tile, head, r0 + r, d, s, sum, top, e0);
             }
         }
     }
@@ -450,17 +473,17 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 
 // ------------------------------------------------------------------ parts of a tile, joined
 
-// Sixteen rows of a tile and one key head: the parts at their common maximum.  part_ml.x is a part's maximum with its
+// Up to sixteen rows of a tile and one key head: the parts at their common maximum.  part_ml.x is a part's maximum with its
 // exponent in it, so that parts whose values have other scales compare.
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(128) cache_join_kernel(const CacheAttn p) {
     pdl_enter();
     const int item = (int)(blockIdx.x / (unsigned)p.heads), head = (int)(blockIdx.x - (unsigned)item * (unsigned)p.heads);
-    if (item >= p.plan[ROWS == kSmallRows ? 3 : 4]) return;
+    if (item >= p.plan[ROWS == kLargeRows ? 4 : 3]) return;
     const CacheTile tile = p.comb[item];
-    const int r0 = blockIdx.y * 16, rows = min(ROWS, tile.n * p.group - tile.tile * ROWS), vecs = p.dim / 4;
+    const int r0 = blockIdx.y * kSmallRows, rows = min(ROWS, tile.n * p.group - tile.tile * ROWS), vecs = p.dim / 4;
     const int64_t step = (int64_t)p.heads * ROWS;
-    for (int i = threadIdx.x; i < 16 * vecs; i += 128) {
+    for (int i = threadIdx.x; i < kSmallRows * vecs; i += 128) {
         const int r = r0 + i / vecs, d = (i - i / vecs * vecs) * 4;
         if (r >= rows) break;
         const int64_t at = ((int64_t)tile.slot * p.heads + head) * ROWS + r;
