@@ -550,7 +550,9 @@ typedef struct {
  *           first rows lie in front of position 0: they are not written, read as zeros and see no key
  *   max_new no sequence has more new tokens (what is beyond is left out); at most `tokens`
  *   q_heads query heads of the attention, a multiple of cache.heads, up to 128 to a key head
- *   table   [dev] sequences rows of max_pages entries, row stride table_stride */
+ *   table   [dev] sequences rows of max_pages entries, row stride table_stride
+ *   causal, window  how the attention calls will mask: what the plan deals their work out by.  A call that masks otherwise
+ *           first deals it out again, in one more launch */
 typedef struct {
     int sequences;
     int64_t tokens;
@@ -558,10 +560,10 @@ typedef struct {
     const int32_t *table;
     int64_t table_stride;
     int max_pages;
+    int causal, window;
 } dybit_cache_batch;
 
-/* Lists of the work of a batch: which pages its new tokens go to, the tiles of its queries, and how the keys of long
- * sequences are cut.  Made once for a batch; every layer's calls with the same batch go by it, on caches of the same
+/* Lists of the work of a batch: which pages its new tokens go to, the tiles of its queries, and how their work is dealt out.  Made once for a batch; every layer's calls with the same batch go by it, on caches of the same
  * pages' size and heads, several calls at once if wanted (they only read it).
  *   starts, lengths  [dev] int32
  *   plan    [dev] dybit_cache_plan_bytes(...) bytes, 16-byte aligned, overwritten.  0 bytes: the arguments are refused */

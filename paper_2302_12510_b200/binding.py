@@ -68,7 +68,7 @@ class _CCache(C.Structure):
 
 class _CCacheBatch(C.Structure):
     _fields_ = [("sequences", C.c_int), ("tokens", C.c_int64), ("max_new", C.c_int), ("q_heads", C.c_int), ("table", C.c_void_p),
-                ("table_stride", C.c_int64), ("max_pages", C.c_int)]
+                ("table_stride", C.c_int64), ("max_pages", C.c_int), ("causal", C.c_int), ("window", C.c_int)]
 
 
 class ConvDesc(NamedTuple):
@@ -985,12 +985,13 @@ def _cache_ints(t: torch.Tensor, name: str, n: int):
         raise ValueError(f"{name} must be a contiguous int32 CUDA tensor of {n} entries")
 
 
-def _cache_batch(cache: KVCache, table: torch.Tensor, tokens: int, q_heads: Optional[int], max_new: Optional[int]) -> _CCacheBatch:
+def _cache_batch(cache: KVCache, table: torch.Tensor, tokens: int, q_heads: Optional[int], max_new: Optional[int], causal: bool = True,
+                 window: int = 0) -> _CCacheBatch:
     if not (table.dtype == torch.int32 and table.is_cuda and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] <= 1)):
         raise ValueError("table must be a 2-D int32 CUDA tensor [sequences][pages] with unit inner stride")
     B, most = table.shape
     return _CCacheBatch(B, int(tokens), int(tokens if max_new is None else min(max_new, tokens)), cache.heads if q_heads is None else int(q_heads),
-                        table.data_ptr(), max(table.stride(0), most) if B > 1 else most, most)
+                        table.data_ptr(), max(table.stride(0), most) if B > 1 else most, most, int(bool(causal)), int(window))
 
 
 def dybit_cache_plan_bytes(cache: KVCache, table: torch.Tensor, tokens: int, q_heads: Optional[int] = None, max_new: Optional[int] = None) -> int:
@@ -998,9 +999,10 @@ def dybit_cache_plan_bytes(cache: KVCache, table: torch.Tensor, tokens: int, q_h
 
 
 def dybit_cache_plan(cache: KVCache, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, tokens: int, q_heads: Optional[int] = None,
-                     max_new: Optional[int] = None, plan: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+                     max_new: Optional[int] = None, causal: bool = True, window: int = 0, plan: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
     """Lists of the work of a batch (see CachePlan).  Returns the plan's buffer (uint8)."""
-    batch = _cache_batch(cache, table, tokens, q_heads, max_new)
+    batch = _cache_batch(cache, table, tokens, q_heads, max_new, causal, window)
     _cache_ints(starts, "starts", batch.sequences + 1)
     _cache_ints(lengths, "lengths", batch.sequences)
     need = int(lib.dybit_cache_plan_bytes(cache.ref, C.byref(batch)))
@@ -1017,15 +1019,16 @@ class CachePlan:
     """The plan of one batch of sequences, for every call on caches of the same pages' size and heads: table int32
     [sequences][pages] with the page of every `page` tokens, starts int32 [sequences + 1] with the rows of each sequence's
     new tokens among the batch's `tokens` rows, lengths int32 [sequences] with the tokens of each sequence, new ones
-    included.  max_new bounds the new tokens of one sequence (default: tokens); the smaller, the less is launched.  The
-    plan and its table have to outlive the calls that use them."""
+    included.  max_new bounds the new tokens of one sequence (default: tokens); the smaller, the less is launched.  causal and
+    window say how the attention will mask; a call that masks otherwise takes one more launch.  The plan and its table have to
+    outlive the calls that use them."""
 
     def __init__(self, cache: KVCache, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, tokens: int, q_heads: Optional[int] = None,
-                 max_new: Optional[int] = None, buffer: Optional[torch.Tensor] = None, stream=None):
+                 max_new: Optional[int] = None, causal: bool = True, window: int = 0, buffer: Optional[torch.Tensor] = None, stream=None):
         self.table, self.T = table, int(tokens)
-        self.batch = _cache_batch(cache, table, tokens, q_heads, max_new)
+        self.batch = _cache_batch(cache, table, tokens, q_heads, max_new, causal, window)
         self.q_heads, self.page, self.heads = self.batch.q_heads, cache.page, cache.heads
-        self.buffer = dybit_cache_plan(cache, table, starts, lengths, tokens, q_heads, max_new, buffer, stream)
+        self.buffer = dybit_cache_plan(cache, table, starts, lengths, tokens, q_heads, max_new, causal, window, buffer, stream)
         self.address, self.ref = self.buffer.data_ptr(), C.byref(self.batch)
         self._ws_bytes = {}
 

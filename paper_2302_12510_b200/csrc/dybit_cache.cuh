@@ -20,16 +20,18 @@ constexpr int kCachePlanThreads = 1024;
 constexpr int kSmallRows = 16;               // query rows (token x query head of one key head) of a small tile at most; half of them
                                              // where no sequence of the batch has more
 constexpr int kLargeRows = 256;              // rows of a large tile: two accumulators of 128
-constexpr int kSmallUnit = 64, kLargeUnit = 128;     // keys in which a split of the key axis is counted
-// CTAs that the key axis is cut for.  Counted as the B200 has them, not asked of the device: the sizes of plans and
-// workspaces depend on them and are the same wherever they are asked for.
-constexpr int kSmallTarget = 148 * 3 * 2, kLargeTarget = 148;
-constexpr int kSmallLeast = 4, kLargeLeast = 8;      // units that a split has at least
+constexpr int kSmallUnit = 64, kLargeUnit = 128;     // keys that work is counted in
+// Blocks that the work of small and of large tiles is dealt out to: one resident wave.  Counted as the B200 has them, not asked of
+// the device: the sizes of plans and workspaces depend on them and are the same wherever they are asked for.
+constexpr int kSmallBlocks = 148 * 3, kLargeBlocks = 148;
+constexpr int kSmallLeast = 4, kLargeLeast = 4;      // units that a block has at least
 
-// New tokens of one sequence that go to one page (page < 0 for tokens in front of the sequence's first position).
+// New tokens of one sequence that go to one page (pos < 0 for tokens in front of the sequence's first position).
 struct CacheItem { int row, pos, count, seq; };
-// A tile of query rows of one sequence, and one of the parts that its keys are cut into.
-struct CacheTile { int row, n, len, seq, tile, split, splits, slot; };
+// A tile of query rows of one sequence: its number, its work and that of the tiles before it, in units, for each head.
+struct CacheTile { int row, n, len, seq, tile, units; int64_t first; };
+// Where a block starts in the work of all tiles and heads, head by head: `off` units into a tile.
+struct CacheStart { int tile, head, off, pad; };
 // What one thread of the plan kernel knows of a sequence.
 struct CacheSeq { int row, n, len, items, small_tiles, large_tiles; };
 
@@ -38,33 +40,27 @@ struct CacheShape {
     int B, page, heads, group, max_new, max_pages;
     int small_tokens;            // a sequence with more new tokens than this takes large tiles
     int small_rows;              // of a small tile: 8 or kSmallRows
+    int causal, window;          // how the calls mask; window INT_MAX for none
 };
 
 // Word offsets of a plan's parts; the capacities bound what the device fills in.
 struct CachePlanLayout {
-    int64_t items_cap, small_cap, large_cap, small_slots, large_slots, small_comb_cap, large_comb_cap;
-    int64_t items, small, large, small_comb, large_comb, words;
+    int64_t items_cap, small_cap, large_cap;
+    int64_t items, small, large, small_starts, large_starts, words;
     __host__ __device__ static int64_t lesser(int64_t a, int64_t b) { return a < b ? a : b; }
     __host__ __device__ explicit CachePlanLayout(const CacheShape &s) {
         const int64_t T = s.T, B = s.B;
         items_cap = lesser(T, T / s.page + 3 * B);
         // new tokens that small tiles take: all of a sequence of at most small_tokens
         const int64_t few = s.small_tokens >= s.max_new ? T : lesser(T, B * (int64_t)s.small_tokens);
-        const int64_t small_tiles = lesser(few * s.group, few * s.group / s.small_rows + B);
-        const int64_t large_tiles = s.max_new > s.small_tokens ? lesser(T, T * s.group / kLargeRows + B) : 0;
-        const int64_t small_parts = kSmallTarget / s.heads + 1, large_parts = kLargeTarget / s.heads + 1;
-        small_cap = small_tiles + small_parts;
-        large_cap = large_tiles > 0 ? large_tiles + large_parts : 0;
-        small_slots = 2 * small_parts;
-        large_slots = large_tiles > 0 ? 2 * large_parts : 0;
-        small_comb_cap = lesser(small_tiles, small_parts);
-        large_comb_cap = large_tiles > 0 ? lesser(large_tiles, large_parts) : 0;
-        int64_t w = 16;                                  // counts: items, small, large, small_comb, large_comb; the rest spare
+        small_cap = lesser(few * s.group, few * s.group / s.small_rows + B);
+        large_cap = s.max_new > s.small_tokens ? lesser(T, T * s.group / kLargeRows + B) : 0;
+        int64_t w = 16;                                  // counts: items, small and large tiles, blocks for each; the rest spare
         items = w, w += 4 * items_cap;
         small = w, w += 8 * small_cap;
         large = w, w += 8 * large_cap;
-        small_comb = w, w += 8 * small_comb_cap;
-        large_comb = w, w += 8 * large_comb_cap;
+        small_starts = w, w += 4 * (kSmallBlocks + 1);
+        large_starts = w, w += large_cap > 0 ? 4 * (kLargeBlocks + 1) : 0;
         words = w;
     }
 };
@@ -93,19 +89,12 @@ __device__ __forceinline__ CacheSeq cache_seq(const CachePlanArgs &a, int b) {
     return q;
 }
 
-// Units of keys that a sequence's tiles are counted with; one at least, so that a tile without keys has a part that
-// writes its zeros.
-__device__ __forceinline__ int cache_units(int len, int unit) { return max(1, cache_div_up(len, unit)); }
-
-// Sum over the block, the same for all threads.
-__device__ __forceinline__ int64_t cache_block_sum(int64_t v, int64_t *s_warp) {
-    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = v;
-    __syncthreads();
-    int64_t all = 0;
-    for (int w = 0; w < kCachePlanThreads / 32; ++w) all += s_warp[w];
-    return all;
+// Units of work of a tile's rows r0 .. r0 + rows - 1: its keys under the mask that is expected; one at least, so that a tile
+// without keys has a block that writes its zeros.
+__device__ __forceinline__ int cache_units(const CacheShape &s, const CacheSeq &q, int r0, int rows, int unit) {
+    if (!s.causal) return max(1, cache_div_up(q.len, unit));
+    const int p0 = q.len - q.n, lo = max(0, p0 + r0 / s.group + 1 - min(s.window, 0x3fffffff)), hi = p0 + min(q.n - 1, (r0 + rows - 1) / s.group) + 1;
+    return hi <= lo ? 1 : cache_div_up(hi, unit) - lo / unit;
 }
 
 // Exclusive prefix sum over the block; *total receives the sum.
@@ -125,79 +114,116 @@ __device__ __forceinline__ int cache_block_scan(int v, int *s_warp, int *total) 
     return before + sum - v;
 }
 
+// One block.  The work of n tiles, for each head, dealt out evenly: `out` gets the tiles with their work, and with what comes before
+// them, under the shape's mask.  Returns the number of blocks that have some.
+__device__ __forceinline__ int cache_deal(const CacheShape &s, const CacheTile *tiles, CacheTile *out, int n, CacheStart *starts, bool large,
+                                          int *s_scan) {
+    const int rows = large ? kLargeRows : s.small_rows, unit = large ? kLargeUnit : kSmallUnit;
+    int64_t units = 0;
+    for (int i0 = 0; i0 < n; i0 += kCachePlanThreads) {
+        const int i = i0 + threadIdx.x;
+        CacheTile t = {};
+        if (i < n) {
+            t = tiles[i];
+            const CacheSeq q = {t.row, t.n, t.len, 0, 0, 0};
+            t.units = cache_units(s, q, t.tile * rows, rows, unit);
+        }
+        int total;
+        t.first = units + cache_block_scan(t.units, s_scan, &total);
+        if (i < n) out[i] = t;
+        units += total;
+    }
+    __syncthreads();
+    if (n == 0) return 0;
+    const int64_t work = units * s.heads;
+    const int blocks = (int)min((int64_t)(large ? kLargeBlocks : kSmallBlocks), max((int64_t)1, work / (large ? kLargeLeast : kSmallLeast)));
+    for (int c = threadIdx.x; c <= blocks; c += kCachePlanThreads) {
+        const int64_t g = c < blocks ? work / blocks * c + work % blocks * c / blocks : work;
+        const int head = (int)(g / units);
+        const int64_t r = g - (int64_t)head * units;
+        int lo = 0, hi = n - 1;                            // the last tile whose work starts at or before r
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (out[mid].first <= r) lo = mid;
+            else hi = mid - 1;
+        }
+        starts[c] = {lo, head, (int)(r - out[lo].first), 0};
+    }
+    return blocks;
+}
+
+// The plan's work dealt out again for calls that mask otherwise than it expects.  to: counts, tiles and starts as in the plan.
+__global__ void __launch_bounds__(kCachePlanThreads) cache_deal_kernel(const CacheShape s, const int *plan, int *to) {
+    __shared__ int s_scan[kCachePlanThreads / 32];
+    pdl_enter();
+    const CachePlanLayout L(s);
+    const int n = plan[1], m = plan[2];
+    const int a = cache_deal(s, reinterpret_cast<const CacheTile *>(plan + L.small), reinterpret_cast<CacheTile *>(to + L.small), n,
+                             reinterpret_cast<CacheStart *>(to + L.small_starts), false, s_scan);
+    const int b = cache_deal(s, reinterpret_cast<const CacheTile *>(plan + L.large), reinterpret_cast<CacheTile *>(to + L.large), m,
+                             reinterpret_cast<CacheStart *>(to + L.large_starts), true, s_scan);
+    if (threadIdx.x == 0) to[1] = n, to[2] = m, to[3] = a, to[4] = b;
+}
+
 // One block.  The lists' capacities hold for starts that never decrease; entries beyond them (starts that do) are dropped,
-// not written.  Integer work of B sequences: counts, the lengths of the parts, then the lists, a warp to a sequence.
+// not written.  Integer work of B sequences: counts and the lists, a warp to a sequence; then the blocks' starts.
 __global__ void __launch_bounds__(kCachePlanThreads) cache_plan_kernel(const CachePlanArgs a) {
-    __shared__ int64_t s_sum[kCachePlanThreads / 32];
     __shared__ int s_scan[kCachePlanThreads / 32];
     pdl_enter();
     const CachePlanLayout L(a.s);
     const int B = a.s.B, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t small_units = 0, large_units = 0;
-    for (int b = threadIdx.x; b < B; b += kCachePlanThreads) {
-        const CacheSeq q = cache_seq(a, b);
-        small_units += (int64_t)q.small_tiles * cache_units(q.len, kSmallUnit);
-        large_units += (int64_t)q.large_tiles * cache_units(q.len, kLargeUnit);
-    }
-    small_units = cache_block_sum(small_units, s_sum);
-    large_units = cache_block_sum(large_units, s_sum);
-    // units of a part: the whole work over the CTAs that are to have some
-    auto part = [&](int64_t units, int target, int least) {
-        const int64_t parts = target / a.s.heads + 1;
-        return (int)min((int64_t)1 << 30, max((int64_t)least, (units + parts - 1) / parts));
-    };
-    const int small_part = part(small_units, kSmallTarget, kSmallLeast), large_part = part(large_units, kLargeTarget, kLargeLeast);
-    int at[7] = {0, 0, 0, 0, 0, 0, 0};                    // items, small, large, small_comb, large_comb, slots of small and large
+    int at[3] = {0, 0, 0};                                // items, small and large tiles
     for (int b0 = 0; b0 < B; b0 += kCachePlanThreads) {
         const int b = b0 + threadIdx.x;
         CacheSeq q = {};
         if (b < B) q = cache_seq(a, b);
-        const int sp = cache_div_up(cache_units(q.len, kSmallUnit), small_part), lp = cache_div_up(cache_units(q.len, kLargeUnit), large_part);
-        const int count[7] = {q.items, q.small_tiles * sp, q.large_tiles * lp, sp > 1 ? q.small_tiles : 0, lp > 1 ? q.large_tiles : 0,
-                              sp > 1 ? q.small_tiles * sp : 0, lp > 1 ? q.large_tiles * lp : 0};
-        int first[7];
+        const int count[3] = {q.items, q.small_tiles, q.large_tiles};
+        int first[3];
 #pragma unroll
-        for (int c = 0; c < 7; ++c) {
+        for (int c = 0; c < 3; ++c) {
             int total;
             first[c] = at[c] + cache_block_scan(count[c], s_scan, &total);
             at[c] += total;
         }
-        // the lists of these sequences, a warp to a sequence: lane k of the warp has what was counted for sequence k of its own
+        // lane k of a warp has what was counted for sequence k of its own
         for (int k = 0; k < 32; ++k) {
             const int seq = b0 + warp * 32 + k;
             if (seq >= B) break;
             auto of = [&](int v) { return __shfl_sync(0xffffffffu, v, k); };
-            const int row = of(q.row), n = of(q.n), len = of(q.len), items = of(q.items), page = a.s.page;
-            const int outside = max(0, n - len), p0 = len - (n - outside), out_items = cache_div_up(outside, page), i0 = of(first[0]);
+            const CacheSeq m = {of(q.row), of(q.n), of(q.len), of(q.items), of(q.small_tiles), of(q.large_tiles)};
+            const int page = a.s.page, outside = max(0, m.n - m.len), p0 = m.len - (m.n - outside), out_items = cache_div_up(outside, page), i0 = of(first[0]);
             CacheItem *list = reinterpret_cast<CacheItem *>(a.plan + L.items) + i0;
-            for (int i = lane; i < items; i += 32) {
+            for (int i = lane; i < m.items; i += 32) {
                 CacheItem it;
                 if (i < out_items) {
-                    it = {row + i * page, -1, min(page, outside - i * page), seq};
+                    it = {m.row + i * page, -1, min(page, outside - i * page), seq};
                 } else {
-                    const int j = p0 / page + (i - out_items), lo = max(p0, j * page), hi = (int)min((int64_t)len, (int64_t)(j + 1) * page);
-                    it = {row + outside + lo - p0, lo, hi - lo, seq};
+                    const int j = p0 / page + (i - out_items), lo = max(p0, j * page), hi = (int)min((int64_t)m.len, (int64_t)(j + 1) * page);
+                    it = {m.row + outside + lo - p0, lo, hi - lo, seq};
                 }
                 if ((unsigned)(i0 + i) < (uint64_t)L.items_cap) list[i] = it;
             }
-            auto tiles = [&](int64_t list_at, int64_t cap, int64_t comb_at, int64_t comb_cap, int n_tiles, int parts, int t0, int c0, int slot0) {
-                CacheTile *out = reinterpret_cast<CacheTile *>(a.plan + list_at) + t0, *comb = reinterpret_cast<CacheTile *>(a.plan + comb_at) + c0;
-                for (int i = lane; i < n_tiles * parts; i += 32) {
-                    // the last tile sees the most keys under a causal mask: it comes first
-                    const int j = i / parts, split = i - j * parts, slot = parts > 1 ? slot0 + j * parts : -1;
-                    const CacheTile t = {row, n, len, seq, n_tiles - 1 - j, split, parts, slot < 0 ? slot : slot + split};
-                    if ((unsigned)(t0 + i) < (uint64_t)cap) out[i] = t;
-                    if (split == 0 && parts > 1 && (unsigned)(c0 + j) < (uint64_t)comb_cap) comb[j] = t;
-                }
+            auto tiles = [&](int64_t list_at, int64_t cap, int n_tiles, int t0) {
+                CacheTile *out = reinterpret_cast<CacheTile *>(a.plan + list_at) + t0;
+                for (int i = lane; i < n_tiles; i += 32)
+                    if ((unsigned)(t0 + i) < (uint64_t)cap) out[i] = {m.row, m.n, m.len, seq, i, 0, 0};
             };
-            tiles(L.small, L.small_cap, L.small_comb, L.small_comb_cap, of(q.small_tiles), of(sp), of(first[1]), of(first[3]), of(first[5]));
-            tiles(L.large, L.large_cap, L.large_comb, L.large_comb_cap, of(q.large_tiles), of(lp), of(first[2]), of(first[4]), of(first[6]));
+            tiles(L.small, L.small_cap, m.small_tiles, of(first[1]));
+            tiles(L.large, L.large_cap, m.large_tiles, of(first[2]));
         }
     }
-    if (threadIdx.x == 0) {
-        const int64_t caps[5] = {L.items_cap, L.small_cap, L.large_cap, L.small_comb_cap, L.large_comb_cap};
+    const int64_t caps[3] = {L.items_cap, L.small_cap, L.large_cap};
 #pragma unroll
-        for (int c = 0; c < 5; ++c) a.plan[c] = (unsigned)at[c] < (uint64_t)caps[c] ? at[c] : (int)caps[c];
+    for (int c = 0; c < 3; ++c) at[c] = (unsigned)at[c] < (uint64_t)caps[c] ? at[c] : (int)caps[c];
+    __syncthreads();
+    CacheTile *small = reinterpret_cast<CacheTile *>(a.plan + L.small), *large = reinterpret_cast<CacheTile *>(a.plan + L.large);
+    const int small_blocks = cache_deal(a.s, small, small, at[1], reinterpret_cast<CacheStart *>(a.plan + L.small_starts), false, s_scan);
+    const int large_blocks = cache_deal(a.s, large, large, at[2], reinterpret_cast<CacheStart *>(a.plan + L.large_starts), true, s_scan);
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int c = 0; c < 3; ++c) a.plan[c] = at[c];
+        a.plan[3] = small_blocks;
+        a.plan[4] = large_blocks;
     }
 }
 

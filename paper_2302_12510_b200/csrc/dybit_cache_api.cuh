@@ -3,6 +3,8 @@
 
 #include <limits.h>
 
+#include <type_traits>
+
 #include "dybit_cache_prefill.cuh"
 
 namespace dybit {
@@ -27,7 +29,7 @@ static dybit_status check_cache_memory(const dybit_cache *c) {
 
 static dybit_status check_batch(const dybit_cache *c, const dybit_cache_batch *b) {
     if (b == nullptr) return DYBIT_ERR_INVALID_ARG;
-    if (b->sequences < 0 || b->tokens < 0 || b->max_new < 0 || b->q_heads < 1 || b->max_pages < 0 || b->table_stride < b->max_pages) return DYBIT_ERR_INVALID_ARG;
+    if (b->sequences < 0 || b->tokens < 0 || b->max_new < 0 || b->q_heads < 1 || b->max_pages < 0 || b->window < 0 || b->table_stride < b->max_pages) return DYBIT_ERR_INVALID_ARG;
     if (b->q_heads % c->heads != 0) return DYBIT_ERR_INVALID_ARG;
     if (b->q_heads / c->heads > kCacheMaxGroup || b->sequences > (1 << 20) || b->tokens > (1 << 26)) return DYBIT_ERR_UNSUPPORTED;
     if (b->tokens * (int64_t)b->q_heads > (1 << 30) || (int64_t)b->max_pages * c->page > INT_MAX - 256) return DYBIT_ERR_UNSUPPORTED;
@@ -47,6 +49,8 @@ static CacheShape cache_shape(const dybit_cache *c, const dybit_cache_batch *b) 
     s.max_new = (int)std::min<int64_t>(b->max_new, b->tokens);
     s.max_pages = b->max_pages;
     s.small_tokens = std::max(1, kSmallMost / s.group);
+    s.causal = b->causal != 0;
+    s.window = b->window > 0 ? b->window : INT_MAX;
     s.small_rows = (int64_t)s.max_new * s.group <= 8 ? 8 : kSmallRows;
     return s;
 }
@@ -136,36 +140,35 @@ static bool make_cache_map(CUtensorMap *map, const void *codes, const dybit_cach
 
 // Parts of the attention's workspace: outputs and {maximum, sum, exponent} of the parts of cut tiles.
 struct CacheWorkspace {
-    int64_t small_y, small_ml, large_y, large_ml, bytes;
+    int64_t small_y, small_ml, large_y, large_ml, plan, bytes;
     CacheWorkspace(const CacheShape &s, int dim) {
         const CachePlanLayout L(s);
         int64_t at = 0;
-        small_y = at, at += round_up(L.small_slots * s.heads * s.small_rows * dim * 4, 1024);
-        small_ml = at, at += round_up(L.small_slots * s.heads * s.small_rows * 16, 1024);
-        large_y = at, at += round_up(L.large_slots * s.heads * kLargeRows * dim * 4, 1024);
-        large_ml = at, at += round_up(L.large_slots * s.heads * kLargeRows * 16, 1024);
+        small_y = at, at += round_up((L.small_cap > 0 ? 2 * kSmallBlocks : 0) * s.small_rows * (int64_t)dim * 4, 1024);
+        small_ml = at, at += round_up((L.small_cap > 0 ? 2 * kSmallBlocks : 0) * s.small_rows * 16, 1024);
+        large_y = at, at += round_up((L.large_cap > 0 ? 2 * kLargeBlocks : 0) * kLargeRows * (int64_t)dim * 4, 1024);
+        large_ml = at, at += round_up((L.large_cap > 0 ? 2 * kLargeBlocks : 0) * kLargeRows * 16, 1024);
+        plan = at, at += round_up(L.words * 4, 1024);      // the work dealt out again, where a call masks otherwise than the plan
         bytes = at;
     }
 };
 
-template <typename T, int DP, int NQ>
-static dybit_status launch_cache_small(const CUtensorMap &mk, const CUtensorMap &mv, const CacheAttn &p, int64_t items, cudaStream_t s) {
+template <typename T, int DP, int NQ, int BOX>
+static dybit_status launch_cache_small(const CUtensorMap &mk, const CUtensorMap &mv, const CacheAttn &p, cudaStream_t s) {
     static std::atomic<int> ready[64];
     int dev = 0;
     DYBIT_CUDA_TRY(cudaGetDevice(&dev));
     if (dev < 0 || dev >= 64) return DYBIT_ERR_CUDA;
     if (ready[dev].load(std::memory_order_acquire) == 0) {
-        DYBIT_CUDA_TRY(cudaFuncSetAttribute(cache_small_kernel<T, DP, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem_bytes<DP>()));
+        DYBIT_CUDA_TRY(cudaFuncSetAttribute(cache_small_kernel<T, DP, NQ, BOX>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem_bytes<DP>()));
         ready[dev].store(1, std::memory_order_release);
     }
-    const int64_t blocks = items * p.heads;
-    if (blocks > kMaxGridX) return DYBIT_ERR_UNSUPPORTED;
-    launch_k(cache_small_kernel<T, DP, NQ>, dim3((unsigned)blocks), dim3(kSmThreads), small_smem_bytes<DP>(), s, mk, mv, p);
+    launch_k(cache_small_kernel<T, DP, NQ, BOX>, dim3(kSmallBlocks), dim3(kSmThreads), small_smem_bytes<DP>(), s, mk, mv, p);
     return launch_status();
 }
 
 template <typename T, int DP>
-static dybit_status launch_cache_large(const dybit_cache *c, const CacheAttn &p, int64_t items, cudaStream_t s) {
+static dybit_status launch_cache_large(const dybit_cache *c, const CacheAttn &p, cudaStream_t s) {
     static std::atomic<int> ready[64];
     int dev = 0;
     DYBIT_CUDA_TRY(cudaGetDevice(&dev));
@@ -174,51 +177,61 @@ static dybit_status launch_cache_large(const dybit_cache *c, const CacheAttn &p,
         DYBIT_CUDA_TRY(cudaFuncSetAttribute(cache_large_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, large_smem_bytes<DP>()));
         ready[dev].store(1, std::memory_order_release);
     }
-    const int64_t blocks = items * p.heads;
-    if (blocks > kMaxGridX) return DYBIT_ERR_UNSUPPORTED;
-    launch_k(cache_large_kernel<T, DP>, dim3((unsigned)blocks), dim3(kLgThreads), large_smem_bytes<DP>(), s,
-             static_cast<const uint8_t *>(c->k_codes), static_cast<const uint8_t *>(c->v_codes), p);
+    launch_k(cache_large_kernel<T, DP>, dim3(kLargeBlocks), dim3(kLgThreads), large_smem_bytes<DP>(), s, static_cast<const uint8_t *>(c->k_codes),
+             static_cast<const uint8_t *>(c->v_codes), p);
     return launch_status();
 }
 
 template <typename T>
-static dybit_status run_cache_attention(const dybit_cache *c, const CacheShape &shape, CacheAttn p, uint8_t *ws, int *plan, cudaStream_t s) {
+static dybit_status run_cache_attention(const dybit_cache *c, const CacheShape &shape, CacheAttn p, uint8_t *ws, const int *plan, cudaStream_t s) {
     const CachePlanLayout L(shape);
     const CacheWorkspace w(shape, c->dim);
-    const int dp = c->dim <= 64 ? 64 : 128;
+    const int dp = c->dim <= 64 ? 64 : 128, box = c->page == 16 ? 16 : 32;
     CUtensorMap mk, mv;
-    if (!make_cache_map(&mk, c->k_codes, c, 16, dp) || !make_cache_map(&mv, c->v_codes, c, 16, dp)) return DYBIT_ERR_CUDA;
+    if (!make_cache_map(&mk, c->k_codes, c, box, dp) || !make_cache_map(&mv, c->v_codes, c, box, dp)) return DYBIT_ERR_CUDA;
+    dybit_status st = DYBIT_OK;
+    if ((p.causal != 0) != (shape.causal != 0) || p.window != shape.window) {
+        CacheShape mine = shape;
+        mine.causal = p.causal, mine.window = p.window;
+        launch_k(cache_deal_kernel, dim3(1), dim3(kCachePlanThreads), 0, s, mine, plan, reinterpret_cast<int *>(ws + w.plan));
+        st = launch_status();
+        if (st != DYBIT_OK) return st;
+        plan = reinterpret_cast<const int *>(ws + w.plan);
+    }
     CacheAttn small = p, large = p;
     small.tiles = reinterpret_cast<const CacheTile *>(plan + L.small);
-    small.comb = reinterpret_cast<const CacheTile *>(plan + L.small_comb);
+    small.starts = reinterpret_cast<const CacheStart *>(plan + L.small_starts);
+    small.n_tiles = plan + 1, small.n_blocks = plan + 3;
     small.part_y = reinterpret_cast<float *>(ws + w.small_y);
     small.part_ml = reinterpret_cast<float4 *>(ws + w.small_ml);
     large.tiles = reinterpret_cast<const CacheTile *>(plan + L.large);
-    large.comb = reinterpret_cast<const CacheTile *>(plan + L.large_comb);
+    large.starts = reinterpret_cast<const CacheStart *>(plan + L.large_starts);
+    large.n_tiles = plan + 2, large.n_blocks = plan + 4;
     large.part_y = reinterpret_cast<float *>(ws + w.large_y);
     large.part_ml = reinterpret_cast<float4 *>(ws + w.large_ml);
-    const int64_t most = (int64_t)shape.max_pages * shape.page;      // keys of a sequence
-    dybit_status st = DYBIT_OK;
     if (L.large_cap > 0) {
-        st = dp == 64 ? launch_cache_large<T, 64>(c, large, L.large_cap, s) : launch_cache_large<T, 128>(c, large, L.large_cap, s);
+        st = dp == 64 ? launch_cache_large<T, 64>(c, large, s) : launch_cache_large<T, 128>(c, large, s);
         if (st != DYBIT_OK) return st;
     }
     const bool few = shape.small_rows == 8;
-    if (dp == 64) st = few ? launch_cache_small<T, 64, 1>(mk, mv, small, L.small_cap, s) : launch_cache_small<T, 64, 2>(mk, mv, small, L.small_cap, s);
-    else st = few ? launch_cache_small<T, 128, 1>(mk, mv, small, L.small_cap, s) : launch_cache_small<T, 128, 2>(mk, mv, small, L.small_cap, s);
+    auto go = [&](auto d, auto q) {
+        constexpr int DP = decltype(d)::value, NQ = decltype(q)::value;
+        return box == 16 ? launch_cache_small<T, DP, NQ, 16>(mk, mv, small, s) : launch_cache_small<T, DP, NQ, 32>(mk, mv, small, s);
+    };
+    using one = std::integral_constant<int, 1>;
+    using two = std::integral_constant<int, 2>;
+    using d64 = std::integral_constant<int, 64>;
+    using d128 = std::integral_constant<int, 128>;
+    st = dp == 64 ? (few ? go(d64(), one()) : go(d64(), two())) : (few ? go(d128(), one()) : go(d128(), two()));
     if (st != DYBIT_OK) return st;
-    // a sequence of at most one part's least length is never cut
-    if (L.large_comb_cap > 0 && most > kLargeLeast * kLargeUnit) {
-        launch_k(cache_join_kernel<T, kLargeRows>, dim3((unsigned)(L.large_comb_cap * p.heads), kLargeRows / kSmallRows), dim3(128), 0, s, large);
+    if (L.large_cap > 0) {
+        launch_k(cache_join_kernel<T, kLargeRows>, dim3(kLargeBlocks - 1, kLargeRows / kSmallRows), dim3(128), 0, s, large);
         st = launch_status();
         if (st != DYBIT_OK) return st;
     }
-    if (most > kSmallLeast * kSmallUnit) {
-        const dim3 grid((unsigned)(L.small_comb_cap * p.heads));
-        if (few) launch_k(cache_join_kernel<T, 8>, grid, dim3(128), 0, s, small);
-        else launch_k(cache_join_kernel<T, kSmallRows>, grid, dim3(128), 0, s, small);
-        st = launch_status();
-    }
+    if (few) launch_k(cache_join_kernel<T, 8>, dim3(kSmallBlocks - 1), dim3(128), 0, s, small);
+    else launch_k(cache_join_kernel<T, kSmallRows>, dim3(kSmallBlocks - 1), dim3(128), 0, s, small);
+    st = launch_status();
     return st;
 }
 
@@ -325,7 +338,7 @@ dybit_status dybit_cache_attention(const dybit_cache *cache, const dybit_cache_b
     if (ws == nullptr || ws_bytes < dybit_cache_attention_workspace_bytes(cache, batch)) return DYBIT_ERR_WORKSPACE;
     if (cache->pages == 0) return DYBIT_ERR_INVALID_ARG;
     CacheAttn p = {};
-    p.plan = static_cast<const int *>(plan);
+    p.minus_one = 0xffffffffu;
     p.table = batch->table, p.table_stride = batch->table_stride;
     p.pages = cache->pages, p.page_shift = log2_of(cache->page), p.heads = cache->heads, p.group = batch->q_heads / cache->heads, p.dim = cache->dim;
     p.k_scales = cache->k_scales, p.v_scales = cache->v_scales;
@@ -338,7 +351,7 @@ dybit_status dybit_cache_attention(const dybit_cache *cache, const dybit_cache_b
     p.y_vec = heads_aligned(y, t, y_token_stride, y_head_stride, 8);
     const CacheShape shape = cache_shape(cache, batch);
     uint8_t *base = static_cast<uint8_t *>(ws);
-    int *words = static_cast<int *>(const_cast<void *>(plan));
+    const int *words = static_cast<const int *>(plan);
     if (t == DYBIT_BF16) return run_cache_attention<__nv_bfloat16>(cache, shape, p, base, words, static_cast<cudaStream_t>(stream));
     return run_cache_attention<__half>(cache, shape, p, base, words, static_cast<cudaStream_t>(stream));
 }

@@ -25,8 +25,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.0f;
 
 struct CacheAttn {
-    const int *plan;             // counts
-    const CacheTile *tiles, *comb;
+    const int *n_tiles, *n_blocks;       // of the plan
+    const CacheTile *tiles;
+    const CacheStart *starts;
     const int *table;
     int64_t table_stride;
     int64_t pages;
@@ -39,9 +40,10 @@ struct CacheAttn {
     float *lse;                  // [T][query heads], or null
     float scale_log2;            // softmax scale * log2(e)
     int causal, window;          // window: keys that a row sees, its own the last; INT_MAX for all
-    float *part_y;               // [slot][head][rows][dim] of parts
-    float4 *part_ml;             // [slot][head][rows]: {m + E0, l, E0, -}
+    float *part_y;               // [slot][rows][dim]: sums of the parts of tiles that several blocks work on
+    float4 *part_ml;             // [slot][rows]: {m + E0, l, E0, -}
     int q_vec, q_vec16, y_vec;   // rows can be moved in pieces of 8 (16) bytes
+    unsigned minus_one;          // see decode_pair
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -50,19 +52,34 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
-// Two codes as a pair of f16 numbers: decode2 in f16 (1024 + c is exact, and the patterns add up to 36 << 10).
+// Four codes of a word as two pairs of 16-bit numbers, the codes of bytes 0 and 2 and those of bytes 1 and 3: decode2 of
+// dybit_code8.cuh, for f16 as well (1024 + c is exact there, and the patterns add up to 36 << 10).  What contracts or carries
+// the codes is free to take every other one, and spreading them by a byte permutation would cost more than any other step
+// (27 us of 132 in a pass over 524 MB of codes).  Logic and integer additions share one half-rate pipe; the subtraction of the
+// patterns is written as a product with minus_one, an argument of the kernel, so that it takes the other one.
 __device__ __forceinline__ __half2 as_half2(unsigned w) { return *reinterpret_cast<const __half2 *>(&w); }
 __device__ __forceinline__ unsigned half2_bits(__half2 v) { return *reinterpret_cast<const unsigned *>(&v); }
-__device__ __forceinline__ unsigned decode2_f16(unsigned w) {
+// codes in bytes 0 and 2 of w, their signs at bits 15 and 31 of s
+template <typename T> __device__ __forceinline__ unsigned decode_pair(unsigned w, unsigned s, unsigned minus_one);
+template <> __device__ __forceinline__ unsigned decode_pair<__half>(unsigned w, unsigned s, unsigned minus_one) {
     const __half2 h = as_half2((w & 0x007f007fu) | 0x64006400u);
     const unsigned g = half2_bits(__hfma2(h, as_half2(0xbc00bc00u), as_half2(0x64806480u)));           // 1152 - h = 128 - c
-    const __half2 curve = as_half2(0x90009000u - g);
+    const __half2 curve = as_half2(g * minus_one + 0x90009000u);
     const __half2 above = __hfma2_relu(h, as_half2(0xa000a000u), as_half2(0x48404840u));               // max(0, 8.5 - h / 128)
-    return half2_bits(__hsub2(curve, above)) | (w & 0x80008000u);
+    return half2_bits(__hsub2(curve, above)) | (s & 0x80008000u);
 }
-template <typename T> __device__ __forceinline__ unsigned decode_pair(unsigned w);
-template <> __device__ __forceinline__ unsigned decode_pair<__nv_bfloat16>(unsigned w) { return decode2<true>(w); }
-template <> __device__ __forceinline__ unsigned decode_pair<__half>(unsigned w) { return decode2_f16(w); }
+template <> __device__ __forceinline__ unsigned decode_pair<__nv_bfloat16>(unsigned w, unsigned s, unsigned minus_one) {
+    const __nv_bfloat162 h = as_bf162((w & 0x007f007fu) | 0x43004300u);
+    const unsigned g = as_u32(__hfma2(h, as_bf162(0xbf80bf80u), as_bf162(0x43804380u)));               // 256 - h = 128 - c
+    const __nv_bfloat162 curve = as_bf162(g * minus_one + 0x82008200u);
+    const __nv_bfloat162 above = __hfma2_relu(h, as_bf162(0xbc00bc00u), as_bf162(0x3fc03fc0u));        // max(0, 1.5 - h / 128)
+    return as_u32(__hsub2(curve, above)) | (s & 0x80008000u);
+}
+template <typename T>
+__device__ __forceinline__ void decode_word(unsigned w, unsigned minus_one, unsigned &even, unsigned &odd) {
+    even = decode_pair<T>(w, w << 8, minus_one);
+    odd = decode_pair<T>(w >> 8, w, minus_one);
+}
 
 // d (16 x 8, fp32) += a (16 x 16) * b (16 x 8) on the legacy tensor path: sixteen rows of codes against eight queries.
 template <typename T>
@@ -97,15 +114,36 @@ __device__ __forceinline__ RowKeys row_keys(const CacheAttn &p, const CacheTile 
     return k;
 }
 
-// The keys [first, last) of this part of a tile whose rows are r0 .. r1 - 1, in units of `unit` keys.
+// A part of a tile: units from .. to - 1 of its work, for one key head.  slot < 0: the whole tile.
+struct CachePart {
+    CacheTile tile;
+    int head, from, to, slot;
+};
+
+// The next part of a block's share, which ends at `end`; false where there is none.  A part that starts inside a tile is
+// the block's first, one that ends inside a tile its last: two slots to a block are enough.
+__device__ __forceinline__ bool cache_next(const CacheAttn &p, int block, CacheStart &at, const CacheStart &end, int n_tiles, CachePart &part) {
+    if (at.head > end.head || (at.head == end.head && (at.tile > end.tile || (at.tile == end.tile && at.off >= end.off)))) return false;
+    part.tile = p.tiles[at.tile];
+    part.head = at.head;
+    part.from = at.off;
+    part.to = at.head == end.head && at.tile == end.tile ? min(end.off, part.tile.units) : part.tile.units;
+    part.slot = part.from == 0 && part.to == part.tile.units ? -1 : 2 * block + (part.from == 0 ? 1 : 0);
+    at.off = 0;
+    if (++at.tile == n_tiles) at.tile = 0, ++at.head;
+    return true;
+}
+
+// The keys [first, last) of a part of a tile whose rows are r0 .. r0 + rows - 1, in units of `unit` keys.
 struct KeyRange { int first, last; };
-__device__ __forceinline__ KeyRange tile_keys(const CacheAttn &p, const CacheTile &t, int r0, int rows, int unit) {
+__device__ __forceinline__ KeyRange part_keys(const CacheAttn &p, const CachePart &part, int r0, int rows, int unit) {
+    const CacheTile &t = part.tile;
     const RowKeys a = row_keys(p, t, r0), z = row_keys(p, t, min(r0 + rows, t.n * p.group) - 1);
     KeyRange k = {0, 0};
     if (z.hi <= a.lo) return k;                            // positions grow with the row
     const int u0 = a.lo / unit, u1 = cache_div_up(z.hi, unit), n = u1 - u0;
-    k.first = (u0 + (int)((int64_t)n * t.split / t.splits)) * unit;
-    k.last = (u0 + (int)((int64_t)n * (t.split + 1) / t.splits)) * unit;
+    k.first = (u0 + (int)((int64_t)n * part.from / t.units)) * unit;
+    k.last = (u0 + (int)((int64_t)n * part.to / t.units)) * unit;
     return k;
 }
 
@@ -138,31 +176,43 @@ constexpr int kSmSegment = 4096;             // keys whose page numbers and scal
 template <int DP> __host__ __device__ constexpr int small_stage_bytes() { return 2 * kSmKeys * DP; }
 template <int DP> __host__ __device__ constexpr int small_smem_bytes() { return kSmWarps * kSmStages * small_stage_bytes<DP>() + 1024; }
 
-// What the score and value loops need of 16 keys.
-struct KeyBlock { float c, e, f; int z, zv; };   // x's factor, values' exponent, 2^-e; coordinates page * heads + head of keys and values
+// Two 16 x 16 matrices of bytes in shared memory, transposed: lane 4 * g + t gets the bytes 4t .. 4t + 3 of column g (r0; second
+// matrix r2) and of column g + 8 (r1, r3).  Lanes 0 .. 15 give the rows of the first matrix, the others those of the second.
+__device__ __forceinline__ void ldmatrix_b8_trans(uint32_t addr, unsigned &r0, unsigned &r1, unsigned &r2, unsigned &r3) {
+    asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3)
+                 : "r"(addr)
+                 : "memory");
+}
+
+// What the score and value loops need of the keys of a box.
+struct alignas(32) KeyBlock {
+    float c, e, f;               // x's factor, values' exponent, 2^-e
+    int y, z, zv;                // token in the page, page * heads + head of keys and of values: the TMA's coordinates
+};
 
 // Four warps share a part's keys, 32 at a time each, with a ring of their own that the TMA fills; they meet at the end.
 // Both products have the codes as their left operand, sixteen rows of them, and 8 * NQ query rows as their right one:
 //     S^T = K Q^T (keys x rows),   Y^T += V^T P^T (head elements x rows)
 // so that an instruction takes twice the codes that it would with the queries on the left.  A stage is read straight into
-// the fragments: contractions over head elements and over keys may run in any order, so a lane takes 16 consecutive codes of
-// its key, and the keys of a block are ordered so that the swizzled reads of a quarter warp hit different banks (key_row).
-// Bound by HBM, then by instruction issue: a pair of codes takes 7 instructions and there is little else.
-template <typename T, int DP, int NQ>
+// the fragments: contractions over head elements and over keys may run in any order.  Of K a lane takes 16 consecutive codes of
+// two neighbouring keys, of V, which the instruction wants with keys side by side, four keys of a head element, by a
+// transposing load of bytes; the keys of both products are numbered by what that load gives (row i of the two halves of 16 keys is
+// key 2i and key 2i + 1).  Bound by HBM, then by instruction issue: a pair of codes takes 7 instructions.
+// BOX: keys of a TMA box, 32 or, on pages of 16 tokens, 16.
+template <typename T, int DP, int NQ, int BOX>
 __global__ void __launch_bounds__(kSmThreads, 3)
 cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const CacheAttn p) {
     constexpr int KS = DP / 16;                            // matrix instructions along a head
-    constexpr int X = DP / 8;                              // head elements of a lane's value column
-    constexpr int ROWS = 8 * NQ;
+    constexpr int ROWS = 8 * NQ, NB = kSmKeys / BOX;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    __shared__ KeyBlock s_block[kSmSegment / 16];
+    __shared__ KeyBlock s_block[kSmSegment / BOX];
     __shared__ uint64_t s_full[kSmWarps][kSmStages];
     __shared__ uint32_t s_abort;
     __shared__ float s_m[kSmWarps][ROWS], s_l[kSmWarps][ROWS];
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int item = (int)(blockIdx.x / (unsigned)p.heads), head = (int)(blockIdx.x - (unsigned)item * (unsigned)p.heads);
     if (threadIdx.x == 0) {
         for (int w = 0; w < kSmWarps; ++w)
             for (int s = 0; s < kSmStages; ++s) mbar_init(&s_full[w][s], 1);
@@ -172,337 +222,335 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         prefetch_tensormap(&map_v);
     }
     pdl_enter();
-    if (item >= p.plan[1]) return;
-    const CacheTile tile = p.tiles[item];
-    const int r0 = tile.tile * ROWS, rows = min(ROWS, tile.n * p.group - r0);
-    const KeyRange range = tile_keys(p, tile, r0, ROWS, kSmKeys);
-    const int *table = p.table + tile.seq * p.table_stride;
-    // this lane's scores are those of rows 8 * q + 2t and 8 * q + 2t + 1
-    RowKeys seen[NQ][2];
-#pragma unroll
-    for (int q = 0; q < NQ; ++q)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) seen[q][h] = row_keys(p, tile, r0 + 8 * q + 2 * t + h);
-    // keys between these two are seen by every row that is there
-    const int all_lo = row_keys(p, tile, r0 + rows - 1).lo, all_hi = row_keys(p, tile, r0).hi;
-
-    // queries as right-hand fragments: row 8 * q + g; k index 2t, 2t+1 (8+2t, 8+2t+1) of step j is head element
-    // 16 * (t + 4 * (j / 4)) + 4 * (j % 4) + 0, 1 (2, 3)
-    unsigned qf[NQ][KS][2];
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-        const int r = r0 + 8 * q + g, token = r / p.group, h = head * p.group + (r - token * p.group);
-        const T *at = 8 * q + g < rows ? static_cast<const T *>(p.q) + (tile.row + token) * p.q_token + h * p.q_head : nullptr;
-#pragma unroll
-        for (int j = 0; j < KS; ++j) {
-            const int d = 16 * (t + 4 * (j / 4)) + 4 * (j % 4);
-            uint2 v = make_uint2(0u, 0u);
-            if (at != nullptr && d < p.dim) {
-                if (p.q_vec) {
-                    v = __ldg(reinterpret_cast<const uint2 *>(at + d));
-                } else {
-                    T e[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) e[i] = at[d + i];
-                    memcpy(&v, e, 8);
-                }
-            }
-            qf[q][j][0] = v.x, qf[q][j][1] = v.y;
-        }
-    }
-
-    // exponent of the first page's value scale
-    float e0 = 0.0f;
-    if (range.last > range.first) {
-        const int pg = __ldg(table + (range.first >> p.page_shift));
-        const float s = (unsigned)pg < (uint64_t)p.pages ? __ldg(p.v_scales + (int64_t)pg * p.heads + head) : 0.0f;
-        e0 = s > 0.0f ? (float)((int)((__float_as_uint(s) >> 23) & 255u) - 127) : 0.0f;
-    }
-
+    const int block = blockIdx.x, n_tiles = __ldg(p.n_tiles), n_blocks = __ldg(p.n_blocks);
+    CacheStart at = p.starts[block];
+    const CacheStart end = p.starts[block + 1];
+    if (block >= n_blocks) return;
+    const unsigned minus = p.minus_one;
     uint8_t *ring = smem + warp * (kSmStages * small_stage_bytes<DP>());
-    // output i: head elements X * g + 2i (o[0], o[1]) and X * g + 2i + 1 (o[2], o[3]) of rows 8q + 2t and 8q + 2t + 1
-    float o[NQ][X / 2][4], m[NQ][2], l[NQ][2];
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-#pragma unroll
-        for (int i = 0; i < X / 2; ++i) o[q][i][0] = o[q][i][1] = o[q][i][2] = o[q][i][3] = 0.0f;
-        m[q][0] = m[q][1] = -INFINITY;
-        l[q][0] = l[q][1] = 0.0f;
-    }
-    // row i of a group of eight keys is key key_row(i): two neighbours lie four (DP 64: an odd number of) rows apart and the rows
-    // of the even ones differ above their lowest bit, which makes both kinds of reads free of bank conflicts
-    auto key_row = [](int i) {
-        if constexpr (DP == 128) {
-            const int h = i >> 1;
-            return (2 * h + (h >> 1)) ^ ((i & 1) << 2);
-        } else {
-            const int h = i >> 1, even = (h & 1) | ((h & 2) << 1);
-            return (i & 1) ? (even ^ 3) : even;
-        }
-    };
-    const int kr = key_row(g), kv0 = key_row(2 * t), kv1 = key_row(2 * t + 1);
     uint32_t it = 0;                                       // stages used by this warp so far
     bool ok = true;
 
-    for (int seg = range.first; seg < range.last; seg += kSmSegment) {
-        const int seg_end = min(range.last, seg + kSmSegment);
-        if (__syncthreads_and(ok) == 0) break;             // a wait that ran out ends the loop for all four warps
-        for (int i = threadIdx.x; i < (seg_end - seg) / 16; i += kSmThreads) {
-            const int key = seg + 16 * i;
-            const int pg = key < tile.len ? __ldg(table + (key >> p.page_shift)) : -1;
-            const int none = (int)(p.pages * p.heads);     // a coordinate outside the pool reads as zeros
-            KeyBlock b = {0.0f, -INFINITY, 0.0f, none, none};                    // not there: seen by no row
-            if ((unsigned)pg < (uint64_t)p.pages) {
-                b.z = (int)((int64_t)pg * p.heads + head);
-                const float ks = __ldg(p.k_scales + b.z), vs = __ldg(p.v_scales + b.z);
-                b.c = ks * p.scale_log2;
-                b.zv = vs > 0.0f ? b.z : none;
-                b.e = vs > 0.0f ? (float)((int)((__float_as_uint(vs) >> 23) & 255u) - 127) - e0 : 0.0f;
-                b.f = __uint_as_float((unsigned)(127 - max(-126, min(126, (int)b.e))) << 23);
-            }
-            s_block[i] = b;
-        }
-        __syncthreads();
-        const int n_tiles = (seg_end - seg) / kSmKeys;
-        auto fetch = [&](int i, uint32_t stage) {          // one lane
-            uint8_t *dst = ring + stage * small_stage_bytes<DP>();
-            uint64_t *bar = &s_full[warp][stage];
-            mbar_arrive_expect_tx(bar, small_stage_bytes<DP>());
+    CachePart part;
+    while (cache_next(p, block, at, end, n_tiles, part)) {
+        // a wait that ran out ends the loop for all four warps; all have read the sums of the part before
+        if (__syncthreads_and(ok) == 0) break;
+        const CacheTile &tile = part.tile;
+        const int head = part.head, r0 = tile.tile * ROWS, rows = min(ROWS, tile.n * p.group - r0);
+        const KeyRange range = part_keys(p, part, r0, ROWS, kSmKeys);
+        const int *table = p.table + tile.seq * p.table_stride;
+        // this lane's scores are those of rows 8 * q + 2t and 8 * q + 2t + 1
+        RowKeys seen[NQ][2];
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int z = s_block[2 * i + b].z, zv = s_block[2 * i + b].zv, y = (seg + kSmKeys * i + 16 * b) & ((1 << p.page_shift) - 1);
-                tma_load_3d(dst + b * 16 * DP, &map_k, 0, y, z, bar);
-                tma_load_3d(dst + (kSmKeys + b * 16) * DP, &map_v, 0, y, zv, bar);
-            }
-        };
-        if (lane == 0) {
+        for (int q = 0; q < NQ; ++q)
 #pragma unroll
-            for (int s = 0; s < kSmStages; ++s)
-                if (warp + s * kSmWarps < n_tiles) fetch(warp + s * kSmWarps, (it + s) % kSmStages);
-        }
-        __syncwarp();
-        for (int i = warp; i < n_tiles; i += kSmWarps, ++it) {
-            const uint32_t stage = it % kSmStages;
-            ok = __all_sync(0xffffffffu, wait_bounded(&s_full[warp][stage], (it / kSmStages) & 1u, &s_abort, 0x81));
-            if (!ok) break;
-            const uint8_t *ks = ring + stage * small_stage_bytes<DP>(), *vs = ks + kSmKeys * DP;
-            // x[b][q][0], [1]: key key_row(g) of block b, rows 8q + 2t and 8q + 2t + 1; [2], [3]: key 8 + key_row(g)
-            float x[2][NQ][4];
+            for (int h = 0; h < 2; ++h) seen[q][h] = row_keys(p, tile, r0 + 8 * q + 2 * t + h);
+        // keys between these two are seen by every row that is there
+        const int all_lo = row_keys(p, tile, r0 + rows - 1).lo, all_hi = row_keys(p, tile, r0).hi;
+
+        // queries as right-hand fragments: row 8 * q + g; k index 2t, 2t+1 (8+2t, 8+2t+1) of step j is head element
+        // 16 * (t + 4 * (j / 4)) + 4 * (j % 4) + 0, 2 (1, 3)
+        unsigned qf[NQ][KS][2];
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                uint4 w[2][DP / 64];
+        for (int q = 0; q < NQ; ++q) {
+            const int r = r0 + 8 * q + g, token = r / p.group, h = head * p.group + (r - token * p.group);
+            const T *row = 8 * q + g < rows ? static_cast<const T *>(p.q) + (tile.row + token) * p.q_token + h * p.q_head : nullptr;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int row = b * 16 + h * 8 + kr;
-                    if constexpr (DP == 128) {
-                        w[h][0] = *reinterpret_cast<const uint4 *>(ks + row * 128 + ((t ^ (row & 7)) << 4));
-                        w[h][1] = *reinterpret_cast<const uint4 *>(ks + row * 128 + (((t + 4) ^ (row & 7)) << 4));
+            for (int j = 0; j < KS; ++j) {
+                const int d = 16 * (t + 4 * (j / 4)) + 4 * (j % 4);
+                uint2 v = make_uint2(0u, 0u);
+                if (row != nullptr && d < p.dim) {
+                    if (p.q_vec) {
+                        v = __ldg(reinterpret_cast<const uint2 *>(row + d));
                     } else {
-                        w[h][0] = *reinterpret_cast<const uint4 *>(ks + row * 64 + ((t ^ ((row >> 1) & 3)) << 4));
+                        T e[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) e[i] = row[d + i];
+                        memcpy(&v, e, 8);
                     }
                 }
+                qf[q][j][0] = __byte_perm(v.x, v.y, 0x5410), qf[q][j][1] = __byte_perm(v.x, v.y, 0x7632);
+            }
+        }
+
+        // exponent of the first page's value scale
+        float e0 = 0.0f;
+        if (range.last > range.first) {
+            const int pg = __ldg(table + (range.first >> p.page_shift));
+            const float s = (unsigned)pg < (uint64_t)p.pages ? __ldg(p.v_scales + (int64_t)pg * p.heads + head) : 0.0f;
+            e0 = s > 0.0f ? (float)((int)((__float_as_uint(s) >> 23) & 255u) - 127) : 0.0f;
+        }
+
+        // output i: head elements 16i + g (o[0], o[1]) and 16i + g + 8 (o[2], o[3]) of rows 8q + 2t and 8q + 2t + 1
+        float o[NQ][KS][4], m[NQ][2], l[NQ][2];
 #pragma unroll
-                for (int q = 0; q < NQ; ++q) x[b][q][0] = x[b][q][1] = x[b][q][2] = x[b][q][3] = 0.0f;
+        for (int q = 0; q < NQ; ++q) {
 #pragma unroll
-                for (int j = 0; j < KS; ++j) {
-                    unsigned c[2];
+            for (int i = 0; i < KS; ++i) o[q][i][0] = o[q][i][1] = o[q][i][2] = o[q][i][3] = 0.0f;
+            m[q][0] = m[q][1] = -INFINITY;
+            l[q][0] = l[q][1] = 0.0f;
+        }
+        for (int seg = range.first; seg < range.last; seg += kSmSegment) {
+            const int seg_end = min(range.last, seg + kSmSegment);
+            if (seg > range.first && __syncthreads_and(ok) == 0) break;
+            for (int i = threadIdx.x; i < (seg_end - seg) / BOX; i += kSmThreads) {
+                const int key = seg + BOX * i;
+                const int pg = key < tile.len ? __ldg(table + (key >> p.page_shift)) : -1;
+                const int none = (int)(p.pages * p.heads);     // a coordinate outside the pool reads as zeros
+                KeyBlock b = {0.0f, -INFINITY, 0.0f, key & ((1 << p.page_shift) - 1), none, none};      // not there: seen by no row
+                if ((unsigned)pg < (uint64_t)p.pages) {
+                    b.z = (int)((int64_t)pg * p.heads + head);
+                    const float ks = __ldg(p.k_scales + b.z), vs = __ldg(p.v_scales + b.z);
+                    b.c = ks * p.scale_log2;
+                    b.zv = vs > 0.0f ? b.z : none;
+                    b.e = vs > 0.0f ? (float)((int)((__float_as_uint(vs) >> 23) & 255u) - 127) - e0 : 0.0f;
+                    b.f = __uint_as_float((unsigned)(127 - max(-126, min(126, (int)b.e))) << 23);
+                }
+                s_block[i] = b;
+            }
+            __syncthreads();
+            const int n_tiles = (seg_end - seg) / kSmKeys;
+            auto fetch = [&](int i, uint32_t stage) {          // one lane
+                uint8_t *dst = ring + stage * small_stage_bytes<DP>();
+                uint64_t *bar = &s_full[warp][stage];
+                mbar_arrive_expect_tx(bar, small_stage_bytes<DP>());
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const KeyBlock &k = s_block[NB * i + b];
+                    tma_load_3d(dst + b * BOX * DP, &map_k, 0, k.y, k.z, bar);
+                    tma_load_3d(dst + (kSmKeys + b * BOX) * DP, &map_v, 0, k.y, k.zv, bar);
+                }
+            };
+            if (lane == 0) {
+#pragma unroll
+                for (int s = 0; s < kSmStages; ++s)
+                    if (warp + s * kSmWarps < n_tiles) fetch(warp + s * kSmWarps, (it + s) % kSmStages);
+            }
+            __syncwarp();
+            for (int i = warp; i < n_tiles; i += kSmWarps, ++it) {
+                const uint32_t stage = it % kSmStages;
+                ok = __all_sync(0xffffffffu, wait_bounded(&s_full[warp][stage], (it / kSmStages) & 1u, &s_abort, 0x81));
+                if (!ok) break;
+                const uint8_t *ks = ring + stage * small_stage_bytes<DP>(), *vs = ks + kSmKeys * DP;
+                // x[b][q][0], [1]: key 2g of block b, rows 8q + 2t and 8q + 2t + 1; [2], [3]: key 2g + 1
+                float x[2][NQ][4];
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    uint4 w[2][DP / 64];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const uint4 &q4 = w[h][j / 4];
-                        c[h] = j % 4 == 0 ? q4.x : j % 4 == 1 ? q4.y : j % 4 == 2 ? q4.z : q4.w;
+                        const int row = b * 16 + 2 * g + h;
+                        if constexpr (DP == 128) {
+                            w[h][0] = *reinterpret_cast<const uint4 *>(ks + row * 128 + ((t ^ (row & 7)) << 4));
+                            w[h][1] = *reinterpret_cast<const uint4 *>(ks + row * 128 + (((t + 4) ^ (row & 7)) << 4));
+                        } else {
+                            w[h][0] = *reinterpret_cast<const uint4 *>(ks + row * 64 + ((t ^ ((row >> 1) & 3)) << 4));
+                        }
                     }
-                    const unsigned a0 = decode_pair<T>(__byte_perm(c[0], 0u, 0x1100)), a1 = decode_pair<T>(__byte_perm(c[1], 0u, 0x1100)),
-                                   a2 = decode_pair<T>(__byte_perm(c[0], 0u, 0x3322)), a3 = decode_pair<T>(__byte_perm(c[1], 0u, 0x3322));
 #pragma unroll
-                    for (int q = 0; q < NQ; ++q) mma_16816<T>(x[b][q], a0, a1, a2, a3, qf[q][j]);
+                    for (int q = 0; q < NQ; ++q) x[b][q][0] = x[b][q][1] = x[b][q][2] = x[b][q][3] = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < KS; ++j) {
+                        unsigned c[2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const uint4 &q4 = w[h][j / 4];
+                            c[h] = j % 4 == 0 ? q4.x : j % 4 == 1 ? q4.y : j % 4 == 2 ? q4.z : q4.w;
+                        }
+                        unsigned a0, a1, a2, a3;
+                        decode_word<T>(c[0], minus, a0, a2);
+                        decode_word<T>(c[1], minus, a1, a3);
+#pragma unroll
+                        for (int q = 0; q < NQ; ++q) mma_16816<T>(x[b][q], a0, a1, a2, a3, qf[q][j]);
+                    }
                 }
-            }
-            const int first = seg + kSmKeys * i;
-            const bool edge = first < all_lo || first + kSmKeys > all_hi;
-            float f[2];
-            float top[NQ][2];
+                const int first = seg + kSmKeys * i;
+                const bool edge = first < all_lo || first + kSmKeys > all_hi;
+                // scores in base 2 are x * c + e; the factor is not negative: the largest product has the largest score
+                float c[2], e[2], f[2], top[NQ][2];
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) top[q][0] = top[q][1] = -INFINITY;
+                for (int b = 0; b < 2; ++b) {
+                    const float4 kb = *reinterpret_cast<const float4 *>(&s_block[NB * i + (NB == 2 ? b : 0)]);
+                    c[b] = kb.x, e[b] = kb.y, f[b] = kb.z;
+                    if (edge) {
+                        const int ka = first + b * 16 + 2 * g;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const KeyBlock kb = s_block[2 * i + b];
-                f[b] = kb.f;
+                        for (int q = 0; q < NQ; ++q)
 #pragma unroll
-                for (int q = 0; q < NQ; ++q)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) x[b][q][k] = __fmaf_rn(x[b][q][k], kb.c, kb.e);
-                if (edge) {
-                    const int ka = first + b * 16 + kr;
+                            for (int k = 0; k < 4; ++k) {
+                                const int key = ka + (k >> 1);
+                                const bool is = key >= seen[q][k & 1].lo && key < seen[q][k & 1].hi;
+                                x[b][q][k] = is ? __fmaf_rn(x[b][q][k], c[b], e[b]) : -INFINITY;
+                            }
+                        c[b] = 1.0f, e[b] = 0.0f;
+                    }
 #pragma unroll
                     for (int q = 0; q < NQ; ++q)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int key = ka + (k >> 1) * 8;
-                            if (key < seen[q][k & 1].lo || key >= seen[q][k & 1].hi) x[b][q][k] = -INFINITY;
+                        for (int h = 0; h < 2; ++h) {
+                            const float a = __fmaf_rn(fmaxf(x[b][q][h], x[b][q][2 + h]), c[b], e[b]);
+                            top[q][h] = b == 0 ? a : fmaxf(top[q][h], a);
                         }
                 }
+                bool raise = false;
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) raise |= top[q][0] > m[q][0] + kRaise || top[q][1] > m[q][1] + kRaise;
+                if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+                    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {          // the row's maximum over the eight lanes that share it
+                            float a = top[q][h];
+#pragma unroll
+                            for (int d = 4; d < 32; d <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
+                            const float n = fmaxf(m[q][h], a), s = m[q][h] == n ? 1.0f : ex2(m[q][h] - n);
+                            m[q][h] = n;
+                            l[q][h] *= s;
+#pragma unroll
+                            for (int d = 0; d < KS; ++d) o[q][d][h] *= s, o[q][d][2 + h] *= s;
+                        }
+                }
+                unsigned pf[2][NQ][2];
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
-                    top[q][0] = fmaxf(top[q][0], fmaxf(x[b][q][0], x[b][q][2]));
-                    top[q][1] = fmaxf(top[q][1], fmaxf(x[b][q][1], x[b][q][3]));
-                }
-            }
-            bool raise = false;
+                    const float u0 = m[q][0] == -INFINITY ? 0.0f : m[q][0], u1 = m[q][1] == -INFINITY ? 0.0f : m[q][1];
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) raise |= top[q][0] > m[q][0] + kRaise || top[q][1] > m[q][1] + kRaise;
-            if (__any_sync(0xffffffffu, raise)) {
-#pragma unroll
-                for (int q = 0; q < NQ; ++q)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {          // the row's maximum over the eight lanes that share it
-                        float a = top[q][h];
-#pragma unroll
-                        for (int d = 4; d < 32; d <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, d));
-                        const float n = fmaxf(m[q][h], a), s = m[q][h] == n ? 1.0f : ex2(m[q][h] - n);
-                        m[q][h] = n;
-                        l[q][h] *= s;
-#pragma unroll
-                        for (int d = 0; d < X / 2; ++d) o[q][d][h] *= s, o[q][d][2 + h] *= s;
+                    for (int b = 0; b < 2; ++b) {
+                        float(&v)[4] = x[b][q];
+                        const float e0 = e[b] - u0, e1 = e[b] - u1;
+                        v[0] = ex2(__fmaf_rn(v[0], c[b], e0)), v[1] = ex2(__fmaf_rn(v[1], c[b], e1));
+                        v[2] = ex2(__fmaf_rn(v[2], c[b], e0)), v[3] = ex2(__fmaf_rn(v[3], c[b], e1));
+                        l[q][0] = __fmaf_rn(v[0] + v[2], f[b], l[q][0]);
+                        l[q][1] = __fmaf_rn(v[1] + v[3], f[b], l[q][1]);
+                        // keys x rows -> rows x keys
+                        pf[b][q][0] = transpose8(pack_f16(v[0], v[1]));
+                        pf[b][q][1] = transpose8(pack_f16(v[2], v[3]));
                     }
-            }
-            unsigned pf[2][NQ][2];
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) {
-                const float u0 = m[q][0] == -INFINITY ? 0.0f : m[q][0], u1 = m[q][1] == -INFINITY ? 0.0f : m[q][1];
+                }
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    float(&v)[4] = x[b][q];
-                    v[0] = ex2(v[0] - u0), v[1] = ex2(v[1] - u1), v[2] = ex2(v[2] - u0), v[3] = ex2(v[3] - u1);
-                    l[q][0] = __fmaf_rn(v[0] + v[2], f[b], l[q][0]);
-                    l[q][1] = __fmaf_rn(v[1] + v[3], f[b], l[q][1]);
-                    // keys x rows -> rows x keys
-                    pf[b][q][0] = transpose8(pack_f16(v[0], v[1]));
-                    pf[b][q][1] = transpose8(pack_f16(v[2], v[3]));
-                }
-            }
+                    const int row = b * 16 + (lane & 15);
+                    const uint32_t at_row = smem_u32(vs) + row * DP;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int ra = b * 16 + kv0, rb = b * 16 + kv1;
-                unsigned v[4][DP / 32];                    // rows of keys 2t, 2t + 1, 8 + 2t, 8 + 2t + 1
+                    for (int i2 = 0; i2 < KS; i2 += 2) {
+                        const int chunk = i2 + (lane >> 4);
+                        unsigned c0, c1, c2, c3, a0, a1, a2, a3;
+                        ldmatrix_b8_trans(at_row + ((chunk ^ (DP == 128 ? row & 7 : (row >> 1) & 3)) << 4), c0, c1, c2, c3);
+                        decode_word<__half>(c0, minus, a0, a2);
+                        decode_word<__half>(c1, minus, a1, a3);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int row = (k & 1 ? rb : ra) + (k >> 1) * 8;
-                    if constexpr (DP == 128) {
-                        const uint4 c = *reinterpret_cast<const uint4 *>(vs + row * 128 + ((g ^ (row & 7)) << 4));
-                        v[k][0] = c.x, v[k][1] = c.y, v[k][2] = c.z, v[k][3] = c.w;
-                    } else {
-                        const uint2 c = *reinterpret_cast<const uint2 *>(vs + row * 64 + (((g >> 1) ^ ((row >> 1) & 3)) << 4) + (g & 1) * 8);
-                        v[k][0] = c.x, v[k][1] = c.y;
+                        for (int q = 0; q < NQ; ++q) mma_16816<__half>(o[q][i2], a0, a1, a2, a3, pf[b][q]);
+                        decode_word<__half>(c2, minus, a0, a2);
+                        decode_word<__half>(c3, minus, a1, a3);
+#pragma unroll
+                        for (int q = 0; q < NQ; ++q) mma_16816<__half>(o[q][i2 + 1], a0, a1, a2, a3, pf[b][q]);
                     }
                 }
+                __syncwarp();
+                if (lane == 0 && i + kSmStages * kSmWarps < n_tiles) fetch(i + kSmStages * kSmWarps, stage);
+            }
+        }
+        if (!ok) {                                             // copies in flight land before the block's memory is given up
+            for (int i = 0; i < 64; ++i) __nanosleep(2000);
+        }
+
+        // the four warps' parts: maxima first, then the sums at the common maximum
 #pragma unroll
-                for (int i2 = 0; i2 < X / 2; ++i2) {
-                    const int w = i2 / 2;
-                    const unsigned s0 = 0x4400u + 0x1111u * (2 * (i2 & 1)), s1 = s0 + 0x1111u;
-                    const unsigned a0 = decode2_f16(__byte_perm(v[0][w], v[1][w], s0)), a1 = decode2_f16(__byte_perm(v[0][w], v[1][w], s1)),
-                                   a2 = decode2_f16(__byte_perm(v[2][w], v[3][w], s0)), a3 = decode2_f16(__byte_perm(v[2][w], v[3][w], s1));
+        for (int q = 0; q < NQ; ++q)
 #pragma unroll
-                    for (int q = 0; q < NQ; ++q) mma_16816<__half>(o[q][i2], a0, a1, a2, a3, pf[b][q]);
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[q][h] += __shfl_xor_sync(0xffffffffu, l[q][h], d);
+                if (g == 0) {
+                    s_m[warp][8 * q + 2 * t + h] = m[q][h];
+                    s_l[warp][8 * q + 2 * t + h] = l[q][h];
                 }
             }
-            __syncwarp();
-            if (lane == 0 && i + kSmStages * kSmWarps < n_tiles) fetch(i + kSmStages * kSmWarps, stage);
-        }
-    }
-    if (!ok) {                                             // copies in flight land before the block's memory is given up
-        for (int i = 0; i < 64; ++i) __nanosleep(2000);
-    }
-
-    // the four warps' parts: maxima first, then the sums at the common maximum
-#pragma unroll
-    for (int q = 0; q < NQ; ++q)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) l[q][h] += __shfl_xor_sync(0xffffffffu, l[q][h], d);
-            if (g == 0) {
-                s_m[warp][8 * q + 2 * t + h] = m[q][h];
-                s_l[warp][8 * q + 2 * t + h] = l[q][h];
-            }
-        }
-    __syncthreads();
-    auto common = [&](int r) {
-        float v = s_m[0][r];
-#pragma unroll
-        for (int w = 1; w < kSmWarps; ++w) v = fmaxf(v, s_m[w][r]);
-        return v;
-    };
-    constexpr int LD = DP + 4;
-    float *const all = reinterpret_cast<float *>(smem);
-    const int vecs = p.dim / 4;
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) {                         // eight rows at a time: the ring holds those of four warps
-        if (q * 8 >= rows) break;
-        if (q > 0) __syncthreads();
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const float top = common(8 * q + 2 * t + h), f = m[q][h] == -INFINITY ? 0.0f : ex2(m[q][h] - top);
-            float *row = all + (warp * 8 + 2 * t + h) * LD + g * X;
-#pragma unroll
-            for (int i = 0; i < X / 2; i += 2)
-                *reinterpret_cast<float4 *>(row + 2 * i) = make_float4(o[q][i][h] * f, o[q][i][2 + h] * f, o[q][i + 1][h] * f, o[q][i + 1][2 + h] * f);
-        }
         __syncthreads();
-        for (int i = threadIdx.x; i < 8 * vecs; i += kSmThreads) {
-            const int lr = i / vecs, d = (i - lr * vecs) * 4, r = q * 8 + lr;
-            if (r >= rows) break;
-            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-            float sum = 0.0f;
-            const float top = common(r);
+        auto common = [&](int r) {
+            float v = s_m[0][r];
 #pragma unroll
-            for (int w = 0; w < kSmWarps; ++w) {
-                const float4 v = *reinterpret_cast<const float4 *>(all + (w * 8 + lr) * LD + d);
-                s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-                sum += s_m[w][r] == -INFINITY ? s_l[w][r] : s_l[w][r] * ex2(s_m[w][r] - top);
+            for (int w = 1; w < kSmWarps; ++w) v = fmaxf(v, s_m[w][r]);
+            return v;
+        };
+        constexpr int LD = DP + 4;
+        float *const all = reinterpret_cast<float *>(smem);
+        const int vecs = p.dim / 4;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {                         // eight rows at a time: the ring holds those of four warps
+            if (q * 8 >= rows) break;
+            if (q > 0) __syncthreads();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float top = common(8 * q + 2 * t + h), f = m[q][h] == -INFINITY ? 0.0f : ex2(m[q][h] - top);
+                float *row = all + (warp * 8 + 2 * t + h) * LD + g;
+#pragma unroll
+                for (int i = 0; i < KS; ++i) row[16 * i] = o[q][i][h] * f, row[16 * i + 8] = o[q][i][2 + h] * f;
             }
-            if (tile.splits > 1) {
-                const int64_t at = ((int64_t)tile.slot * p.heads + head) * ROWS + r;
-                *reinterpret_cast<float4 *>(p.part_y + at * p.dim + d) = s;
-                if (d == 0) p.part_ml[at] = make_float4(top + e0, sum, e0, 0.0f);
-            } else {
-                store_attention_row<T>(p, tile, head, r0 + r, d, s, sum, top, e0);
+            __syncthreads();
+            for (int i = threadIdx.x; i < 8 * vecs; i += kSmThreads) {
+                const int lr = i / vecs, d = (i - lr * vecs) * 4, r = q * 8 + lr;
+                if (r >= rows) break;
+                float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+                float sum = 0.0f;
+                const float top = common(r);
+#pragma unroll
+                for (int w = 0; w < kSmWarps; ++w) {
+                    const float4 v = *reinterpret_cast<const float4 *>(all + (w * 8 + lr) * LD + d);
+                    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+                    sum += s_m[w][r] == -INFINITY ? s_l[w][r] : s_l[w][r] * ex2(s_m[w][r] - top);
+                }
+                if (part.slot >= 0) {
+                    const int64_t to = (int64_t)part.slot * ROWS + r;
+                    *reinterpret_cast<float4 *>(p.part_y + to * p.dim + d) = s;
+                    if (d == 0) p.part_ml[to] = make_float4(top + e0, sum, e0, 0.0f);
+                } else {
+                    store_attention_row<T>(p, tile, head, r0 + r, d, s, sum, top, e0);
+                }
             }
         }
+        fence_proxy_async_smem();                          // the ring is the TMA's again
     }
 }
 
 // ------------------------------------------------------------------ parts of a tile, joined
 
-// Up to sixteen rows of a tile and one key head: the parts at their common maximum.  part_ml.x is a part's maximum with its
-// exponent in it, so that parts whose values have other scales compare.
+// One block for each block of the attention kernel but the first: if the tile that it starts inside of is not shared with one
+// before the last, it joins the tile's parts at their common maximum, sixteen rows at a time.  part_ml.x is a part's maximum with
+// its exponent in it, so that parts whose values have other scales compare.
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(128) cache_join_kernel(const CacheAttn p) {
     pdl_enter();
-    const int item = (int)(blockIdx.x / (unsigned)p.heads), head = (int)(blockIdx.x - (unsigned)item * (unsigned)p.heads);
-    if (item >= p.plan[ROWS == kLargeRows ? 4 : 3]) return;
-    const CacheTile tile = p.comb[item];
+    const int block = blockIdx.x + 1, n_blocks = __ldg(p.n_blocks);
+    const CacheStart before = p.starts[block - 1], start = p.starts[block];
+    if (block >= n_blocks || start.off == 0) return;
+    auto inside = [&](const CacheStart &s) { return s.tile == start.tile && s.head == start.head && s.off > 0; };
+    if (inside(before)) return;
+    int parts = 2;
+    while (block + parts - 1 < n_blocks && inside(p.starts[block + parts - 1])) ++parts;
+    const CacheTile tile = p.tiles[start.tile];
     const int r0 = blockIdx.y * kSmallRows, rows = min(ROWS, tile.n * p.group - tile.tile * ROWS), vecs = p.dim / 4;
-    const int64_t step = (int64_t)p.heads * ROWS;
+    // slots of the parts: the second one of the block before, then the first ones of this and those behind it
+    auto slot_of = [&](int k) { return (int64_t)(k == 0 ? 2 * block - 1 : 2 * (block + k - 1)) * ROWS; };
     for (int i = threadIdx.x; i < kSmallRows * vecs; i += 128) {
         const int r = r0 + i / vecs, d = (i - i / vecs * vecs) * 4;
         if (r >= rows) break;
-        const int64_t at = ((int64_t)tile.slot * p.heads + head) * ROWS + r;
-        const float4 *ml = p.part_ml + at;
-        const float *y = p.part_y + at * p.dim + d;
+        const float4 *ml = p.part_ml + r;
+        const float *y = p.part_y + (int64_t)r * p.dim + d;
         float m = -INFINITY;
-#pragma unroll 8
-        for (int k = 0; k < tile.splits; ++k) m = fmaxf(m, __ldcg(ml + k * step).x);
-        const float e = ml->z;
+#pragma unroll 4
+        for (int k = 0; k < parts; ++k) m = fmaxf(m, __ldcg(ml + slot_of(k)).x);
+        const float e = __ldcg(ml + slot_of(0)).z;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
         float l = 0.0f;
-#pragma unroll 8
-        for (int k = 0; k < tile.splits; ++k) {
-            const float4 a = __ldcg(ml + k * step), v = __ldcg(reinterpret_cast<const float4 *>(y + k * step * p.dim));
+#pragma unroll 4
+        for (int k = 0; k < parts; ++k) {
+            const float4 a = __ldcg(ml + slot_of(k)), v = __ldcg(reinterpret_cast<const float4 *>(y + slot_of(k) * p.dim));
             const float w = a.x == -INFINITY ? 0.0f : ex2(a.x - m);
             s.x += v.x * w, s.y += v.y * w, s.z += v.z * w, s.w += v.w * w;
             l += (a.x == -INFINITY ? a.y : a.y * w) * ex2(e - a.z);
         }
-        store_attention_row<T>(p, tile, head, tile.tile * ROWS + r, d, s, l, m - e, e);
+        store_attention_row<T>(p, tile, start.head, tile.tile * ROWS + r, d, s, l, m - e, e);
     }
 }
 

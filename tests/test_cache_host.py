@@ -19,7 +19,7 @@ def cache(k=64, v=64, ks=64, vs=64, pages=100, page=64, heads=8, dim=128):
 
 
 def batch(sequences=4, tokens=100, max_new=50, q_heads=32, table=64, stride=10, max_pages=10):
-    return dy.binding._CCacheBatch(sequences, tokens, max_new, q_heads, table, stride, max_pages)
+    return dy.binding._CCacheBatch(sequences, tokens, max_new, q_heads, table, stride, max_pages, 1, 0)
 
 
 def plan_bytes(c, b):
