@@ -23,8 +23,12 @@ constexpr int kLargeRows = 256;              // rows of a large tile: two accumu
 constexpr int kSmallUnit = 64, kLargeUnit = 128;     // keys that work is counted in
 // Blocks that the work of small and of large tiles is dealt out to: one resident wave.  Counted as the B200 has them, not asked of
 // the device: the sizes of plans and workspaces depend on them and are the same wherever they are asked for.
-constexpr int kSmallBlocks = 148 * 3, kLargeBlocks = 148;
-constexpr int kSmallLeast = 4, kLargeLeast = 4;      // units that a block has at least
+constexpr int kLargeBlocks = 148;
+// Small tiles' blocks are warps, as many to an SM as its registers hold.
+__host__ __device__ constexpr int small_per_sm(int rows) { return rows == 8 ? 16 : 12; }
+__host__ __device__ constexpr int small_blocks(int rows) { return 148 * small_per_sm(rows); }
+constexpr int kSmallLeast = 2, kLargeLeast = 4;      // units that a block has at least
+constexpr int kTileUnits = 1;                        // what a tile costs beside its keys, in units
 
 // New tokens of one sequence that go to one page (pos < 0 for tokens in front of the sequence's first position).
 struct CacheItem { int row, pos, count, seq; };
@@ -59,7 +63,7 @@ struct CachePlanLayout {
         items = w, w += 4 * items_cap;
         small = w, w += 8 * small_cap;
         large = w, w += 8 * large_cap;
-        small_starts = w, w += 4 * (kSmallBlocks + 1);
+        small_starts = w, w += 4 * (small_blocks(s.small_rows) + 1);
         large_starts = w, w += large_cap > 0 ? 4 * (kLargeBlocks + 1) : 0;
         words = w;
     }
@@ -92,9 +96,9 @@ __device__ __forceinline__ CacheSeq cache_seq(const CachePlanArgs &a, int b) {
 // Units of work of a tile's rows r0 .. r0 + rows - 1: its keys under the mask that is expected; one at least, so that a tile
 // without keys has a block that writes its zeros.
 __device__ __forceinline__ int cache_units(const CacheShape &s, const CacheSeq &q, int r0, int rows, int unit) {
-    if (!s.causal) return max(1, cache_div_up(q.len, unit));
+    if (!s.causal) return max(1, cache_div_up(q.len, unit)) + kTileUnits;
     const int p0 = q.len - q.n, lo = max(0, p0 + r0 / s.group + 1 - min(s.window, 0x3fffffff)), hi = p0 + min(q.n - 1, (r0 + rows - 1) / s.group) + 1;
-    return hi <= lo ? 1 : cache_div_up(hi, unit) - lo / unit;
+    return (hi <= lo ? 1 : cache_div_up(hi, unit) - lo / unit) + kTileUnits;
 }
 
 // Exclusive prefix sum over the block; *total receives the sum.
@@ -136,7 +140,7 @@ __device__ __forceinline__ int cache_deal(const CacheShape &s, const CacheTile *
     __syncthreads();
     if (n == 0) return 0;
     const int64_t work = units * s.heads;
-    const int blocks = (int)min((int64_t)(large ? kLargeBlocks : kSmallBlocks), max((int64_t)1, work / (large ? kLargeLeast : kSmallLeast)));
+    const int blocks = (int)min((int64_t)(large ? kLargeBlocks : small_blocks(s.small_rows)), max((int64_t)1, work / (large ? kLargeLeast : kSmallLeast)));
     for (int c = threadIdx.x; c <= blocks; c += kCachePlanThreads) {
         const int64_t g = c < blocks ? work / blocks * c + work % blocks * c / blocks : work;
         const int head = (int)(g / units);

@@ -9,8 +9,6 @@
 
 namespace dybit {
 
-constexpr int kCacheMaxDim = 128, kCacheMaxGroup = 128;
-
 static dybit_status check_cache(const dybit_cache *c) {
     if (c == nullptr) return DYBIT_ERR_INVALID_ARG;
     if (c->pages < 0 || c->heads < 1 || c->dim < 1 || c->page < 1) return DYBIT_ERR_INVALID_ARG;
@@ -144,8 +142,8 @@ struct CacheWorkspace {
     CacheWorkspace(const CacheShape &s, int dim) {
         const CachePlanLayout L(s);
         int64_t at = 0;
-        small_y = at, at += round_up((L.small_cap > 0 ? 2 * kSmallBlocks : 0) * s.small_rows * (int64_t)dim * 4, 1024);
-        small_ml = at, at += round_up((L.small_cap > 0 ? 2 * kSmallBlocks : 0) * s.small_rows * 16, 1024);
+        small_y = at, at += round_up((L.small_cap > 0 ? 2 * small_blocks(s.small_rows) : 0) * s.small_rows * (int64_t)dim * 4, 1024);
+        small_ml = at, at += round_up((L.small_cap > 0 ? 2 * small_blocks(s.small_rows) : 0) * s.small_rows * 16, 1024);
         large_y = at, at += round_up((L.large_cap > 0 ? 2 * kLargeBlocks : 0) * kLargeRows * (int64_t)dim * 4, 1024);
         large_ml = at, at += round_up((L.large_cap > 0 ? 2 * kLargeBlocks : 0) * kLargeRows * 16, 1024);
         plan = at, at += round_up(L.words * 4, 1024);      // the work dealt out again, where a call masks otherwise than the plan
@@ -160,10 +158,10 @@ static dybit_status launch_cache_small(const CUtensorMap &mk, const CUtensorMap 
     DYBIT_CUDA_TRY(cudaGetDevice(&dev));
     if (dev < 0 || dev >= 64) return DYBIT_ERR_CUDA;
     if (ready[dev].load(std::memory_order_acquire) == 0) {
-        DYBIT_CUDA_TRY(cudaFuncSetAttribute(cache_small_kernel<T, DP, NQ, BOX>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem_bytes<DP>()));
+        DYBIT_CUDA_TRY(cudaFuncSetAttribute(cache_small_kernel<T, DP, NQ, BOX>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(8 * NQ)));
         ready[dev].store(1, std::memory_order_release);
     }
-    launch_k(cache_small_kernel<T, DP, NQ, BOX>, dim3(kSmallBlocks), dim3(kSmThreads), small_smem_bytes<DP>(), s, mk, mv, p);
+    launch_k(cache_small_kernel<T, DP, NQ, BOX>, dim3(148), dim3(32 * small_per_sm(8 * NQ)), small_smem(8 * NQ), s, mk, mv, p);
     return launch_status();
 }
 
@@ -225,12 +223,12 @@ static dybit_status run_cache_attention(const dybit_cache *c, const CacheShape &
     st = dp == 64 ? (few ? go(d64(), one()) : go(d64(), two())) : (few ? go(d128(), one()) : go(d128(), two()));
     if (st != DYBIT_OK) return st;
     if (L.large_cap > 0) {
-        launch_k(cache_join_kernel<T, kLargeRows>, dim3(kLargeBlocks - 1, kLargeRows / kSmallRows), dim3(128), 0, s, large);
+        launch_k(cache_join_kernel<T, kLargeRows>, dim3(kLargeBlocks - 1, 16), dim3(128), 0, s, large);
         st = launch_status();
         if (st != DYBIT_OK) return st;
     }
-    if (few) launch_k(cache_join_kernel<T, 8>, dim3(kSmallBlocks - 1), dim3(128), 0, s, small);
-    else launch_k(cache_join_kernel<T, kSmallRows>, dim3(kSmallBlocks - 1), dim3(128), 0, s, small);
+    if (few) launch_k(cache_join_kernel<T, 8>, dim3(small_blocks(8) - 1), dim3(128), 0, s, small);
+    else launch_k(cache_join_kernel<T, kSmallRows>, dim3(small_blocks(kSmallRows) - 1), dim3(128), 0, s, small);
     st = launch_status();
     return st;
 }
@@ -348,7 +346,7 @@ dybit_status dybit_cache_attention(const dybit_cache *cache, const dybit_cache_b
     p.scale_log2 = scale * kLog2e;
     p.causal = causal != 0, p.window = window > 0 ? window : INT_MAX;
     p.q_vec = heads_aligned(q, t, q_token_stride, q_head_stride, 8), p.q_vec16 = heads_aligned(q, t, q_token_stride, q_head_stride, 16);
-    p.y_vec = heads_aligned(y, t, y_token_stride, y_head_stride, 8);
+    p.y_vec = heads_aligned(y, t, y_token_stride, y_head_stride, 8), p.y_vec16 = heads_aligned(y, t, y_token_stride, y_head_stride, 16);
     const CacheShape shape = cache_shape(cache, batch);
     uint8_t *base = static_cast<uint8_t *>(ws);
     const int *words = static_cast<const int *>(plan);

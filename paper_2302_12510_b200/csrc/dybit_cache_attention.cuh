@@ -16,6 +16,8 @@
 // hardly ever rescaled.
 #pragma once
 
+#include <limits.h>
+
 #include "dybit_cache.cuh"
 #include "dybit_wait.cuh"
 
@@ -23,6 +25,7 @@ namespace dybit {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.0f;
+constexpr int kCacheMaxDim = 128, kCacheMaxGroup = 128;
 
 struct CacheAttn {
     const int *n_tiles, *n_blocks;       // of the plan
@@ -42,7 +45,7 @@ struct CacheAttn {
     int causal, window;          // window: keys that a row sees, its own the last; INT_MAX for all
     float *part_y;               // [slot][rows][dim]: sums of the parts of tiles that several blocks work on
     float4 *part_ml;             // [slot][rows]: {m + E0, l, E0, -}
-    int q_vec, q_vec16, y_vec;   // rows can be moved in pieces of 8 (16) bytes
+    int q_vec, q_vec16, y_vec, y_vec16;  // rows can be moved in pieces of 8 (16) bytes
     unsigned minus_one;          // see decode_pair
 };
 
@@ -168,13 +171,10 @@ __device__ __forceinline__ void store_attention_row(const CacheAttn &p, const Ca
 
 // ------------------------------------------------------------------ tiles of 8 or 16 rows
 
-constexpr int kSmThreads = 128, kSmWarps = 4;
-constexpr int kSmKeys = 32;                  // keys of a stage: two boxes of 16
-constexpr int kSmStages = 2;
-constexpr int kSmSegment = 4096;             // keys whose page numbers and scales are held in shared memory at a time
-
-template <int DP> __host__ __device__ constexpr int small_stage_bytes() { return 2 * kSmKeys * DP; }
-template <int DP> __host__ __device__ constexpr int small_smem_bytes() { return kSmWarps * kSmStages * small_stage_bytes<DP>() + 1024; }
+constexpr int kSmSegment = 1024;             // keys whose page numbers and scales are held in shared memory at a time
+constexpr int kSmBytes = 4096;               // codes of the keys (of the values) that a warp takes at a time
+constexpr int kSmLead = 2;                   // rounds that a warp may be ahead of another of its scheduler
+__host__ __device__ constexpr int small_smem(int rows) { return small_per_sm(rows) * 2 * kSmBytes + 1024; }
 
 // Two 16 x 16 matrices of bytes in shared memory, transposed: lane 4 * g + t gets the bytes 4t .. 4t + 3 of column g (r0; second
 // matrix r2) and of column g + 8 (r1, r3).  Lanes 0 .. 15 give the rows of the first matrix, the others those of the second.
@@ -191,7 +191,11 @@ struct alignas(32) KeyBlock {
     int y, z, zv;                // token in the page, page * heads + head of keys and of values: the TMA's coordinates
 };
 
-// Four warps share a part's keys, 32 at a time each, with a ring of their own that the TMA fills; they meet at the end.
+// Every warp has a share of its own, 32 keys (heads of up to 64: 64) to a round; a tile that is cut is joined afterwards.  The TMA
+// fills a buffer for keys and one for values; both are read into registers at once and filled again while their codes are worked
+// on.  Shares are equal, but a scheduler favours its older warps: left alone, the four of one end after 74, 86, 101 and 111 us, the
+// last one without others to fill its waits.  So a warp that is more than two rounds ahead of another of its scheduler sleeps a
+// little (a hint: nothing depends on it).
 // Both products have the codes as their left operand, sixteen rows of them, and 8 * NQ query rows as their right one:
 //     S^T = K Q^T (keys x rows),   Y^T += V^T P^T (head elements x rows)
 // so that an instruction takes twice the codes that it would with the queries on the left.  A stage is read straight into
@@ -201,43 +205,52 @@ struct alignas(32) KeyBlock {
 // key 2i and key 2i + 1).  Bound by HBM, then by instruction issue: a pair of codes takes 7 instructions.
 // BOX: keys of a TMA box, 32 or, on pages of 16 tokens, 16.
 template <typename T, int DP, int NQ, int BOX>
-__global__ void __launch_bounds__(kSmThreads, 3)
+__global__ void __launch_bounds__(32 * small_per_sm(8 * NQ), 1)
 cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const CacheAttn p) {
     constexpr int KS = DP / 16;                            // matrix instructions along a head
-    constexpr int ROWS = 8 * NQ, NB = kSmKeys / BOX;
+    constexpr int ROWS = 8 * NQ, WARPS = small_per_sm(ROWS), KEYS = kSmBytes / DP, BL = KEYS / 16, NB = KEYS / BOX;      // blocks of 16 keys, boxes
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    __shared__ KeyBlock s_block[kSmSegment / BOX];
-    __shared__ uint64_t s_full[kSmWarps][kSmStages];
+    __shared__ KeyBlock s_blocks[WARPS][kSmSegment / BOX];
+    __shared__ uint64_t s_full[WARPS][2];
     __shared__ uint32_t s_abort;
-    __shared__ float s_m[kSmWarps][ROWS], s_l[kSmWarps][ROWS];
+    __shared__ int4 s_rounds[4];                           // per scheduler: rounds that its warps have done
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    if (threadIdx.x == 0) {
-        for (int w = 0; w < kSmWarps; ++w)
-            for (int s = 0; s < kSmStages; ++s) mbar_init(&s_full[w][s], 1);
-        s_abort = 0;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    KeyBlock *const s_block = s_blocks[warp];
+    uint64_t *const k_full = &s_full[warp][0], *const v_full = &s_full[warp][1];
+    volatile int *const my_rounds = reinterpret_cast<volatile int *>(&s_rounds[warp & 3]) + (warp >> 2);
+    if (lane == 0) {
+        mbar_init(k_full, 1);
+        mbar_init(v_full, 1);
+        *my_rounds = 0;
+        if (WARPS == 12 && warp < 4) my_rounds[3] = INT_MAX;
+        if (warp == 0) s_abort = 0;
         fence_mbar_init();
+    }
+    if (threadIdx.x == 0) {
         prefetch_tensormap(&map_k);
         prefetch_tensormap(&map_v);
     }
+    __syncthreads();
     pdl_enter();
-    const int block = blockIdx.x, n_tiles = __ldg(p.n_tiles), n_blocks = __ldg(p.n_blocks);
+    const int block = warp * (int)gridDim.x + (int)blockIdx.x, n_tiles = __ldg(p.n_tiles), n_blocks = __ldg(p.n_blocks);
     CacheStart at = p.starts[block];
     const CacheStart end = p.starts[block + 1];
-    if (block >= n_blocks) return;
+    if (block >= n_blocks) {
+        if (lane == 0) *my_rounds = INT_MAX;
+        return;
+    }
     const unsigned minus = p.minus_one;
-    uint8_t *ring = smem + warp * (kSmStages * small_stage_bytes<DP>());
-    uint32_t it = 0;                                       // stages used by this warp so far
+    uint8_t *ks = smem + warp * (2 * kSmBytes), *vs = ks + kSmBytes;
+    uint32_t it = 0;                                       // rounds so far
     bool ok = true;
 
     CachePart part;
-    while (cache_next(p, block, at, end, n_tiles, part)) {
-        // a wait that ran out ends the loop for all four warps; all have read the sums of the part before
-        if (__syncthreads_and(ok) == 0) break;
+    while (ok && cache_next(p, block, at, end, n_tiles, part)) {
         const CacheTile &tile = part.tile;
         const int head = part.head, r0 = tile.tile * ROWS, rows = min(ROWS, tile.n * p.group - r0);
-        const KeyRange range = part_keys(p, part, r0, ROWS, kSmKeys);
+        const KeyRange range = part_keys(p, part, r0, ROWS, KEYS);
         const int *table = p.table + tile.seq * p.table_stride;
         // this lane's scores are those of rows 8 * q + 2t and 8 * q + 2t + 1
         RowKeys seen[NQ][2];
@@ -290,10 +303,10 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             m[q][0] = m[q][1] = -INFINITY;
             l[q][0] = l[q][1] = 0.0f;
         }
-        for (int seg = range.first; seg < range.last; seg += kSmSegment) {
+        for (int seg = range.first; seg < range.last && ok; seg += kSmSegment) {
             const int seg_end = min(range.last, seg + kSmSegment);
-            if (seg > range.first && __syncthreads_and(ok) == 0) break;
-            for (int i = threadIdx.x; i < (seg_end - seg) / BOX; i += kSmThreads) {
+            __syncwarp();
+            for (int i = lane; i < (seg_end - seg) / BOX; i += 32) {
                 const int key = seg + BOX * i;
                 const int pg = key < tile.len ? __ldg(table + (key >> p.page_shift)) : -1;
                 const int none = (int)(p.pages * p.heads);     // a coordinate outside the pool reads as zeros
@@ -308,45 +321,51 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 }
                 s_block[i] = b;
             }
-            __syncthreads();
-            const int n_tiles = (seg_end - seg) / kSmKeys;
-            auto fetch = [&](int i, uint32_t stage) {          // one lane
-                uint8_t *dst = ring + stage * small_stage_bytes<DP>();
-                uint64_t *bar = &s_full[warp][stage];
-                mbar_arrive_expect_tx(bar, small_stage_bytes<DP>());
+            __syncwarp();
+            const int rounds = (seg_end - seg) / KEYS;
+            auto fetch = [&](int i, bool values) {         // one lane
+                uint64_t *bar = values ? v_full : k_full;
+                mbar_arrive_expect_tx(bar, kSmBytes);
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
                     const KeyBlock &k = s_block[NB * i + b];
-                    tma_load_3d(dst + b * BOX * DP, &map_k, 0, k.y, k.z, bar);
-                    tma_load_3d(dst + (kSmKeys + b * BOX) * DP, &map_v, 0, k.y, k.zv, bar);
+                    tma_load_3d((values ? vs : ks) + b * BOX * DP, values ? &map_v : &map_k, 0, k.y, values ? k.zv : k.z, bar);
                 }
             };
             if (lane == 0) {
-#pragma unroll
-                for (int s = 0; s < kSmStages; ++s)
-                    if (warp + s * kSmWarps < n_tiles) fetch(warp + s * kSmWarps, (it + s) % kSmStages);
+                fetch(0, false);
+                fetch(0, true);
             }
             __syncwarp();
-            for (int i = warp; i < n_tiles; i += kSmWarps, ++it) {
-                const uint32_t stage = it % kSmStages;
-                ok = __all_sync(0xffffffffu, wait_bounded(&s_full[warp][stage], (it / kSmStages) & 1u, &s_abort, 0x81));
+            for (int i = 0; i < rounds; ++i, ++it) {
+                const bool more = lane == 0 && i + 1 < rounds;
+                for (int k = 0; k < 8; ++k) {
+                    const volatile int *all = reinterpret_cast<const volatile int *>(&s_rounds[warp & 3]);
+                    if ((int)it <= min(min(all[0], all[1]), min(all[2], all[3])) + kSmLead) break;
+                    __nanosleep(400);
+                }
+                ok = __all_sync(0xffffffffu, wait_bounded(k_full, it & 1u, &s_abort, 0x81));
                 if (!ok) break;
-                const uint8_t *ks = ring + stage * small_stage_bytes<DP>(), *vs = ks + kSmKeys * DP;
-                // x[b][q][0], [1]: key 2g of block b, rows 8q + 2t and 8q + 2t + 1; [2], [3]: key 2g + 1
-                float x[2][NQ][4];
+                // keys 2g and 2g + 1 of each block; a fragment is 16 codes
+                uint4 w[BL][2][DP / 64];
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    uint4 w[2][DP / 64];
+                for (int b = 0; b < BL; ++b)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int row = b * 16 + 2 * g + h;
                         if constexpr (DP == 128) {
-                            w[h][0] = *reinterpret_cast<const uint4 *>(ks + row * 128 + ((t ^ (row & 7)) << 4));
-                            w[h][1] = *reinterpret_cast<const uint4 *>(ks + row * 128 + (((t + 4) ^ (row & 7)) << 4));
+                            w[b][h][0] = *reinterpret_cast<const uint4 *>(ks + row * 128 + ((t ^ (row & 7)) << 4));
+                            w[b][h][1] = *reinterpret_cast<const uint4 *>(ks + row * 128 + (((t + 4) ^ (row & 7)) << 4));
                         } else {
-                            w[h][0] = *reinterpret_cast<const uint4 *>(ks + row * 64 + ((t ^ ((row >> 1) & 3)) << 4));
+                            w[b][h][0] = *reinterpret_cast<const uint4 *>(ks + row * 64 + ((t ^ ((row >> 1) & 3)) << 4));
                         }
                     }
+                __syncwarp();
+                if (more) fetch(i + 1, false);
+                // x[b][q][0], [1]: key 2g of block b, rows 8q + 2t and 8q + 2t + 1; [2], [3]: key 2g + 1
+                float x[BL][NQ][4];
+#pragma unroll
+                for (int b = 0; b < BL; ++b) {
 #pragma unroll
                     for (int q = 0; q < NQ; ++q) x[b][q][0] = x[b][q][1] = x[b][q][2] = x[b][q][3] = 0.0f;
 #pragma unroll
@@ -354,7 +373,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                         unsigned c[2];
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const uint4 &q4 = w[h][j / 4];
+                            const uint4 &q4 = w[b][h][j / 4];
                             c[h] = j % 4 == 0 ? q4.x : j % 4 == 1 ? q4.y : j % 4 == 2 ? q4.z : q4.w;
                         }
                         unsigned a0, a1, a2, a3;
@@ -364,13 +383,13 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                         for (int q = 0; q < NQ; ++q) mma_16816<T>(x[b][q], a0, a1, a2, a3, qf[q][j]);
                     }
                 }
-                const int first = seg + kSmKeys * i;
-                const bool edge = first < all_lo || first + kSmKeys > all_hi;
+                const int first = seg + KEYS * i;
+                const bool edge = first < all_lo || first + KEYS > all_hi;
                 // scores in base 2 are x * c + e; the factor is not negative: the largest product has the largest score
-                float c[2], e[2], f[2], top[NQ][2];
+                float c[BL], e[BL], f[BL], top[NQ][2];
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const float4 kb = *reinterpret_cast<const float4 *>(&s_block[NB * i + (NB == 2 ? b : 0)]);
+                for (int b = 0; b < BL; ++b) {
+                    const float4 kb = *reinterpret_cast<const float4 *>(&s_block[NB * i + b * 16 / BOX]);
                     c[b] = kb.x, e[b] = kb.y, f[b] = kb.z;
                     if (edge) {
                         const int ka = first + b * 16 + 2 * g;
@@ -392,7 +411,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                             top[q][h] = b == 0 ? a : fmaxf(top[q][h], a);
                         }
                 }
-                bool raise = false;
+            bool raise = false;
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) raise |= top[q][0] > m[q][0] + kRaise || top[q][1] > m[q][1] + kRaise;
                 if (__any_sync(0xffffffffu, raise)) {
@@ -410,16 +429,16 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                             for (int d = 0; d < KS; ++d) o[q][d][h] *= s, o[q][d][2 + h] *= s;
                         }
                 }
-                unsigned pf[2][NQ][2];
+                unsigned pf[BL][NQ][2];
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
                     const float u0 = m[q][0] == -INFINITY ? 0.0f : m[q][0], u1 = m[q][1] == -INFINITY ? 0.0f : m[q][1];
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) {
+                    for (int b = 0; b < BL; ++b) {
                         float(&v)[4] = x[b][q];
-                        const float e0 = e[b] - u0, e1 = e[b] - u1;
-                        v[0] = ex2(__fmaf_rn(v[0], c[b], e0)), v[1] = ex2(__fmaf_rn(v[1], c[b], e1));
-                        v[2] = ex2(__fmaf_rn(v[2], c[b], e0)), v[3] = ex2(__fmaf_rn(v[3], c[b], e1));
+                        const float s0 = e[b] - u0, s1 = e[b] - u1;
+                        v[0] = ex2(__fmaf_rn(v[0], c[b], s0)), v[1] = ex2(__fmaf_rn(v[1], c[b], s1));
+                        v[2] = ex2(__fmaf_rn(v[2], c[b], s0)), v[3] = ex2(__fmaf_rn(v[3], c[b], s1));
                         l[q][0] = __fmaf_rn(v[0] + v[2], f[b], l[q][0]);
                         l[q][1] = __fmaf_rn(v[1] + v[3], f[b], l[q][1]);
                         // keys x rows -> rows x keys
@@ -427,130 +446,159 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                         pf[b][q][1] = transpose8(pack_f16(v[2], v[3]));
                     }
                 }
+                ok = __all_sync(0xffffffffu, wait_bounded(v_full, it & 1u, &s_abort, 0x8a));
+                if (!ok) break;
+                unsigned z[BL][KS][2];                     // four keys of head elements 16j + g and 16j + g + 8
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
+                for (int b = 0; b < BL; ++b) {
                     const int row = b * 16 + (lane & 15);
-                    const uint32_t at_row = smem_u32(vs) + row * DP;
 #pragma unroll
-                    for (int i2 = 0; i2 < KS; i2 += 2) {
-                        const int chunk = i2 + (lane >> 4);
-                        unsigned c0, c1, c2, c3, a0, a1, a2, a3;
-                        ldmatrix_b8_trans(at_row + ((chunk ^ (DP == 128 ? row & 7 : (row >> 1) & 3)) << 4), c0, c1, c2, c3);
-                        decode_word<__half>(c0, minus, a0, a2);
-                        decode_word<__half>(c1, minus, a1, a3);
-#pragma unroll
-                        for (int q = 0; q < NQ; ++q) mma_16816<__half>(o[q][i2], a0, a1, a2, a3, pf[b][q]);
-                        decode_word<__half>(c2, minus, a0, a2);
-                        decode_word<__half>(c3, minus, a1, a3);
-#pragma unroll
-                        for (int q = 0; q < NQ; ++q) mma_16816<__half>(o[q][i2 + 1], a0, a1, a2, a3, pf[b][q]);
-                    }
+                    for (int j = 0; j < KS; j += 2)
+                        ldmatrix_b8_trans(smem_u32(vs) + row * DP + (((j + (lane >> 4)) ^ (DP == 128 ? row & 7 : (row >> 1) & 3)) << 4), z[b][j][0], z[b][j][1],
+                                          z[b][j + 1][0], z[b][j + 1][1]);
                 }
                 __syncwarp();
-                if (lane == 0 && i + kSmStages * kSmWarps < n_tiles) fetch(i + kSmStages * kSmWarps, stage);
+                if (more) fetch(i + 1, true);
+#pragma unroll
+                for (int b = 0; b < BL; ++b)
+#pragma unroll
+                    for (int j = 0; j < KS; ++j) {
+                        unsigned a0, a1, a2, a3;
+                        decode_word<__half>(z[b][j][0], minus, a0, a2);
+                        decode_word<__half>(z[b][j][1], minus, a1, a3);
+#pragma unroll
+                        for (int q = 0; q < NQ; ++q) mma_16816<__half>(o[q][j], a0, a1, a2, a3, pf[b][q]);
+                    }
+                if (lane == 0) *my_rounds = (int)it + 1;
             }
         }
         if (!ok) {                                             // copies in flight land before the block's memory is given up
             for (int i = 0; i < 64; ++i) __nanosleep(2000);
         }
 
-        // the four warps' parts: maxima first, then the sums at the common maximum
+        // through shared memory, so that a lane has four elements of a row side by side
 #pragma unroll
         for (int q = 0; q < NQ; ++q)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) l[q][h] += __shfl_xor_sync(0xffffffffu, l[q][h], d);
-                if (g == 0) {
-                    s_m[warp][8 * q + 2 * t + h] = m[q][h];
-                    s_l[warp][8 * q + 2 * t + h] = l[q][h];
-                }
-            }
-        __syncthreads();
-        auto common = [&](int r) {
-            float v = s_m[0][r];
-#pragma unroll
-            for (int w = 1; w < kSmWarps; ++w) v = fmaxf(v, s_m[w][r]);
-            return v;
-        };
         constexpr int LD = DP + 4;
-        float *const all = reinterpret_cast<float *>(smem);
+        float *const all = reinterpret_cast<float *>(ks), *const stats = all + 8 * LD;
         const int vecs = p.dim / 4;
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) {                         // eight rows at a time: the ring holds those of four warps
+        for (int q = 0; q < NQ; ++q) {
             if (q * 8 >= rows) break;
-            if (q > 0) __syncthreads();
+            __syncwarp();
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float top = common(8 * q + 2 * t + h), f = m[q][h] == -INFINITY ? 0.0f : ex2(m[q][h] - top);
-                float *row = all + (warp * 8 + 2 * t + h) * LD + g;
+                float *row = all + (2 * t + h) * LD + g;
 #pragma unroll
-                for (int i = 0; i < KS; ++i) row[16 * i] = o[q][i][h] * f, row[16 * i + 8] = o[q][i][2 + h] * f;
+                for (int i = 0; i < KS; ++i) row[16 * i] = o[q][i][h], row[16 * i + 8] = o[q][i][2 + h];
+                if (g == 0) stats[2 * (2 * t + h)] = m[q][h], stats[2 * (2 * t + h) + 1] = l[q][h];
             }
-            __syncthreads();
-            for (int i = threadIdx.x; i < 8 * vecs; i += kSmThreads) {
+            __syncwarp();
+            for (int i = lane; i < 8 * vecs; i += 32) {
                 const int lr = i / vecs, d = (i - lr * vecs) * 4, r = q * 8 + lr;
                 if (r >= rows) break;
-                float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-                float sum = 0.0f;
-                const float top = common(r);
-#pragma unroll
-                for (int w = 0; w < kSmWarps; ++w) {
-                    const float4 v = *reinterpret_cast<const float4 *>(all + (w * 8 + lr) * LD + d);
-                    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-                    sum += s_m[w][r] == -INFINITY ? s_l[w][r] : s_l[w][r] * ex2(s_m[w][r] - top);
-                }
+                const float4 v = *reinterpret_cast<const float4 *>(all + lr * LD + d);
+                const float top = stats[2 * lr], sum = stats[2 * lr + 1];
                 if (part.slot >= 0) {
                     const int64_t to = (int64_t)part.slot * ROWS + r;
-                    *reinterpret_cast<float4 *>(p.part_y + to * p.dim + d) = s;
+                    *reinterpret_cast<float4 *>(p.part_y + to * p.dim + d) = v;
                     if (d == 0) p.part_ml[to] = make_float4(top + e0, sum, e0, 0.0f);
                 } else {
-                    store_attention_row<T>(p, tile, head, r0 + r, d, s, sum, top, e0);
+                    store_attention_row<T>(p, tile, head, r0 + r, d, v, sum, top, e0);
                 }
             }
         }
-        fence_proxy_async_smem();                          // the ring is the TMA's again
+        fence_proxy_async_smem();                          // the buffers are the TMA's again
+        __syncwarp();
     }
+    __syncwarp();
+    if (lane == 0) *my_rounds = INT_MAX;
 }
 
 // ------------------------------------------------------------------ parts of a tile, joined
 
-// One block for each block of the attention kernel but the first: if the tile that it starts inside of is not shared with one
-// before the last, it joins the tile's parts at their common maximum, sixteen rows at a time.  part_ml.x is a part's maximum with
-// its exponent in it, so that parts whose values have other scales compare.
+// One block for each block of the attention kernel but the first.  Those that start inside one tile share its rows and join
+// its parts at their common maximum.  part_ml.x is a part's maximum with its exponent in it, so that parts whose values have other
+// scales compare.
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(128) cache_join_kernel(const CacheAttn p) {
+    __shared__ float4 s_sum[4][kCacheMaxDim / 4];
+    __shared__ float s_l[4];
     pdl_enter();
-    const int block = blockIdx.x + 1, n_blocks = __ldg(p.n_blocks);
-    const CacheStart before = p.starts[block - 1], start = p.starts[block];
+    const int block = blockIdx.x + 1, n_blocks = __ldg(p.n_blocks), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const CacheStart start = p.starts[block];
     if (block >= n_blocks || start.off == 0) return;
-    auto inside = [&](const CacheStart &s) { return s.tile == start.tile && s.head == start.head && s.off > 0; };
-    if (inside(before)) return;
-    int parts = 2;
-    while (block + parts - 1 < n_blocks && inside(p.starts[block + parts - 1])) ++parts;
+    // blocks in a row that start inside this tile, next to `block`, in direction `step`
+    auto count = [&](int step) {
+        int n = 0;
+        for (;;) {
+            const int i = block + step * (1 + n + lane);
+            bool in = false;
+            if (i >= 1 && i < n_blocks) {
+                const CacheStart s = p.starts[i];
+                in = s.tile == start.tile && s.head == start.head && s.off > 0;
+            }
+            const unsigned all = __ballot_sync(0xffffffffu, in);
+            if (all != 0xffffffffu) return n + __ffs(~all) - 1;
+            n += 32;
+        }
+    };
+    const int mine = count(-1), sharing = mine + 1 + count(1), first = block - mine, parts = sharing + 1;
     const CacheTile tile = p.tiles[start.tile];
-    const int r0 = blockIdx.y * kSmallRows, rows = min(ROWS, tile.n * p.group - tile.tile * ROWS), vecs = p.dim / 4;
-    // slots of the parts: the second one of the block before, then the first ones of this and those behind it
-    auto slot_of = [&](int k) { return (int64_t)(k == 0 ? 2 * block - 1 : 2 * (block + k - 1)) * ROWS; };
-    for (int i = threadIdx.x; i < kSmallRows * vecs; i += 128) {
-        const int r = r0 + i / vecs, d = (i - i / vecs * vecs) * 4;
-        if (r >= rows) break;
-        const float4 *ml = p.part_ml + r;
-        const float *y = p.part_y + (int64_t)r * p.dim + d;
+    const int rows = min(ROWS, tile.n * p.group - tile.tile * ROWS), d = lane * 4;
+    // slots of the parts: the second one of the block before, then the first ones of the blocks that start in the tile
+    auto slot_of = [&](int k) { return (int64_t)(k == 0 ? 2 * first - 1 : 2 * (first + k - 1)) * ROWS; };
+    auto add = [&](int r, int k, float m, float e, float4 &s, float &l) {
+        const float4 a = __ldcg(p.part_ml + slot_of(k) + r);
+        const float4 v = d < p.dim ? __ldcg(reinterpret_cast<const float4 *>(p.part_y + (slot_of(k) + r) * p.dim + d)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float w = a.x == -INFINITY ? 0.0f : ex2(a.x - m);
+        s.x += v.x * w, s.y += v.y * w, s.z += v.z * w, s.w += v.w * w;
+        l += (a.x == -INFINITY ? a.y : a.y * w) * ex2(e - a.z);
+    };
+    auto maximum = [&](int r) {
         float m = -INFINITY;
-#pragma unroll 4
-        for (int k = 0; k < parts; ++k) m = fmaxf(m, __ldcg(ml + slot_of(k)).x);
-        const float e = __ldcg(ml + slot_of(0)).z;
+        for (int k = lane; k < parts; k += 32) m = fmaxf(m, __ldcg(p.part_ml + slot_of(k) + r).x);
+#pragma unroll
+        for (int i = 16; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
+        return m;
+    };
+    if (ROWS == kLargeRows || parts <= 8) {
+        // a warp to a row; blockIdx.y takes a sixteenth of a large tile's rows
+        const int r1 = ROWS == kLargeRows ? min(rows, (int)(blockIdx.y + 1) * 16) : rows;
+        for (int r = (ROWS == kLargeRows ? blockIdx.y * 16 : 0) + mine + sharing * warp; r < r1; r += 4 * sharing) {
+            const float m = maximum(r), e = __ldcg(p.part_ml + slot_of(0) + r).z;
+            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+            float l = 0.0f;
+#pragma unroll 2
+            for (int k = 0; k < parts; ++k) add(r, k, m, e, s, l);
+            if (d < p.dim) store_attention_row<T>(p, tile, start.head, tile.tile * ROWS + r, d, s, l, m - e, e);
+        }
+        return;
+    }
+    // many parts: the four warps share them, row by row
+    for (int r = mine; r < rows; r += sharing) {
+        const float m = maximum(r), e = __ldcg(p.part_ml + slot_of(0) + r).z;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
         float l = 0.0f;
 #pragma unroll 4
-        for (int k = 0; k < parts; ++k) {
-            const float4 a = __ldcg(ml + slot_of(k)), v = __ldcg(reinterpret_cast<const float4 *>(y + slot_of(k) * p.dim));
-            const float w = a.x == -INFINITY ? 0.0f : ex2(a.x - m);
-            s.x += v.x * w, s.y += v.y * w, s.z += v.z * w, s.w += v.w * w;
-            l += (a.x == -INFINITY ? a.y : a.y * w) * ex2(e - a.z);
+        for (int k = warp; k < parts; k += 4) add(r, k, m, e, s, l);
+        s_sum[warp][lane] = s;
+        if (lane == 0) s_l[warp] = l;
+        __syncthreads();
+        if (warp == 0 && d < p.dim) {
+#pragma unroll
+            for (int w = 1; w < 4; ++w) {
+                const float4 v = s_sum[w][lane];
+                s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+                l += s_l[w];
+            }
+            store_attention_row<T>(p, tile, start.head, tile.tile * ROWS + r, d, s, l, m - e, e);
         }
-        store_attention_row<T>(p, tile, start.head, tile.tile * ROWS + r, d, s, l, m - e, e);
+        __syncthreads();
     }
 }
 

@@ -488,6 +488,10 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
             }
             if (ok && 32 * warp < rows) {                  // whole warps
                 const int64_t to_row = (int64_t)w.part.slot * kLargeRows + r;
+                const int token = (w.r0 + r) / p.group, h = head * p.group + (w.r0 + r - token * p.group);
+                T *y = static_cast<T *>(p.y) + (tile.row + token) * p.y_token + h * p.y_head;
+                // a row that sees no key: zeros (and minus infinity)
+                const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l), up = __uint_as_float((unsigned)((int)e0 + 127) << 23);
 #pragma unroll 1
                 for (int c = 0; c < DP / 16; ++c) {
                     uint32_t v[16];
@@ -498,19 +502,35 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
 #pragma unroll
                         for (int j = 0; j < 16; ++j) v[j] = 0u;
                     }
-                    if (r < rows && c * 16 < p.dim) {
+                    float f[16];                           // (columns lie as the values were decoded)
 #pragma unroll
-                        for (int j = 0; j < 16; j += 4) {
-                            // (columns lie as the values were decoded)
-                            const float4 s = make_float4(__uint_as_float(v[j]), __uint_as_float(v[j + 2]), __uint_as_float(v[j + 1]), __uint_as_float(v[j + 3]));
-                            const int d = c * 16 + j;
-                            if (w.part.slot >= 0) *reinterpret_cast<float4 *>(p.part_y + to_row * p.dim + d) = s;
-                            else store_attention_row<T>(p, tile, head, w.r0 + r, d, s, l, m, e0);
+                    for (int j = 0; j < 16; ++j) f[j] = __uint_as_float(v[(j & ~3) | ((j & 1) << 1) | ((j >> 1) & 1)]);
+                    if (r < rows && c * 16 < p.dim && DYBIT_CHECK(token < tile.n, 0x87)) {
+                        if (w.part.slot >= 0) {
+#pragma unroll
+                            for (int j = 0; j < 16; j += 4)
+                                *reinterpret_cast<float4 *>(p.part_y + to_row * p.dim + c * 16 + j) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
+                        } else {
+                            uint32_t u[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) u[j] = pack2<T>(f[2 * j] * inv * up, f[2 * j + 1] * inv * up);
+                            if (p.y_vec16) {
+                                *reinterpret_cast<uint4 *>(y + c * 16) = make_uint4(u[0], u[1], u[2], u[3]);
+                                *reinterpret_cast<uint4 *>(y + c * 16 + 8) = make_uint4(u[4], u[5], u[6], u[7]);
+                            } else {
+                                T e[16];
+                                memcpy(e, u, 32);
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) y[c * 16 + j] = e[j];
+                            }
                         }
                     }
                     __syncwarp();
                 }
-                if (w.part.slot >= 0 && r < rows) p.part_ml[to_row] = make_float4(m + e0, l, e0, 0.0f);
+                if (r < rows) {
+                    if (w.part.slot >= 0) p.part_ml[to_row] = make_float4(m + e0, l, e0, 0.0f);
+                    else if (p.lse != nullptr) p.lse[(int64_t)(tile.row + token) * (p.heads * p.group) + h] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+                }
                 tc_fence_before_sync();
             }
         }
