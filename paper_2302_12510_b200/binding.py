@@ -1046,9 +1046,9 @@ class CachePlan:
 def _heads3(x: torch.Tensor, name: str, T: int, heads: int, dim: int, code: Optional[int] = None) -> Tuple[int, int, int]:
     """Checks a tensor [T][heads][dim] with unit inner stride; returns (dybit_dtype, token stride, head stride)."""
     t = _DTYPE_CODE.get(x.dtype)
-    if t is None or not x.is_cuda or tuple(x.shape) != (T, heads, dim) or x.stride(2) != 1 or (code is not None and t != code):
+    st, sh, inner = x.stride() if x.dim() == 3 else (0, 0, 0)
+    if t is None or not x.is_cuda or x.shape != (T, heads, dim) or inner != 1 or (code is not None and t != code):
         raise ValueError(f"{name} must be a CUDA tensor [{T}][{heads}][{dim}] with unit inner stride, of float32, bfloat16 or float16 as its fellows")
-    st, sh, _ = x.stride()
     if (T > 1 and st < dim) or (heads > 1 and sh < dim):
         raise ValueError(f"the tokens and heads of {name} must not overlap")
     # (torch gives an axis of one entry any stride)
@@ -1071,13 +1071,17 @@ def dybit_cache_read(cache: KVCache, plan: CachePlan, dtype: torch.dtype = torch
     plan._for(cache)
     if dtype not in _DTYPE_CODE:
         raise ValueError("dtype must be float32, bfloat16 or float16")
-    shape = (plan.T, cache.heads, cache.dim)
-    if k is None:
-        k = _new(cache.k_codes, shape, dtype if v is None else v.dtype, stream)
-    if v is None:
-        v = _new(cache.k_codes, shape, k.dtype, stream)
-    t, kt, kh = _heads3(k, "k", *shape)
-    _, vt, vh = _heads3(v, "v", *shape, t)
+    T, H, D = shape = (plan.T, cache.heads, cache.dim)
+    kt, kh, vt, vh = H * D, D, H * D, D
+    if k is None and v is None:
+        t, k, v = _DTYPE_CODE[dtype], _new(cache.k_codes, shape, dtype, stream), _new(cache.k_codes, shape, dtype, stream)
+    else:
+        if k is None:
+            k = _new(cache.k_codes, shape, v.dtype, stream)
+        if v is None:
+            v = _new(cache.k_codes, shape, k.dtype, stream)
+        t, kt, kh = _heads3(k, "k", T, H, D)
+        _, vt, vh = _heads3(v, "v", T, H, D, t)
     _check(lib.dybit_cache_read(cache.ref, plan.ref, plan.address, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, t, _stream(stream)),
            "dybit_cache_read")
     return k, v

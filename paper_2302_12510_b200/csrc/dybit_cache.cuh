@@ -34,8 +34,11 @@ constexpr int kTileUnits = 1;                        // what a tile costs beside
 struct CacheItem { int row, pos, count, seq; };
 // A tile of query rows of one sequence: its number, its work and that of the tiles before it, in units, for each head.
 struct CacheTile { int row, n, len, seq, tile, units; int64_t first; };
-// Where a block starts in the work of all tiles and heads, head by head: `off` units into a tile.
-struct CacheStart { int tile, head, off, pad; };
+// Where a block starts in the work of all tiles and heads, head by head: `off` units into a tile, which it has a copy of.
+struct CacheStart {
+    int tile, head, off, pad;
+    CacheTile t;
+};
 // What one thread of the plan kernel knows of a sequence.
 struct CacheSeq { int row, n, len, items, small_tiles, large_tiles; };
 
@@ -63,8 +66,8 @@ struct CachePlanLayout {
         items = w, w += 4 * items_cap;
         small = w, w += 8 * small_cap;
         large = w, w += 8 * large_cap;
-        small_starts = w, w += 4 * (small_blocks(s.small_rows) + 1);
-        large_starts = w, w += large_cap > 0 ? 4 * (kLargeBlocks + 1) : 0;
+        small_starts = w, w += 12 * (small_blocks(s.small_rows) + 1);
+        large_starts = w, w += large_cap > 0 ? 12 * (kLargeBlocks + 1) : 0;
         words = w;
     }
 };
@@ -151,7 +154,7 @@ __device__ __forceinline__ int cache_deal(const CacheShape &s, const CacheTile *
             if (out[mid].first <= r) lo = mid;
             else hi = mid - 1;
         }
-        starts[c] = {lo, head, (int)(r - out[lo].first), 0};
+        starts[c] = {lo, head, (int)(r - out[lo].first), 0, out[lo]};
     }
     return blocks;
 }

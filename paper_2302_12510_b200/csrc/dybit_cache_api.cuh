@@ -165,6 +165,22 @@ static dybit_status launch_cache_small(const CUtensorMap &mk, const CUtensorMap 
     return launch_status();
 }
 
+// The kernel that joins parts.  It asks for the split of L1 and shared memory that the attention kernels have: an SM has to run
+// empty to change it.
+template <typename T, int ROWS>
+static dybit_status launch_cache_join(const CacheAttn &p, dim3 grid, cudaStream_t s) {
+    static std::atomic<int> ready[64];
+    int dev = 0;
+    DYBIT_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return DYBIT_ERR_CUDA;
+    if (ready[dev].load(std::memory_order_acquire) == 0) {
+        DYBIT_CUDA_TRY(cudaFuncSetAttribute(cache_join_kernel<T, ROWS>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
+        ready[dev].store(1, std::memory_order_release);
+    }
+    launch_k(cache_join_kernel<T, ROWS>, grid, dim3(128), 0, s, p);
+    return launch_status();
+}
+
 template <typename T, int DP>
 static dybit_status launch_cache_large(const dybit_cache *c, const CacheAttn &p, cudaStream_t s) {
     static std::atomic<int> ready[64];
@@ -223,13 +239,11 @@ static dybit_status run_cache_attention(const dybit_cache *c, const CacheShape &
     st = dp == 64 ? (few ? go(d64(), one()) : go(d64(), two())) : (few ? go(d128(), one()) : go(d128(), two()));
     if (st != DYBIT_OK) return st;
     if (L.large_cap > 0) {
-        launch_k(cache_join_kernel<T, kLargeRows>, dim3(kLargeBlocks - 1, 16), dim3(128), 0, s, large);
-        st = launch_status();
+        st = launch_cache_join<T, kLargeRows>(large, dim3(kLargeBlocks - 1, 16), s);
         if (st != DYBIT_OK) return st;
     }
-    if (few) launch_k(cache_join_kernel<T, 8>, dim3(small_blocks(8) - 1), dim3(128), 0, s, small);
-    else launch_k(cache_join_kernel<T, kSmallRows>, dim3(small_blocks(kSmallRows) - 1), dim3(128), 0, s, small);
-    st = launch_status();
+    if (few) st = launch_cache_join<T, 8>(small, dim3(small_blocks(8) - 1), s);
+    else st = launch_cache_join<T, kSmallRows>(small, dim3(small_blocks(kSmallRows) - 1), s);
     return st;
 }
 

@@ -123,11 +123,14 @@ struct CachePart {
     int head, from, to, slot;
 };
 
-// The next part of a block's share, which ends at `end`; false where there is none.  A part that starts inside a tile is
-// the block's first, one that ends inside a tile its last: two slots to a block are enough.
-__device__ __forceinline__ bool cache_next(const CacheAttn &p, int block, CacheStart &at, const CacheStart &end, int n_tiles, CachePart &part) {
+// Where a block is in the work.
+struct CachePlace { int tile, head, off; };
+__device__ __forceinline__ CachePlace cache_place(const CacheStart &s) { return {s.tile, s.head, s.off}; }
+
+// The next part of a block's share, which ends at `end`; false where there is none.  part.tile is the tile at `at` already.  A part
+// that starts inside a tile is the block's first, one that ends inside a tile its last: two slots to a block are enough.
+__device__ __forceinline__ bool cache_next(const CacheAttn &p, int block, CachePlace &at, const CachePlace &end, int n_tiles, CachePart &part) {
     if (at.head > end.head || (at.head == end.head && (at.tile > end.tile || (at.tile == end.tile && at.off >= end.off)))) return false;
-    part.tile = p.tiles[at.tile];
     part.head = at.head;
     part.from = at.off;
     part.to = at.head == end.head && at.tile == end.tile ? min(end.off, part.tile.units) : part.tile.units;
@@ -235,8 +238,10 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     __syncthreads();
     pdl_enter();
     const int block = warp * (int)gridDim.x + (int)blockIdx.x, n_tiles = __ldg(p.n_tiles), n_blocks = __ldg(p.n_blocks);
-    CacheStart at = p.starts[block];
-    const CacheStart end = p.starts[block + 1];
+    CachePart part;
+    part.tile = p.starts[block].t;
+    CachePlace at = cache_place(p.starts[block]);
+    const CachePlace end = cache_place(p.starts[block + 1]);
     if (block >= n_blocks) {
         if (lane == 0) *my_rounds = INT_MAX;
         return;
@@ -246,7 +251,6 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     uint32_t it = 0;                                       // rounds so far
     bool ok = true;
 
-    CachePart part;
     while (ok && cache_next(p, block, at, end, n_tiles, part)) {
         const CacheTile &tile = part.tile;
         const int head = part.head, r0 = tile.tile * ROWS, rows = min(ROWS, tile.n * p.group - r0);
@@ -286,14 +290,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             }
         }
 
-        // exponent of the first page's value scale
-        float e0 = 0.0f;
-        if (range.last > range.first) {
-            const int pg = __ldg(table + (range.first >> p.page_shift));
-            const float s = (unsigned)pg < (uint64_t)p.pages ? __ldg(p.v_scales + (int64_t)pg * p.heads + head) : 0.0f;
-            e0 = s > 0.0f ? (float)((int)((__float_as_uint(s) >> 23) & 255u) - 127) : 0.0f;
-        }
-
+        float e0 = 0.0f;                                   // exponent of the first keys' value scale
         // output i: head elements 16i + g (o[0], o[1]) and 16i + g + 8 (o[2], o[3]) of rows 8q + 2t and 8q + 2t + 1
         float o[NQ][KS][4], m[NQ][2], l[NQ][2];
 #pragma unroll
@@ -306,20 +303,36 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         for (int seg = range.first; seg < range.last && ok; seg += kSmSegment) {
             const int seg_end = min(range.last, seg + kSmSegment);
             __syncwarp();
-            for (int i = lane; i < (seg_end - seg) / BOX; i += 32) {
+            const int boxes = (seg_end - seg) / BOX, none = (int)(p.pages * p.heads);      // a coordinate outside the pool reads as zeros
+            auto box_of = [&](int i) {
                 const int key = seg + BOX * i;
-                const int pg = key < tile.len ? __ldg(table + (key >> p.page_shift)) : -1;
-                const int none = (int)(p.pages * p.heads);     // a coordinate outside the pool reads as zeros
-                KeyBlock b = {0.0f, -INFINITY, 0.0f, key & ((1 << p.page_shift) - 1), none, none};      // not there: seen by no row
-                if ((unsigned)pg < (uint64_t)p.pages) {
-                    b.z = (int)((int64_t)pg * p.heads + head);
-                    const float ks = __ldg(p.k_scales + b.z), vs = __ldg(p.v_scales + b.z);
-                    b.c = ks * p.scale_log2;
-                    b.zv = vs > 0.0f ? b.z : none;
-                    b.e = vs > 0.0f ? (float)((int)((__float_as_uint(vs) >> 23) & 255u) - 127) - e0 : 0.0f;
+                const int pg = i < boxes && key < tile.len ? __ldg(table + (key >> p.page_shift)) : -1;
+                return (unsigned)pg < (uint64_t)p.pages ? (int)((int64_t)pg * p.heads + head) : none;
+            };
+            int z = box_of(lane);
+            if (lane < NB) {                               // the first keys are on their way before anything else is known
+                if (lane == 0) mbar_arrive_expect_tx(k_full, kSmBytes);
+                __syncwarp((1u << NB) - 1u);
+                tma_load_3d(ks + lane * BOX * DP, &map_k, 0, (seg + BOX * lane) & ((1 << p.page_shift) - 1), z, k_full);
+            }
+            __syncwarp();
+            for (int i0 = 0; i0 < boxes; i0 += 32) {
+                const int i = i0 + lane;
+                KeyBlock b = {0.0f, -INFINITY, 0.0f, (seg + BOX * i) & ((1 << p.page_shift) - 1), z, none};      // not there: seen by no row
+                float vs = 0.0f;
+                if (z != none) {
+                    vs = __ldg(p.v_scales + z);
+                    b.c = __ldg(p.k_scales + z) * p.scale_log2;
+                    b.zv = vs > 0.0f ? z : none;
+                }
+                const float e = vs > 0.0f ? (float)((int)((__float_as_uint(vs) >> 23) & 255u) - 127) : 0.0f;
+                if (i0 == 0 && seg == range.first) e0 = __shfl_sync(0xffffffffu, e, 0);
+                if (z != none) {
+                    b.e = vs > 0.0f ? e - e0 : 0.0f;
                     b.f = __uint_as_float((unsigned)(127 - max(-126, min(126, (int)b.e))) << 23);
                 }
-                s_block[i] = b;
+                if (i < boxes) s_block[i] = b;
+                z = box_of(i + 32);
             }
             __syncwarp();
             const int rounds = (seg_end - seg) / KEYS;
@@ -332,10 +345,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                     tma_load_3d((values ? vs : ks) + b * BOX * DP, values ? &map_v : &map_k, 0, k.y, values ? k.zv : k.z, bar);
                 }
             };
-            if (lane == 0) {
-                fetch(0, false);
-                fetch(0, true);
-            }
+            if (lane == 0) fetch(0, true);
             __syncwarp();
             for (int i = 0; i < rounds; ++i, ++it) {
                 const bool more = lane == 0 && i + 1 < rounds;
@@ -512,6 +522,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 }
             }
         }
+        part.tile = p.tiles[at.tile];
         fence_proxy_async_smem();                          // the buffers are the TMA's again
         __syncwarp();
     }

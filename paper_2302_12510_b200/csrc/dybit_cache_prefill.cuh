@@ -1,46 +1,54 @@
 // Attention over the 8-bit cache for tiles of 256 query rows: both products on the tensor cores (tcgen05).
 //
-// A block of the tile takes its keys 128 at a time.  Roles, a warp each or several:
+// A block takes a tile's keys 64 at a time.  Roles, a warp each or several:
 //   decode    codes -> f16 or bf16 keys and f16 values in shared memory, in the operands' swizzled layouts (nothing but
 //             codes crosses the memory system, and the 256 rows share what is decoded); four warps for keys, four for values
-//   issue     S_t = Q_t K^T into TMEM and O_t += P_t V with P_t read from TMEM, for the two halves t of the rows in turn
+//   issue     a warp to each half t of the rows: S_t = Q_t K^T into TMEM and O_t += P_t V with P_t read from TMEM
 //   softmax   four warps to a half, a thread to a row: S_t -> P_t in place (f16), the running maximum and sum, and now and then a
 //             factor on O_t
-// While one half's scores are on their way through the softmax the tensor core works for the other half.  Per 128 keys
-// and SM the products take 2048 clocks of the tensor core, the exponentials 2048 of the special-function units, decoding
-// and softmax together about 1800 issue slots of each scheduler, and the operands about 2048 clocks of shared memory.
+// Scores have two buffers for each half and run two blocks ahead, so that the softmax warps find the next block's ready.
+// Per 128 keys and SM the products take 2048 clocks of the tensor core, the exponentials 2048 of the special-function units,
+// decoding and softmax together about 1800 issue slots of each scheduler, and the operands about 2300 clocks of shared memory.
 #pragma once
 
 #include "dybit_cache_attention.cuh"
 
 namespace dybit {
 
-constexpr int kLgKeys = 128;                 // keys of a block
-constexpr int kLgWarps = 17, kLgThreads = 32 * kLgWarps;     // 2 x 4 softmax, 4 + 4 decode, 1 issue
-constexpr int kLgStages = 2;
+constexpr int kLgKeys = 64;                  // keys of a block
+constexpr int kLgThreads = 576;              // warps: 2 x 4 softmax, 4 + 4 decode, 2 issue
+constexpr int kLgStages = 4;
 
-template <int DP> __host__ __device__ constexpr int large_panel_bytes() { return 128 * 128; }       // 128 rows of 64 16-bit elements
-template <int DP> __host__ __device__ constexpr int large_tile_bytes() { return (DP / 64) * 128 * 128; }
-template <int DP> __host__ __device__ constexpr int large_smem_bytes() { return (2 + 2 * kLgStages) * large_tile_bytes<DP>() + 1024; }
+constexpr int kLgQPanel = 128 * 128, kLgPanel = kLgKeys * 128;       // bytes of 64 head elements of a half's queries, of a block's keys or values
+template <int DP> __host__ __device__ constexpr int large_smem_bytes() { return (DP / 64) * (2 * kLgQPanel + 2 * kLgStages * kLgPanel) + 1024; }
 
-// Operand whose rows (128 bytes, 64 columns) run along the contraction: groups of eight rows 1024 bytes apart, the next 64 columns a
-// panel further on.
-__device__ __forceinline__ uint64_t large_desc_values(uint32_t smem_addr) {
-    uint64_t d = 0;
-    d |= (uint64_t)((smem_addr & 0x3ffffu) >> 4);
-    d |= (uint64_t)((128 * 128) >> 4) << 16;
-    d |= (uint64_t)(1024 >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
-}
+// Descriptor of an operand whose rows (128 bytes, 64 columns) run along the contraction: groups of eight rows 1024 bytes apart, the
+// next 64 columns a panel further on.
+__device__ __forceinline__ uint32_t large_values_lo(uint32_t smem_addr) { return ((smem_addr & 0x3ffffu) >> 4) | ((uint32_t)(kLgPanel >> 4) << 16); }
+__host__ __device__ constexpr uint32_t large_values_hi() { return (uint32_t)(1024 >> 4) | (1u << 14) | (2u << 29); }
 
-// D (128 x N, TMEM) += A (128 x 16 f16, TMEM, two elements to a column) * B
-__device__ __forceinline__ void umma_ts_f16(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+// What an issuing warp asks of the tensor core: all lanes take part, one of them issues.  (A warp that stays together keeps addresses
+// and descriptors in uniform registers, where the instructions want them.)
+//   D (128 x N, TMEM) (+)= A (128 x 16, shared memory) * B
+__device__ __forceinline__ void umma_ss_elect(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(tmem_d),
-        "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        "{\n.reg .pred p, q;\n.reg .b64 da, db;\nelect.sync _|q, 0xffffffff;\nsetp.ne.b32 p, %5, 0;\nmov.b64 da, {%1, %3};\nmov.b64 db, {%2, %3};\n"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n}\n" ::"r"(tmem_d),
+        "r"(a_lo), "r"(b_lo), "r"(desc_hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+//   D (128 x N, TMEM) (+)= A (128 x 16 f16, TMEM, two elements to a column) * B
+__device__ __forceinline__ void umma_ts_elect(uint32_t tmem_d, uint32_t tmem_a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n.reg .pred p, q;\n.reg .b64 db;\nelect.sync _|q, 0xffffffff;\nsetp.ne.b32 p, %5, 0;\nmov.b64 db, {%2, %3};\n"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n}\n" ::"r"(tmem_d),
+        "r"(tmem_a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// Arrives on the barrier once every product that the warp has asked for is done (the same lane is elected every time).
+__device__ __forceinline__ void umma_commit_elect(uint32_t bar_addr) {
+    asm volatile(
+        "{\n.reg .pred q;\nelect.sync _|q, 0xffffffff;\n@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar_addr)
         : "memory");
 }
 
@@ -55,6 +63,14 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r
 __device__ __forceinline__ void tmem_st_32x8(uint32_t taddr, const uint32_t (&r)[8]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
                  "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr)
+                 : "memory");
+}
+// The wait for a load whose registers are used behind it only.
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
+                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :
                  : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -94,7 +110,8 @@ struct LargePart {
     const int *table;
 };
 
-__device__ __forceinline__ bool large_next(const CacheAttn &p, CacheStart &at, const CacheStart &end, int n_tiles, LargePart &w) {
+__device__ __forceinline__ bool large_next(const CacheAttn &p, CachePlace &at, const CachePlace &end, int n_tiles, LargePart &w) {
+    w.part.tile = p.tiles[at.tile];
     if (!cache_next(p, blockIdx.x, at, end, n_tiles, w.part)) return false;
     const CacheTile &t = w.part.tile;
     w.r0 = t.tile * kLargeRows;
@@ -131,35 +148,35 @@ __device__ __forceinline__ int large_page(const CacheAttn &p, const int *table, 
 template <typename T, int DP, bool VALUES>
 __device__ __forceinline__ bool large_decode(const CacheAttn &p, const LargePart &t, const uint8_t *__restrict__ codes, uint8_t *tiles, uint64_t *full,
                                              uint64_t *empty, volatile uint32_t *abort_flag, uint32_t &n) {
-    constexpr int UNITS = DP / 16, ROWS = 128 / UNITS, PASSES = kLgKeys / ROWS, HALF = PASSES / 2, PANEL = large_panel_bytes<DP>();
+    constexpr int UNITS = DP / 16, ROWS = 128 / UNITS, PASSES = kLgKeys / ROWS, HALF = PASSES / 2, TILE = (DP / 64) * kLgPanel;
     const int lane = threadIdx.x & 31, i = threadIdx.x & 127, u = i % UNITS, row0 = i / UNITS;
     const bool in_dim = u * 16 < p.dim;
     const int page_mask = (1 << p.page_shift) - 1;
     const int64_t page_bytes = (int64_t)p.heads * p.dim << p.page_shift;
     const int head = t.part.head;
     const uint8_t *base = codes + ((int64_t)head * p.dim << p.page_shift) + u * 16;
-    auto load = [&](int key, int pg) {
+    auto load = [&](int key, int pg) {                     // key: its number in the sequence
         uint4 v = make_uint4(0u, 0u, 0u, 0u);
         if (pg >= 0 && in_dim) v = __ldg(reinterpret_cast<const uint4 *>(base + pg * page_bytes + (key & page_mask) * p.dim));
         return v;
     };
-    auto page_at = [&](int b) { return b < t.last ? large_page(p, t.table, t.part.tile.len, b * kLgKeys + 16 * (lane & 7)) : -1; };
+    auto page_at = [&](int b) { return b < t.last ? large_page(p, t.table, t.part.tile.len, b * kLgKeys + 16 * (lane & 3)) : -1; };
     // values whose scale is 0 are zeros whatever their codes
     auto held = [&](int pg) { return !VALUES || (pg >= 0 && __ldg(p.v_scales + (int64_t)pg * p.heads + head) > 0.0f); };
-    // lane k < 8 has the page of 16 keys k of a block
+    // lane k < 4 has the page of 16 keys k of a block
     int page_now = page_at(t.first), page_next = page_at(t.first + 1);
     bool held_now = held(page_now);
     uint4 c[HALF];
 #pragma unroll
     for (int s = 0; s < HALF; ++s) {
         const int key = row0 + s * ROWS;
-        c[s] = load(key, __shfl_sync(0xffffffffu, page_now, key >> 4));
+        c[s] = load(t.first * kLgKeys + key, __shfl_sync(0xffffffffu, page_now, key >> 4));
     }
     // threads of the second panel store their second half first: eight lanes then fill eight different 16-byte columns
     const bool swap = DP == 128 && (u & 4) != 0;
     const int chunk = 2 * (u & 3) + (swap ? 1 : 0);
     const unsigned minus = p.minus_one;
-    uint8_t *const dst0 = tiles + (u >> 2) * PANEL + row0 * 128;
+    uint8_t *const dst0 = tiles + (u >> 2) * kLgPanel + row0 * 128;
     for (int b = t.first; b < t.last; ++b, ++n) {
         const uint32_t stage = n % kLgStages;
         const int page_after = page_at(b + 2);
@@ -168,14 +185,14 @@ __device__ __forceinline__ bool large_decode(const CacheAttn &p, const LargePart
         const uint32_t holds = __ballot_sync(0xffffffffu, held_now);
 #pragma unroll 1
         for (int h = 0; h < 2; ++h) {
-            uint8_t *dst = dst0 + stage * large_tile_bytes<DP>() + h * (HALF * ROWS * 128);
+            uint8_t *dst = dst0 + stage * TILE + h * (HALF * ROWS * 128);
             const int ahead = h == 0 ? page_now : page_next;
 #pragma unroll
             for (int s = 0; s < HALF; ++s) {
                 const int key = row0 + (h * HALF + s) * ROWS, next = row0 + ((h ^ 1) * HALF + s) * ROWS;
                 uint4 w = c[s];
                 if (VALUES && !((holds >> (key >> 4)) & 1u)) w = make_uint4(0u, 0u, 0u, 0u);
-                c[s] = load(next, __shfl_sync(0xffffffffu, ahead, next >> 4));
+                c[s] = load((b + h) * kLgKeys + next, __shfl_sync(0xffffffffu, ahead, next >> 4));
                 const unsigned a0 = swap ? w.z : w.x, a1 = swap ? w.w : w.y, a2 = swap ? w.x : w.z, a3 = swap ? w.y : w.w;
                 uint4 lo, hi;
                 decode_word<T>(a0, minus, lo.x, lo.y);
@@ -195,27 +212,28 @@ __device__ __forceinline__ bool large_decode(const CacheAttn &p, const LargePart
     return true;
 }
 
-// The largest of a row's 128 scores (TMEM address ts), times 16 keys' factor plus their exponent.
+// The largest of a row's scores (TMEM address ts), times 16 keys' factor plus their exponent.  The loops of all roles are kept
+// short: written out they no longer fit the instruction caches together, and a block of keys took twice the time.
 template <bool EDGE>
 __device__ __forceinline__ float large_row_max(uint32_t ts, const float4 *blk, int lo, int hi) {
     float top = -INFINITY;
 #pragma unroll 2
-    for (int c = 0; c < 8; ++c) {
-        uint32_t v[16];
-        tmem_ld_32x16(ts + c * 16, v);
+    for (int c = 0; c < kLgKeys / 16; ++c) {
+        uint32_t x[16];
+        tmem_ld_32x16(ts + c * 16, x);
         const float4 f = blk[c];
-        tmem_ld_wait();
+        tmem_ld_wait_for(x);
         if (EDGE) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                const float x = __fmaf_rn(__uint_as_float(v[j]), f.x, f.y);
-                top = c * 16 + j >= lo && c * 16 + j < hi ? fmaxf(top, x) : top;
+                const float y = __fmaf_rn(__uint_as_float(x[j]), f.x, f.y);
+                top = c * 16 + j >= lo && c * 16 + j < hi ? fmaxf(top, y) : top;
             }
-        } else {                                           // the factor is not negative: the largest product has the largest x
-            float a = __uint_as_float(v[0]);
+        } else {                                           // the factor is not negative: the largest product has the largest score
+            float a = __uint_as_float(x[0]);
 #pragma unroll
-            for (int j = 1; j < 15; j += 2) a = fmaxf(fmaxf(a, __uint_as_float(v[j])), __uint_as_float(v[j + 1]));
-            a = fmaxf(a, __uint_as_float(v[15]));
+            for (int j = 1; j < 15; j += 2) a = fmaxf(fmaxf(a, __uint_as_float(x[j])), __uint_as_float(x[j + 1]));
+            a = fmaxf(a, __uint_as_float(x[15]));
             top = fmaxf(top, __fmaf_rn(a, f.x, f.y));
         }
     }
@@ -226,28 +244,28 @@ __device__ __forceinline__ float large_row_max(uint32_t ts, const float4 *blk, i
 template <bool EDGE>
 __device__ __forceinline__ float large_row_exp(uint32_t ts, const float4 *blk, int lo, int hi, float um, float l) {
 #pragma unroll 2
-    for (int c = 0; c < 8; ++c) {
-        uint32_t v[16], pr[8];
-        tmem_ld_32x16(ts + c * 16, v);
+    for (int c = 0; c < kLgKeys / 16; ++c) {
+        uint32_t x[16], pr[8];
+        tmem_ld_32x16(ts + c * 16, x);
         const float4 f = blk[c];
         const float shift = f.y - um;
         const uint64_t cc = pack_f32x2(f.x, f.x), ss = pack_f32x2(shift, shift);
         uint64_t sum = 0;
-        tmem_ld_wait();
+        tmem_ld_wait_for(x);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float2 x = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), cc, ss));
+            float2 s = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), cc, ss));
             if (EDGE) {
-                if (c * 16 + 2 * j < lo || c * 16 + 2 * j >= hi) x.x = -INFINITY;
-                if (c * 16 + 2 * j + 1 < lo || c * 16 + 2 * j + 1 >= hi) x.y = -INFINITY;
+                if (c * 16 + 2 * j < lo || c * 16 + 2 * j >= hi) s.x = -INFINITY;
+                if (c * 16 + 2 * j + 1 < lo || c * 16 + 2 * j + 1 >= hi) s.y = -INFINITY;
             }
-            x.x = ex2(x.x), x.y = ex2(x.y);
-            sum = j == 0 ? pack_f32x2(x.x, x.y) : add_f32x2(sum, pack_f32x2(x.x, x.y));
-            pr[j] = pack_f16(x.x, x.y);
+            s.x = ex2(s.x), s.y = ex2(s.y);
+            sum = j == 0 ? pack_f32x2(s.x, s.y) : add_f32x2(sum, pack_f32x2(s.x, s.y));
+            pr[j] = pack_f16(s.x, s.y);
         }
         const float2 s = unpack_f32x2(sum);
         l = __fmaf_rn(s.x + s.y, f.z, l);
-        tmem_st_32x8(ts + c * 8, pr);
+        tmem_st_32x8(ts + c * 8, pr);                      // (columns whose scores have been read)
     }
     return l;
 }
@@ -255,27 +273,30 @@ __device__ __forceinline__ float large_row_exp(uint32_t ts, const float4 *blk, i
 template <typename T, int DP>
 __global__ void __launch_bounds__(kLgThreads, 1)
 cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restrict__ v_codes, const CacheAttn p) {
-    constexpr int KS = DP / 16, PANEL = large_panel_bytes<DP>(), TILE = large_tile_bytes<DP>();
+    constexpr int KS = DP / 16, QTILE = (DP / 64) * kLgQPanel, TILE = (DP / 64) * kLgPanel;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t *s_q = smem, *s_k = smem + 2 * TILE, *s_v = s_k + kLgStages * TILE;
-    __shared__ uint64_t k_full[kLgStages], k_empty[kLgStages], v_full[kLgStages], v_empty[kLgStages], q_full[2], s_full[2], p_full[2], o_full[2];
+    uint8_t *s_q = smem, *s_k = smem + 2 * QTILE, *s_v = s_k + kLgStages * TILE;
+    // s_full, p_full: per half and score buffer;  o_done: a half's products with values, block by block
+    __shared__ uint64_t k_full[kLgStages], k_empty[kLgStages], v_full[kLgStages], v_empty[kLgStages], q_full[2], s_full[2][2], p_full[2][2], o_done[2];
     __shared__ uint32_t s_tmem, s_abort;
-    __shared__ float4 s_info[8][2][8];                     // softmax warp, parity, 16 keys: {x's factor, values' exponent, 2^-exponent, -}
+    __shared__ float4 s_info[8][2][kLgKeys / 16];          // softmax warp, parity, 16 keys: {x's factor, values' exponent, 2^-exponent, -}
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kLgStages; ++s) {
             mbar_init(&k_full[s], 4);
-            mbar_init(&k_empty[s], 1);
+            mbar_init(&k_empty[s], 2);
             mbar_init(&v_full[s], 4);
-            mbar_init(&v_empty[s], 1);
+            mbar_init(&v_empty[s], 2);
         }
         for (int t = 0; t < 2; ++t) {
             mbar_init(&q_full[t], 4);
-            mbar_init(&s_full[t], 1);
-            mbar_init(&p_full[t], 4);
-            mbar_init(&o_full[t], 1);
+            mbar_init(&o_done[t], 1);
+            for (int j = 0; j < 2; ++j) {
+                mbar_init(&s_full[t][j], 1);
+                mbar_init(&p_full[t][j], 4);
+            }
         }
         s_abort = 0;
         fence_mbar_init();
@@ -289,10 +310,10 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
     tc_fence_after_sync();
     pdl_enter();
     const int n_tiles = __ldg(p.n_tiles), n_blocks = __ldg(p.n_blocks);
-    CacheStart at = p.starts[blockIdx.x], end = at;
-    if ((int)blockIdx.x < n_blocks) end = p.starts[blockIdx.x + 1];
+    CachePlace at = {0, 0, 0}, end = {0, 0, 0};
+    if ((int)blockIdx.x < n_blocks) at = cache_place(p.starts[blockIdx.x]), end = cache_place(p.starts[blockIdx.x + 1]);
     const uint32_t tmem = s_tmem;
-    // columns: scores of the halves (their first 64 become the probabilities), then the outputs
+    // columns: two buffers of 64 scores for each half (32 of which become the probabilities), then the outputs
     const uint32_t t_o = tmem + 256;
     LargePart w;
 
@@ -306,111 +327,102 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
         } else {
             while (large_next(p, at, end, n_tiles, w) && large_decode<__half, DP, true>(p, w, v_codes, s_v, v_full, v_empty, &s_abort, n)) {}
         }
-    } else if (warp == 16) {
-        // ------------------------------------------------ issue
-        if (lane == 0) {
-            constexpr uint32_t ab = __is_same(T, __half) ? 0u : 1u;
-            constexpr uint32_t idesc_s = umma_idesc(1u, ab, 128, kLgKeys), idesc_o = umma_idesc(1u, 0u, 128, DP) | (1u << 16);
-            uint32_t phase_p[2] = {0, 0}, phase_q[2] = {0, 0}, n = 0;      // n: blocks so far
-            bool ok = true;
-            auto scores = [&](int t, uint32_t stage) {
-                const uint32_t qa = smem_u32(s_q + t * TILE), ka = smem_u32(s_k + stage * TILE);
+    } else if (warp >= 16) {
+        // ------------------------------------------------ issue: warp 16 + t for half t
+        constexpr uint32_t ab = __is_same(T, __half) ? 0u : 1u;
+        constexpr uint32_t idesc_s = umma_idesc(1u, ab, 128, kLgKeys), idesc_o = umma_idesc(1u, 0u, 128, DP) | (1u << 16);
+        const int t = warp - 16;
+        const uint32_t d_s = tmem + t * 128, d_o = t_o + t * 128, q_lo = umma_desc_lo(smem_u32(s_q + t * QTILE));
+        const uint32_t k_lo = umma_desc_lo(smem_u32(s_k)), v_lo = large_values_lo(smem_u32(s_v));
+        uint32_t done = 0, asked = 0, parts = 0, n = 0;    // blocks so far: of the half (outputs, scores), its parts, blocks of both halves
+        bool ok = true;
+        auto uniform = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
+        while (ok && large_next(p, at, end, n_tiles, w)) {
+            const int first = uniform(w.first), last = uniform(w.last), h_first = uniform(t == 0 ? w.half[0].first : w.half[1].first),
+                      h_last = uniform(t == 0 ? w.half[0].last : w.half[1].last);
+            // the half's queries are there, and the part before has taken what lies in its columns
+            if (h_first < h_last) ok = __all_sync(0xffffffffu, wait_bounded(&q_full[t], parts++ & 1u, &s_abort, 0x89));
+            // scores run two blocks ahead of the outputs
+#pragma unroll 1
+            for (int b = first - 2; ok && b < last; ++b) {
+                if (b >= first) {
+                    const uint32_t stage = n % kLgStages;
+                    // (a half that does not see the block lets go of it in its turn all the same, once it has been there)
+                    ok = __all_sync(0xffffffffu, wait_bounded(&v_full[stage], (n / kLgStages) & 1u, &s_abort, 0x84));
+                    if (ok && b >= h_first && b < h_last) {
+                        ok = __all_sync(0xffffffffu, wait_bounded(&p_full[t][done & 1u], (done >> 1) & 1u, &s_abort, 0x85));
+                        if (!ok) break;
+                        tc_fence_after_sync();
+                        const uint32_t a = d_s + (done & 1u) * 64, v = v_lo + stage * (TILE >> 4);
 #pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    const uint32_t off = (uint32_t)((k >> 2) * PANEL + (k & 3) * 32);
-                    umma<Kind::F16>(tmem + t * 128, umma_desc_kmajor<128>(qa + off), umma_desc_kmajor<128>(ka + off), idesc_s, (uint32_t)(k != 0));
-                }
-                umma_commit(&s_full[t]);
-            };
-            auto outputs = [&](int t, uint32_t stage, bool first) {
-                const uint64_t vd = large_desc_values(smem_u32(s_v + stage * TILE));
-#pragma unroll
-                for (int k = 0; k < kLgKeys / 16; ++k)     // 16 keys are 2048 bytes of values and 8 columns of probabilities
-                    umma_ts_f16(t_o + t * 128, tmem + t * 128 + k * 8, vd + (uint64_t)(k * 128), idesc_o, (uint32_t)(!first || k != 0));
-            };
-            while (ok && large_next(p, at, end, n_tiles, w)) {
-                auto active = [&](int t, int b) { return b >= w.half[t].first && b < w.half[t].last; };
-                if (w.first == w.last) continue;
-                // a half's queries are there, and the part before has taken what lies in its columns
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    if (ok && w.half[t].first < w.half[t].last) {
-                        ok = wait_bounded(&q_full[t], phase_q[t], &s_abort, 0x89);
-                        phase_q[t] ^= 1u;
+                        for (int k = 0; k < kLgKeys / 16; ++k)         // 16 keys are 2048 bytes of values and 8 columns of probabilities
+                            umma_ts_elect(d_o, a + k * 8, v + k * 128, large_values_hi(), idesc_o, (uint32_t)(b != h_first || k != 0));
+                        umma_commit_elect(smem_u32(&o_done[t]));
+                        ++done;
                     }
-                if (ok) ok = wait_bounded(&k_full[n % kLgStages], (n / kLgStages) & 1u, &s_abort, 0x83);
-                if (!ok) break;
-                tc_fence_after_sync();
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    if (active(t, w.first)) scores(t, n % kLgStages);
-                umma_commit(&k_empty[n % kLgStages]);
-                for (int b = w.first; b < w.last; ++b, ++n) {
-                    const uint32_t stage = n % kLgStages, next = (n + 1) % kLgStages;
-                    ok = wait_bounded(&v_full[stage], (n / kLgStages) & 1u, &s_abort, 0x84);
-                    bool fetched = false;
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        if (ok && active(t, b)) {
-                            ok = wait_bounded(&p_full[t], phase_p[t], &s_abort, 0x85);
-                            phase_p[t] ^= 1u;
-                            tc_fence_after_sync();
-                            if (ok) {
-                                outputs(t, stage, b == w.half[t].first);
-                                if (!active(t, b + 1)) umma_commit(&o_full[t]);
-                            }
-                        }
-                        if (ok && b + 1 < w.last && active(t, b + 1)) {
-                            if (!fetched) {
-                                ok = wait_bounded(&k_full[next], ((n + 1) / kLgStages) & 1u, &s_abort, 0x86);
-                                tc_fence_after_sync();
-                                fetched = true;
-                            }
-                            if (ok) scores(t, next);
-                        }
-                    }
-                    if (ok && b + 1 < w.last && !fetched) ok = wait_bounded(&k_full[next], ((n + 1) / kLgStages) & 1u, &s_abort, 0x86);
                     if (!ok) break;
-                    umma_commit(&v_empty[stage]);
-                    if (b + 1 < w.last) umma_commit(&k_empty[next]);
+                    umma_commit_elect(smem_u32(&v_empty[stage]));
+                    ++n;
                 }
-            }
-            if (!ok) {                                     // products in flight end before their memory is given up
-                for (int i = 0; i < 64; ++i) __nanosleep(2000);
+                if (b + 2 < last) {
+                    const uint32_t i = n + (b < first ? b + 2 - first : 1), stage = i % kLgStages;       // (n counts block b already)
+                    ok = __all_sync(0xffffffffu, wait_bounded(&k_full[stage], (i / kLgStages) & 1u, &s_abort, 0x86));
+                    if (!ok) break;
+                    if (b + 2 >= h_first && b + 2 < h_last) {
+                        tc_fence_after_sync();
+                        const uint32_t d = d_s + (asked & 1u) * 64, kd = k_lo + stage * (TILE >> 4);
+#pragma unroll
+                        for (int k = 0; k < KS; ++k)
+                            umma_ss_elect(d, q_lo + (((k >> 2) * kLgQPanel + (k & 3) * 32) >> 4), kd + (((k >> 2) * kLgPanel + (k & 3) * 32) >> 4), umma_desc_hi<128>(),
+                                          idesc_s, (uint32_t)(k != 0));
+                        umma_commit_elect(smem_u32(&s_full[t][asked & 1u]));
+                        ++asked;
+                    }
+                    umma_commit_elect(smem_u32(&k_empty[stage]));
+                }
             }
         }
-    } else if (warp < 8) {
+        if (!ok) {                                         // products in flight end before their memory is given up
+            for (int i = 0; i < 64; ++i) __nanosleep(2000);
+        }
+    } else {
         // ------------------------------------------------ softmax
         const int t = warp >> 2, r = warp * 32 + lane, w4 = warp & 3, row = r & 127;
-        const uint32_t ts = tmem + t * 128 + ((uint32_t)(w4 * 32) << 16), to = t_o + t * 128 + ((uint32_t)(w4 * 32) << 16);
-        uint32_t n = 0, parts = 0;                         // blocks of this half so far, parts in which it had some
+        const uint32_t t_s = tmem + t * 128 + ((uint32_t)(w4 * 32) << 16), to = t_o + t * 128 + ((uint32_t)(w4 * 32) << 16);
+        uint32_t n = 0;                                    // blocks of this half so far
         bool ok = true;
         while (ok && large_next(p, at, end, n_tiles, w)) {
             const CacheTile &tile = w.part.tile;
             const LargeHalf half = t == 0 ? w.half[0] : w.half[1];
             const int head = w.part.head, rows = w.rows;
             const bool any = half.first < half.last;
+            const int token = (w.r0 + r) / p.group, h = head * p.group + (w.r0 + r - token * p.group);
             if (any) {
-                // a thread loads its row of queries
-                const int token = (w.r0 + r) / p.group, h = head * p.group + (w.r0 + r - token * p.group);
-                const T *q = r < rows ? static_cast<const T *>(p.q) + (tile.row + token) * p.q_token + h * p.q_head : nullptr;
-                uint8_t *dst = s_q + t * TILE + row * 128;
-#pragma unroll 8
+                // a thread loads its row of queries; keys lie in the order that their codes are decoded in: of every four elements
+                // 0, 2, 1, 3
+                const T *q = static_cast<const T *>(p.q) + (tile.row + token) * p.q_token + h * p.q_head;
+                uint8_t *dst = s_q + t * QTILE + row * 128;
+                auto chunk = [&](int c) { return dst + (c >> 3) * kLgQPanel + (((c & 7) ^ (row & 7)) << 4); };
+#pragma unroll 1
                 for (int c = 0; c < DP / 8; ++c) {
-                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                    if (q != nullptr && c * 8 < p.dim) {
-                        if (p.q_vec16) {
-                            v = __ldg(reinterpret_cast<const uint4 *>(q) + c);
-                        } else {
-                            T e[8];
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) e[i] = q[c * 8 + i];
-                            memcpy(&v, e, 16);
-                        }
+                    const bool in = r < rows && c * 8 < p.dim;
+                    if (!in) {
+                        *reinterpret_cast<uint4 *>(chunk(c)) = make_uint4(0u, 0u, 0u, 0u);
+                    } else if (p.q_vec16) {
+                        cp_async_16_full(smem_u32(chunk(c)), q + c * 8);
+                    } else {
+                        T *e = reinterpret_cast<T *>(chunk(c));
+#pragma unroll 1
+                        for (int i = 0; i < 8; ++i) e[i] = q[c * 8 + i];
                     }
-                    // keys lie in the order that their codes are decoded in: of every four elements 0, 2, 1, 3
-                    v = make_uint4(__byte_perm(v.x, v.y, 0x5410), __byte_perm(v.x, v.y, 0x7632), __byte_perm(v.z, v.w, 0x5410), __byte_perm(v.z, v.w, 0x7632));
-                    *reinterpret_cast<uint4 *>(dst + (c >> 3) * PANEL + (((c & 7) ^ (row & 7)) << 4)) = v;
+                }
+                cp_async_commit();
+                cp_async_wait_group<0>();
+#pragma unroll 2
+                for (int c = 0; c < DP / 8; ++c) {
+                    uint4 *at_c = reinterpret_cast<uint4 *>(chunk(c));
+                    const uint4 v = *at_c;
+                    *at_c = make_uint4(__byte_perm(v.x, v.y, 0x5410), __byte_perm(v.x, v.y, 0x7632), __byte_perm(v.z, v.w, 0x5410), __byte_perm(v.z, v.w, 0x7632));
                 }
                 fence_proxy_async_smem();
                 tc_fence_before_sync();
@@ -421,8 +433,8 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
             // keys between these two are seen by every row of the warp that is there
             const int all_lo = row_keys(p, tile, w.r0 + min(rows - 1, 32 * warp + 31)).lo, all_hi = row_keys(p, tile, w.r0 + min(rows - 1, 32 * warp)).hi;
             float m = -INFINITY, l = 0.0f, e0 = 0.0f;
-            auto page_of = [&](int b) { return b < half.last ? large_page(p, w.table, tile.len, b * kLgKeys + 16 * (lane & 7)) : -1; };
-            // what 16 keys' scores are scaled by: lane k < 8 fetches it for 16 keys k, a block ahead
+            auto page_of = [&](int b) { return b < half.last ? large_page(p, w.table, tile.len, b * kLgKeys + 16 * (lane & 3)) : -1; };
+            // what 16 keys' scores are scaled by: lane k < 4 fetches it for 16 keys k, a block ahead
             auto info_of = [&](int pg) {
                 float4 f = make_float4(0.0f, -INFINITY, 0.0f, 0.0f);      // not there: seen by no row
                 if (pg >= 0) {
@@ -446,23 +458,27 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
             }
             for (int b = half.first; b < half.last; ++b, ++n) {
                 float4 *blk = s_info[warp][n & 1];
-                if (lane < 8) blk[lane] = info;
+                if (lane < kLgKeys / 16) blk[lane] = info;
                 __syncwarp();
                 if (b + 1 < half.last) {
                     info = info_of(page_next);
                     page_next = page_of(b + 2);
                 }
-                ok = __all_sync(0xffffffffu, wait_bounded(&s_full[t], n & 1u, &s_abort, 0x87));
+                ok = __all_sync(0xffffffffu, wait_bounded(&s_full[t][n & 1u], (n >> 1) & 1u, &s_abort, 0x87));
                 if (!ok) break;
                 tc_fence_after_sync();
                 const int key0 = b * kLgKeys;
+                const uint32_t ts = t_s + (n & 1u) * 64;
                 const bool edge = key0 < all_lo || key0 + kLgKeys > all_hi;
                 const float top = edge ? large_row_max<true>(ts, blk, keys.lo - key0, keys.hi - key0) : large_row_max<false>(ts, blk, 0, 0);
                 if (__any_sync(0xffffffffu, top > m + kRaise)) {
                     const float raised = fmaxf(m, top), f = m == raised ? 1.0f : ex2(m - raised);
                     m = raised;
                     l *= f;
-                    if (b > half.first) {                  // the products up to the last block have ended: s_full comes behind them
+                    if (b > half.first) {                  // once the products up to the last block have ended
+                        ok = __all_sync(0xffffffffu, wait_bounded(&o_done[t], (n - 1u) & 1u, &s_abort, 0x88));
+                        if (!ok) break;
+                        tc_fence_after_sync();
 #pragma unroll 1
                         for (int c = 0; c < DP / 16; ++c) {
                             uint32_t v[16];
@@ -479,16 +495,15 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
                 tmem_st_wait();
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[t]);
+                if (lane == 0) mbar_arrive(&p_full[t][n & 1u]);
             }
             if (any && ok) {
-                ok = __all_sync(0xffffffffu, wait_bounded(&o_full[t], parts & 1u, &s_abort, 0x88));
+                // (the last scores that were there say that all but two products are: each phase is waited for in turn)
+                ok = __all_sync(0xffffffffu, wait_bounded(&o_done[t], (n - 2u) & 1u, &s_abort, 0x88) && wait_bounded(&o_done[t], (n - 1u) & 1u, &s_abort, 0x88));
                 tc_fence_after_sync();
-                ++parts;
             }
             if (ok && 32 * warp < rows) {                  // whole warps
                 const int64_t to_row = (int64_t)w.part.slot * kLargeRows + r;
-                const int token = (w.r0 + r) / p.group, h = head * p.group + (w.r0 + r - token * p.group);
                 T *y = static_cast<T *>(p.y) + (tile.row + token) * p.y_token + h * p.y_head;
                 // a row that sees no key: zeros (and minus infinity)
                 const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l), up = __uint_as_float((unsigned)((int)e0 + 127) << 23);
@@ -518,10 +533,8 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
                                 *reinterpret_cast<uint4 *>(y + c * 16) = make_uint4(u[0], u[1], u[2], u[3]);
                                 *reinterpret_cast<uint4 *>(y + c * 16 + 8) = make_uint4(u[4], u[5], u[6], u[7]);
                             } else {
-                                T e[16];
-                                memcpy(e, u, 32);
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) y[c * 16 + j] = e[j];
+                                for (int j = 0; j < 16; ++j) y[c * 16 + j] = from_f32<T>(f[j] * inv * up);
                             }
                         }
                     }
