@@ -39,6 +39,11 @@ struct CacheStart {
     int tile, head, off, pad;
     CacheTile t;
 };
+// A tile and head that several blocks work on: the first block that starts inside it, and the parts.
+struct CacheJoin {
+    CacheTile t;
+    int head, first, parts, pad;
+};
 // What one thread of the plan kernel knows of a sequence.
 struct CacheSeq { int row, n, len, items, small_tiles, large_tiles; };
 
@@ -53,7 +58,7 @@ struct CacheShape {
 // Word offsets of a plan's parts; the capacities bound what the device fills in.
 struct CachePlanLayout {
     int64_t items_cap, small_cap, large_cap;
-    int64_t items, small, large, small_starts, large_starts, words;
+    int64_t items, small, large, small_starts, large_starts, small_joins, large_joins, words;
     __host__ __device__ static int64_t lesser(int64_t a, int64_t b) { return a < b ? a : b; }
     __host__ __device__ explicit CachePlanLayout(const CacheShape &s) {
         const int64_t T = s.T, B = s.B;
@@ -62,15 +67,20 @@ struct CachePlanLayout {
         const int64_t few = s.small_tokens >= s.max_new ? T : lesser(T, B * (int64_t)s.small_tokens);
         small_cap = lesser(few * s.group, few * s.group / s.small_rows + B);
         large_cap = s.max_new > s.small_tokens ? lesser(T, T * s.group / kLargeRows + B) : 0;
-        int64_t w = 16;                                  // counts: items, small and large tiles, blocks for each; the rest spare
+        int64_t w = 16;                                  // counts: items; tiles, blocks and joins, of small and of large; the rest spare
         items = w, w += 4 * items_cap;
         small = w, w += 8 * small_cap;
         large = w, w += 8 * large_cap;
         small_starts = w, w += 12 * (small_blocks(s.small_rows) + 1);
         large_starts = w, w += large_cap > 0 ? 12 * (kLargeBlocks + 1) : 0;
+        small_joins = w, w += 12 * (small_blocks(s.small_rows) - 1);
+        large_joins = w, w += large_cap > 0 ? 12 * (kLargeBlocks - 1) : 0;
         words = w;
     }
 };
+
+constexpr int kPlanSmall = 1, kPlanLarge = 5;        // where a plan has their four counts
+constexpr int kFewParts = 8;                 // joins of more than these are listed from the end of the list
 
 struct CachePlanArgs {
     CacheShape s;
@@ -122,9 +132,9 @@ __device__ __forceinline__ int cache_block_scan(int v, int *s_warp, int *total) 
 }
 
 // One block.  The work of n tiles, for each head, dealt out evenly: `out` gets the tiles with their work, and with what comes before
-// them, under the shape's mask.  Returns the number of blocks that have some.
-__device__ __forceinline__ int cache_deal(const CacheShape &s, const CacheTile *tiles, CacheTile *out, int n, CacheStart *starts, bool large,
-                                          int *s_scan) {
+// them, under the shape's mask.  counts: tiles, blocks that have some work, joins of few parts and of many.
+__device__ __forceinline__ void cache_deal(const CacheShape &s, const CacheTile *tiles, CacheTile *out, int n, CacheStart *starts, CacheJoin *joins, bool large,
+                                           int *counts, int *s_scan) {
     const int rows = large ? kLargeRows : s.small_rows, unit = large ? kLargeUnit : kSmallUnit;
     int64_t units = 0;
     for (int i0 = 0; i0 < n; i0 += kCachePlanThreads) {
@@ -141,7 +151,10 @@ __device__ __forceinline__ int cache_deal(const CacheShape &s, const CacheTile *
         units += total;
     }
     __syncthreads();
-    if (n == 0) return 0;
+    if (n == 0) {
+        if (threadIdx.x == 0) counts[0] = counts[1] = counts[2] = counts[3] = 0;
+        return;
+    }
     const int64_t work = units * s.heads;
     const int blocks = (int)min((int64_t)(large ? kLargeBlocks : small_blocks(s.small_rows)), max((int64_t)1, work / (large ? kLargeLeast : kSmallLeast)));
     for (int c = threadIdx.x; c <= blocks; c += kCachePlanThreads) {
@@ -156,7 +169,27 @@ __device__ __forceinline__ int cache_deal(const CacheShape &s, const CacheTile *
         }
         starts[c] = {lo, head, (int)(r - out[lo].first), 0, out[lo]};
     }
-    return blocks;
+    __syncthreads();
+    int n_joins[2] = {0, 0};
+    const int last = (large ? kLargeBlocks : small_blocks(s.small_rows)) - 2;
+    for (int c0 = 1; c0 < blocks; c0 += kCachePlanThreads) {
+        const int c = c0 + threadIdx.x;
+        int parts = 0;
+        if (c < blocks && starts[c].off > 0) {
+            const CacheStart &b = starts[c - 1];
+            if (b.tile != starts[c].tile || b.head != starts[c].head || b.off == 0) parts = 2;      // the block before, and those that start inside
+            while (parts > 0 && c + parts - 1 < blocks && starts[c + parts - 1].tile == starts[c].tile && starts[c + parts - 1].head == starts[c].head) ++parts;
+        }
+#pragma unroll
+        for (int many = 0; many < 2; ++many) {
+            const bool is = parts > 0 && (parts > kFewParts && !large) == (many != 0);
+            int total;
+            const int at = n_joins[many] + cache_block_scan(is ? 1 : 0, s_scan, &total);
+            if (is) joins[many ? last - at : at] = {starts[c].t, starts[c].head, c, parts, 0};
+            n_joins[many] += total;
+        }
+    }
+    if (threadIdx.x == 0) counts[0] = n, counts[1] = blocks, counts[2] = n_joins[0], counts[3] = n_joins[1];
 }
 
 // The plan's work dealt out again for calls that mask otherwise than it expects.  to: counts, tiles and starts as in the plan.
@@ -164,12 +197,11 @@ __global__ void __launch_bounds__(kCachePlanThreads) cache_deal_kernel(const Cac
     __shared__ int s_scan[kCachePlanThreads / 32];
     pdl_enter();
     const CachePlanLayout L(s);
-    const int n = plan[1], m = plan[2];
-    const int a = cache_deal(s, reinterpret_cast<const CacheTile *>(plan + L.small), reinterpret_cast<CacheTile *>(to + L.small), n,
-                             reinterpret_cast<CacheStart *>(to + L.small_starts), false, s_scan);
-    const int b = cache_deal(s, reinterpret_cast<const CacheTile *>(plan + L.large), reinterpret_cast<CacheTile *>(to + L.large), m,
-                             reinterpret_cast<CacheStart *>(to + L.large_starts), true, s_scan);
-    if (threadIdx.x == 0) to[1] = n, to[2] = m, to[3] = a, to[4] = b;
+    cache_deal(s, reinterpret_cast<const CacheTile *>(plan + L.small), reinterpret_cast<CacheTile *>(to + L.small), plan[kPlanSmall],
+               reinterpret_cast<CacheStart *>(to + L.small_starts), reinterpret_cast<CacheJoin *>(to + L.small_joins), false, to + kPlanSmall, s_scan);
+    __syncthreads();
+    cache_deal(s, reinterpret_cast<const CacheTile *>(plan + L.large), reinterpret_cast<CacheTile *>(to + L.large), plan[kPlanLarge],
+               reinterpret_cast<CacheStart *>(to + L.large_starts), reinterpret_cast<CacheJoin *>(to + L.large_joins), true, to + kPlanLarge, s_scan);
 }
 
 // One block.  The lists' capacities hold for starts that never decrease; entries beyond them (starts that do) are dropped,
@@ -224,14 +256,12 @@ __global__ void __launch_bounds__(kCachePlanThreads) cache_plan_kernel(const Cac
     for (int c = 0; c < 3; ++c) at[c] = (unsigned)at[c] < (uint64_t)caps[c] ? at[c] : (int)caps[c];
     __syncthreads();
     CacheTile *small = reinterpret_cast<CacheTile *>(a.plan + L.small), *large = reinterpret_cast<CacheTile *>(a.plan + L.large);
-    const int small_blocks = cache_deal(a.s, small, small, at[1], reinterpret_cast<CacheStart *>(a.plan + L.small_starts), false, s_scan);
-    const int large_blocks = cache_deal(a.s, large, large, at[2], reinterpret_cast<CacheStart *>(a.plan + L.large_starts), true, s_scan);
-    if (threadIdx.x == 0) {
-#pragma unroll
-        for (int c = 0; c < 3; ++c) a.plan[c] = at[c];
-        a.plan[3] = small_blocks;
-        a.plan[4] = large_blocks;
-    }
+    if (threadIdx.x == 0) a.plan[0] = at[0];
+    cache_deal(a.s, small, small, at[1], reinterpret_cast<CacheStart *>(a.plan + L.small_starts), reinterpret_cast<CacheJoin *>(a.plan + L.small_joins), false,
+               a.plan + kPlanSmall, s_scan);
+    __syncthreads();
+    cache_deal(a.s, large, large, at[2], reinterpret_cast<CacheStart *>(a.plan + L.large_starts), reinterpret_cast<CacheJoin *>(a.plan + L.large_joins), true,
+               a.plan + kPlanLarge, s_scan);
 }
 
 // ------------------------------------------------------------------ write

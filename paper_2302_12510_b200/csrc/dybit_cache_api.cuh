@@ -215,12 +215,14 @@ static dybit_status run_cache_attention(const dybit_cache *c, const CacheShape &
     CacheAttn small = p, large = p;
     small.tiles = reinterpret_cast<const CacheTile *>(plan + L.small);
     small.starts = reinterpret_cast<const CacheStart *>(plan + L.small_starts);
-    small.n_tiles = plan + 1, small.n_blocks = plan + 3;
+    small.joins = reinterpret_cast<const CacheJoin *>(plan + L.small_joins);
+    small.counts = plan + kPlanSmall;
     small.part_y = reinterpret_cast<float *>(ws + w.small_y);
     small.part_ml = reinterpret_cast<float4 *>(ws + w.small_ml);
     large.tiles = reinterpret_cast<const CacheTile *>(plan + L.large);
     large.starts = reinterpret_cast<const CacheStart *>(plan + L.large_starts);
-    large.n_tiles = plan + 2, large.n_blocks = plan + 4;
+    large.joins = reinterpret_cast<const CacheJoin *>(plan + L.large_joins);
+    large.counts = plan + kPlanLarge;
     large.part_y = reinterpret_cast<float *>(ws + w.large_y);
     large.part_ml = reinterpret_cast<float4 *>(ws + w.large_ml);
     if (L.large_cap > 0) {
@@ -239,11 +241,11 @@ static dybit_status run_cache_attention(const dybit_cache *c, const CacheShape &
     st = dp == 64 ? (few ? go(d64(), one()) : go(d64(), two())) : (few ? go(d128(), one()) : go(d128(), two()));
     if (st != DYBIT_OK) return st;
     if (L.large_cap > 0) {
-        st = launch_cache_join<T, kLargeRows>(large, dim3(kLargeBlocks - 1, 16), s);
+        st = launch_cache_join<T, kLargeRows>(large, dim3(kLargeBlocks - 1, 8), s);
         if (st != DYBIT_OK) return st;
     }
-    if (few) st = launch_cache_join<T, 8>(small, dim3(small_blocks(8) - 1), s);
-    else st = launch_cache_join<T, kSmallRows>(small, dim3(small_blocks(kSmallRows) - 1), s);
+    if (few) st = launch_cache_join<T, 8>(small, dim3(4 * 148), s);
+    else st = launch_cache_join<T, kSmallRows>(small, dim3(4 * 148), s);
     return st;
 }
 

@@ -28,9 +28,10 @@ constexpr float kRaise = 8.0f;
 constexpr int kCacheMaxDim = 128, kCacheMaxGroup = 128;
 
 struct CacheAttn {
-    const int *n_tiles, *n_blocks;       // of the plan
+    const int *counts;           // of the plan: tiles, blocks, joins of few parts and of many
     const CacheTile *tiles;
     const CacheStart *starts;
+    const CacheJoin *joins;
     const int *table;
     int64_t table_stride;
     int64_t pages;
@@ -237,7 +238,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     }
     __syncthreads();
     pdl_enter();
-    const int block = warp * (int)gridDim.x + (int)blockIdx.x, n_tiles = __ldg(p.n_tiles), n_blocks = __ldg(p.n_blocks);
+    const int block = warp * (int)gridDim.x + (int)blockIdx.x, n_tiles = __ldg(p.counts), n_blocks = __ldg(p.counts + 1);
     CachePart part;
     part.tile = p.starts[block].t;
     CachePlace at = cache_place(p.starts[block]);
@@ -532,84 +533,91 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 
 // ------------------------------------------------------------------ parts of a tile, joined
 
-// One block for each block of the attention kernel but the first.  Those that start inside one tile share its rows and join
-// its parts at their common maximum.  part_ml.x is a part's maximum with its exponent in it, so that parts whose values have other
-// scales compare.
+// Where element d of row r of a large tile's part lies: rows of 32 side by side, four elements each, as the threads that hold them
+// write them.
+__device__ __forceinline__ int64_t large_part_at(int64_t r, int d, int dim) { return ((r >> 5) * (dim / 4) + d / 4) * 128 + (r & 31) * 4; }
+
+// Joins the parts of tiles at their common maximum.  part_ml.x is a part's maximum with its exponent in it, so that parts whose
+// values have other scales compare.  Small tiles of few parts take a warp each, those of many a block to a row.  Large tiles: a lane
+// to a row, blockIdx.y and the warps share the head's elements.
+struct JoinSum { float4 s; float m, l; };
+
+// l counts in the first part's exponent already
+__device__ __forceinline__ void join_add(JoinSum &a, float m, float l, const float4 &s) {
+    const float top = fmaxf(a.m, m), f = a.m == -INFINITY ? 0.0f : ex2(a.m - top), w = m == -INFINITY ? 0.0f : ex2(m - top);
+    a.s.x = a.s.x * f + s.x * w, a.s.y = a.s.y * f + s.y * w, a.s.z = a.s.z * f + s.z * w, a.s.w = a.s.w * f + s.w * w;
+    a.l = a.l * f + l * w;
+    a.m = top;
+}
+
+template <int ROWS>
+__device__ __forceinline__ int64_t join_row(const CacheJoin &j, int k, int r) {
+    // slots of the parts: the second one of the block before, then the first ones of the blocks that start in the tile
+    return (int64_t)(k == 0 ? 2 * j.first - 1 : 2 * (j.first + k - 1)) * ROWS + r;
+}
+
+// Parts first, first + step ... of elements d .. d + 3 of row r; e: the first part's exponent.
+template <int ROWS>
+__device__ __forceinline__ JoinSum join_parts(const CacheAttn &p, const CacheJoin &j, int r, int d, int first, int step, float e) {
+    JoinSum a = {make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.0f};
+#pragma unroll 4
+    for (int k = first; k < j.parts; k += step) {
+        const int64_t at = join_row<ROWS>(j, k, r);
+        const float4 ml = __ldcg(p.part_ml + at);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (d < p.dim) v = __ldcg(reinterpret_cast<const float4 *>(p.part_y + (ROWS == kLargeRows ? large_part_at(at, d, p.dim) : at * p.dim + d)));
+        join_add(a, ml.x, ml.y * ex2(e - ml.z), v);
+    }
+    return a;
+}
+
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(128) cache_join_kernel(const CacheAttn p) {
     __shared__ float4 s_sum[4][kCacheMaxDim / 4];
-    __shared__ float s_l[4];
+    __shared__ float2 s_ml[4];
     pdl_enter();
-    const int block = blockIdx.x + 1, n_blocks = __ldg(p.n_blocks), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const CacheStart start = p.starts[block];
-    if (block >= n_blocks || start.off == 0) return;
-    // blocks in a row that start inside this tile, next to `block`, in direction `step`
-    auto count = [&](int step) {
-        int n = 0;
-        for (;;) {
-            const int i = block + step * (1 + n + lane);
-            bool in = false;
-            if (i >= 1 && i < n_blocks) {
-                const CacheStart s = p.starts[i];
-                in = s.tile == start.tile && s.head == start.head && s.off > 0;
+    const int few = __ldg(p.counts + 2), many = __ldg(p.counts + 3), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    auto rows_of = [&](const CacheJoin &j) { return min(ROWS, j.t.n * p.group - j.t.tile * ROWS); };
+    auto store = [&](const CacheJoin &j, int r, int d, const JoinSum &a, float e) {
+        if (d < p.dim) store_attention_row<T>(p, j.t, j.head, j.t.tile * ROWS + r, d, a.s, a.l, a.m - e, e);
+    };
+    if constexpr (ROWS == kLargeRows) {
+        for (int i = blockIdx.x; i < few; i += gridDim.x) {
+            const CacheJoin j = p.joins[i];
+            for (int r = lane; r < rows_of(j); r += 32) {
+                const float e = __ldcg(p.part_ml + join_row<ROWS>(j, 0, r)).z;
+                for (int d = (blockIdx.y * 4 + warp) * 4; d < p.dim; d += gridDim.y * 16) store(j, r, d, join_parts<ROWS>(p, j, r, d, 0, 1, e), e);
             }
-            const unsigned all = __ballot_sync(0xffffffffu, in);
-            if (all != 0xffffffffu) return n + __ffs(~all) - 1;
-            n += 32;
         }
-    };
-    const int mine = count(-1), sharing = mine + 1 + count(1), first = block - mine, parts = sharing + 1;
-    const CacheTile tile = p.tiles[start.tile];
-    const int rows = min(ROWS, tile.n * p.group - tile.tile * ROWS), d = lane * 4;
-    // slots of the parts: the second one of the block before, then the first ones of the blocks that start in the tile
-    auto slot_of = [&](int k) { return (int64_t)(k == 0 ? 2 * first - 1 : 2 * (first + k - 1)) * ROWS; };
-    auto add = [&](int r, int k, float m, float e, float4 &s, float &l) {
-        const float4 a = __ldcg(p.part_ml + slot_of(k) + r);
-        const float4 v = d < p.dim ? __ldcg(reinterpret_cast<const float4 *>(p.part_y + (slot_of(k) + r) * p.dim + d)) : make_float4(0.f, 0.f, 0.f, 0.f);
-        const float w = a.x == -INFINITY ? 0.0f : ex2(a.x - m);
-        s.x += v.x * w, s.y += v.y * w, s.z += v.z * w, s.w += v.w * w;
-        l += (a.x == -INFINITY ? a.y : a.y * w) * ex2(e - a.z);
-    };
-    auto maximum = [&](int r) {
-        float m = -INFINITY;
-        for (int k = lane; k < parts; k += 32) m = fmaxf(m, __ldcg(p.part_ml + slot_of(k) + r).x);
+    } else {
+        // a tile's rows go to as many blocks (warps) as there are
+        const int blocks = many > 0 ? min(ROWS, max(1, (int)gridDim.x / many)) : 1;
+        for (int i = blockIdx.x; i < blocks * many; i += gridDim.x) {
+            const CacheJoin j = p.joins[small_blocks(ROWS) - 2 - i / blocks];
+            for (int r = i % blocks; r < rows_of(j); r += blocks) {
+                const float e = __ldcg(p.part_ml + join_row<ROWS>(j, 0, r)).z;
+                JoinSum a = join_parts<ROWS>(p, j, r, lane * 4, warp, 4, e);
+                s_sum[warp][lane] = a.s;
+                if (lane == 0) s_ml[warp] = make_float2(a.m, a.l);
+                __syncthreads();
+                if (warp == 0) {
 #pragma unroll
-        for (int i = 16; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
-        return m;
-    };
-    if (ROWS == kLargeRows || parts <= 8) {
-        // a warp to a row; blockIdx.y takes a sixteenth of a large tile's rows
-        const int r1 = ROWS == kLargeRows ? min(rows, (int)(blockIdx.y + 1) * 16) : rows;
-        for (int r = (ROWS == kLargeRows ? blockIdx.y * 16 : 0) + mine + sharing * warp; r < r1; r += 4 * sharing) {
-            const float m = maximum(r), e = __ldcg(p.part_ml + slot_of(0) + r).z;
-            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-            float l = 0.0f;
+                    for (int w = 1; w < 4; ++w) join_add(a, s_ml[w].x, s_ml[w].y, s_sum[w][lane]);
+                    store(j, r, lane * 4, a, e);
+                }
+                __syncthreads();
+            }
+        }
+        const int warps = few > 0 ? min(ROWS, max(1, 4 * (int)gridDim.x / few)) : 1;
+        for (int i = blockIdx.x + warp * gridDim.x; i < warps * few; i += 4 * gridDim.x) {
+            const CacheJoin j = p.joins[i / warps];
+            const int rows = rows_of(j);
 #pragma unroll 2
-            for (int k = 0; k < parts; ++k) add(r, k, m, e, s, l);
-            if (d < p.dim) store_attention_row<T>(p, tile, start.head, tile.tile * ROWS + r, d, s, l, m - e, e);
-        }
-        return;
-    }
-    // many parts: the four warps share them, row by row
-    for (int r = mine; r < rows; r += sharing) {
-        const float m = maximum(r), e = __ldcg(p.part_ml + slot_of(0) + r).z;
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        float l = 0.0f;
-#pragma unroll 4
-        for (int k = warp; k < parts; k += 4) add(r, k, m, e, s, l);
-        s_sum[warp][lane] = s;
-        if (lane == 0) s_l[warp] = l;
-        __syncthreads();
-        if (warp == 0 && d < p.dim) {
-#pragma unroll
-            for (int w = 1; w < 4; ++w) {
-                const float4 v = s_sum[w][lane];
-                s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-                l += s_l[w];
+            for (int r = i % warps; r < rows; r += warps) {
+                const float e = __ldcg(p.part_ml + join_row<ROWS>(j, 0, r)).z;
+                store(j, r, lane * 4, join_parts<ROWS>(p, j, r, lane * 4, 0, 1, e), e);
             }
-            store_attention_row<T>(p, tile, start.head, tile.tile * ROWS + r, d, s, l, m - e, e);
         }
-        __syncthreads();
     }
 }
 

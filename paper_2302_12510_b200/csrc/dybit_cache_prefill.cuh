@@ -60,16 +60,13 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r
         "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
         : "memory");
 }
-__device__ __forceinline__ void tmem_st_32x8(uint32_t taddr, const uint32_t (&r)[8]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
-                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr)
-                 : "memory");
-}
 // The wait for a load whose registers are used behind it only.
-__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
-                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                   "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                   "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
                  :
                  : "memory");
 }
@@ -217,24 +214,28 @@ __device__ __forceinline__ bool large_decode(const CacheAttn &p, const LargePart
 template <bool EDGE>
 __device__ __forceinline__ float large_row_max(uint32_t ts, const float4 *blk, int lo, int hi) {
     float top = -INFINITY;
-#pragma unroll 2
-    for (int c = 0; c < kLgKeys / 16; ++c) {
-        uint32_t x[16];
-        tmem_ld_32x16(ts + c * 16, x);
-        const float4 f = blk[c];
-        tmem_ld_wait_for(x);
-        if (EDGE) {
+#pragma unroll 1
+    for (int c = 0; c < kLgKeys / 32; ++c) {
+        uint32_t v[32];
+        tmem_ld_32x32(ts + c * 32, v);
+        tmem_ld_wait_for(v);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const float y = __fmaf_rn(__uint_as_float(x[j]), f.x, f.y);
-                top = c * 16 + j >= lo && c * 16 + j < hi ? fmaxf(top, y) : top;
+        for (int g = 0; g < 2; ++g) {
+            const float4 f = blk[2 * c + g];
+            if (EDGE) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float y = __fmaf_rn(__uint_as_float(v[g * 16 + j]), f.x, f.y);
+                    const int key = c * 32 + g * 16 + j;
+                    top = key >= lo && key < hi ? fmaxf(top, y) : top;
+                }
+            } else {                                       // the factor is not negative: the largest product has the largest score
+                float a = __uint_as_float(v[g * 16]);
+#pragma unroll
+                for (int j = 1; j < 15; j += 2) a = fmaxf(fmaxf(a, __uint_as_float(v[g * 16 + j])), __uint_as_float(v[g * 16 + j + 1]));
+                a = fmaxf(a, __uint_as_float(v[g * 16 + 15]));
+                top = fmaxf(top, __fmaf_rn(a, f.x, f.y));
             }
-        } else {                                           // the factor is not negative: the largest product has the largest score
-            float a = __uint_as_float(x[0]);
-#pragma unroll
-            for (int j = 1; j < 15; j += 2) a = fmaxf(fmaxf(a, __uint_as_float(x[j])), __uint_as_float(x[j + 1]));
-            a = fmaxf(a, __uint_as_float(x[15]));
-            top = fmaxf(top, __fmaf_rn(a, f.x, f.y));
         }
     }
     return top;
@@ -243,29 +244,33 @@ __device__ __forceinline__ float large_row_max(uint32_t ts, const float4 *blk, i
 // The row's probabilities at maximum um, written over its scores; returns l with their sum.
 template <bool EDGE>
 __device__ __forceinline__ float large_row_exp(uint32_t ts, const float4 *blk, int lo, int hi, float um, float l) {
-#pragma unroll 2
-    for (int c = 0; c < kLgKeys / 16; ++c) {
-        uint32_t x[16], pr[8];
-        tmem_ld_32x16(ts + c * 16, x);
-        const float4 f = blk[c];
-        const float shift = f.y - um;
-        const uint64_t cc = pack_f32x2(f.x, f.x), ss = pack_f32x2(shift, shift);
-        uint64_t sum = 0;
-        tmem_ld_wait_for(x);
+#pragma unroll 1
+    for (int c = 0; c < kLgKeys / 32; ++c) {
+        uint32_t v[32], pr[16];
+        tmem_ld_32x32(ts + c * 32, v);
+        tmem_ld_wait_for(v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float2 s = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), cc, ss));
-            if (EDGE) {
-                if (c * 16 + 2 * j < lo || c * 16 + 2 * j >= hi) s.x = -INFINITY;
-                if (c * 16 + 2 * j + 1 < lo || c * 16 + 2 * j + 1 >= hi) s.y = -INFINITY;
+        for (int g = 0; g < 2; ++g) {
+            const float4 f = blk[2 * c + g];
+            const float shift = f.y - um;
+            const uint64_t cc = pack_f32x2(f.x, f.x), ss = pack_f32x2(shift, shift);
+            uint64_t sum = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float2 s = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[g * 16 + 2 * j]), __uint_as_float(v[g * 16 + 2 * j + 1])), cc, ss));
+                if (EDGE) {
+                    const int key = c * 32 + g * 16 + 2 * j;
+                    if (key < lo || key >= hi) s.x = -INFINITY;
+                    if (key + 1 < lo || key + 1 >= hi) s.y = -INFINITY;
+                }
+                s.x = ex2(s.x), s.y = ex2(s.y);
+                sum = j == 0 ? pack_f32x2(s.x, s.y) : add_f32x2(sum, pack_f32x2(s.x, s.y));
+                pr[g * 8 + j] = pack_f16(s.x, s.y);
             }
-            s.x = ex2(s.x), s.y = ex2(s.y);
-            sum = j == 0 ? pack_f32x2(s.x, s.y) : add_f32x2(sum, pack_f32x2(s.x, s.y));
-            pr[j] = pack_f16(s.x, s.y);
+            const float2 s = unpack_f32x2(sum);
+            l = __fmaf_rn(s.x + s.y, f.z, l);
         }
-        const float2 s = unpack_f32x2(sum);
-        l = __fmaf_rn(s.x + s.y, f.z, l);
-        tmem_st_32x8(ts + c * 8, pr);                      // (columns whose scores have been read)
+        tmem_st_32x16(ts + c * 16, pr);                    // (columns whose scores have been read)
     }
     return l;
 }
@@ -309,7 +314,7 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
     __syncthreads();
     tc_fence_after_sync();
     pdl_enter();
-    const int n_tiles = __ldg(p.n_tiles), n_blocks = __ldg(p.n_blocks);
+    const int n_tiles = __ldg(p.counts), n_blocks = __ldg(p.counts + 1);
     CachePlace at = {0, 0, 0}, end = {0, 0, 0};
     if ((int)blockIdx.x < n_blocks) at = cache_place(p.starts[blockIdx.x]), end = cache_place(p.starts[blockIdx.x + 1]);
     const uint32_t tmem = s_tmem;
@@ -387,7 +392,7 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
         }
     } else {
         // ------------------------------------------------ softmax
-        const int t = warp >> 2, r = warp * 32 + lane, w4 = warp & 3, row = r & 127;
+        const int t = warp >> 2, r = warp * 32 + lane, w4 = warp & 3, row0 = 32 * w4;
         const uint32_t t_s = tmem + t * 128 + ((uint32_t)(w4 * 32) << 16), to = t_o + t * 128 + ((uint32_t)(w4 * 32) << 16);
         uint32_t n = 0;                                    // blocks of this half so far
         bool ok = true;
@@ -398,29 +403,33 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
             const bool any = half.first < half.last;
             const int token = (w.r0 + r) / p.group, h = head * p.group + (w.r0 + r - token * p.group);
             if (any) {
-                // a thread loads its row of queries; keys lie in the order that their codes are decoded in: of every four elements
-                // 0, 2, 1, 3
-                const T *q = static_cast<const T *>(p.q) + (tile.row + token) * p.q_token + h * p.q_head;
-                uint8_t *dst = s_q + t * QTILE + row * 128;
-                auto chunk = [&](int c) { return dst + (c >> 3) * kLgQPanel + (((c & 7) ^ (row & 7)) << 4); };
+                // the warp's rows of queries, 16 bytes to a lane; keys lie in the order that their codes are decoded in: of every four
+                // elements 0, 2, 1, 3
+                constexpr int CH = DP / 8, PER = 32 / CH;  // chunks of a row, rows at a time
+                const int c = lane % CH;
+                uint8_t *const dst = s_q + t * QTILE + (c >> 3) * kLgQPanel;
+                auto chunk = [&](int i) { return dst + (row0 + i) * 128 + (((c & 7) ^ ((row0 + i) & 7)) << 4); };
+                const int qr = w.r0 + 32 * warp + lane / CH;
+                int qt = qr / p.group, qh = qr - qt * p.group;
 #pragma unroll 1
-                for (int c = 0; c < DP / 8; ++c) {
-                    const bool in = r < rows && c * 8 < p.dim;
-                    if (!in) {
-                        *reinterpret_cast<uint4 *>(chunk(c)) = make_uint4(0u, 0u, 0u, 0u);
+                for (int i = lane / CH; i < 32; i += PER) {
+                    const T *q = static_cast<const T *>(p.q) + (tile.row + qt) * p.q_token + (head * p.group + qh) * p.q_head + c * 8;
+                    for (qh += PER; qh >= p.group; qh -= p.group) ++qt;
+                    if (32 * warp + i >= rows || c * 8 >= p.dim) {
+                        *reinterpret_cast<uint4 *>(chunk(i)) = make_uint4(0u, 0u, 0u, 0u);
                     } else if (p.q_vec16) {
-                        cp_async_16_full(smem_u32(chunk(c)), q + c * 8);
+                        cp_async_16_full(smem_u32(chunk(i)), q);
                     } else {
-                        T *e = reinterpret_cast<T *>(chunk(c));
+                        T *e = reinterpret_cast<T *>(chunk(i));
 #pragma unroll 1
-                        for (int i = 0; i < 8; ++i) e[i] = q[c * 8 + i];
+                        for (int j = 0; j < 8; ++j) e[j] = q[j];
                     }
                 }
                 cp_async_commit();
                 cp_async_wait_group<0>();
 #pragma unroll 2
-                for (int c = 0; c < DP / 8; ++c) {
-                    uint4 *at_c = reinterpret_cast<uint4 *>(chunk(c));
+                for (int i = lane / CH; i < 32; i += PER) {
+                    uint4 *at_c = reinterpret_cast<uint4 *>(chunk(i));
                     const uint4 v = *at_c;
                     *at_c = make_uint4(__byte_perm(v.x, v.y, 0x5410), __byte_perm(v.x, v.y, 0x7632), __byte_perm(v.z, v.w, 0x5410), __byte_perm(v.z, v.w, 0x7632));
                 }
@@ -524,7 +533,7 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
                         if (w.part.slot >= 0) {
 #pragma unroll
                             for (int j = 0; j < 16; j += 4)
-                                *reinterpret_cast<float4 *>(p.part_y + to_row * p.dim + c * 16 + j) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
+                                *reinterpret_cast<float4 *>(p.part_y + large_part_at(to_row, c * 16 + j, p.dim)) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
                         } else {
                             uint32_t u[8];
 #pragma unroll
