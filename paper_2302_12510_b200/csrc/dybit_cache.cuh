@@ -131,10 +131,21 @@ __device__ __forceinline__ int cache_block_scan(int v, int *s_warp, int *total) 
     return before + sum - v;
 }
 
+// Shared memory of the kernels that are one block.
+constexpr int kDealTiles = 2048;             // tiles whose prefix sums are searched in shared memory; more are searched in the plan
+union CachePlanShared {
+    struct { CacheSeq q; int first[3]; } seqs[kCachePlanThreads];
+    struct {
+        int64_t first[kDealTiles];
+        short head[small_blocks(8) + 1];
+        int tile[small_blocks(8) + 1], off[small_blocks(8) + 1];
+    } deal;
+};
+
 // One block.  The work of n tiles, for each head, dealt out evenly: `out` gets the tiles with their work, and with what comes before
 // them, under the shape's mask.  counts: tiles, blocks that have some work, joins of few parts and of many.
 __device__ __forceinline__ void cache_deal(const CacheShape &s, const CacheTile *tiles, CacheTile *out, int n, CacheStart *starts, CacheJoin *joins, bool large,
-                                           int *counts, int *s_scan) {
+                                           int *counts, int *s_scan, CachePlanShared &sh) {
     const int rows = large ? kLargeRows : s.small_rows, unit = large ? kLargeUnit : kSmallUnit;
     int64_t units = 0;
     for (int i0 = 0; i0 < n; i0 += kCachePlanThreads) {
@@ -148,6 +159,7 @@ __device__ __forceinline__ void cache_deal(const CacheShape &s, const CacheTile 
         int total;
         t.first = units + cache_block_scan(t.units, s_scan, &total);
         if (i < n) out[i] = t;
+        if (i < n && i < kDealTiles) sh.deal.first[i] = t.first;
         units += total;
     }
     __syncthreads();
@@ -164,10 +176,13 @@ __device__ __forceinline__ void cache_deal(const CacheShape &s, const CacheTile 
         int lo = 0, hi = n - 1;                            // the last tile whose work starts at or before r
         while (lo < hi) {
             const int mid = (lo + hi + 1) / 2;
-            if (out[mid].first <= r) lo = mid;
+            if ((n <= kDealTiles ? sh.deal.first[mid] : out[mid].first) <= r) lo = mid;
             else hi = mid - 1;
         }
-        starts[c] = {lo, head, (int)(r - out[lo].first), 0, out[lo]};
+        const CacheTile t = out[lo];
+        const int off = (int)(r - t.first);
+        starts[c] = {lo, head, off, 0, t};
+        sh.deal.tile[c] = lo, sh.deal.head[c] = (short)head, sh.deal.off[c] = off;
     }
     __syncthreads();
     int n_joins[2] = {0, 0};
@@ -175,17 +190,17 @@ __device__ __forceinline__ void cache_deal(const CacheShape &s, const CacheTile 
     for (int c0 = 1; c0 < blocks; c0 += kCachePlanThreads) {
         const int c = c0 + threadIdx.x;
         int parts = 0;
-        if (c < blocks && starts[c].off > 0) {
-            const CacheStart &b = starts[c - 1];
-            if (b.tile != starts[c].tile || b.head != starts[c].head || b.off == 0) parts = 2;      // the block before, and those that start inside
-            while (parts > 0 && c + parts - 1 < blocks && starts[c + parts - 1].tile == starts[c].tile && starts[c + parts - 1].head == starts[c].head) ++parts;
+        auto same = [&](int i) { return sh.deal.tile[i] == sh.deal.tile[c] && sh.deal.head[i] == sh.deal.head[c]; };
+        if (c < blocks && sh.deal.off[c] > 0) {
+            if (!same(c - 1) || sh.deal.off[c - 1] == 0) parts = 2;      // the block before, and those that start inside
+            while (parts > 0 && c + parts - 1 < blocks && same(c + parts - 1)) ++parts;
         }
 #pragma unroll
         for (int many = 0; many < 2; ++many) {
             const bool is = parts > 0 && (parts > kFewParts && !large) == (many != 0);
             int total;
             const int at = n_joins[many] + cache_block_scan(is ? 1 : 0, s_scan, &total);
-            if (is) joins[many ? last - at : at] = {starts[c].t, starts[c].head, c, parts, 0};
+            if (is) joins[many ? last - at : at] = {out[sh.deal.tile[c]], sh.deal.head[c], c, parts, 0};
             n_joins[many] += total;
         }
     }
@@ -195,19 +210,21 @@ __device__ __forceinline__ void cache_deal(const CacheShape &s, const CacheTile 
 // The plan's work dealt out again for calls that mask otherwise than it expects.  to: counts, tiles and starts as in the plan.
 __global__ void __launch_bounds__(kCachePlanThreads) cache_deal_kernel(const CacheShape s, const int *plan, int *to) {
     __shared__ int s_scan[kCachePlanThreads / 32];
+    __shared__ CachePlanShared sh;
     pdl_enter();
     const CachePlanLayout L(s);
     cache_deal(s, reinterpret_cast<const CacheTile *>(plan + L.small), reinterpret_cast<CacheTile *>(to + L.small), plan[kPlanSmall],
-               reinterpret_cast<CacheStart *>(to + L.small_starts), reinterpret_cast<CacheJoin *>(to + L.small_joins), false, to + kPlanSmall, s_scan);
+               reinterpret_cast<CacheStart *>(to + L.small_starts), reinterpret_cast<CacheJoin *>(to + L.small_joins), false, to + kPlanSmall, s_scan, sh);
     __syncthreads();
     cache_deal(s, reinterpret_cast<const CacheTile *>(plan + L.large), reinterpret_cast<CacheTile *>(to + L.large), plan[kPlanLarge],
-               reinterpret_cast<CacheStart *>(to + L.large_starts), reinterpret_cast<CacheJoin *>(to + L.large_joins), true, to + kPlanLarge, s_scan);
+               reinterpret_cast<CacheStart *>(to + L.large_starts), reinterpret_cast<CacheJoin *>(to + L.large_joins), true, to + kPlanLarge, s_scan, sh);
 }
 
 // One block.  The lists' capacities hold for starts that never decrease; entries beyond them (starts that do) are dropped,
 // not written.  Integer work of B sequences: counts and the lists, a warp to a sequence; then the blocks' starts.
 __global__ void __launch_bounds__(kCachePlanThreads) cache_plan_kernel(const CachePlanArgs a) {
     __shared__ int s_scan[kCachePlanThreads / 32];
+    __shared__ CachePlanShared sh;
     pdl_enter();
     const CachePlanLayout L(a.s);
     const int B = a.s.B, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -224,13 +241,15 @@ __global__ void __launch_bounds__(kCachePlanThreads) cache_plan_kernel(const Cac
             first[c] = at[c] + cache_block_scan(count[c], s_scan, &total);
             at[c] += total;
         }
-        // lane k of a warp has what was counted for sequence k of its own
-        for (int k = 0; k < 32; ++k) {
-            const int seq = b0 + warp * 32 + k;
-            if (seq >= B) break;
-            auto of = [&](int v) { return __shfl_sync(0xffffffffu, v, k); };
-            const CacheSeq m = {of(q.row), of(q.n), of(q.len), of(q.items), of(q.small_tiles), of(q.large_tiles)};
-            const int page = a.s.page, outside = max(0, m.n - m.len), p0 = m.len - (m.n - outside), out_items = cache_div_up(outside, page), i0 = of(first[0]);
+        __syncthreads();
+        sh.seqs[threadIdx.x] = {q, {first[0], first[1], first[2]}};
+        __syncthreads();
+        // a warp to a sequence
+        for (int k = warp; k < kCachePlanThreads && b0 + k < B; k += kCachePlanThreads / 32) {
+            const int seq = b0 + k;
+            const CacheSeq m = sh.seqs[k].q;
+            const int i0 = sh.seqs[k].first[0];
+            const int page = a.s.page, outside = max(0, m.n - m.len), p0 = m.len - (m.n - outside), out_items = cache_div_up(outside, page);
             CacheItem *list = reinterpret_cast<CacheItem *>(a.plan + L.items) + i0;
             for (int i = lane; i < m.items; i += 32) {
                 CacheItem it;
@@ -247,8 +266,8 @@ __global__ void __launch_bounds__(kCachePlanThreads) cache_plan_kernel(const Cac
                 for (int i = lane; i < n_tiles; i += 32)
                     if ((unsigned)(t0 + i) < (uint64_t)cap) out[i] = {m.row, m.n, m.len, seq, i, 0, 0};
             };
-            tiles(L.small, L.small_cap, m.small_tiles, of(first[1]));
-            tiles(L.large, L.large_cap, m.large_tiles, of(first[2]));
+            tiles(L.small, L.small_cap, m.small_tiles, sh.seqs[k].first[1]);
+            tiles(L.large, L.large_cap, m.large_tiles, sh.seqs[k].first[2]);
         }
     }
     const int64_t caps[3] = {L.items_cap, L.small_cap, L.large_cap};
@@ -258,10 +277,10 @@ __global__ void __launch_bounds__(kCachePlanThreads) cache_plan_kernel(const Cac
     CacheTile *small = reinterpret_cast<CacheTile *>(a.plan + L.small), *large = reinterpret_cast<CacheTile *>(a.plan + L.large);
     if (threadIdx.x == 0) a.plan[0] = at[0];
     cache_deal(a.s, small, small, at[1], reinterpret_cast<CacheStart *>(a.plan + L.small_starts), reinterpret_cast<CacheJoin *>(a.plan + L.small_joins), false,
-               a.plan + kPlanSmall, s_scan);
+               a.plan + kPlanSmall, s_scan, sh);
     __syncthreads();
     cache_deal(a.s, large, large, at[2], reinterpret_cast<CacheStart *>(a.plan + L.large_starts), reinterpret_cast<CacheJoin *>(a.plan + L.large_joins), true,
-               a.plan + kPlanLarge, s_scan);
+               a.plan + kPlanLarge, s_scan, sh);
 }
 
 // ------------------------------------------------------------------ write

@@ -177,7 +177,7 @@ static dybit_status launch_cache_join(const CacheAttn &p, dim3 grid, cudaStream_
         DYBIT_CUDA_TRY(cudaFuncSetAttribute(cache_join_kernel<T, ROWS>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
         ready[dev].store(1, std::memory_order_release);
     }
-    launch_k(cache_join_kernel<T, ROWS>, grid, dim3(128), 0, s, p);
+    launch_k(cache_join_kernel<T, ROWS>, grid, dim3(ROWS == kLargeRows ? 256 : 128), 0, s, p);
     return launch_status();
 }
 
@@ -228,6 +228,7 @@ static dybit_status run_cache_attention(const dybit_cache *c, const CacheShape &
     if (L.large_cap > 0) {
         st = dp == 64 ? launch_cache_large<T, 64>(c, large, s) : launch_cache_large<T, 128>(c, large, s);
         if (st != DYBIT_OK) return st;
+        small.beside = 1;
     }
     const bool few = shape.small_rows == 8;
     auto go = [&](auto d, auto q) {

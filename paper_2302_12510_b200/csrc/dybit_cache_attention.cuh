@@ -6,6 +6,10 @@
 // kernels: this one for tiles of 8 or 16 rows, bound by the one pass over the codes, and dybit_cache_prefill.cuh for
 // tiles of 256 rows, bound by the tensor cores.
 //
+// Launches of a call that do not need one another run side by side as far as there is room: a kernel waits for what came before the
+// call's first kernel through that one (which lets its successor start only behind its own wait), and for its neighbour before it
+// ends, so that the end of the last one is the end of all.
+//
 // What both have in common.  The running maximum of a row goes over x + log2 of the values' scale (base 2), so
 //     p'_j = 2^(x_j + e_j - m),   e_j = log2 s_V(page) - E0
 // is at most a small constant and the second product takes the bare values of the codes, exact in f16 (seven significant
@@ -22,6 +26,14 @@
 #include "dybit_wait.cuh"
 
 namespace dybit {
+
+__device__ __forceinline__ void enter_beside(int beside) {
+    if (!beside) asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void leave_beside(int beside) {
+    if (beside) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.0f;
@@ -48,6 +60,7 @@ struct CacheAttn {
     float4 *part_ml;             // [slot][rows]: {m + E0, l, E0, -}
     int q_vec, q_vec16, y_vec, y_vec16;  // rows can be moved in pieces of 8 (16) bytes
     unsigned minus_one;          // see decode_pair
+    int beside;                  // this launch may run beside the one before it, whose own wait covers what both read
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -237,7 +250,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         prefetch_tensormap(&map_v);
     }
     __syncthreads();
-    pdl_enter();
+    enter_beside(p.beside);
     const int block = warp * (int)gridDim.x + (int)blockIdx.x, n_tiles = __ldg(p.counts), n_blocks = __ldg(p.counts + 1);
     CachePart part;
     part.tile = p.starts[block].t;
@@ -245,6 +258,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     const CachePlace end = cache_place(p.starts[block + 1]);
     if (block >= n_blocks) {
         if (lane == 0) *my_rounds = INT_MAX;
+        leave_beside(p.beside);
         return;
     }
     const unsigned minus = p.minus_one;
@@ -529,6 +543,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     }
     __syncwarp();
     if (lane == 0) *my_rounds = INT_MAX;
+    leave_beside(p.beside);
 }
 
 // ------------------------------------------------------------------ parts of a tile, joined
@@ -539,7 +554,7 @@ __device__ __forceinline__ int64_t large_part_at(int64_t r, int d, int dim) { re
 
 // Joins the parts of tiles at their common maximum.  part_ml.x is a part's maximum with its exponent in it, so that parts whose
 // values have other scales compare.  Small tiles of few parts take a warp each, those of many a block to a row.  Large tiles: a lane
-// to a row, blockIdx.y and the warps share the head's elements.
+// to a row, blockIdx.y a group of 32 rows, the warps share the head's elements.
 struct JoinSum { float4 s; float m, l; };
 
 // l counts in the first part's exponent already
@@ -572,10 +587,10 @@ __device__ __forceinline__ JoinSum join_parts(const CacheAttn &p, const CacheJoi
 }
 
 template <typename T, int ROWS>
-__global__ void __launch_bounds__(128) cache_join_kernel(const CacheAttn p) {
+__global__ void __launch_bounds__(256) cache_join_kernel(const CacheAttn p) {
     __shared__ float4 s_sum[4][kCacheMaxDim / 4];
     __shared__ float2 s_ml[4];
-    pdl_enter();
+    enter_beside(p.beside);
     const int few = __ldg(p.counts + 2), many = __ldg(p.counts + 3), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     auto rows_of = [&](const CacheJoin &j) { return min(ROWS, j.t.n * p.group - j.t.tile * ROWS); };
     auto store = [&](const CacheJoin &j, int r, int d, const JoinSum &a, float e) {
@@ -584,9 +599,11 @@ __global__ void __launch_bounds__(128) cache_join_kernel(const CacheAttn p) {
     if constexpr (ROWS == kLargeRows) {
         for (int i = blockIdx.x; i < few; i += gridDim.x) {
             const CacheJoin j = p.joins[i];
-            for (int r = lane; r < rows_of(j); r += 32) {
+            const int r = blockIdx.y * 32 + lane;
+            if (r < rows_of(j)) {
                 const float e = __ldcg(p.part_ml + join_row<ROWS>(j, 0, r)).z;
-                for (int d = (blockIdx.y * 4 + warp) * 4; d < p.dim; d += gridDim.y * 16) store(j, r, d, join_parts<ROWS>(p, j, r, d, 0, 1, e), e);
+#pragma unroll 2
+                for (int d = warp * 4; d < p.dim; d += 32) store(j, r, d, join_parts<ROWS>(p, j, r, d, 0, 1, e), e);
             }
         }
     } else {
@@ -619,6 +636,7 @@ __global__ void __launch_bounds__(128) cache_join_kernel(const CacheAttn p) {
             }
         }
     }
+    leave_beside(p.beside);
 }
 
 }  // namespace dybit
