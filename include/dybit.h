@@ -534,7 +534,7 @@ dybit_status dybit_adapters_backward(int64_t T, int64_t K, int64_t N, int R, con
  * table[b * table_stride + p / page], at its token p % page.  An entry outside 0 .. pages-1 is a page that is not there:
  * its tokens are not written, read as zeros, and are seen by no query.
  *   dim    a multiple of 16 up to 128;  page  16, 32, 64 or 128;  others: DYBIT_ERR_UNSUPPORTED
- *   k_codes, v_codes [dev] 16-byte aligned;  pages * heads < 2^31 - 1 */
+ *   k_codes, v_codes [dev] 16-byte aligned;  heads up to 4096, pages * heads < 2^31 - 1 */
 typedef struct {
     void *k_codes, *v_codes;
     float *k_scales, *v_scales;
@@ -552,7 +552,8 @@ typedef struct {
  *   q_heads query heads of the attention, a multiple of cache.heads, up to 128 to a key head
  *   table   [dev] sequences rows of max_pages entries, row stride table_stride
  *   causal, window  how the attention calls will mask: what the plan deals their work out by.  A call that masks otherwise
- *           first deals it out again, in one more launch */
+ *           first deals it out again, in one more launch
+ * Up to 2^20 sequences, 2^26 tokens, tokens * q_heads 2^30, max_pages * page 2^26; more: DYBIT_ERR_UNSUPPORTED. */
 typedef struct {
     int sequences;
     int64_t tokens;
@@ -563,8 +564,9 @@ typedef struct {
     int causal, window;
 } dybit_cache_batch;
 
-/* Lists of the work of a batch: which pages its new tokens go to, the tiles of its queries, and how their work is dealt out.  Made once for a batch; every layer's calls with the same batch go by it, on caches of the same
- * pages' size and heads, several calls at once if wanted (they only read it).
+/* Lists of the work of a batch: which pages its new tokens go to, the tiles of its queries, and how their work is dealt
+ * out.  Made once for a batch; every layer's calls with the same batch go by it, on caches of the same pages' size and
+ * heads, several calls at once if wanted (they only read it).
  *   starts, lengths  [dev] int32
  *   plan    [dev] dybit_cache_plan_bytes(...) bytes, 16-byte aligned, overwritten.  0 bytes: the arguments are refused */
 size_t dybit_cache_plan_bytes(const dybit_cache *cache, const dybit_cache_batch *batch);
@@ -578,7 +580,8 @@ dybit_status dybit_cache_plan(const dybit_cache *cache, const dybit_cache_batch 
  *             max(need, the scale it has)        otherwise
  *     code  = encode(x / scale)                  the encoder of dybit_quantize_pack; 0 for scale 0
  * Where a begun page's scale grows, its older codes are encoded again, x being what they stand for: each time by half a
- * step at most.  NaN -> code 0; infinities saturate.  Two sequences of a batch must not write to the same page (they may share pages that they read).
+ * step at most.  NaN -> code 0; infinities saturate.  Two sequences of a batch must not write to the same page (they may
+ * share pages that they read).
  *   k, v  [dev]  tokens x heads x dim, unit inner stride, strides in elements.  (16-byte aligned rows run fastest.)
  *   top   0 .. 6; 2 keeps most of a bell-shaped block where codes are finest */
 dybit_status dybit_cache_write(const dybit_cache *cache, const dybit_cache_batch *batch, const void *plan, const void *k, int64_t k_token_stride,
@@ -598,8 +601,9 @@ dybit_status dybit_cache_read(const dybit_cache *cache, const dybit_cache_batch 
  * A row that sees no key is 0, its lse minus infinity.  Sums, maxima and statistics are fp32; q meets the keys as it is,
  * probabilities meet the values as f16 numbers (2^-12 off at most, relative to the row's largest), y is rounded once.
  * A row of q that is not finite makes its own y and lse not finite, and no other's.  The scales of the values that a row
- * sees lie within 2^100 of each other.
+ * sees lie within 2^100 of each other (and of 1, where some of them are 0).
  *   q, y [dev]  tokens x q_heads x dim, unit inner stride, strides in elements;  t  bf16 or f16 (f32: DYBIT_ERR_UNSUPPORTED)
+ *   scale  0 .. 2e38
  *   lse  [dev]  tokens x q_heads floats, dense, or NULL
  *   ws   [dev]  dybit_cache_attention_workspace_bytes(...) bytes, 1024-byte aligned; calls that run at once need one each */
 size_t dybit_cache_attention_workspace_bytes(const dybit_cache *cache, const dybit_cache_batch *batch);

