@@ -195,9 +195,14 @@ __device__ __forceinline__ void cache_deal(const CacheShape &s, const CacheTile 
         const int c = c0 + threadIdx.x;
         int parts = 0;
         auto same = [&](int i) { return sh.deal.tile[i] == sh.deal.tile[c] && sh.deal.head[i] == sh.deal.head[c]; };
-        if (c < blocks && sh.deal.off[c] > 0) {
-            if (!same(c - 1) || sh.deal.off[c - 1] == 0) parts = 2;      // the block before, and those that start inside
-            while (parts > 0 && c + parts - 1 < blocks && same(c + parts - 1)) ++parts;
+        if (c < blocks && sh.deal.off[c] > 0 && (!same(c - 1) || sh.deal.off[c - 1] == 0)) {
+            int lo = c, hi = blocks - 1;                   // the last block that starts inside, too: starts go up
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) / 2;
+                if (same(mid)) lo = mid;
+                else hi = mid - 1;
+            }
+            parts = lo - c + 2;                            // those and the block before
         }
 #pragma unroll
         for (int many = 0; many < 2; ++many) {

@@ -179,7 +179,7 @@ static dybit_status launch_cache_join(const CacheAttn &p, dim3 grid, cudaStream_
         DYBIT_CUDA_TRY(cudaFuncSetAttribute(cache_join_kernel<T, ROWS>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
         ready[dev].store(1, std::memory_order_release);
     }
-    launch_k(cache_join_kernel<T, ROWS>, grid, dim3(ROWS == kLargeRows ? 256 : 128), 0, s, p);
+    launch_k(cache_join_kernel<T, ROWS>, grid, dim3(256), 0, s, p);
     return launch_status();
 }
 
