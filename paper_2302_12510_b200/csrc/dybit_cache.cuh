@@ -216,17 +216,18 @@ __device__ __forceinline__ void cache_deal(const CacheShape &s, const CacheTile 
     if (threadIdx.x == 0) counts[0] = n, counts[1] = blocks, counts[2] = n_joins[0], counts[3] = n_joins[1];
 }
 
-// The plan's work dealt out again for calls that mask otherwise than it expects.  to: counts, tiles and starts as in the plan.
+// The plan's work dealt out again for calls that mask otherwise than it expects: block 0 the small tiles', block 1 the large ones'.
+// to: counts, tiles and starts as in the plan.
 __global__ void __launch_bounds__(kCachePlanThreads) cache_deal_kernel(const CacheShape s, const int *plan, int *to) {
     __shared__ int s_scan[kCachePlanThreads / 32];
     __shared__ CachePlanShared sh;
     pdl_enter();
     const CachePlanLayout L(s);
-    cache_deal(s, reinterpret_cast<const CacheTile *>(plan + L.small), reinterpret_cast<CacheTile *>(to + L.small), plan[kPlanSmall],
-               reinterpret_cast<CacheStart *>(to + L.small_starts), reinterpret_cast<CacheJoin *>(to + L.small_joins), false, to + kPlanSmall, s_scan, sh);
-    __syncthreads();
-    cache_deal(s, reinterpret_cast<const CacheTile *>(plan + L.large), reinterpret_cast<CacheTile *>(to + L.large), plan[kPlanLarge],
-               reinterpret_cast<CacheStart *>(to + L.large_starts), reinterpret_cast<CacheJoin *>(to + L.large_joins), true, to + kPlanLarge, s_scan, sh);
+    const bool large = blockIdx.x != 0;
+    const int64_t tiles = large ? L.large : L.small, starts = large ? L.large_starts : L.small_starts, joins = large ? L.large_joins : L.small_joins;
+    const int counts = large ? kPlanLarge : kPlanSmall;
+    cache_deal(s, reinterpret_cast<const CacheTile *>(plan + tiles), reinterpret_cast<CacheTile *>(to + tiles), plan[counts],
+               reinterpret_cast<CacheStart *>(to + starts), reinterpret_cast<CacheJoin *>(to + joins), large, to + counts, s_scan, sh);
 }
 
 // One block.  The lists' capacities hold for starts that never decrease; entries beyond them (starts that do) are dropped,

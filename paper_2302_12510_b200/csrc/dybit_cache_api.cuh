@@ -37,7 +37,8 @@ static dybit_status check_batch(const dybit_cache *c, const dybit_cache_batch *b
 // Rows of a sequence that small tiles take, the others large ones: two tiles of 16, or four where the batch is small.  A large tile
 // costs its keys the same however full it is, small ones each cost them; but a block of large tiles takes longer to begin and to
 // end.  8 key heads of 4 queries, 4096 keys, small against large tiles: 16 sequences of 32 rows 97 : 113 us, of 48 rows 137 : 113 us, of 64
-// rows 166 : 114 us; one sequence of 48 rows 27 : 44 us, of 64 rows 28 : 44 us.
+// rows 166 : 114 us; one sequence of 48 rows 27 : 44 us, of 64 rows 28 : 44 us.  Groups of 128 heads, one token of each of 64 sequences
+// 160 : 74 us, of one 23 : 41 us: a small batch's single tokens take small tiles whatever their group.
 constexpr int kSmallMost = 32, kSmallMostAlone = 64, kAloneRows = 2048;
 static CacheShape cache_shape(const dybit_cache *c, const dybit_cache_batch *b) {
     CacheShape s = {};
@@ -48,7 +49,7 @@ static CacheShape cache_shape(const dybit_cache *c, const dybit_cache_batch *b) 
     s.group = b->q_heads / c->heads;
     s.max_new = (int)std::min<int64_t>(b->max_new, b->tokens);
     s.max_pages = b->max_pages;
-    s.small_tokens = std::max(1, (b->tokens * b->q_heads <= kAloneRows ? kSmallMostAlone : kSmallMost) / s.group);
+    s.small_tokens = b->tokens * b->q_heads <= kAloneRows ? std::max(1, kSmallMostAlone / s.group) : kSmallMost / s.group;
     s.causal = b->causal != 0;
     s.window = b->window > 0 ? b->window : INT_MAX;
     s.small_rows = (int64_t)s.max_new * s.group <= 8 ? 8 : kSmallRows;
@@ -209,7 +210,7 @@ static dybit_status run_cache_attention(const dybit_cache *c, const CacheShape &
     if ((p.causal != 0) != (shape.causal != 0) || p.window != shape.window) {
         CacheShape mine = shape;
         mine.causal = p.causal, mine.window = p.window;
-        launch_k(cache_deal_kernel, dim3(1), dim3(kCachePlanThreads), 0, s, mine, plan, reinterpret_cast<int *>(ws + w.plan));
+        launch_k(cache_deal_kernel, dim3(L.large_cap > 0 ? 2 : 1), dim3(kCachePlanThreads), 0, s, mine, plan, reinterpret_cast<int *>(ws + w.plan));
         st = launch_status();
         if (st != DYBIT_OK) return st;
         plan = reinterpret_cast<const int *>(ws + w.plan);
@@ -241,12 +242,15 @@ static dybit_status run_cache_attention(const dybit_cache *c, const CacheShape &
     using two = std::integral_constant<int, 2>;
     using d64 = std::integral_constant<int, 64>;
     using d128 = std::integral_constant<int, 128>;
-    st = dp == 64 ? (few ? go(d64(), one()) : go(d64(), two())) : (few ? go(d128(), one()) : go(d128(), two()));
-    if (st != DYBIT_OK) return st;
+    if (L.small_cap > 0) {
+        st = dp == 64 ? (few ? go(d64(), one()) : go(d64(), two())) : (few ? go(d128(), one()) : go(d128(), two()));
+        if (st != DYBIT_OK) return st;
+    }
     if (L.large_cap > 0) {
         st = launch_cache_join<T, kLargeRows>(large, dim3(kLargeBlocks - 1, 8), s);
         if (st != DYBIT_OK) return st;
     }
+    if (L.small_cap == 0) return DYBIT_OK;
     if (few) st = launch_cache_join<T, 8>(small, dim3(4 * 148), s);
     else st = launch_cache_join<T, kSmallRows>(small, dim3(4 * 148), s);
     return st;

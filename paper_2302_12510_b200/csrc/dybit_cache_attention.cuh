@@ -553,11 +553,11 @@ __device__ __forceinline__ int64_t join_row(const CacheJoin &j, int k, int r) {
     return (int64_t)(k == 0 ? 2 * j.first - 1 : 2 * (j.first + k - 1)) * ROWS + r;
 }
 
-// Parts first, first + step ... of elements d .. d + 3 of row r; e: the first part's exponent.
-template <int ROWS>
+// Parts first, first + step ... of elements d .. d + 3 of row r, AHEAD of them on their way at once; e: the first part's exponent.
+template <int ROWS, int AHEAD>
 __device__ __forceinline__ JoinSum join_parts(const CacheAttn &p, const CacheJoin &j, int r, int d, int first, int step, float e) {
     JoinSum a = {make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.0f};
-#pragma unroll 8
+#pragma unroll AHEAD
     for (int k = first; k < j.parts; k += step) {
         const int64_t at = join_row<ROWS>(j, k, r);
         const float4 ml = __ldcg(p.part_ml + at);
@@ -585,7 +585,7 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const CacheAttn p) {
             if (r < rows_of(j)) {
                 const float e = __ldcg(p.part_ml + join_row<ROWS>(j, 0, r)).z;
 #pragma unroll 2
-                for (int d = warp * 4; d < p.dim; d += 32) store(j, r, d, join_parts<ROWS>(p, j, r, d, 0, 1, e), e);
+                for (int d = warp * 4; d < p.dim; d += 32) store(j, r, d, join_parts<ROWS, 4>(p, j, r, d, 0, 1, e), e);
             }
         }
     } else {
@@ -595,7 +595,7 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const CacheAttn p) {
             const CacheJoin j = p.joins[small_blocks(ROWS) - 2 - i / blocks];
             for (int r = i % blocks; r < rows_of(j); r += blocks) {
                 const float e = __ldcg(p.part_ml + join_row<ROWS>(j, 0, r)).z;
-                JoinSum a = join_parts<ROWS>(p, j, r, lane * 4, warp, 8, e);
+                JoinSum a = join_parts<ROWS, 8>(p, j, r, lane * 4, warp, 8, e);
                 s_sum[warp][lane] = a.s;
                 if (lane == 0) s_ml[warp] = make_float2(a.m, a.l);
                 __syncthreads();
@@ -614,7 +614,7 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const CacheAttn p) {
 #pragma unroll 2
             for (int r = i % warps; r < rows; r += warps) {
                 const float e = __ldcg(p.part_ml + join_row<ROWS>(j, 0, r)).z;
-                store(j, r, lane * 4, join_parts<ROWS>(p, j, r, lane * 4, 0, 1, e), e);
+                store(j, r, lane * 4, join_parts<ROWS, 4>(p, j, r, lane * 4, 0, 1, e), e);
             }
         }
     }
