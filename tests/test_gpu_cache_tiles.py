@@ -27,6 +27,13 @@ def test_around_the_choice_of_tiles(group, news):
     attention_case(ref.Batch(lengths + [600], news + [600], 32, 2, 64, seed=group), group, BF)
 
 
+@pytest.mark.parametrize("group,heads,dim", [(128, 1, 64), (40, 2, 32)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 20), (False, 0)])
+def test_large_batches_of_large_groups_have_no_small_tiles(group, heads, dim, causal, window):
+    news = [1, 0, 1, 2] * 8
+    attention_case(ref.Batch([(37 * i) % 190 + (i > 0) for i in range(32)], news, 16, heads, dim, seed=group, gap=2), group, BF, causal=causal, window=window)
+
+
 @pytest.mark.parametrize("window", [1, 63, 64, 65, 127, 128, 500])
 @pytest.mark.parametrize("dtype,page,dim,group", [(BF, 16, 128, 3), (H, 128, 64, 4)])
 def test_windows_of_large_tiles(window, dtype, page, dim, group):
