@@ -15,6 +15,7 @@
 #pragma once
 
 #include "dybit_cache_attention.cuh"
+#include "dybit_cache_turns.cuh"
 
 namespace dybit {
 
@@ -135,6 +136,12 @@ __device__ __forceinline__ bool large_next(const CacheAttn &p, CachePlace &at, c
     w.last = none0 ? w.half[1].last : none1 ? w.half[0].last : max(w.half[0].last, w.half[1].last);
     if (none0 && none1) w.last = w.first;
     return true;
+}
+
+// Waits for block n's phase of a pair of barriers.
+__device__ __forceinline__ bool wait_turn(uint64_t (&bars)[2], uint32_t n, volatile uint32_t *abort_flag, unsigned site) {
+    const Turn w = turn_of(n);
+    return wait_bounded(&bars[w.bar], w.parity, abort_flag, site);
 }
 
 // Page of the 16 keys from `key` on, or -1.
@@ -284,8 +291,8 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *s_q = smem, *s_k = smem + 2 * QTILE, *s_v = s_k + kLgStages * TILE;
-    // s_full, p_full: per half and score buffer;  o_done: a half's products with values, block by block
-    __shared__ uint64_t k_full[kLgStages], k_empty[kLgStages], v_full[kLgStages], v_empty[kLgStages], q_full[2], s_full[2][2], p_full[2][2], o_done[2];
+    // s_full, p_full, o_done: a half's scores, probabilities and products with values, its blocks in turn
+    __shared__ uint64_t k_full[kLgStages], k_empty[kLgStages], v_full[kLgStages], v_empty[kLgStages], q_full[2], s_full[2][2], p_full[2][2], o_done[2][2];
     __shared__ uint32_t s_tmem, s_abort;
     __shared__ float4 s_info[8][2][kLgKeys / 16];          // softmax warp, parity, 16 keys: {x's factor, values' exponent, 2^-exponent, -}
 
@@ -299,8 +306,8 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
         }
         for (int t = 0; t < 2; ++t) {
             mbar_init(&q_full[t], 4);
-            mbar_init(&o_done[t], 1);
             for (int j = 0; j < 2; ++j) {
+                mbar_init(&o_done[t][j], 1);
                 mbar_init(&s_full[t][j], 1);
                 mbar_init(&p_full[t][j], 4);
             }
@@ -357,14 +364,14 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
                     // (a half that does not see the block lets go of it in its turn all the same, once it has been there)
                     ok = __all_sync(0xffffffffu, wait_bounded(&v_full[stage], (n / kLgStages) & 1u, &s_abort, 0x84));
                     if (ok && b >= h_first && b < h_last) {
-                        ok = __all_sync(0xffffffffu, wait_bounded(&p_full[t][done & 1u], (done >> 1) & 1u, &s_abort, 0x85));
+                        ok = __all_sync(0xffffffffu, wait_turn(p_full[t], done, &s_abort, 0x85));
                         if (!ok) break;
                         tc_fence_after_sync();
                         const uint32_t a = d_s + (done & 1u) * 64, v = v_lo + stage * (TILE >> 4);
 #pragma unroll
                         for (int k = 0; k < kLgKeys / 16; ++k)         // 16 keys are 2048 bytes of values and 8 columns of probabilities
                             umma_ts_elect(d_o, a + k * 8, v + k * 128, large_values_hi(), idesc_o, (uint32_t)(b != h_first || k != 0));
-                        umma_commit_elect(smem_u32(&o_done[t]));
+                        umma_commit_elect(smem_u32(&o_done[t][turn_of(done).bar]));
                         ++done;
                     }
                     if (!ok) break;
@@ -382,7 +389,7 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
                         for (int k = 0; k < KS; ++k)
                             umma_ss_elect(d, q_lo + (((k >> 2) * kLgQPanel + (k & 3) * 32) >> 4), kd + (((k >> 2) * kLgPanel + (k & 3) * 32) >> 4), umma_desc_hi<128>(),
                                           idesc_s, (uint32_t)(k != 0));
-                        umma_commit_elect(smem_u32(&s_full[t][asked & 1u]));
+                        umma_commit_elect(smem_u32(&s_full[t][turn_of(asked).bar]));
                         ++asked;
                     }
                     umma_commit_elect(smem_u32(&k_empty[stage]));
@@ -475,7 +482,7 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
                     info = info_of(page_next);
                     page_next = page_of(b + 2);
                 }
-                ok = __all_sync(0xffffffffu, wait_bounded(&s_full[t][n & 1u], (n >> 1) & 1u, &s_abort, 0x87));
+                ok = __all_sync(0xffffffffu, wait_turn(s_full[t], n, &s_abort, 0x87));
                 if (!ok) break;
                 tc_fence_after_sync();
                 const int key0 = b * kLgKeys;
@@ -487,7 +494,7 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
                     m = raised;
                     l *= f;
                     if (b > half.first) {                  // once the products up to the last block have ended
-                        ok = __all_sync(0xffffffffu, wait_bounded(&o_done[t], (n - 1u) & 1u, &s_abort, 0x88));
+                        ok = __all_sync(0xffffffffu, wait_turn(o_done[t], n - 1u, &s_abort, 0x88));
                         if (!ok) break;
                         tc_fence_after_sync();
 #pragma unroll 1
@@ -506,11 +513,11 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
                 tmem_st_wait();
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[t][n & 1u]);
+                if (lane == 0) mbar_arrive(&p_full[t][turn_of(n).bar]);
             }
             if (any && ok) {
-                // (the last scores that were there say that all but two products are: each phase is waited for in turn)
-                ok = __all_sync(0xffffffffu, wait_bounded(&o_done[t], (n - 2u) & 1u, &s_abort, 0x88) && wait_bounded(&o_done[t], (n - 1u) & 1u, &s_abort, 0x88));
+                // (products end in the order that they are asked for: the last block's is the end of all)
+                ok = __all_sync(0xffffffffu, wait_turn(o_done[t], n - 1u, &s_abort, 0x88));
                 tc_fence_after_sync();
             }
             if (ok && 32 * warp < rows) {                  // whole warps
