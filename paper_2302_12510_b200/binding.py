@@ -990,8 +990,11 @@ def _cache_batch(cache: KVCache, table: torch.Tensor, tokens: int, q_heads: Opti
     if not (table.dtype == torch.int32 and table.is_cuda and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] <= 1)):
         raise ValueError("table must be a 2-D int32 CUDA tensor [sequences][pages] with unit inner stride")
     B, most = table.shape
+    stride = table.stride(0) if B > 1 else most            # (torch gives a single row any stride)
+    if stride < most:
+        raise ValueError("the rows of table must not overlap: give a copy of a table that is expanded or slides over another")
     return _CCacheBatch(B, int(tokens), int(tokens if max_new is None else min(max_new, tokens)), cache.heads if q_heads is None else int(q_heads),
-                        table.data_ptr(), max(table.stride(0), most) if B > 1 else most, most, int(bool(causal)), int(window))
+                        table.data_ptr(), stride, most, int(bool(causal)), int(window))
 
 
 def dybit_cache_plan_bytes(cache: KVCache, table: torch.Tensor, tokens: int, q_heads: Optional[int] = None, max_new: Optional[int] = None) -> int:
@@ -1017,7 +1020,7 @@ def dybit_cache_plan(cache: KVCache, table: torch.Tensor, starts: torch.Tensor, 
 
 class CachePlan:
     """The plan of one batch of sequences, for every call on caches of the same pages' size and heads: table int32
-    [sequences][pages] with the page of every `page` tokens, starts int32 [sequences + 1] with the rows of each sequence's
+    [sequences][pages] with the page of every `page` tokens (rows of any stride that do not overlap), starts int32 [sequences + 1] with the rows of each sequence's
     new tokens among the batch's `tokens` rows, lengths int32 [sequences] with the tokens of each sequence, new ones
     included.  max_new bounds the new tokens of one sequence (default: tokens); the smaller, the less is launched.  causal and
     window say how the attention will mask; a call that masks otherwise takes one more launch.  The plan and its table have to
