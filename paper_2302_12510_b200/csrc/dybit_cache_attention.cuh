@@ -15,7 +15,8 @@
 // is at most a small constant and the second product takes the bare values of the codes, exact in f16 (seven significant
 // bits), with p' rounded to f16: 2^-12 of it, as fine as f16 outputs need.  The sum of the probabilities is
 //     l = sum_j p'_j * 2^-e_j    in fp32, one product per page,
-// and y = 2^E0 * (sum_j p'_j value_j) / l.  E0 is the exponent of the first page that a part looks at.  The maximum is
+// and y = 2^E0 * (sum_j p'_j value_j) / l.  E0 is the exponent of the first page that a row of the part sees: a page that all rows
+// have slid past may hold anything.  The maximum is
 // raised only when it would grow by more than 2^8 (p' stays below that, far from f16's end), so the accumulators are
 // hardly ever rescaled.
 #pragma once
@@ -266,7 +267,9 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll
             for (int h = 0; h < 2; ++h) seen[q][h] = row_keys(p, tile, r0 + 8 * q + 2 * t + h);
         // keys between these two are seen by every row that is there
-        const int all_lo = row_keys(p, tile, r0 + rows - 1).lo, all_hi = row_keys(p, tile, r0).hi;
+        const RowKeys head_row = row_keys(p, tile, r0);
+        const int all_lo = row_keys(p, tile, r0 + rows - 1).lo, all_hi = head_row.hi;
+        const int first_seen = max(0, head_row.lo - range.first) / BOX;      // box of the part's first key that a row sees
 
         // queries as right-hand fragments: row 8 * q + g; k index 2t, 2t+1 (8+2t, 8+2t+1) of step j is head element
         // 16 * (t + 4 * (j / 4)) + 4 * (j % 4) + 0, 2 (1, 3)
@@ -293,7 +296,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             }
         }
 
-        float e0 = 0.0f;                                   // exponent of the first keys' value scale
+        float e0 = 0.0f;                                   // exponent of the value scale of the first keys that are seen
         // output i: head elements 16i + g (o[0], o[1]) and 16i + g + 8 (o[2], o[3]) of rows 8q + 2t and 8q + 2t + 1
         float o[NQ][KS][4], m[NQ][2], l[NQ][2];
 #pragma unroll
@@ -329,7 +332,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                     b.zv = vs > 0.0f ? z : none;
                 }
                 const float e = vs > 0.0f ? (float)((int)((__float_as_uint(vs) >> 23) & 255u) - 127) : 0.0f;
-                if (i0 == 0 && seg == range.first) e0 = __shfl_sync(0xffffffffu, e, 0);
+                if (i0 == 0 && seg == range.first) e0 = __shfl_sync(0xffffffffu, e, first_seen);
                 if (z != none) {
                     b.e = vs > 0.0f ? e - e0 : 0.0f;
                     b.f = __uint_as_float((unsigned)(127 - max(-126, min(126, (int)b.e))) << 23);

@@ -469,9 +469,10 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
             if (any) {
                 const int pg = page_of(half.first);
                 page_next = page_of(half.first + 1);
-                // exponent of the first keys' value scale
+                // exponent of the value scale of the first keys that a row of the half sees
                 const float s = pg >= 0 ? __ldg(p.v_scales + (int64_t)pg * p.heads + head) : 0.0f;
-                e0 = __shfl_sync(0xffffffffu, s > 0.0f ? (float)((int)((__float_as_uint(s) >> 23) & 255u) - 127) : 0.0f, 0);
+                const int first_seen = max(0, row_keys(p, tile, w.r0 + 128 * t).lo - half.first * kLgKeys) / 16;
+                e0 = __shfl_sync(0xffffffffu, s > 0.0f ? (float)((int)((__float_as_uint(s) >> 23) & 255u) - 127) : 0.0f, first_seen);
                 info = info_of(pg);
             }
             for (int b = half.first; b < half.last; ++b, ++n) {
