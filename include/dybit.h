@@ -546,9 +546,11 @@ typedef struct {
  * starts[b + 1] - 1 are the last, new tokens of sequence b, which has lengths[b] tokens with them.  So row starts[b] + i
  * is position lengths[b] - (starts[b + 1] - starts[b]) + i.  Rows that belong to no sequence are left as they are.
  *   starts  sequences + 1 int32 that do not decrease, the last at most `tokens`
- *   lengths at most max_pages * page (what is beyond is cut off); a sequence of fewer tokens than new rows is one whose
+ *   lengths at most max_pages * page; a sequence of fewer tokens than new rows is one whose
  *           first rows lie in front of position 0: they are not written, read as zeros and see no key
- *   max_new no sequence has more new tokens (what is beyond is left out); at most `tokens`
+ *   max_new no sequence has more new tokens; at most `tokens`
+ *           New tokens beyond max_new, or behind the table's last page, are left out as if their sequence ended in front of
+ *           them: their rows are left as they are, the rows before keep their positions
  *   q_heads query heads of the attention, a multiple of cache.heads, up to 128 to a key head
  *   table   [dev] sequences rows of max_pages entries, row stride table_stride
  *   causal, window  how the attention calls will mask: what the plan deals their work out by.  A call that masks otherwise

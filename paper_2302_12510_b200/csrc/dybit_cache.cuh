@@ -98,10 +98,14 @@ __device__ __forceinline__ CacheSeq cache_seq(const CachePlanArgs &a, int b) {
     CacheSeq q;
     const int T = (int)a.s.T;
     const int lo = min(max(a.starts[b], 0), T), hi = min(max(a.starts[b + 1], lo), T);
+    // Tokens beyond max_new, or beyond the table's last page, are left out as if the sequence ended in front of them: its other
+    // tokens keep their positions.  (len may then be negative, where every row that is left lies in front of position 0.)
+    const int len = max(a.lengths[b], 0);
+    const int beyond = min(hi - lo, max(hi - lo - a.s.max_new, max(0, len - a.s.max_pages * a.s.page)));
     q.row = lo;
-    q.n = min(hi - lo, a.s.max_new);
-    q.len = (int)min((int64_t)max(a.lengths[b], 0), (int64_t)a.s.max_pages * a.s.page);
-    const int outside = max(0, q.n - q.len), inside = q.n - outside, p0 = q.len - inside;
+    q.n = hi - lo - beyond;
+    q.len = len - beyond;
+    const int outside = min(q.n, max(0, q.n - q.len)), inside = q.n - outside, p0 = q.len - inside;
     q.items = cache_div_up(outside, a.s.page) + (inside > 0 ? (q.len - 1) / a.s.page - p0 / a.s.page + 1 : 0);
     const int rows = q.n * a.s.group;
     const bool small = q.n <= a.s.small_tokens;
@@ -259,7 +263,7 @@ __global__ void __launch_bounds__(kCachePlanThreads) cache_plan_kernel(const Cac
             const int seq = b0 + k;
             const CacheSeq m = sh.seqs[k].q;
             const int i0 = sh.seqs[k].first[0];
-            const int page = a.s.page, outside = max(0, m.n - m.len), p0 = m.len - (m.n - outside), out_items = cache_div_up(outside, page);
+            const int page = a.s.page, outside = min(m.n, max(0, m.n - m.len)), p0 = m.len - (m.n - outside), out_items = cache_div_up(outside, page);
             CacheItem *list = reinterpret_cast<CacheItem *>(a.plan + L.items) + i0;
             for (int i = lane; i < m.items; i += 32) {
                 CacheItem it;
