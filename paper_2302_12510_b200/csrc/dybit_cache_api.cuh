@@ -34,6 +34,10 @@ static dybit_status check_batch(const dybit_cache *c, const dybit_cache_batch *b
     return DYBIT_OK;
 }
 
+// The window as the kernels take it.  No sequence has more than 2^26 tokens, so one of 2^26 holds all of them; a longer one would
+// pass 32 bits where it is taken from a position in front of the first.
+static int window_or_none(int window) { return window > 0 && window < (1 << 26) ? window : INT_MAX; }
+
 // Rows of a sequence that small tiles take, the others large ones: two tiles of 16, or four where the batch is small.  A large tile
 // costs its keys the same however full it is, small ones each cost them; but a block of large tiles takes longer to begin and to
 // end.  8 key heads of 4 queries, 4096 keys, small against large tiles: 16 sequences of 32 rows 97 : 113 us, of 48 rows 137 : 113 us, of 64
@@ -51,7 +55,7 @@ static CacheShape cache_shape(const dybit_cache *c, const dybit_cache_batch *b) 
     s.max_pages = b->max_pages;
     s.small_tokens = b->tokens * b->q_heads <= kAloneRows ? std::max(1, kSmallMostAlone / s.group) : kSmallMost / s.group;
     s.causal = b->causal != 0;
-    s.window = b->window > 0 ? b->window : INT_MAX;
+    s.window = window_or_none(b->window);
     s.small_rows = (int64_t)s.max_new * s.group <= 8 ? 8 : kSmallRows;
     return s;
 }
@@ -366,7 +370,7 @@ dybit_status dybit_cache_attention(const dybit_cache *cache, const dybit_cache_b
     p.y = y, p.y_token = y_token_stride, p.y_head = y_head_stride;
     p.lse = lse;
     p.scale_log2 = scale * kLog2e;
-    p.causal = causal != 0, p.window = window > 0 ? window : INT_MAX;
+    p.causal = causal != 0, p.window = window_or_none(window);
     p.q_vec = heads_aligned(q, t, q_token_stride, q_head_stride, 8), p.q_vec16 = heads_aligned(q, t, q_token_stride, q_head_stride, 16);
     p.y_vec = heads_aligned(y, t, y_token_stride, y_head_stride, 8), p.y_vec16 = heads_aligned(y, t, y_token_stride, y_head_stride, 16);
     const CacheShape shape = cache_shape(cache, batch);
