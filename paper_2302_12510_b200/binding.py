@@ -954,6 +954,19 @@ def dybit_adapters_backward(dY: torch.Tensor, codes: torch.Tensor, fmt, scales: 
 
 # ---------------------------------------------------------------- key-value cache in 8-bit codes
 
+def _c_int(value, name: str) -> int:
+    """An argument that the library takes in 32 bits, which ctypes would cut it to."""
+    value = int(value)
+    if not -2**31 <= value < 2**31:
+        raise ValueError(f"{name} does not fit 32 bits")
+    return value
+
+
+def _window(window) -> int:
+    """A window of any size: one of 2^31 - 1 holds every sequence whole already."""
+    return _c_int(min(int(window), 2**31 - 1), "window")
+
+
 class KVCache:
     """A pool of `pages` pages for the keys and values of `heads` heads of `dim` elements, `page` tokens to a page: codes
     uint8 [pages][heads][page][dim] and scales float32 [pages][heads], for keys and for values.  Buffers that are not given
@@ -961,7 +974,7 @@ class KVCache:
 
     def __init__(self, pages: int, page: int, heads: int, dim: int, device=None, k_codes: Optional[torch.Tensor] = None,
                  v_codes: Optional[torch.Tensor] = None, k_scales: Optional[torch.Tensor] = None, v_scales: Optional[torch.Tensor] = None):
-        self.pages, self.page, self.heads, self.dim = int(pages), int(page), int(heads), int(dim)
+        self.pages, self.page, self.heads, self.dim = int(pages), _c_int(page, "page"), _c_int(heads, "heads"), _c_int(dim, "dim")
         given = next((t for t in (k_codes, v_codes, k_scales, v_scales) if t is not None), None)
         device = given.device if given is not None else device or torch.device("cuda", torch.cuda.current_device())
 
@@ -993,8 +1006,9 @@ def _cache_batch(cache: KVCache, table: torch.Tensor, tokens: int, q_heads: Opti
     stride = table.stride(0) if B > 1 else most            # (torch gives a single row any stride)
     if stride < most:
         raise ValueError("the rows of table must not overlap: give a copy of a table that is expanded or slides over another")
-    return _CCacheBatch(B, int(tokens), int(tokens if max_new is None else min(max_new, tokens)), cache.heads if q_heads is None else int(q_heads),
-                        table.data_ptr(), stride, most, int(bool(causal)), int(window))
+    return _CCacheBatch(_c_int(B, "the number of sequences"), _c_int(tokens, "tokens"), _c_int(tokens if max_new is None else min(max_new, tokens), "max_new"),
+                        cache.heads if q_heads is None else _c_int(q_heads, "q_heads"), table.data_ptr(), stride, _c_int(most, "the table's width"),
+                        int(bool(causal)), _window(window))
 
 
 def dybit_cache_plan_bytes(cache: KVCache, table: torch.Tensor, tokens: int, q_heads: Optional[int] = None, max_new: Optional[int] = None) -> int:
@@ -1063,7 +1077,7 @@ def dybit_cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, plan: Ca
     plan._for(cache)
     t, kt, kh = _heads3(k, "k", plan.T, cache.heads, cache.dim)
     _, vt, vh = _heads3(v, "v", plan.T, cache.heads, cache.dim, t)
-    _check(lib.dybit_cache_write(cache.ref, plan.ref, plan.address, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, t, top, _stream(stream)),
+    _check(lib.dybit_cache_write(cache.ref, plan.ref, plan.address, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, t, _c_int(top, "top"), _stream(stream)),
            "dybit_cache_write")
 
 
@@ -1110,6 +1124,6 @@ def dybit_cache_attention(q: torch.Tensor, cache: KVCache, plan: CachePlan, scal
     at, size, ws = _workspace(plan._workspace_bytes(cache), ws, q, stream)
     _check(lib.dybit_cache_attention(cache.ref, plan.ref, plan.address, q.data_ptr(), t, qt, qh, out.data_ptr(), yt, yh,
                                      None if lse is None else _dense(lse, "lse", (plan.T, plan.q_heads)),
-                                     cache.dim ** -0.5 if scale is None else scale, int(bool(causal)), int(window), at, size, _stream(stream)),
+                                     cache.dim ** -0.5 if scale is None else scale, int(bool(causal)), _window(window), at, size, _stream(stream)),
            "dybit_cache_attention")
     return out

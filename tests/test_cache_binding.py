@@ -43,3 +43,52 @@ def test_every_row_of_a_table_lies_in_it(table, stride):
     if table.numel() > 0:
         last = (b.sequences - 1) * b.table_stride + b.max_pages - 1 + table.storage_offset()
         assert last < table.untyped_storage().nbytes() // 4
+
+
+# ---------------------------------------------------------------- whole numbers that the library takes in 32 bits
+
+@pytest.mark.parametrize("window,want", [(0, 0), (16, 16), (2**31 - 1, 2**31 - 1), (2**31, 2**31 - 1), (2**32 + 16, 2**31 - 1), (2**40, 2**31 - 1), (-1, -1)])
+def test_a_window_is_not_cut(window, want):
+    assert batch(INTS.view(4, 10), window=window).window == want
+    assert Calls().attention(window=window)[-4] == want
+
+
+@pytest.mark.parametrize("bad", [2**31, 2**32 + 4, -2**31 - 1, -2**32 + 4])
+def test_other_numbers_beyond_32_bits_are_refused(bad):
+    table, calls = Table(INTS.view(4, 10)), Calls()
+    makes = [lambda: binding._cache_batch(CACHE, table, 8, bad, None), lambda: binding.KVCache(0, bad, 1, 64), lambda: binding.KVCache(0, 16, bad, 64),
+             lambda: binding.KVCache(0, 16, 1, bad), lambda: calls.write(top=bad), lambda: binding._cache_batch(CACHE, table, bad, 4, None)]
+    if bad < 0:
+        makes += [lambda: batch(INTS.view(4, 10), window=bad), lambda: calls.attention(window=bad), lambda: binding._cache_batch(CACHE, table, 8, 4, bad)]
+    for make in makes:
+        with pytest.raises(ValueError):
+            make()
+    # (max_new bounds what there is: any number at or above it)
+    assert binding._cache_batch(CACHE, table, 8, 4, 2**40).max_new == 8
+
+
+class Calls:
+    """The calls with a library that only notes its arguments."""
+
+    def __init__(self):
+        self.cache = SimpleNamespace(heads=2, dim=64, page=16, ref=None)
+        self.plan = SimpleNamespace(T=3, q_heads=4, ref=None, address=0, _for=lambda cache: None, _workspace_bytes=lambda cache: 64)
+        self.tensor = lambda *shape: Table(torch.zeros(shape, dtype=torch.bfloat16))
+
+    def noted(self, name, call):
+        seen, lib = [], binding.lib
+        binding.lib = SimpleNamespace(**{name: lambda *args: seen.append(args) or 0})
+        try:
+            call()
+        finally:
+            binding.lib = lib
+        return seen[0]
+
+    def attention(self, q=None, out=None, **more):
+        q, out = q or self.tensor(3, 4, 64), out or self.tensor(3, 4, 64)
+        return self.noted("dybit_cache_attention", lambda: binding.dybit_cache_attention(q, self.cache, self.plan, out=out, stream=0,
+                                                                                         ws=Table(torch.zeros(4096, dtype=torch.uint8)), **more))
+
+    def write(self, **more):
+        k = self.tensor(3, 2, 64)
+        return self.noted("dybit_cache_write", lambda: binding.dybit_cache_write(self.cache, k, k, self.plan, stream=0, **more))
