@@ -13,7 +13,7 @@ static dybit_status check_cache(const dybit_cache *c) {
     if (c == nullptr) return DYBIT_ERR_INVALID_ARG;
     if (c->pages < 0 || c->heads < 1 || c->dim < 1 || c->page < 1) return DYBIT_ERR_INVALID_ARG;
     if (c->dim % 16 != 0 || c->dim > kCacheMaxDim || (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128)) return DYBIT_ERR_UNSUPPORTED;
-    if (c->heads > 4096 || c->pages * c->heads > 0x7ffffffe) return DYBIT_ERR_UNSUPPORTED;
+    if (c->heads > 4096 || c->pages > 0x7ffffffe / c->heads) return DYBIT_ERR_UNSUPPORTED;
     return DYBIT_OK;
 }
 
