@@ -1018,7 +1018,8 @@ def dybit_cache_plan_bytes(cache: KVCache, table: torch.Tensor, tokens: int, q_h
 def dybit_cache_plan(cache: KVCache, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, tokens: int, q_heads: Optional[int] = None,
                      max_new: Optional[int] = None, causal: bool = True, window: int = 0, plan: Optional[torch.Tensor] = None,
                      stream=None) -> torch.Tensor:
-    """Lists of the work of a batch (see CachePlan).  Returns the plan's buffer (uint8)."""
+    """Lists of the work of a batch (see CachePlan).  Returns the plan's buffer (uint8).  On another stream than their own, starts
+    and lengths have to outlive the call's work, and the table that of all calls that go by the plan."""
     batch = _cache_batch(cache, table, tokens, q_heads, max_new, causal, window)
     _cache_ints(starts, "starts", batch.sequences + 1)
     _cache_ints(lengths, "lengths", batch.sequences)
@@ -1037,12 +1038,13 @@ class CachePlan:
     [sequences][pages] with the page of every `page` tokens (rows of any stride that do not overlap), starts int32 [sequences + 1] with the rows of each sequence's
     new tokens among the batch's `tokens` rows, lengths int32 [sequences] with the tokens of each sequence, new ones
     included.  max_new bounds the new tokens of one sequence (default: tokens); the smaller, the less is launched.  causal and
-    window say how the attention will mask; a call that masks otherwise takes one more launch.  The plan and its table have to
-    outlive the calls that use them."""
+    window say how the attention will mask; a call that masks otherwise takes one more launch.  The plan has to outlive the calls
+    that use it (or its tensors take record_stream), as any tensor that is used on another stream than its own; it keeps
+    the table, starts and lengths alive."""
 
     def __init__(self, cache: KVCache, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, tokens: int, q_heads: Optional[int] = None,
                  max_new: Optional[int] = None, causal: bool = True, window: int = 0, buffer: Optional[torch.Tensor] = None, stream=None):
-        self.table, self.T = table, int(tokens)
+        self.table, self.starts, self.lengths, self.T = table, starts, lengths, int(tokens)
         self.batch = _cache_batch(cache, table, tokens, q_heads, max_new, causal, window)
         self.q_heads, self.page, self.heads = self.batch.q_heads, cache.page, cache.heads
         self.buffer = dybit_cache_plan(cache, table, starts, lengths, tokens, q_heads, max_new, causal, window, buffer, stream)

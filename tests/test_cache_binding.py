@@ -1,5 +1,6 @@
 """The key-value cache's binding: what it tells the library of its arguments, and what it refuses before the library is called.
 Nothing is launched; tensors are stand-ins that say they lie on the GPU."""
+import weakref
 from types import SimpleNamespace
 
 import pytest
@@ -92,3 +93,20 @@ class Calls:
     def write(self, **more):
         k = self.tensor(3, 2, 64)
         return self.noted("dybit_cache_write", lambda: binding.dybit_cache_write(self.cache, k, k, self.plan, stream=0, **more))
+
+
+# ---------------------------------------------------------------- what a plan keeps
+
+def test_a_plan_keeps_what_its_launch_reads():
+    # tensors made for the call alone: on another stream than their own their memory could be another's before the launch has read them
+    made = [Table(INTS.view(4, 10)), Table(torch.arange(5, dtype=torch.int32)), Table(torch.full((4,), 9, dtype=torch.int32))]
+    alive, lib = [weakref.ref(t) for t in made], binding.lib
+    binding.lib = SimpleNamespace(dybit_cache_plan_bytes=lambda *args: 64, dybit_cache_plan=lambda *args: 0)
+    try:
+        plan = binding.CachePlan(SimpleNamespace(heads=2, page=16, ref=None), *made, 4, buffer=Table(torch.zeros(64, dtype=torch.uint8)), stream=0)
+    finally:
+        binding.lib = lib
+    del made
+    assert all(ref() is not None for ref in alive)
+    del plan
+    assert all(ref() is None for ref in alive)
