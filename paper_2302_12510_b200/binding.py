@@ -990,7 +990,16 @@ class KVCache:
         self.k_scales, self.v_scales = buffer(k_scales, "k_scales", scales, torch.float32), buffer(v_scales, "v_scales", scales, torch.float32)
         self.c = _CCache(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(), self.v_scales.data_ptr(),
                          self.pages, self.page, self.heads, self.dim)
-        self.ref = C.byref(self.c)
+        self.ref, self.device = C.byref(self.c), self.k_codes.get_device()
+
+
+def _on(device: int, *tensors: Optional[torch.Tensor]):
+    """The calls run on the current device, and what they are given lies there."""
+    if device != (_raw_device or torch.cuda.current_device)():
+        raise ValueError(f"the cache or the table lies on device {device}, which is not the current one")
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"a tensor on {t.device} with a cache or a table on device {device}")
 
 
 def _cache_ints(t: torch.Tensor, name: str, n: int):
@@ -1021,6 +1030,7 @@ def dybit_cache_plan(cache: KVCache, table: torch.Tensor, starts: torch.Tensor, 
     """Lists of the work of a batch (see CachePlan).  Returns the plan's buffer (uint8).  On another stream than their own, starts
     and lengths have to outlive the call's work, and the table that of all calls that go by the plan."""
     batch = _cache_batch(cache, table, tokens, q_heads, max_new, causal, window)
+    _on(table.get_device(), starts, lengths, plan)
     _cache_ints(starts, "starts", batch.sequences + 1)
     _cache_ints(lengths, "lengths", batch.sequences)
     need = int(lib.dybit_cache_plan_bytes(cache.ref, C.byref(batch)))
@@ -1044,16 +1054,17 @@ class CachePlan:
 
     def __init__(self, cache: KVCache, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, tokens: int, q_heads: Optional[int] = None,
                  max_new: Optional[int] = None, causal: bool = True, window: int = 0, buffer: Optional[torch.Tensor] = None, stream=None):
-        self.table, self.starts, self.lengths, self.T = table, starts, lengths, int(tokens)
+        self.table, self.starts, self.lengths, self.T, self.device = table, starts, lengths, int(tokens), table.get_device()
         self.batch = _cache_batch(cache, table, tokens, q_heads, max_new, causal, window)
         self.q_heads, self.page, self.heads = self.batch.q_heads, cache.page, cache.heads
         self.buffer = dybit_cache_plan(cache, table, starts, lengths, tokens, q_heads, max_new, causal, window, buffer, stream)
         self.address, self.ref = self.buffer.data_ptr(), C.byref(self.batch)
         self._ws_bytes = {}
 
-    def _for(self, cache: KVCache):
-        if cache.page != self.page or cache.heads != self.heads:
-            raise ValueError("the plan was made for a cache of other pages or heads")
+    def _for(self, cache: KVCache, *tensors: Optional[torch.Tensor]):
+        if cache.page != self.page or cache.heads != self.heads or cache.device != self.device:
+            raise ValueError("the plan was made for a cache of other pages or heads, or on another device")
+        _on(cache.device, *tensors)
 
     def _workspace_bytes(self, cache: KVCache) -> int:
         need = self._ws_bytes.get(cache.dim)
@@ -1076,7 +1087,7 @@ def _heads3(x: torch.Tensor, name: str, T: int, heads: int, dim: int, code: Opti
 
 def dybit_cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, plan: CachePlan, top: int = 2, stream=None) -> None:
     """Stores the keys and values [tokens][heads][dim] of a batch's new tokens in the pages of the plan's table."""
-    plan._for(cache)
+    plan._for(cache, k, v)
     t, kt, kh = _heads3(k, "k", plan.T, cache.heads, cache.dim)
     _, vt, vh = _heads3(v, "v", plan.T, cache.heads, cache.dim, t)
     _check(lib.dybit_cache_write(cache.ref, plan.ref, plan.address, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, t, _c_int(top, "top"), _stream(stream)),
@@ -1087,7 +1098,7 @@ def dybit_cache_read(cache: KVCache, plan: CachePlan, dtype: torch.dtype = torch
                      v: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The keys and values [tokens][heads][dim] that the cache holds for a batch's new tokens.  Rows of no sequence are
     left as they are."""
-    plan._for(cache)
+    plan._for(cache, k, v)
     if dtype not in _DTYPE_CODE:
         raise ValueError("dtype must be float32, bfloat16 or float16")
     T, H, D = shape = (plan.T, cache.heads, cache.dim)
@@ -1115,7 +1126,7 @@ def dybit_cache_attention(q: torch.Tensor, cache: KVCache, plan: CachePlan, scal
     """Attention of a batch's new tokens q [tokens][q_heads][dim] (bfloat16 or float16) over their sequences' caches; scale
     defaults to dim ** -0.5, window > 0 lets a token see the last `window` keys, its own among them.  Returns the outputs
     [tokens][q_heads][dim]; lse, float32 [tokens][q_heads], receives the logarithms of the rows' sums where it is given."""
-    plan._for(cache)
+    plan._for(cache, q, out, lse)
     t, qt, qh = _heads3(q, "q", plan.T, plan.q_heads, cache.dim)
     if t == 0:
         raise ValueError("q must be bfloat16 or float16")

@@ -11,11 +11,22 @@ from paper_2302_12510_b200 import binding
 CACHE = SimpleNamespace(heads=2)
 
 
-class Table:
-    """A host tensor that passes for one of the device."""
+@pytest.fixture(autouse=True)
+def current_device(monkeypatch):
+    """The stand-ins' device is the current one."""
+    now = [0]
+    monkeypatch.setattr(binding, "_raw_device", lambda: now[0])
+    return now
 
-    def __init__(self, t):
-        self.t, self.dtype, self.is_cuda, self.shape = t, t.dtype, True, t.shape
+
+class Table:
+    """A host tensor that passes for one of a device."""
+
+    def __init__(self, t, device="cuda:0"):
+        self.t, self.dtype, self.is_cuda, self.shape, self.device = t, t.dtype, True, t.shape, torch.device(device)
+
+    def get_device(self):
+        return self.device.index
 
     def __getattr__(self, name):
         return getattr(self.t, name)
@@ -72,9 +83,10 @@ class Calls:
     """The calls with a library that only notes its arguments."""
 
     def __init__(self):
-        self.cache = SimpleNamespace(heads=2, dim=64, page=16, ref=None)
-        self.plan = SimpleNamespace(T=3, q_heads=4, ref=None, address=0, _for=lambda cache: None, _workspace_bytes=lambda cache: 64)
-        self.tensor = lambda *shape: Table(torch.zeros(shape, dtype=torch.bfloat16))
+        self.cache = SimpleNamespace(heads=2, dim=64, page=16, ref=None, device=0)
+        self.plan = binding.CachePlan.__new__(binding.CachePlan)
+        self.plan.__dict__.update(T=3, q_heads=4, ref=None, address=0, page=16, heads=2, device=0, _ws_bytes={64: 64})
+        self.tensor = lambda *shape, device="cuda:0": Table(torch.zeros(shape, dtype=torch.bfloat16), device)
 
     def noted(self, name, call):
         seen, lib = [], binding.lib
@@ -110,3 +122,32 @@ def test_a_plan_keeps_what_its_launch_reads():
     assert all(ref() is not None for ref in alive)
     del plan
     assert all(ref() is None for ref in alive)
+
+
+# ---------------------------------------------------------------- devices
+
+def test_tensors_of_other_devices_are_refused(current_device):
+    calls, far = Calls(), lambda *shape, dtype=torch.bfloat16: Table(torch.zeros(shape, dtype=dtype), "cuda:1")
+    calls.attention(), calls.write()
+    ints = [Table(INTS.view(4, 10)), Table(INTS[:5]), Table(INTS[:4])]
+    plan = lambda *t, **more: binding.dybit_cache_plan(calls.cache, *t, 8, 4, stream=0, **more)
+    refused = [lambda: calls.attention(q=far(3, 4, 64)), lambda: calls.attention(out=far(3, 4, 64)),
+               lambda: calls.attention(lse=far(3, 4, dtype=torch.float32)), lambda: plan(ints[0], Table(INTS[:5], "cuda:1"), ints[2]),
+               lambda: plan(*ints[:2], Table(INTS[:4], "cuda:1")), lambda: plan(*ints, plan=far(4096)),
+               lambda: binding.dybit_cache_read(calls.cache, calls.plan, k=far(3, 2, 64), v=calls.tensor(3, 2, 64), stream=0),
+               lambda: binding.dybit_cache_write(calls.cache, calls.tensor(3, 2, 64), far(3, 2, 64), calls.plan, stream=0)]
+    for call in refused:
+        with pytest.raises(ValueError):
+            call()
+    calls.plan.device = 1                                  # a plan of one device, a cache of another
+    with pytest.raises(ValueError):
+        calls.write()
+
+
+def test_another_device_than_the_current_one_is_refused(current_device):
+    calls, ints = Calls(), [Table(INTS.view(4, 10)), Table(INTS[:5]), Table(INTS[:4])]
+    current_device[0] = 1
+    for call in (calls.attention, calls.write, lambda: binding.dybit_cache_plan(calls.cache, *ints, 8, 4, stream=0),
+                 lambda: binding.dybit_cache_read(calls.cache, calls.plan, k=calls.tensor(3, 2, 64), v=calls.tensor(3, 2, 64), stream=0)):
+        with pytest.raises(ValueError):
+            call()
