@@ -267,9 +267,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll
             for (int h = 0; h < 2; ++h) seen[q][h] = row_keys(p, tile, r0 + 8 * q + 2 * t + h);
         // keys between these two are seen by every row that is there
-        const RowKeys head_row = row_keys(p, tile, r0);
-        const int all_lo = row_keys(p, tile, r0 + rows - 1).lo, all_hi = head_row.hi;
-        const int first_seen = max(0, head_row.lo - range.first) / BOX;      // box of the part's first key that a row sees
+        const int all_lo = row_keys(p, tile, r0 + rows - 1).lo, all_hi = row_keys(p, tile, r0).hi;
 
         // queries as right-hand fragments: row 8 * q + g; k index 2t, 2t+1 (8+2t, 8+2t+1) of step j is head element
         // 16 * (t + 4 * (j / 4)) + 4 * (j % 4) + 0, 2 (1, 3)
@@ -332,7 +330,13 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                     b.zv = vs > 0.0f ? z : none;
                 }
                 const float e = vs > 0.0f ? (float)((int)((__float_as_uint(vs) >> 23) & 255u) - 127) : 0.0f;
-                if (i0 == 0 && seg == range.first) e0 = __shfl_sync(0xffffffffu, e, first_seen);
+                if (i0 == 0 && seg == range.first) {
+                    // of the first round's boxes the one with the first key that all rows see, or else the last, which some row sees
+                    int at = 0;
+#pragma unroll
+                    for (int k = 1; k < NB; ++k) at += all_lo >= seg + k * BOX ? 1 : 0;
+                    e0 = __shfl_sync(0xffffffffu, e, at);
+                }
                 if (z != none) {
                     b.e = vs > 0.0f ? e - e0 : 0.0f;
                     b.f = __uint_as_float((unsigned)(127 - max(-126, min(126, (int)b.e))) << 23);

@@ -469,10 +469,11 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
             if (any) {
                 const int pg = page_of(half.first);
                 page_next = page_of(half.first + 1);
-                // exponent of the value scale of the first keys that a row of the half sees
+                // exponent of a value scale that a row sees: of the first block's 16 keys those with the first key that all rows of the warp
+                // see, or else the last
                 const float s = pg >= 0 ? __ldg(p.v_scales + (int64_t)pg * p.heads + head) : 0.0f;
-                const int first_seen = max(0, row_keys(p, tile, w.r0 + 128 * t).lo - half.first * kLgKeys) / 16;
-                e0 = __shfl_sync(0xffffffffu, s > 0.0f ? (float)((int)((__float_as_uint(s) >> 23) & 255u) - 127) : 0.0f, first_seen);
+                const int seen = min(max(0, all_lo - half.first * kLgKeys) / 16, kLgKeys / 16 - 1);
+                e0 = __shfl_sync(0xffffffffu, s > 0.0f ? (float)((int)((__float_as_uint(s) >> 23) & 255u) - 127) : 0.0f, seen);
                 info = info_of(pg);
             }
             for (int b = half.first; b < half.last; ++b, ++n) {
