@@ -95,6 +95,13 @@ __device__ __forceinline__ void decode_word(unsigned w, unsigned &even, unsigned
     odd = decode_pair<T>(w >> 8, w);
 }
 
+// Two query elements, infinities as NaN (x * 0 + x; exact for every other number): a row with one then has NaN for every score and is NaN
+// itself.  Infinite scores would look like scores of keys that are not there.
+template <typename T> __device__ __forceinline__ unsigned nan_for_infinity(unsigned w) {
+    if constexpr (__is_same(T, __half)) return half2_bits(__hfma2(as_half2(w), as_half2(0u), as_half2(w)));
+    else return as_u32(__hfma2(as_bf162(w), as_bf162(0u), as_bf162(w)));
+}
+
 // d (16 x 8, fp32) += a (16 x 16) * b (16 x 8) on the legacy tensor path: sixteen rows of codes against eight queries.
 template <typename T>
 __device__ __forceinline__ void mma_16816(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, const unsigned (&b)[2]) {
@@ -290,6 +297,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                         memcpy(&v, e, 8);
                     }
                 }
+                v.x = nan_for_infinity<T>(v.x), v.y = nan_for_infinity<T>(v.y);
                 qf[q][j][0] = __byte_perm(v.x, v.y, 0x5410), qf[q][j][1] = __byte_perm(v.x, v.y, 0x7632);
             }
         }

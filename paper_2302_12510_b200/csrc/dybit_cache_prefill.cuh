@@ -439,7 +439,8 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
 #pragma unroll 2
                 for (int i = lane / CH; i < 32; i += PER) {
                     uint4 *at_c = reinterpret_cast<uint4 *>(chunk(i));
-                    const uint4 v = *at_c;
+                    uint4 v = *at_c;
+                    v.x = nan_for_infinity<T>(v.x), v.y = nan_for_infinity<T>(v.y), v.z = nan_for_infinity<T>(v.z), v.w = nan_for_infinity<T>(v.w);
                     *at_c = make_uint4(__byte_perm(v.x, v.y, 0x5410), __byte_perm(v.x, v.y, 0x7632), __byte_perm(v.z, v.w, 0x5410), __byte_perm(v.z, v.w, 0x7632));
                 }
                 fence_proxy_async_smem();
