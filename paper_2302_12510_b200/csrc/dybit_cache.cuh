@@ -401,7 +401,8 @@ __global__ void __launch_bounds__(kCkptThreads) cache_write_kernel(const CacheWr
                              encode4_8<true, false>(decode4<true>(c.z), ratio), encode4_8<true, false>(decode4<true>(c.w), ratio));
         }
     }
-    if (W > 1) named_tile_sync<TPR>(sub);                  // every thread of the tile has read the old scale
+    if constexpr (W > 1) named_tile_sync<TPR>(sub);        // every thread of the tile has read the old scale
+    else __syncwarp();
     if (t == 0 && (grown || off == 0)) *scale_at = scale;
 }
 
