@@ -189,7 +189,7 @@ __device__ __forceinline__ void cache_deal(const CacheShape &s, const CacheTile 
         }
         const CacheTile t = out[lo];
         const int off = (int)(r - t.first);
-        starts[c] = {lo, head, off, 0, t};
+        if (DYBIT_CHECK(c <= (large ? kLargeBlocks : small_blocks(s.small_rows)) && head <= s.heads, 0x8b)) starts[c] = {lo, head, off, 0, t};
         sh.deal.tile[c] = lo, sh.deal.head[c] = (short)head, sh.deal.off[c] = off;
     }
     __syncthreads();
@@ -213,7 +213,8 @@ __device__ __forceinline__ void cache_deal(const CacheShape &s, const CacheTile 
             const bool is = parts > 0 && (parts > kFewParts && !large) == (many != 0);
             int total;
             const int at = n_joins[many] + cache_block_scan(is ? 1 : 0, s_scan, &total);
-            if (is) joins[many ? last - at : at] = {out[sh.deal.tile[c]], sh.deal.head[c], c, parts, 0};
+            const int to = many ? last - at : at;
+            if (is && DYBIT_CHECK(to >= 0 && to <= last, 0x8c)) joins[to] = {out[sh.deal.tile[c]], sh.deal.head[c], c, parts, 0};
             n_joins[many] += total;
         }
     }
@@ -420,6 +421,7 @@ struct CacheRead {
     int64_t token_stride[2], head_stride[2];
     const uint8_t *codes[2];
     const float *scales[2];
+    int64_t tokens;
 };
 
 // A block per page and head, of the keys or of the values: codes are fetched four vectors ahead, one vector of
@@ -461,7 +463,7 @@ __global__ void __launch_bounds__(kCkptThreads) cache_read_kernel(const CacheRea
                 f[4 * h + 2] = __fmul_rn(d.z, scale), f[4 * h + 3] = __fmul_rn(d.w, scale);
             }
             T *dst = y + row * p.token_stride[kv] + c;
-            if (!DYBIT_CHECK(c + E <= p.dim && row < it.count, 0x86)) continue;
+            if (!DYBIT_CHECK(c + E <= p.dim && row < it.count && it.row >= 0 && it.row + row < p.tokens, 0x86)) continue;
             if constexpr (VEC) {
                 uint4 o;
                 if constexpr (E == 4) {

@@ -331,7 +331,7 @@ dybit_status dybit_cache_read(const dybit_cache *cache, const dybit_cache_batch 
     p.table = batch->table, p.table_stride = batch->table_stride;
     p.pages = cache->pages, p.page = cache->page, p.heads = cache->heads, p.dim = cache->dim;
     p.vpr = cache->dim * dtype_bytes(t) / 16, p.vpr_mul = ((1 << 20) + p.vpr - 1) / p.vpr;
-    p.y[0] = k, p.y[1] = v;
+    p.y[0] = k, p.y[1] = v, p.tokens = batch->tokens;
     p.token_stride[0] = k_token_stride, p.token_stride[1] = v_token_stride;
     p.head_stride[0] = k_head_stride, p.head_stride[1] = v_head_stride;
     p.codes[0] = static_cast<const uint8_t *>(cache->k_codes), p.codes[1] = static_cast<const uint8_t *>(cache->v_codes);
@@ -368,7 +368,7 @@ dybit_status dybit_cache_attention(const dybit_cache *cache, const dybit_cache_b
     p.k_scales = cache->k_scales, p.v_scales = cache->v_scales;
     p.q = q, p.q_token = q_token_stride, p.q_head = q_head_stride;
     p.y = y, p.y_token = y_token_stride, p.y_head = y_head_stride;
-    p.lse = lse;
+    p.lse = lse, p.tokens = batch->tokens;
     p.scale_log2 = scale * kLog2e;
     p.causal = causal != 0, p.window = window_or_none(window);
     p.q_vec = heads_aligned(q, t, q_token_stride, q_head_stride, 8), p.q_vec16 = heads_aligned(q, t, q_token_stride, q_head_stride, 16);

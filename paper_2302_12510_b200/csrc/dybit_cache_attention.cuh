@@ -59,6 +59,7 @@ struct CacheAttn {
     float4 *part_ml;             // [slot][rows]: {m + E0, l, E0, -}
     int q_vec, q_vec16, y_vec, y_vec16;  // rows can be moved in pieces of 8 (16) bytes
     int beside;                  // this launch may run beside the one before it, whose own wait covers what both read
+    int64_t tokens;              // rows of q and y
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -180,7 +181,7 @@ __device__ __forceinline__ void store_attention_row(const CacheAttn &p, const Ca
     const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l), up = __uint_as_float((unsigned)((int)e0 + 127) << 23);
     T *y = static_cast<T *>(p.y) + (tile.row + token) * p.y_token + h * p.y_head + d;
     const float f0 = s.x * inv * up, f1 = s.y * inv * up, f2 = s.z * inv * up, f3 = s.w * inv * up;
-    if (!DYBIT_CHECK(token < tile.n && d + 4 <= p.dim, 0x87)) return;
+    if (!DYBIT_CHECK(token < tile.n && tile.row >= 0 && tile.row + token < p.tokens && d + 4 <= p.dim, 0x87)) return;
     if (p.y_vec) {
         *reinterpret_cast<uint2 *>(y) = make_uint2(pack2<T>(f0, f1), pack2<T>(f2, f3));
     } else {
@@ -526,6 +527,7 @@ cache_small_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 const float4 v = *reinterpret_cast<const float4 *>(all + lr * LD + d);
                 const float top = stats[2 * lr], sum = stats[2 * lr + 1];
                 if (part.slot >= 0) {
+                    if (!DYBIT_CHECK(part.slot < 2 * small_blocks(ROWS) && r < ROWS && d + 4 <= p.dim, 0x8d)) continue;
                     const int64_t to = (int64_t)part.slot * ROWS + r;
                     *reinterpret_cast<float4 *>(p.part_y + to * p.dim + d) = v;
                     if (d == 0) p.part_ml[to] = make_float4(top + e0, sum, e0, 0.0f);

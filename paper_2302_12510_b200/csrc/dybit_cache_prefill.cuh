@@ -526,6 +526,9 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
             if (ok && 32 * warp < rows) {                  // whole warps
                 const int64_t to_row = (int64_t)w.part.slot * kLargeRows + r;
                 T *y = static_cast<T *>(p.y) + (tile.row + token) * p.y_token + h * p.y_head;
+                [[maybe_unused]] auto in_range = [&](int d) {
+                    return token < tile.n && tile.row >= 0 && tile.row + token < p.tokens && d <= p.dim && w.part.slot < 2 * kLargeBlocks && r < kLargeRows;
+                };
                 // a row that sees no key: zeros (and minus infinity)
                 const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l), up = __uint_as_float((unsigned)((int)e0 + 127) << 23);
 #pragma unroll 1
@@ -541,7 +544,7 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
                     float f[16];                           // (columns lie as the values were decoded)
 #pragma unroll
                     for (int j = 0; j < 16; ++j) f[j] = __uint_as_float(v[(j & ~3) | ((j & 1) << 1) | ((j >> 1) & 1)]);
-                    if (r < rows && c * 16 < p.dim && DYBIT_CHECK(token < tile.n, 0x87)) {
+                    if (r < rows && c * 16 < p.dim && DYBIT_CHECK(in_range(c * 16 + 16), 0x87)) {
                         if (w.part.slot >= 0) {
 #pragma unroll
                             for (int j = 0; j < 16; j += 4)
@@ -561,7 +564,7 @@ cache_large_kernel(const uint8_t *__restrict__ k_codes, const uint8_t *__restric
                     }
                     __syncwarp();
                 }
-                if (r < rows) {
+                if (r < rows && DYBIT_CHECK(in_range(0), 0x8e)) {
                     if (w.part.slot >= 0) p.part_ml[to_row] = make_float4(m + e0, l, e0, 0.0f);
                     else if (p.lse != nullptr) p.lse[(int64_t)(tile.row + token) * (p.heads * p.group) + h] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
                 }
