@@ -547,7 +547,8 @@ typedef struct {
  * is position lengths[b] - (starts[b + 1] - starts[b]) + i.  Rows that belong to no sequence are left as they are.
  *   starts  sequences + 1 int32 that do not decrease, the last at most `tokens`
  *   lengths at most max_pages * page; a sequence of fewer tokens than new rows is one whose
- *           first rows lie in front of position 0: they are not written, read as zeros and see no key
+ *           first rows lie in front of position 0: they are not written, read as zeros, and see no key under a causal
+ *           mask (and every key of their sequence without one)
  *   max_new no sequence has more new tokens; at most `tokens`
  *           New tokens beyond max_new, or behind the table's last page, are left out as if their sequence ended in front of
  *           them: their rows are left as they are, the rows before keep their positions

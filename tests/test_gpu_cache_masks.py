@@ -1,4 +1,4 @@
-"""Masks of the attention over the cache at the ends of their range."""
+"""Masks of the attention over the cache at the ends of their range, and rows in front of a sequence's first position."""
 import pytest
 import torch
 
@@ -26,3 +26,21 @@ def test_windows_that_hold_everything(lengths, news):
         assert torch.equal(dy.dybit_cache_attention(qd, cache, plan, scale=0.125, window=window), full), window
         other = dy.CachePlan(cache, *b.to(DEV), b.T, 8, max(news), window=window)
         assert torch.equal(dy.dybit_cache_attention(qd, cache, other, scale=0.125), full), window
+
+
+@pytest.mark.parametrize("lengths,news", BATCHES)
+def test_rows_in_front_of_the_first_position(lengths, news):
+    # they see nothing under a causal mask, with and without a window, and every key without one
+    b = ref.Batch(lengths, news, 16, 2, 64, seed=47)
+    pools = [b.pool(), b.pool()]
+    cache = device_cache(b, *pools)
+    q, qd = activations(b, 8, BF, 3)
+    plan = dy.CachePlan(cache, *b.to(DEV), b.T, 8, max(news))
+    front = [(i, r) for i in range(len(news)) for r in b.rows(i) if b.position(i, r) < 0]
+    assert front
+    for causal, window in ((True, 0), (True, 7), (False, 0)):
+        lse = torch.empty((b.T, 8), device=DEV)
+        y = dy.dybit_cache_attention(qd, cache, plan, scale=0.125, causal=causal, window=window, lse=lse)
+        ref.check_attention(y, lse, ref.attention(b, q, *pools, 0.125, causal, window), BF)
+        for i, r in front:
+            assert bool((y[r] == 0).all() and (lse[r] == -torch.inf).all()) == (causal or lengths[i] == 0)
