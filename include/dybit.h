@@ -602,10 +602,12 @@ dybit_status dybit_cache_read(const dybit_cache *cache, const dybit_cache_batch 
  *     j <= i                 if causal, every j < lengths[b] otherwise
  *     j >  i - window        if window > 0 (causal only): the last `window` keys, its own among them
  * A row that sees no key is 0, its lse minus infinity.  Sums, maxima and statistics are fp32; q meets the keys as it is,
- * probabilities meet the values as f16 numbers (2^-12 off at most, relative to the row's largest), y is rounded once.
- * A row of q that is not finite makes its own y and lse not finite, and no other's.  The scales of the values that the
- * new tokens of a sequence see lie within 2^100 of each other (and of 1, where some of them are 0 or some pages are not
- * there).  Pages that none of them sees hold anything.
+ * probabilities (times their values' scales) meet the values as f16 numbers, each off by 2^-11 of itself at most, or by
+ * 2^-25 of the row's largest where it is below 2^-14 of that; the sum takes them in fp32.  y is rounded once.
+ * A row of q with an infinity or NaN makes its own y and lse NaN where it sees a key, and no other's.  Sums of
+ * q[d] * value(code) stay within fp32 (|q| below 2^114 does).  The scales of the values that the new tokens of a sequence
+ * see lie within 2^100 of each other (and of 1, where some of them are 0 or some pages are not there).  Pages that none of
+ * them sees hold anything.
  *   q, y [dev]  tokens x q_heads x dim, unit inner stride, strides in elements;  t  bf16 or f16 (f32: DYBIT_ERR_UNSUPPORTED)
  *   scale  0 .. 2e38
  *   lse  [dev]  tokens x q_heads floats, dense, or NULL

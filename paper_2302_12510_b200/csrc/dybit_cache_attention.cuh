@@ -13,7 +13,9 @@
 // What both have in common.  The running maximum of a row goes over x + log2 of the values' scale (base 2), so
 //     p'_j = 2^(x_j + e_j - m),   e_j = log2 s_V(page) - E0
 // is at most a small constant and the second product takes the bare values of the codes, exact in f16 (seven significant
-// bits), with p' rounded to f16: 2^-12 of it, as fine as f16 outputs need.  The sum of the probabilities is
+// bits), with p' rounded to f16: half a step is 2^-11 of it, that of an f16 output.  (Below 2^-14 of the row's largest, 2^-25 of that.
+// On prompts and decode steps outputs in f16 are 2.5e-4 from the formula, where fp32 probabilities give 2.0e-4; in bf16 the
+// outputs' own rounding, 1.6e-3, hides it.)  The sum of the probabilities is
 //     l = sum_j p'_j * 2^-e_j    in fp32, one product per page,
 // and y = 2^E0 * (sum_j p'_j value_j) / l.  E0 is the exponent of the first page that a row of the part sees: a page that all rows
 // have slid past may hold anything.  The maximum is
