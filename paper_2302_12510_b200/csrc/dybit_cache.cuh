@@ -236,7 +236,8 @@ __global__ void __launch_bounds__(kCachePlanThreads) cache_deal_kernel(const Cac
 }
 
 // One block.  The lists' capacities hold for starts that never decrease; entries beyond them (starts that do) are dropped,
-// not written.  Integer work of B sequences: counts and the lists, a warp to a sequence; then the blocks' starts.
+// not written.  Integer work of B sequences: counts and the lists, a warp to a sequence; then the blocks' starts.  Some kilobytes: bound by
+// the block's barriers and searches, 10 us for a few sequences, 22 for 64 (2368 starts, each found by bisection).
 __global__ void __launch_bounds__(kCachePlanThreads) cache_plan_kernel(const CachePlanArgs a) {
     __shared__ int s_scan[kCachePlanThreads / 32];
     __shared__ CachePlanShared sh;
@@ -326,6 +327,8 @@ __device__ __forceinline__ int64_t cache_page(const int *table, int64_t stride, 
 // in registers between the maximum and the codes; the rest is read twice, the second time from the caches.
 //   scale = the larger of what the page has and 2^(ceil(log2 amax) - top) of the new tokens
 // Where a begun page's scale grows, its older codes are rounded once more at the new scale, a larger power of two.
+// Four prompts of 2048 tokens, 8 heads of 128 in bf16 (50 MB): 16.6 us, floor 7.7.  Bound by latency: 74 registers leave a third of
+// the warps, issue 53 %, DRAM 23 %.
 template <typename T, bool VEC, int W>
 __global__ void __launch_bounds__(kCkptThreads) cache_write_kernel(const CacheWrite p) {
     constexpr int E = 16 / (int)sizeof(T), NV = 8, TPR = W * 32;

@@ -8,7 +8,8 @@
 //
 // Launches of a call that do not need one another run side by side as far as there is room: a kernel waits for what came before the
 // call's first kernel through that one (which lets its successor start only behind its own wait), and for its neighbour before it
-// ends, so that the end of the last one is the end of all.
+// ends, so that the end of the last one is the end of all.  (Blocks of the two kinds of tiles do not share an SM: 55,296 and 64,512 or
+// 65,536 registers.  Small tiles begin where a block of large ones has ended or has no work.)
 //
 // What both have in common.  The running maximum of a row goes over x + log2 of the values' scale (base 2), so
 //     p'_j = 2^(x_j + e_j - m),   e_j = log2 s_V(page) - E0
@@ -224,7 +225,8 @@ struct alignas(32) KeyBlock {
 // the fragments: contractions over head elements and over keys may run in any order.  Of K a lane takes 16 consecutive codes of
 // two neighbouring keys, of V, which the instruction wants with keys side by side, four keys of a head element, by a
 // transposing load of bytes; the keys of both products are numbered by what that load gives (row i of the two halves of 16 keys is
-// key 2i and key 2i + 1).  Bound by HBM, then by instruction issue: a pair of codes takes 7 instructions.
+// key 2i and key 2i + 1).  Bound by instruction issue, then by HBM: 64 requests of 4000 keys take 88 M warp instructions, 57 M of them to decode
+// (7 to a pair of codes), at 74 % of the issue slots 122 us where the codes' bytes take 80.
 // BOX: keys of a TMA box, 32 or, on pages of 16 tokens, 16.
 template <typename T, int DP, int NQ, int BOX>
 __global__ void __launch_bounds__(32 * small_per_sm(8 * NQ), 1)
