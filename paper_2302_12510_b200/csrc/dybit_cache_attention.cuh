@@ -18,10 +18,9 @@
 // On prompts and decode steps outputs in f16 are 2.5e-4 from the formula, where fp32 probabilities give 2.0e-4; in bf16 the
 // outputs' own rounding, 1.6e-3, hides it.)  The sum of the probabilities is
 //     l = sum_j p'_j * 2^-e_j    in fp32, one product per page,
-// and y = 2^E0 * (sum_j p'_j value_j) / l.  E0 is the exponent of the first page that a row of the part sees: a page that all rows
-// have slid past may hold anything.  The maximum is
-// raised only when it would grow by more than 2^8 (p' stays below that, far from f16's end), so the accumulators are
-// hardly ever rescaled.
+// and y = 2^E0 * (sum_j p'_j value_j) / l.  E0 is the exponent of one of the first pages of a part that a row of the tile
+// sees: a page that all rows have slid past may hold anything.  The maximum is raised only when it would grow by more than 2^8 (p'
+// stays below that, far from f16's end), so the accumulators are hardly ever rescaled.
 #pragma once
 
 #include "dybit_cache.cuh"
